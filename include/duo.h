@@ -489,6 +489,115 @@ duo_status duo_attention(const void* Q, const void* K, const void* V, int64_t ld
 duo_status duo_silu_mul(const void* G, const void* U, int64_t m, int64_t n, int64_t ld, void* Y, int64_t ldy,
                         void* stream);
 
+/*
+ * Serving a pruned model: prompts of different lengths packed one behind the
+ * other, a paged key-value cache in 16, 8 or 4 bits, and attention with grouped
+ * heads over both.  As in the harness above activations are bf16, token-major,
+ * arithmetic fp32, everything stream ordered and argument errors found before
+ * anything is enqueued.  Numbers that these calls read on the device (positions,
+ * slots, pages, lengths, offsets) cannot be checked on the host: one that points
+ * outside what the call was given is skipped as each call says, and no access
+ * outside is made.
+ */
+
+/* duo_rope_at - duo_rope with a position for every row: in each head of row t of
+ *   X (m x heads*head_dim bf16, ldx) the pair (i, i + head_dim/2) is rotated by
+ *   the angle pos[t] * theta^(-2i/head_dim) (reduced in fp64; cosine, sine and
+ *   the rotation in fp32, one rounding).  pos: m int32.  Y: m x heads*head_dim
+ *   (ldy); may equal X (with ldy == ldx), else must not overlap it.  head_dim
+ *   even, at most 256 (else DUO_ERR_UNSUPPORTED). */
+duo_status duo_rope_at(const void* X, int64_t m, int64_t heads, int64_t head_dim, int64_t ldx, const int32_t* pos,
+                       double theta, void* Y, int64_t ldy, void* stream);
+
+/*
+ * The cache.  Pages of page_size tokens (16, 32, 64, 128 or 256); in a page each
+ * K/V head has one block of bytes, at data + (page * kv_heads + head) * block:
+ *   page_size K rows, page_size V rows (head_dim numbers each, in `format`), then
+ *   for 8 and 4 bits page_size rows of K scales and as many of V scales, one
+ *   bf16 per group of 32 channels.
+ * A token's slot is page * page_size + its row.  A row is head_dim bf16
+ * (DUO_KV_BF16), bytes (DUO_KV_I8: code + 128) or half bytes (DUO_KV_I4: code + 8,
+ * channel 2i in the lower half of byte i), a number being code * scale.
+ * Codes of a group (32 channels of one token and head) are
+ *   s = bf16(max |x| / q) with q = 127 or 7,  code = rint(x / s) within [-q, q],
+ * roundings to nearest even.  A group whose s is below 2^-126 holds zeros; one with
+ * a NaN or infinity among its numbers is NaN throughout.  (Groups of 32 of a single
+ * token: a token is written once and never touched again, and one large channel
+ * coarsens 31 others, not the whole row.  bf16 scales keep bf16's whole range
+ * and cost 1/16 or 1/8 of the codes' bytes.)
+ * data: num_pages * duo_kv_page_bytes() bytes of device memory, 16-byte aligned,
+ * with any contents at first: rows that were never written are not used.
+ */
+enum { DUO_KV_BF16 = 0, DUO_KV_I8 = 1, DUO_KV_I4 = 2 };
+typedef struct {
+  void* data;
+  int64_t num_pages;
+  int32_t page_size;
+  int32_t kv_heads;
+  int32_t head_dim; /* 64 or 128 */
+  int32_t format;
+} duo_kv_cache;
+
+/* Bytes of one page (0 for a size or format that is not supported). */
+size_t duo_kv_page_bytes(int32_t format, int32_t page_size, int32_t kv_heads, int32_t head_dim);
+
+/* duo_kv_write - row t of K and V (m x kv_heads*head_dim bf16, ldk and ldv) into
+ *   slot slots[t] (m int64) of the cache, in its format.  A slot outside
+ *   [0, num_pages * page_size), such as -1 for a padding row, is skipped; no
+ *   slot may be named twice (what it holds then is undefined).  K, V 16-byte
+ *   aligned, ldk % 8 == ldv % 8 == 0 (else DUO_ERR_UNSUPPORTED). */
+duo_status duo_kv_write(const duo_kv_cache* cache, const void* K, int64_t ldk, const void* V, int64_t ldv,
+                        const int64_t* slots, int64_t m, void* stream);
+
+/* duo_kv_read - the rows at slots[t] back, as bf16 (8 and 4 bits: code * scale
+ *   rounded once, finite numbers to finite ones): K and V m x kv_heads*head_dim
+ *   (ldk, ldv).  A slot outside the cache gives a row of zeros.  Alignment as
+ *   duo_kv_write. */
+duo_status duo_kv_read(const duo_kv_cache* cache, const int64_t* slots, int64_t m, void* K, int64_t ldk, void* V,
+                       int64_t ldv, void* stream);
+
+/* duo_attention_packed - causal attention of nseq sequences of different lengths,
+ *   packed one behind the other, with grouped heads: query head h reads K/V head
+ *   h / (heads / kv_heads).  Sequence s has the rows cu_q[s] .. cu_q[s+1] - 1 of Q
+ *   and O and the rows cu_k[s] .. cu_k[s+1] - 1 of K and V (nseq + 1 int32 each;
+ *   cu_k NULL: cu_q).  With lq queries and lk keys its query i sees the keys
+ *   j <= i + lk - lq (the queries are the last tokens of the keys' sequence):
+ *     O_i = sum_j p_j V_j,  p = softmax_j(scale Q_i . K_j),
+ *   and a query that sees no key (lk < lq) gets 0.  Keys and values that a query
+ *   does not see have no influence on it, whatever they hold.  Scores, maxima,
+ *   sums and O are fp32, in one pass over the keys; the probabilities are rounded
+ *   to bf16 before the product with V, relative to the largest score so far.
+ *   Q total_q x heads*head_dim (ldq), K and V total_k x kv_heads*head_dim (ldk,
+ *   ldv), O total_q x heads*head_dim (ldo, not overlapping the inputs), bf16.
+ *   Offsets are taken as within [0, total] (larger ones as total, a sequence whose
+ *   end lies before its start as empty); rows of O in no sequence are left alone.
+ *   scale finite.  heads % kv_heads == 0, head_dim 64 or 128; Q, K, V 16-byte
+ *   aligned with ldq, ldk, ldv % 8 == 0 (else DUO_ERR_UNSUPPORTED).  No scratch
+ *   memory. */
+duo_status duo_attention_packed(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
+                                const int32_t* cu_q, int64_t total_q, const int32_t* cu_k, int64_t total_k,
+                                int64_t nseq, int64_t heads, int64_t kv_heads, int64_t head_dim, double scale, void* O,
+                                int64_t ldo, void* stream);
+
+/* duo_attention_paged - attention of one query per sequence over its cached tokens:
+ *   row s of Q (nseq x heads*head_dim, ldq) against the first lens[s] tokens of
+ *   the sequence, token t in page table[s * ldt + t / page_size] (table: nseq rows
+ *   of int32), heads grouped as above (heads % cache->kv_heads == 0).  lens[s] is
+ *   taken as within [0, max_len]; a sequence of length 0 gets 0, one with a token
+ *   in a page outside the cache NaN.  The rows after a sequence's last token have
+ *   no influence.  O: nseq x heads*head_dim bf16 (ldo, not overlapping Q).
+ *   Scores are exact products of bf16 queries and cached codes summed in fp32,
+ *   times the group's scale; probabilities, in 8 and 4 bits times the scale of V,
+ *   are rounded to bf16 before the product with V.  Long sequences are split over
+ *   their length and joined; where is a matter of the sizes alone (nseq, max_len,
+ *   heads), so results are deterministic.  ldt * page_size >= max_len.  Workspace: duo_attention_paged_workspace_size
+ *   with the same sizes (it never falls with a larger max_len or nseq). */
+size_t duo_attention_paged_workspace_size(int64_t nseq, int64_t heads, int64_t kv_heads, int64_t head_dim,
+                                          int64_t max_len);
+duo_status duo_attention_paged(const void* Q, int64_t ldq, const duo_kv_cache* cache, const int32_t* table, int64_t ldt,
+                               const int32_t* lens, int64_t nseq, int64_t max_len, int64_t heads, double scale, void* O,
+                               int64_t ldo, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -12,7 +12,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libduo.so")
 SOURCES = ["abi.hip", "hessian.hip", "gemm_f32.hip", "split.hip", "chol.hip", "score.hip", "sweep.hip", "profile.hip",
-           "block.hip", "permute.hip", "decode.hip"]
+           "block.hip", "permute.hip", "decode.hip", "cache.hip", "packed.hip", "paged.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 FLAGS = [

@@ -19,6 +19,7 @@
 #include <mutex>
 
 #include "internal.h"
+#include "mfma.h"
 #include "pingpong.h"
 
 using namespace duo;
@@ -120,16 +121,6 @@ __global__ void silu_mul_kernel(const uint16_t* __restrict__ G, const uint16_t* 
   const int64_t t = id / n, c = id % n;
   const float g = bf16_bits_to_f32(G[t * ld + c]), u = bf16_bits_to_f32(U[t * ld + c]);
   Y[t * ldy + c] = f32_to_bf16_bits(g / (1.0f + expf(-g)) * u);
-}
-
-typedef __bf16 bf16v2 __attribute__((ext_vector_type(2)));
-typedef float f32v2 __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  const bf16v2 v = __builtin_convertvector(f32v2{lo, hi}, bf16v2);  // round to nearest even
-  uint32_t u;
-  __builtin_memcpy(&u, &v, 4);
-  return u;
 }
 
 // A row of 8 16-byte chunks stored at chunk position c ^ ((r >> 1) & 7): the 16
@@ -437,16 +428,6 @@ __global__ void lin_plain_kernel(const uint16_t* __restrict__ X, int64_t ldx, co
 // V in that XCD's L2, but for heads left over from groups of eight: one head (of
 // 128, 16384 tokens) on one XCD 1357 us, over all of them 608; nine heads 1558 and 1050.
 // ---------------------------------------------------------------------------
-typedef short s16v4 __attribute__((ext_vector_type(4)));
-typedef float f16x __attribute__((ext_vector_type(16)));
-
-__device__ __forceinline__ f16x mma32_bf16(const u32x4& a, const u32x4& b, f16x c) {
-  bf16x8 av, bv;
-  __builtin_memcpy(&av, &a, 16);
-  __builtin_memcpy(&bv, &b, 16);
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, bv, c, 0, 0, 0);
-}
-
 // (Sequence, head) pairs left over from groups of eight, one per XCD; seven run as a
 // group (spread over all XCDs they read every K and V eight times: 5 % slower up to
 // 8192 tokens).

@@ -1,0 +1,304 @@
+// The paged key-value cache: writing rows into it (quantised as they are written),
+// reading them back, and the rotation of rows by given positions that comes
+// before.
+//
+// A group of 32 channels of one token and head has one scale,
+//   s = bf16(max |x| / q),  code = rint(x / s),  q = 127 (8 bits) or 7 (4 bits).
+// x and s have eight significant bits, so a quotient that is no half integer is at
+// least 2^-16 (relative) away from one, and x / s in fp32 rounds to the code of the
+// exact quotient, ties included where the division is exact at them.  The kernel
+// forms x (1/s) and corrects it by its exact remainder once, which is exact at ties.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "cache.h"
+#include "internal.h"
+#include "mfma.h"
+
+using namespace duo;
+
+namespace {
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) % 16) == 0; }
+
+// ---------------------------------------------------------------------------
+// rotation by positions
+// ---------------------------------------------------------------------------
+constexpr int kMaxHalf = 128;
+
+// Turns per position of every pair, theta^(-2i/head_dim) / 2 pi, computed on the host.
+struct Turns {
+  double f[kMaxHalf];
+};
+
+// A workgroup takes `per` tokens; the cosines and sines of a token are computed once
+// (the angle in turns and its fraction in fp64, the rest in fp32) and shared by all
+// of its heads through LDS.  V: pairs per access (8 in 16-byte accesses, or 1).
+template <int V>
+__global__ __launch_bounds__(256) void rope_at_kernel(const uint16_t* X, int64_t ldx, int64_t m, int heads, int half,
+                                                      const int32_t* __restrict__ pos, Turns turns, uint16_t* Y,
+                                                      int64_t ldy, int per) {
+  extern __shared__ float2 cs[];  // [token][pair]: cosine, sine
+  const int64_t t0 = (int64_t)blockIdx.x * per;
+  const int nt = (int)min((int64_t)per, m - t0);
+  for (int e = threadIdx.x; e < nt * half; e += 256) {
+    const double turn = (double)pos[t0 + e / half] * turns.f[e % half];
+    const float a = (float)((turn - rint(turn)) * 6.283185307179586);
+    float sn, cn;
+    sincosf(a, &sn, &cn);
+    cs[e] = make_float2(cn, sn);
+  }
+  __syncthreads();
+  const int cpr = half / V, items = nt * heads * cpr;  // accesses of half a head
+  for (int e = threadIdx.x; e < items; e += 256) {
+    const int c = e % cpr, h = e / cpr % heads, t = e / cpr / heads;
+    const int64_t col = (int64_t)h * 2 * half + c * V;
+    const uint16_t* x = X + (t0 + t) * ldx + col;
+    uint16_t* y = Y + (t0 + t) * ldy + col;
+    const float2* w = cs + t * half + c * V;
+    if constexpr (V == 8) {
+      const u32x4 a = *(const u32x4*)x, b = *(const u32x4*)(x + half);
+      u32x4 ya, yb;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float a0 = __uint_as_float(a[j] << 16), a1 = __uint_as_float(a[j] & 0xffff0000u);
+        const float b0 = __uint_as_float(b[j] << 16), b1 = __uint_as_float(b[j] & 0xffff0000u);
+        const float2 w0 = w[2 * j], w1 = w[2 * j + 1];
+        ya[j] = pack_bf16(a0 * w0.x - b0 * w0.y, a1 * w1.x - b1 * w1.y);
+        yb[j] = pack_bf16(b0 * w0.x + a0 * w0.y, b1 * w1.x + a1 * w1.y);
+      }
+      *(u32x4*)y = ya;
+      *(u32x4*)(y + half) = yb;
+    } else {
+      const float a = bf16_bits_to_f32(x[0]), b = bf16_bits_to_f32(x[half]);
+      y[0] = f32_to_bf16_bits(a * w[0].x - b * w[0].y);
+      y[half] = f32_to_bf16_bits(b * w[0].x + a * w[0].y);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// writing
+// ---------------------------------------------------------------------------
+
+// One thread per 8 channels of one row of K (which = 0) or V; the four threads of a
+// group of 32 agree on its scale.
+template <int FMT, int HD>
+__global__ __launch_bounds__(256) void kv_write_kernel(const uint16_t* __restrict__ K, int64_t ldk,
+                                                       const uint16_t* __restrict__ V, int64_t ldv,
+                                                       const int64_t* __restrict__ slots, int64_t m, KvGeo g) {
+  constexpr int C = HD / 8;  // threads per row
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int c = (int)(id % C);
+  const int64_t r = id / C;
+  const int which = (int)(r % 2), h = (int)(r / 2 % g.heads);
+  const int64_t t = r / 2 / g.heads;
+  const bool in = t < m;
+  const int64_t slot = in ? slots[t] : -1;
+  const bool ok = slot >= 0 && slot < g.pages << g.shift;
+  const uint16_t* src = (which ? V + (in ? t : 0) * ldv : K + (in ? t : 0) * ldk) + h * HD + 8 * c;
+  const u32x4 x = in ? *(const u32x4*)src : u32x4{0u, 0u, 0u, 0u};
+  const int64_t page = ok ? slot >> g.shift : 0;
+  const int row = ok ? (int)(slot & ((1 << g.shift) - 1)) : 0;
+  uint8_t* blk = g.data + (page * g.heads + h) * g.block;
+  uint8_t* dst = blk + kv_rows_at<FMT, HD>(which, g.shift) + row * KvFmt<FMT>::row(HD);
+  if constexpr (FMT == DUO_KV_BF16) {
+    if (ok) *(u32x4*)(dst + 16 * c) = x;
+  } else {
+    uint32_t mag = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) mag = max(mag, max(x[j] & 0x7fffu, x[j] >> 16 & 0x7fffu));
+    mag = max(mag, (uint32_t)__shfl_xor((int)mag, 1));
+    mag = max(mag, (uint32_t)__shfl_xor((int)mag, 2));
+    constexpr int most = KvFmt<FMT>::most, bias = KvFmt<FMT>::bias;
+    const bool fin = mag < 0x7f80u;
+    uint16_t sb = f32_to_bf16_bits(bf16_bits_to_f32((uint16_t)mag) / (float)most);
+    float s = bf16_bits_to_f32(sb);
+    const bool some = fin && s >= 1.1754943508222875e-38f;
+    if (!some) sb = fin ? 0 : 0x7fc0u;
+    const float inv = some ? 1.0f / s : 0.f;
+    s = some ? s : 0.f;
+    uint32_t code[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float v = some ? bf16_bits_to_f32((uint16_t)(x[j >> 1] >> (16 * (j & 1)))) : 0.f;
+      const float q = v * inv;
+      const float n = rintf(fmaf(fmaf(-q, s, v), inv, q));
+      code[j] = (uint32_t)((int)fminf(fmaxf(n, (float)-most), (float)most) + bias);
+    }
+    if (ok) {
+      if constexpr (FMT == DUO_KV_I8) {
+        uint2 w;
+        w.x = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
+        w.y = code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24;
+        *(uint2*)(dst + 8 * c) = w;
+      } else {
+        uint32_t w = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w |= code[j] << (4 * j);
+        *(uint32_t*)(dst + 4 * c) = w;
+      }
+      if (c % 4 == 0)
+        *(uint16_t*)(blk + kv_scales_at<FMT, HD>(which, g.shift) + row * KvFmt<FMT>::scales(HD) + c / 4 * 2) = sb;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// reading
+// ---------------------------------------------------------------------------
+template <int FMT, int HD>
+__global__ __launch_bounds__(256) void kv_read_kernel(KvGeo g, const int64_t* __restrict__ slots, int64_t m,
+                                                      uint16_t* __restrict__ K, int64_t ldk, uint16_t* __restrict__ V,
+                                                      int64_t ldv) {
+  constexpr int C = HD / 8;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int c = (int)(id % C);
+  const int64_t r = id / C;
+  const int which = (int)(r % 2), h = (int)(r / 2 % g.heads);
+  const int64_t t = r / 2 / g.heads;
+  if (t >= m) return;
+  const int64_t slot = slots[t];
+  u32x4 y = {0u, 0u, 0u, 0u};
+  if (slot >= 0 && slot < g.pages << g.shift) {
+    const int row = (int)(slot & ((1 << g.shift) - 1));
+    const uint8_t* blk = g.data + ((slot >> g.shift) * g.heads + h) * g.block;
+    const uint8_t* src = blk + kv_rows_at<FMT, HD>(which, g.shift) + row * KvFmt<FMT>::row(HD);
+    if constexpr (FMT == DUO_KV_BF16) {
+      y = *(const u32x4*)(src + 16 * c);
+    } else {
+      const float s = bf16_bits_to_f32(
+          *(const uint16_t*)(blk + kv_scales_at<FMT, HD>(which, g.shift) + row * KvFmt<FMT>::scales(HD) + c / 4 * 2));
+      uint2 w;
+      if constexpr (FMT == DUO_KV_I8)
+        w = *(const uint2*)(src + 8 * c);
+      else
+        w.x = *(const uint32_t*)(src + 4 * c);
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t n = FMT == DUO_KV_I8 ? ((j < 4 ? w.x : w.y) >> (8 * (j & 3)) & 255u) : (w.x >> (4 * j) & 15u);
+        const float p = (float)((int)n - KvFmt<FMT>::bias) * s;
+        // a code times a scale near bf16's end may round past it; NaN stays NaN
+        v[j] = fabsf(p) > 3.3895313892515355e38f ? copysignf(3.3895313892515355e38f, p) : p;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+    }
+  }
+  *(u32x4*)((which ? V + t * ldv : K + t * ldk) + h * HD + 8 * c) = y;
+}
+
+// Common checks of duo_kv_write and duo_kv_read.
+duo_status rows_ok(const duo_kv_cache* c, const void* K, int64_t ldk, const void* V, int64_t ldv, const int64_t* slots,
+                   int64_t m, KvGeo* g) {
+  if (m < 0) return DUO_ERR_INVALID_ARG;
+  if (duo_status e = kv_geo(c, g); e != DUO_OK) return e;
+  const int64_t w = (int64_t)c->kv_heads * c->head_dim;
+  if (ldk < w || ldv < w) return DUO_ERR_INVALID_ARG;
+  if (m == 0) return DUO_OK;
+  if (!K || !V || !slots) return DUO_ERR_INVALID_ARG;
+  if (ldk % 8 || ldv % 8 || !aligned16(K) || !aligned16(V)) return DUO_ERR_UNSUPPORTED;
+  if (m > INT32_MAX || cdiv(m * 2 * w / 8, 256) > INT32_MAX) return DUO_ERR_UNSUPPORTED;
+  return DUO_OK;
+}
+
+}  // namespace
+
+namespace duo {
+
+duo_status kv_geo(const duo_kv_cache* c, KvGeo* g) {
+  if (!c) return DUO_ERR_INVALID_ARG;
+  const size_t bytes = duo_kv_page_bytes(c->format, c->page_size, c->kv_heads, c->head_dim);
+  if (bytes == 0) return c->format < 0 || c->format > DUO_KV_I4 || c->page_size < 1 || c->kv_heads < 1 || c->head_dim < 1
+                             ? DUO_ERR_INVALID_ARG
+                             : DUO_ERR_UNSUPPORTED;
+  if (c->num_pages < 1 || !c->data) return DUO_ERR_INVALID_ARG;
+  if (!aligned16(c->data)) return DUO_ERR_INVALID_ARG;
+  if (c->num_pages > INT32_MAX || c->num_pages > ((int64_t)1 << 46) / (int64_t)bytes) return DUO_ERR_UNSUPPORTED;
+  g->data = (uint8_t*)c->data;
+  g->pages = c->num_pages;
+  g->heads = c->kv_heads;
+  g->block = (int64_t)(bytes / c->kv_heads);
+  g->shift = 0;
+  while (1 << g->shift < c->page_size) ++g->shift;
+  return DUO_OK;
+}
+
+}  // namespace duo
+
+extern "C" {
+
+size_t duo_kv_page_bytes(int32_t format, int32_t page_size, int32_t kv_heads, int32_t head_dim) {
+  if (kv_heads < 1 || kv_heads > 65535 || (head_dim != 64 && head_dim != 128)) return 0;
+  if (page_size < 16 || page_size > 256 || (page_size & (page_size - 1))) return 0;
+  int row;
+  switch (format) {
+    case DUO_KV_BF16: row = KvFmt<DUO_KV_BF16>::row(head_dim); break;
+    case DUO_KV_I8: row = KvFmt<DUO_KV_I8>::row(head_dim) + KvFmt<DUO_KV_I8>::scales(head_dim); break;
+    case DUO_KV_I4: row = KvFmt<DUO_KV_I4>::row(head_dim) + KvFmt<DUO_KV_I4>::scales(head_dim); break;
+    default: return 0;
+  }
+  return (size_t)2 * row * page_size * kv_heads;
+}
+
+duo_status duo_rope_at(const void* X, int64_t m, int64_t heads, int64_t head_dim, int64_t ldx, const int32_t* pos,
+                       double theta, void* Y, int64_t ldy, void* stream) {
+  if (m < 0 || heads < 1 || head_dim < 2 || (head_dim & 1) || heads > INT32_MAX || !(theta > 0.0) || !std::isfinite(theta))
+    return DUO_ERR_INVALID_ARG;
+  if (head_dim > 2 * kMaxHalf || heads * head_dim > INT32_MAX / 2) return DUO_ERR_UNSUPPORTED;
+  if (ldx < heads * head_dim || ldy < heads * head_dim) return DUO_ERR_INVALID_ARG;
+  if (m == 0) return DUO_OK;
+  if (!X || !Y || !pos || (X == Y && ldx != ldy)) return DUO_ERR_INVALID_ARG;
+  if (m > INT32_MAX) return DUO_ERR_UNSUPPORTED;
+  if (duo_status d = device_ok(); d != DUO_OK) return d;
+  const int half = (int)head_dim / 2;
+  Turns tr;
+  for (int i = 0; i < half; ++i) tr.f[i] = std::pow(theta, -2.0 * i / (double)head_dim) / 6.283185307179586;
+  const bool vec = half % 8 == 0 && ldx % 8 == 0 && ldy % 8 == 0 && aligned16(X) && aligned16(Y);
+  const int64_t items = heads * (half / (vec ? 8 : 1));  // of one token
+  const int per = (int)std::max<int64_t>(1, 256 / items);
+  const dim3 grid((unsigned)cdiv(m, per));
+  const size_t lds = (size_t)per * half * sizeof(float2);
+  if (vec)
+    hipLaunchKernelGGL(rope_at_kernel<8>, grid, dim3(256), lds, (hipStream_t)stream, (const uint16_t*)X, ldx, m,
+                       (int)heads, half, pos, tr, (uint16_t*)Y, ldy, per);
+  else
+    hipLaunchKernelGGL(rope_at_kernel<1>, grid, dim3(256), lds, (hipStream_t)stream, (const uint16_t*)X, ldx, m,
+                       (int)heads, half, pos, tr, (uint16_t*)Y, ldy, per);
+  DUO_LAUNCH_CHECK();
+  return DUO_OK;
+}
+
+duo_status duo_kv_write(const duo_kv_cache* cache, const void* K, int64_t ldk, const void* V, int64_t ldv,
+                        const int64_t* slots, int64_t m, void* stream) {
+  KvGeo g;
+  if (duo_status e = rows_ok(cache, K, ldk, V, ldv, slots, m, &g); e != DUO_OK) return e;
+  if (m == 0) return DUO_OK;
+  if (duo_status d = device_ok(); d != DUO_OK) return d;
+  return kv_by_format(cache, [&](auto fmt, auto hd) -> duo_status {
+    constexpr int FMT = decltype(fmt)::value, HD = decltype(hd)::value;
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_write_kernel<FMT, HD>), dim3((unsigned)cdiv(m * 2 * g.heads * (HD / 8), 256)),
+                       dim3(256), 0, (hipStream_t)stream, (const uint16_t*)K, ldk, (const uint16_t*)V, ldv, slots, m, g);
+    DUO_LAUNCH_CHECK();
+    return DUO_OK;
+  });
+}
+
+duo_status duo_kv_read(const duo_kv_cache* cache, const int64_t* slots, int64_t m, void* K, int64_t ldk, void* V,
+                       int64_t ldv, void* stream) {
+  KvGeo g;
+  if (duo_status e = rows_ok(cache, K, ldk, V, ldv, slots, m, &g); e != DUO_OK) return e;
+  if (m == 0) return DUO_OK;
+  if (duo_status d = device_ok(); d != DUO_OK) return d;
+  return kv_by_format(cache, [&](auto fmt, auto hd) -> duo_status {
+    constexpr int FMT = decltype(fmt)::value, HD = decltype(hd)::value;
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_read_kernel<FMT, HD>), dim3((unsigned)cdiv(m * 2 * g.heads * (HD / 8), 256)),
+                       dim3(256), 0, (hipStream_t)stream, g, slots, m, (uint16_t*)K, ldk, (uint16_t*)V, ldv);
+    DUO_LAUNCH_CHECK();
+    return DUO_OK;
+  });
+}
+
+}  // extern "C"

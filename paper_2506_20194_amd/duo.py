@@ -30,10 +30,12 @@ EXPORTED = (
     "duo_prune_layer", "duo_profile_enable", "duo_profile_read", "duo_block_workspace_size", "duo_rmsnorm",
     "duo_act_sparsify", "duo_linear", "duo_rope", "duo_attention", "duo_silu_mul", "duo_act_order",
     "duo_permute", "duo_permute_mask", "duo_dsc_workspace_size", "duo_dsc_layout", "duo_dsc_pack",
-    "duo_dsc_gemv", "duo_dsc_gemv_noalloc", "duo_hessian_status",
+    "duo_dsc_gemv", "duo_dsc_gemv_noalloc", "duo_hessian_status", "duo_rope_at", "duo_kv_page_bytes", "duo_kv_write",
+    "duo_kv_read", "duo_attention_packed", "duo_attention_paged_workspace_size", "duo_attention_paged",
 )
 PROF = dict(gram=0, hessian=1, chol=2, score=3, sweep=4, inblock=5, trail=6, select=7, decode=8)
 DUO_BOP_ACT_SPARSIFY, DUO_BOP_LINEAR, DUO_BOP_ATTENTION = 0, 1, 2
+DUO_KV_BF16, DUO_KV_I8, DUO_KV_I4 = 0, 1, 2
 
 
 class DuoError(RuntimeError):
@@ -58,6 +60,11 @@ FORMS = {None: 0, "auto": 0, "d": 1, "y": 2}
 
 class CholInfo(ctypes.Structure):
     _fields_ = [("lam", ctypes.c_double), ("fail_index", ctypes.c_int64), ("status", ctypes.c_int32)]
+
+
+class KvCache(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("num_pages", ctypes.c_int64), ("page_size", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("format", ctypes.c_int32)]
 
 
 _lib = None
@@ -129,6 +136,21 @@ def lib():
         L.duo_dsc_gemv.argtypes = [P, I32, I64, I64, ActRule, P, P, P, P, P, P, SZ, P]
         L.duo_dsc_gemv_noalloc.restype = I32
         L.duo_dsc_gemv_noalloc.argtypes = [P, I32, I64, I64, ActRule, P, P, P, P, P, P]
+        L.duo_rope_at.restype = I32
+        L.duo_rope_at.argtypes = [P, I64, I64, I64, I64, P, F64, P, I64, P]
+        KV = ctypes.POINTER(KvCache)
+        L.duo_kv_page_bytes.restype = SZ
+        L.duo_kv_page_bytes.argtypes = [I32, I32, I32, I32]
+        L.duo_kv_write.restype = I32
+        L.duo_kv_write.argtypes = [KV, P, I64, P, I64, P, I64, P]
+        L.duo_kv_read.restype = I32
+        L.duo_kv_read.argtypes = [KV, P, I64, P, I64, P, I64, P]
+        L.duo_attention_packed.restype = I32
+        L.duo_attention_packed.argtypes = [P, I64, P, I64, P, I64, P, I64, P, I64, I64, I64, I64, I64, F64, P, I64, P]
+        L.duo_attention_paged_workspace_size.restype = SZ
+        L.duo_attention_paged_workspace_size.argtypes = [I64, I64, I64, I64, I64]
+        L.duo_attention_paged.restype = I32
+        L.duo_attention_paged.argtypes = [P, I64, KV, P, I64, P, I64, I64, I64, F64, P, I64, P, SZ, P]
         L.duo_profile_enable.restype = I32
         L.duo_profile_enable.argtypes = [I32]
         L.duo_profile_read.restype = I32
@@ -697,3 +719,148 @@ def duo_silu_mul(G, U, out=None):
     _check(lib().duo_silu_mul(_ptr(G), _ptr(U), m, n, _bf16_rows(G, "G"), _ptr(Y), _bf16_rows(Y, "Y"),
                               _stream(G.device)), "duo_silu_mul")
     return Y
+
+
+# ---------------------------------------------------------------------------
+# serving: rotation by positions, paged key-value cache, packed and paged attention
+# ---------------------------------------------------------------------------
+
+KV_FORMATS = {"bf16": DUO_KV_BF16, "int8": DUO_KV_I8, "int4": DUO_KV_I4}
+
+
+def _ints(t, dtype, shape, name):
+    if t.dtype != dtype:
+        raise TypeError(f"duo: {name} must be {dtype}")
+    _shape(t, shape, name)
+    _contig(t, name)
+
+
+class KVCache:
+    """A paged key-value cache over `data`, a contiguous uint8 tensor (pages,
+    kv_heads, bytes of a head's block; see include/duo.h for what a block
+    holds).  fmt: "bf16", "int8" or "int4".  KVCache.empty allocates one."""
+
+    __slots__ = ("data", "page_size", "kv_heads", "head_dim", "fmt", "c")
+
+    def __init__(self, data, page_size, kv_heads, head_dim, fmt="bf16"):
+        if fmt not in KV_FORMATS:
+            raise ValueError(f"fmt must be one of {list(KV_FORMATS)}")
+        nbytes = kv_page_bytes(page_size, kv_heads, head_dim, fmt)
+        if data.dtype != torch.uint8:
+            raise TypeError("duo: a cache's data must be uint8")
+        _shape(data, (data.shape[0], kv_heads, nbytes // kv_heads), "data")
+        _contig(data, "data")
+        self.data, self.page_size, self.kv_heads, self.head_dim, self.fmt = data, page_size, kv_heads, head_dim, fmt
+        self.c = KvCache(data.data_ptr(), data.shape[0], page_size, kv_heads, head_dim, KV_FORMATS[fmt])
+
+    @classmethod
+    def empty(cls, pages, page_size, kv_heads, head_dim, fmt="bf16", device="cuda"):
+        nbytes = kv_page_bytes(page_size, kv_heads, head_dim, fmt)
+        return cls(torch.empty((pages, kv_heads, nbytes // kv_heads), dtype=torch.uint8, device=device), page_size,
+                   kv_heads, head_dim, fmt)
+
+    def slots(self, table, seq, pos):
+        """Slots (int64) of the tokens at positions pos of the sequences seq
+        (integer tensors of one length), whose pages are rows of table; a decoding
+        step or prompt needs them once for all layers that share the table."""
+        seq, pos = seq.long(), pos.long()
+        return table[seq, pos // self.page_size].long() * self.page_size + pos % self.page_size
+
+
+def kv_page_bytes(page_size, kv_heads, head_dim, fmt="bf16") -> int:
+    n = int(lib().duo_kv_page_bytes(KV_FORMATS[fmt], page_size, kv_heads, head_dim))
+    if n == 0:
+        raise DuoError(DUO_ERR_UNSUPPORTED, "duo_kv_page_bytes")
+    return n
+
+
+def duo_rope_at(X, heads, head_dim, pos, theta=1e4, out=None):
+    """Rows of X rotated by the angles of the positions pos (m int32); out may be X."""
+    m = X.shape[0]
+    if X.shape[1] != heads * head_dim:
+        raise ValueError("duo: X must be heads * head_dim wide")
+    Y = torch.empty((m, X.shape[1]), dtype=torch.bfloat16, device=X.device) if out is None else out
+    _same_device(X, pos, Y)
+    _shape(Y, X.shape, "out")
+    _ints(pos, torch.int32, (m,), "pos")
+    _check(lib().duo_rope_at(_ptr(X), m, heads, head_dim, _bf16_rows(X, "X"), _ptr(pos), float(theta), _ptr(Y),
+                             _bf16_rows(Y, "out"), _stream(X.device)), "duo_rope_at")
+    return Y
+
+
+def duo_kv_write(cache, K, V, slots):
+    """Rows of K and V (m x kv_heads*head_dim bf16) into their slots (m int64)."""
+    m, w = K.shape[0], cache.kv_heads * cache.head_dim
+    _same_device(cache.data, K, V, slots)
+    _shape(K, (m, w), "K")
+    _shape(V, (m, w), "V")
+    _ints(slots, torch.int64, (m,), "slots")
+    _check(lib().duo_kv_write(ctypes.byref(cache.c), _ptr(K), _bf16_rows(K, "K"), _ptr(V), _bf16_rows(V, "V"),
+                              _ptr(slots), m, _stream(K.device)), "duo_kv_write")
+
+
+def duo_kv_read(cache, slots, out=None):
+    """(K, V) bf16 rows at the slots (m int64); out: a pair to write into."""
+    shape = (slots.shape[0], cache.kv_heads * cache.head_dim)
+    K, V = out if out is not None else (torch.empty(shape, dtype=torch.bfloat16, device=slots.device) for _ in "KV")
+    _same_device(cache.data, K, V, slots)
+    _shape(K, shape, "K")
+    _shape(V, shape, "V")
+    _ints(slots, torch.int64, shape[:1], "slots")
+    _check(lib().duo_kv_read(ctypes.byref(cache.c), _ptr(slots), shape[0], _ptr(K), _bf16_rows(K, "K"), _ptr(V),
+                             _bf16_rows(V, "V"), _stream(slots.device)), "duo_kv_read")
+    return K, V
+
+
+def duo_attention_packed(Q, K, V, cu_q, heads, kv_heads, head_dim, cu_k=None, scale=None, out=None):
+    """Causal attention of packed sequences: Q total_q x heads*head_dim, K and V
+    total_k x kv_heads*head_dim, cu_q and cu_k (None: cu_q) the sequences' first
+    rows, nseq + 1 int32 each.  scale: None for head_dim^-1/2.  Rows of the result
+    that lie in no sequence are not written."""
+    n = cu_q.shape[0] - 1
+    O = torch.empty((Q.shape[0], heads * head_dim), dtype=torch.bfloat16, device=Q.device) if out is None else out
+    _same_device(Q, K, V, cu_q, cu_k, O)
+    _shape(Q, (Q.shape[0], heads * head_dim), "Q")
+    _shape(K, (K.shape[0], kv_heads * head_dim), "K")
+    _shape(V, K.shape, "V")
+    _shape(O, Q.shape, "out")
+    _ints(cu_q, torch.int32, (n + 1,), "cu_q")
+    if cu_k is not None:
+        _ints(cu_k, torch.int32, (n + 1,), "cu_k")
+    _check(lib().duo_attention_packed(_ptr(Q), _bf16_rows(Q, "Q"), _ptr(K), _bf16_rows(K, "K"), _ptr(V),
+                                      _bf16_rows(V, "V"), _ptr(cu_q), Q.shape[0], _ptr(cu_k), K.shape[0], n, heads,
+                                      kv_heads, head_dim, head_dim ** -0.5 if scale is None else float(scale), _ptr(O),
+                                      _bf16_rows(O, "out"), _stream(Q.device)), "duo_attention_packed")
+    return O
+
+
+def attention_paged_workspace(nseq, heads, kv_heads, head_dim, max_len, device):
+    n = int(lib().duo_attention_paged_workspace_size(nseq, heads, kv_heads, head_dim, max_len))
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def duo_attention_paged(Q, cache, table, lens, heads, max_len=None, scale=None, out=None, ws=None):
+    """Attention of one query per sequence (Q: nseq x heads*head_dim) over its
+    first lens[s] cached tokens, whose pages are row s of table (both int32).
+    max_len: a bound of lens known to the caller (None: all that table holds)."""
+    n = Q.shape[0]
+    O = torch.empty((n, heads * cache.head_dim), dtype=torch.bfloat16, device=Q.device) if out is None else out
+    if max_len is None:
+        max_len = table.shape[1] * cache.page_size
+    if ws is None:
+        ws = attention_paged_workspace(n, heads, cache.kv_heads, cache.head_dim, max_len, Q.device)
+    _same_device(Q, cache.data, table, lens, O, ws)
+    _shape(Q, (n, heads * cache.head_dim), "Q")
+    _shape(O, Q.shape, "out")
+    _ints(lens, torch.int32, (n,), "lens")
+    if table.dtype != torch.int32:
+        raise TypeError("duo: table must be torch.int32")
+    _shape(table, (n, table.shape[1]), "table")
+    if max_len > table.shape[1] * cache.page_size:
+        raise ValueError("duo: table holds fewer than max_len tokens")
+    _check(lib().duo_attention_paged(_ptr(Q), _bf16_rows(Q, "Q"), ctypes.byref(cache.c), _ptr(table), _ld(table),
+                                     _ptr(lens), n, max_len, heads,
+                                     cache.head_dim ** -0.5 if scale is None else float(scale), _ptr(O),
+                                     _bf16_rows(O, "out"), _ptr(ws), ws.numel(), _stream(Q.device)),
+           "duo_attention_paged")
+    return O
