@@ -1,63 +1,669 @@
-// Attention of one query per sequence over the paged key-value cache.
+// Attention of one query per sequence over the paged key-value cache, split over
+// the cache's length and joined.
+//
+// The work is a list of tiles (32 cached tokens in 16 bits, 64 in 8 and 4) of rows,
+// a row being one sequence, one K/V head and up to 16 of its query heads.  Tiles of
+// all rows are counted through, and every workgroup takes an equal share of
+// consecutive tiles, wherever rows begin and end: sequences of any mix of lengths
+// load the CUs evenly, and no launch size depends on the lengths, which only the
+// device knows.  A workgroup's four waves take the tiles of a row in turn, each with
+// its own running maximum and sum, and join at the row's end; a row that lies in
+// one workgroup is finished there, the parts of one that does not go to the
+// workspace and are joined by a second launch.
+//
+// A wave computes transposed, with v_mfma_f32_16x16x32_bf16:
+//   S^T = K Q^T  (16 keys x 16 heads per instruction): a lane's scores belong to one
+//                head, and to the keys 16 b + 4 (lane / 16) + 0..3;
+//   O^T = V^T P^T: P^T's fragments are the lane's own probabilities (keys 4 g + 0..3
+//                of two blocks of 16), and V^T's take the same keys from the
+//                row-major tile with transposing LDS reads.
+// Heads that do not fill 16 columns waste matrix work only, of which there is
+// plenty: the bound is the cache's bytes.  Tiles go global -> LDS directly, and a
+// wave issues the next tile's K as soon as this one's K has been read into registers,
+// V likewise, so that one of the two is always in flight and one buffer for each
+// suffices (8 waves x 17 KB per CU at head_dim 128).  A wave needs no other wave for
+// that, so the loop has no barrier.
+//
+// 8 and 4 bits.  Codes keep what is added to them: a byte 0..255 converts to a bf16
+// number exactly, and a nibble n becomes 128 + n by setting its bits into 0x4300.
+// The excess (bias 128, 136) leaves again in the accumulator, which starts at
+// -bias sum(q) of the group for S and gets -bias sum(p) from one more MFMA for O.  A
+// score is the sum of its groups' products times their scales, in fp32; the scale
+// of V goes into the probability before that is rounded to bf16.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "cache.h"
 #include "internal.h"
 #include "mfma.h"
+#include "pingpong.h"
 
 using namespace duo;
+using namespace duo::pp;
 
 namespace {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) % 16) == 0; }
 
+constexpr int kCols = 16;       // query heads per row
+constexpr int kMaxWg = 1024;    // workgroups of a launch, at most
+constexpr int kMinTiles = 4;    // tiles per workgroup, at least
+constexpr int kMinKeys = 32;    // tokens of the smallest tile
+
 template <int FMT, int HD>
-__device__ float kv_number(const uint8_t* blk, int which, int shift, int row, int ch) {
-  const uint8_t* p = blk + kv_rows_at<FMT, HD>(which, shift) + row * KvFmt<FMT>::row(HD);
-  if constexpr (FMT == DUO_KV_BF16) {
-    return bf16_bits_to_f32(*(const uint16_t*)(p + 2 * ch));
-  } else {
-    const float s = bf16_bits_to_f32(*(const uint16_t*)(blk + kv_scales_at<FMT, HD>(which, shift) +
-                                                        row * KvFmt<FMT>::scales(HD) + ch / kKvGroup * 2));
-    const int n = FMT == DUO_KV_I8 ? p[ch] : p[ch / 2] >> (4 * (ch & 1)) & 15;
-    return (float)(n - KvFmt<FMT>::bias) * s;
+struct PagedGeo {
+  static constexpr int KEYS = FMT == DUO_KV_BF16 ? 32 : 64;
+  static constexpr int NB = KEYS / 16;                     // blocks of 16 keys
+  static constexpr int CK = HD / 32;                       // MFMA steps over head_dim, groups with a scale
+  static constexpr int RB = KvFmt<FMT>::row(HD), CH = RB / 16;
+  static constexpr int RPL = 64 / CH, NL = KEYS / RPL;     // rows per wave-wide load, loads per operand
+  static constexpr int SB = KvFmt<FMT>::scales(HD);
+  static constexpr int NS = (KEYS * SB + 255) / 256;       // loads of scales per operand
+  static constexpr int ROWS = KEYS * RB;                   // bytes of one operand's rows
+  static constexpr int WAVE = 2 * (ROWS + 2 * NS * 256);   // LDS of a wave; scales have two buffers
+  static constexpr int OLD = HD + 4;                       // row stride of the join's fp32 outputs
+  static_assert(kCols * OLD * 4 <= WAVE, "the join uses a wave's tile space");
+  static constexpr int WGS = 4 * WAVE > 40960 ? 2 : FMT != DUO_KV_BF16 ? 3 : 4;  // workgroups per CU: LDS, registers
+};
+
+// What both launches need to know of the work.
+struct PagedWork {
+  const int32_t* lens;
+  int nseq, max_len, rows;  // rows per sequence
+  int wgs;
+};
+
+// Tiles of all rows counted through.  cum[i]: tiles of one row of every sequence up to the
+// end of bucket i (`per` sequences each); *total of all of them, of one row each.
+struct Count {
+  int64_t cum[256];
+  int64_t wave[4];
+};
+
+__device__ inline int seq_len(const PagedWork& w, int s) { return min(max(w.lens[s], 0), w.max_len); }
+
+// 256 threads; ends with a barrier.
+template <int KEYS>
+__device__ inline void count_tiles(const PagedWork& w, Count& c, int per) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  int64_t n = 0;
+  for (int i = 0; i < per; ++i) {
+    const int64_t s = (int64_t)tid * per + i;
+    if (s < w.nseq) n += (seq_len(w, (int)s) + KEYS - 1) / KEYS;
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t up = __shfl_up(n, o);
+    if (lane >= o) n += up;
+  }
+  if (lane == 63) c.wave[tid >> 6] = n;
+  __syncthreads();
+  for (int i = 0; i < tid >> 6; ++i) n += c.wave[i];
+  c.cum[tid] = n;
+  __syncthreads();
+}
+
+// First tile of workgroup i of n, of `total` tiles.
+__device__ inline int64_t share(int64_t total, int n, int i) { return total * i / n; }
+
+__device__ inline int shares(int64_t total, int wgs) {
+  return (int)max((int64_t)1, min((int64_t)wgs, (total + kMinTiles - 1) / kMinTiles));
+}
+
+// max over the four lanes that hold one column
+__device__ __forceinline__ float col_max(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float col_sum(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+__device__ __forceinline__ float lo16(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float hi16(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+
+// Eight codes as bf16 with their bias: bytes in order; nibbles j and j + 4 in register j.
+__device__ __forceinline__ u32x4 widen8(uint32_t a, uint32_t b) {
+  auto f = [](uint32_t v, int i) { return (float)(v >> (8 * i) & 255u); };
+  return u32x4{pack_bf16(f(a, 0), f(a, 1)), pack_bf16(f(a, 2), f(a, 3)), pack_bf16(f(b, 0), f(b, 1)),
+               pack_bf16(f(b, 2), f(b, 3))};
+}
+__device__ __forceinline__ u32x4 widen4(uint32_t a) {
+  u32x4 r;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) r[j] = (a >> (4 * j) & 0x000f000fu) | 0x43004300u;
+  return r;
+}
+
+// Position of 16-byte chunk c of row r in an LDS tile, so that the rows that one
+// fragment read touches lie in different banks.
+template <int FMT, int CH>
+__device__ __forceinline__ int k_at(int r, int c) {
+  return c ^ (CH == 16 ? r & 15 : CH == 8 ? r >> 1 & 7 : CH == 4 ? r >> 2 & 3 : r >> 3 & 1);
+}
+template <int FMT, int CH>
+__device__ __forceinline__ int v_at(int r, int c) {
+  if constexpr (FMT == DUO_KV_BF16)  // 8 keys x 32 bytes at once
+    return c ^ (CH == 16 ? 2 * (r & 7) : 2 * (r >> 1 & 3));
+  else if constexpr (CH == 8)        // keys 0..7 and 16..23, or 8..15 and 24..31, x 16 bytes
+    return c ^ ((r >> 1 & 3) | (r >> 2 & 4));
+  else if constexpr (CH == 4)
+    return c ^ ((r >> 2 & 1) | (r >> 3 & 2));
+  else
+    return c ^ (r >> 4 & 1);
+}
+
+template <int FMT, int HD>
+__global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
+    const uint16_t* __restrict__ Q, int64_t ldq, KvGeo kv, const int32_t* __restrict__ table, int64_t ldt, PagedWork work,
+    int group, int cols, int per, float cexp, uint32_t flip, uint16_t* __restrict__ O, int64_t ldo,
+    float* __restrict__ part, int vec) {
+  using G = PagedGeo<FMT, HD>;
+  constexpr int KEYS = G::KEYS, NB = G::NB, CK = G::CK, RB = G::RB, CH = G::CH, RPL = G::RPL, NL = G::NL, NS = G::NS;
+  constexpr int NK = NL + NS;  // loads per operand and tile
+  constexpr bool QUANT = FMT != DUO_KV_BF16;
+  constexpr float BIAS = FMT == DUO_KV_I8 ? 128.f : 136.f;
+  extern __shared__ __attribute__((aligned(16))) uint8_t lsm[];
+  __shared__ Count cnt;
+  __shared__ float jm[4][kCols], jl[4][kCols];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int l16 = lane & 15, g = lane >> 4;
+
+  // sequences without tokens
+  for (int s = blockIdx.x; s < work.nseq; s += gridDim.x)
+    if (seq_len(work, s) == 0)
+      for (int e = tid; e < group * kv.heads * HD; e += 256) O[(int64_t)s * ldo + e] = 0;
+
+  count_tiles<KEYS>(work, cnt, per);
+  const int64_t total = cnt.cum[255] * work.rows;
+  const int n = shares(total, work.wgs);
+  if ((int)blockIdx.x >= n) return;
+  int64_t u = share(total, n, blockIdx.x);
+  const int64_t u1 = share(total, n, blockIdx.x + 1);
+  if (u >= u1) return;
+  const int64_t first_u = u;
+  // the sequence of tile u: its bucket (the first whose end lies behind u), then one by one
+  int s = 0;
+  int64_t before = 0;  // tiles of the sequences before s, all rows
+  {
+    int lo = 0, hi = 255;
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (cnt.cum[mid] * work.rows > u) hi = mid; else lo = mid + 1;
+    }
+    s = lo * per;
+    before = lo ? cnt.cum[lo - 1] * work.rows : 0;
+  }
+  uint8_t* const sK = lsm + wave * G::WAVE;
+  uint8_t* const sV = sK + G::ROWS;
+  uint8_t* const sS = sV + G::ROWS;  // scales: [parity of the tile's turn][K, V]
+
+  for (; u < u1; ++s) {
+    const int len = __builtin_amdgcn_readfirstlane(seq_len(work, s));
+    const int64_t tiles = (len + KEYS - 1) / KEYS;
+    if (before + tiles * work.rows <= u) {
+      before += tiles * work.rows;
+      continue;
+    }
+    const int32_t* const pages = table + (int64_t)s * ldt;
+    const int last_page = (len - 1) >> kv.shift;
+    for (; u < u1 && u < before + tiles * work.rows;) {
+      // one row, or what of it is in this share
+      const int row = (int)((u - before) / tiles);
+      const int t0 = (int)((u - before) % tiles);
+      const int t1 = (int)min(tiles, t0 + (u1 - u));
+      const int h = row % kv.heads, c0 = row / kv.heads * kCols;  // K/V head, first of its query heads
+      const int nc = min(cols, group - c0);
+      const uint16_t* const q = Q + (int64_t)s * ldq + (h * group + c0) * HD;
+      const uint8_t* const block0 = kv.data + h * kv.block;
+      const int64_t page_bytes = kv.heads * kv.block;
+
+      // Q^T's fragments, heads past the last as zeros; -bias sum(q) of every group
+      u32x4 qf[CK];
+      float qs[CK];
+#pragma unroll
+      for (int c = 0; c < CK; ++c) {
+        u32x4 v = {0u, 0u, 0u, 0u};
+        if (l16 < nc) v = *(const u32x4*)(q + l16 * HD + 32 * c + 8 * g);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] ^= flip;
+        if constexpr (QUANT) {
+          float t = 0.f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) t += lo16(v[j]) + hi16(v[j]);
+          qs[c] = -BIAS * col_sum(t);
+        }
+        if constexpr (FMT == DUO_KV_I4)  // channels j and j + 4 together, as widen4 gives them
+          v = u32x4{(v[0] & 0xffffu) | v[2] << 16, v[0] >> 16 | (v[2] & 0xffff0000u), (v[1] & 0xffffu) | v[3] << 16,
+                    v[1] >> 16 | (v[3] & 0xffff0000u)};
+        qf[c] = v;
+      }
+
+      // 64 pages of the table in one register, the next 64 in another
+      bool bad = false;
+      int win = 0, pid = 0, nid = 0;
+      auto ids = [&](int p) {
+        int id = pages[min(p + lane, last_page)];
+        const bool out = id < 0 || id >= kv.pages;
+        bad |= out;
+        return out ? 0 : id;
+      };
+      // this wave's loads of tile t's K (which = 0) or V rows and scales; K first
+      auto issue = [&](int t, auto which_c, uint8_t* rows, uint8_t* scales) {
+        constexpr int which = decltype(which_c)::value;
+        const int k0 = t * KEYS;
+        if (which == 0 && k0 >> kv.shift >= win + 64) {  // four tiles never reach further than the next window
+          pid = nid;
+          win += 64;
+          nid = ids(win + 64);
+        }
+        const int rows_at = kv_rows_at<FMT, HD>(which, kv.shift), scales_at = kv_scales_at<FMT, HD>(which, kv.shift);
+        const int mask = (1 << kv.shift) - 1;
+        auto chunk = [&](int r) {
+          const int p = lane % CH;
+          return 16 * (which ? v_at<FMT, CH>(r, p) : k_at<FMT, CH>(r, p));
+        };
+        if (k0 + KEYS <= len && RPL <= 16) {
+          // whole tile: each group of 16 keys lies in one page, the same for all lanes
+          const uint8_t* base[NB];
+          int in[NB];
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            const int key = k0 + 16 * b;
+            const int id = __builtin_amdgcn_readlane(pid, (key >> kv.shift) - win);
+            base[b] = block0 + id * page_bytes;
+            in[b] = key & mask;
+          }
+#pragma unroll
+          for (int i = 0; i < NL; ++i) {
+            const int r = i * RPL + lane / CH, b = i * RPL / 16;
+            const uint8_t* at = base[b] + (rows_at + in[b] * RB);
+            __builtin_amdgcn_global_load_lds((const void*)(at + (uint32_t)((r & 15) * RB + chunk(r))),
+                                             (__attribute__((address_space(3))) void*)(rows + i * 1024), 16, 0, 0);
+          }
+          if constexpr (QUANT) {
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+              constexpr int BPL = 256 / (16 * G::SB);  // blocks of 16 keys per load
+              const int bl = lane * 4 / (16 * G::SB);
+              const uint8_t* at = base[i * BPL] + (scales_at + in[i * BPL] * G::SB);
+#pragma unroll
+              for (int b = 1; b < BPL; ++b) {
+                const uint8_t* x = base[i * BPL + b] + (scales_at + in[i * BPL + b] * G::SB);
+                at = bl == b ? x : at;
+              }
+              __builtin_amdgcn_global_load_lds((const void*)(at + (uint32_t)(lane * 4 % (16 * G::SB))),
+                                               (__attribute__((address_space(3))) void*)(scales + i * 256), 4, 0, 0);
+            }
+          }
+        } else {
+          // the row's last tile: rows past its end are taken from its last token,
+          // whose numbers its result holds anyway
+          auto place = [&](int r) {
+            const int key = min(k0 + r, len - 1);
+            const int id = __shfl(pid, (key >> kv.shift) - win);
+            return std::make_pair(block0 + id * page_bytes, key & mask);
+          };
+#pragma unroll 1
+          for (int i = 0; i < NL; ++i) {
+            const int r = i * RPL + lane / CH;
+            const auto [b, in] = place(r);
+            __builtin_amdgcn_global_load_lds((const void*)(b + rows_at + in * RB + chunk(r)),
+                                             (__attribute__((address_space(3))) void*)(rows + i * 1024), 16, 0, 0);
+          }
+          if constexpr (QUANT) {
+#pragma unroll 1
+            for (int i = 0; i < NS; ++i) {
+              const int e = i * 256 + lane * 4;
+              const auto [b, in] = place(e / G::SB);
+              __builtin_amdgcn_global_load_lds((const void*)(b + scales_at + in * G::SB + e % G::SB),
+                                               (__attribute__((address_space(3))) void*)(scales + i * 256), 4, 0, 0);
+            }
+          }
+        }
+      };
+      constexpr std::integral_constant<int, 0> kK{};
+      constexpr std::integral_constant<int, 1> kV{};
+
+      float m = -INFINITY, mc = -INFINITY, l = 0.f;  // of this lane's column; l of its keys alone
+      f4 o[2 * CK];
+#pragma unroll
+      for (int d = 0; d < 2 * CK; ++d) o[d] = f4{0.f, 0.f, 0.f, 0.f};
+
+      int t = t0 + wave;
+      if (t < t1) {
+        win = (t * KEYS >> kv.shift) & ~3;  // a tile's pages, four at most, lie in one window
+        pid = ids(win);
+        nid = ids(win + 64);
+        issue(t, kK, sK, sS);
+        issue(t, kV, sV, sS + NS * 256);
+      }
+      for (uint8_t* sc = sS; t < t1; t += 4) {
+        const bool more = t + 4 < t1;
+        uint8_t* const sn = sc == sS ? sS + 2 * NS * 256 : sS;  // the next tile's scales
+        wait_vm<NK>();  // K of this tile
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        // ---- scores
+        float x[NB][4];
+        if constexpr (!QUANT) {
+          u32x4 kf[NB][CK];
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int c = 0; c < CK; ++c)
+              kf[b][c] = *(const u32x4*)(sK + (16 * b + l16) * RB + 16 * k_at<FMT, CH>(16 * b + l16, 4 * c + g));
+          wait_lds<0>();
+          if (more) issue(t + 4, kK, sK, sn);
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            f4 a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < CK; ++c) a = mma_bf16(kf[b][c], qf[c], a);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[b][r] = a[r];
+          }
+        } else {
+          uint2 kr[NB][CK];
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            const int r = 16 * b + l16;
+#pragma unroll
+            for (int c = 0; c < CK; ++c) {
+              if constexpr (FMT == DUO_KV_I8)
+                kr[b][c] = *(const uint2*)(sK + r * RB + 16 * k_at<FMT, CH>(r, 2 * c + g / 2) + 8 * (g & 1));
+              else
+                kr[b][c].x = *(const uint32_t*)(sK + r * RB + 16 * k_at<FMT, CH>(r, c) + 4 * g);
+            }
+          }
+          wait_lds<0>();
+          if (more) issue(t + 4, kK, sK, sn);
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            uint32_t ks[2 * CK];  // scales of the lane's four keys
+#pragma unroll
+            for (int j = 0; j < 2 * CK; j += 4) *(u32x4*)&ks[j] = *(const u32x4*)(sc + (16 * b + 4 * g) * G::SB + 4 * j);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[b][r] = 0.f;
+#pragma unroll
+            for (int c = 0; c < CK; ++c) {
+              const u32x4 kf = FMT == DUO_KV_I8 ? widen8(kr[b][c].x, kr[b][c].y) : widen4(kr[b][c].x);
+              const f4 a = mma_bf16(kf, qf[c], f4{qs[c], qs[c], qs[c], qs[c]});
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const uint32_t w = ks[(r * CK + c) / 2];
+                x[b][r] = fmaf((r * CK + c) & 1 ? hi16(w) : lo16(w), a[r], x[b][r]);
+              }
+            }
+          }
+        }
+        // ---- probabilities relative to the running maximum
+        const int left = len - t * KEYS;  // tokens of the row from this tile on
+        const bool tail = left < KEYS;
+        if (tail)
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (16 * b + 4 * g + r >= left) x[b][r] = -INFINITY;
+        float mt = x[0][0];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) mt = fmaxf(mt, x[b][r]);
+        mt = col_max(mt);
+        if (__any(mt > m)) {
+          const float mn = fmaxf(m, mt);
+          const float mcn = mn == -INFINITY ? -INFINITY : mn * cexp;
+          const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - mcn);
+          m = mn;
+          mc = mcn;
+          l *= f;
+#pragma unroll
+          for (int d = 0; d < 2 * CK; ++d)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[d][r] *= f;
+        }
+        const float base = m == -INFINITY ? 0.f : mc;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x[b][r] = __builtin_amdgcn_exp2f(fmaf(x[b][r], cexp, -base));
+        if (tail)
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (16 * b + 4 * g + r >= left) x[b][r] = 0.f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) l += x[b][r];
+        // ---- times V
+        if (more)
+          wait_vm<NK>();  // V of this tile; K of the next may be in flight
+        else
+          wait_vm<0>();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!QUANT) {
+          typedef __attribute__((address_space(3))) s16v4 lds4;
+          u32x4 vf[2 * CK];
+#pragma unroll
+          for (int d = 0; d < 2 * CK; ++d) {
+            // 16 lanes: four keys (by l16 / 4) x 16 channels
+            const int r0 = 4 * g + (l16 >> 2), r1 = r0 + 16, c = 2 * d + (l16 >> 1 & 1), e = 8 * (l16 & 1);
+            const s16v4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(sV + r0 * RB + 16 * v_at<FMT, CH>(r0, c) + e));
+            const s16v4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(sV + r1 * RB + 16 * v_at<FMT, CH>(r1, c) + e));
+            __builtin_memcpy(&vf[d], &a, 8);
+            __builtin_memcpy((char*)&vf[d] + 8, &b, 8);
+          }
+          wait_lds<0>();
+          if (more) issue(t + 4, kV, sV, sn + NS * 256);
+          const u32x4 pf = {pack_bf16(x[0][0], x[0][1]), pack_bf16(x[0][2], x[0][3]), pack_bf16(x[1][0], x[1][1]),
+                            pack_bf16(x[1][2], x[1][3])};
+#pragma unroll
+          for (int d = 0; d < 2 * CK; ++d) o[d] = mma_bf16(vf[d], pf, o[d]);
+        } else {
+          typedef int v2i __attribute__((ext_vector_type(2)));
+          typedef __attribute__((address_space(3))) v2i lds2;
+          v2i vr[FMT == DUO_KV_I8 ? 2 : 1][2 * CK];
+#pragma unroll
+          for (int d = 0; d < 2 * CK; ++d) {
+            if constexpr (FMT == DUO_KV_I8) {
+#pragma unroll
+              for (int st = 0; st < 2; ++st) {  // 16 lanes: eight keys (by l16 / 2) x 16 channels
+                const int i = l16 >> 1, r = 32 * st + (i < 4 ? 4 * g + i : 12 + 4 * g + i);
+                vr[st][d] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                    (lds2*)(sV + r * RB + 16 * v_at<FMT, CH>(r, d) + 8 * (l16 & 1)));
+              }
+            } else {  // 16 lanes: sixteen keys x 16 channels
+              const int i = l16 & 7, r = 32 * (l16 >> 3) + (i < 4 ? 4 * g + i : 12 + 4 * g + i);
+              vr[0][d] =
+                  __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds2*)(sV + r * RB + 16 * v_at<FMT, CH>(r, d / 2) + 8 * (d & 1)));
+            }
+          }
+          wait_lds<0>();
+          if (more) issue(t + 4, kV, sV, sn + NS * 256);
+          const uint32_t nb = pack_bf16(-BIAS, -BIAS);
+          const u32x4 bias = {nb, nb, nb, nb};
+#pragma unroll
+          for (int st = 0; st < 2; ++st) {
+            uint32_t vs[2][2 * CK];
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+              for (int j = 0; j < 2 * CK; j += 4)
+                *(u32x4*)&vs[b][j] = *(const u32x4*)(sc + NS * 256 + (32 * st + 16 * b + 4 * g) * G::SB + 4 * j);
+#pragma unroll
+            for (int c = 0; c < CK; ++c) {
+              float p[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const int b = 2 * st + (e >> 2), r = e & 3;
+                const uint32_t w = vs[e >> 2][(r * CK + c) / 2];
+                p[e] = x[b][r] * ((r * CK + c) & 1 ? hi16(w) : lo16(w));
+              }
+              u32x4 pf;
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                pf[j] = FMT == DUO_KV_I8 ? pack_bf16(p[2 * j], p[2 * j + 1]) : pack_bf16(p[j], p[j + 4]);
+#pragma unroll
+              for (int d = 2 * c; d < 2 * c + 2; ++d) {
+                const u32x4 vf = FMT == DUO_KV_I8 ? widen8((uint32_t)vr[st][d][0], (uint32_t)vr[st][d][1])
+                                                  : widen4((uint32_t)vr[0][d][st]);
+                o[d] = mma_bf16(vf, pf, mma_bf16(bias, pf, o[d]));
+              }
+            }
+          }
+        }
+        sc = sn;
+      }
+      // ---- the four waves joined: outputs relative to the largest maximum, added up in LDS
+#pragma unroll
+      for (int d = 0; d < 2 * CK; ++d) asm volatile("s_nop 7" : "+v"(o[d]));  // the last products have been written
+      if (__any(bad)) l = NAN;
+      l = col_sum(l);
+      if (g == 0) jm[wave][l16] = mc, jl[wave][l16] = l;
+      __syncthreads();
+      const float top = fmaxf(fmaxf(jm[0][l16], jm[1][l16]), fmaxf(jm[2][l16], jm[3][l16]));
+      {
+        const float f = mc == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - top);
+        float* y = (float*)sK + l16 * G::OLD + 4 * g;
+#pragma unroll
+        for (int d = 0; d < 2 * CK; ++d) {
+          // a wave without a finite score holds zeros, or NaN that has to stay
+          const f4 v = {o[d][0] * f, o[d][1] * f, o[d][2] * f, o[d][3] * f};
+          *(f4*)(y + 16 * d) = v;
+        }
+      }
+      __syncthreads();
+      const bool whole = t0 == 0 && t1 == tiles;
+      const int64_t slot = 2 * (int64_t)blockIdx.x + (u != first_u);
+      float* const ps = part + slot * cols * (HD + 2);
+      for (int e = tid; e < nc * (HD / 2); e += 256) {
+        const int c = e / (HD / 2), d = e % (HD / 2) * 2;
+        const float big = fmaxf(fmaxf(jm[0][c], jm[1][c]), fmaxf(jm[2][c], jm[3][c]));
+        float sum = 0.f, v0 = 0.f, v1 = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const float f = jm[w][c] == -INFINITY ? (jl[w][c] == 0.f ? 0.f : jl[w][c]) : __builtin_amdgcn_exp2f(jm[w][c] - big);
+          sum += jl[w][c] * f;
+          const float* y = (const float*)(lsm + w * G::WAVE) + c * G::OLD + d;
+          v0 += y[0];
+          v1 += y[1];
+        }
+        if (whole) {
+          uint16_t* const y = O + (int64_t)s * ldo + (h * group + c0 + c) * HD + d;
+          const uint32_t two = pack_bf16(v0 / sum, v1 / sum);
+          if (vec)
+            *(uint32_t*)y = two;
+          else
+            y[0] = (uint16_t)two, y[1] = (uint16_t)(two >> 16);
+        } else {
+          float* const y = ps + c * (HD + 2);
+          *(float2*)(y + d) = make_float2(v0, v1);
+          if (d == 0) *(float2*)(y + HD) = make_float2(big, sum);
+        }
+      }
+      __syncthreads();
+      u += t1 - t0;
+    }
+    before += tiles * work.rows;
   }
 }
 
-// One wave per sequence and head: lane l holds channels l and l + 64.
-template <int FMT, int HD>
-__global__ __launch_bounds__(64) void paged_plain_kernel(const uint16_t* __restrict__ Q, int64_t ldq, KvGeo g,
-                                                         const int32_t* __restrict__ table, int64_t ldt,
-                                                         const int32_t* __restrict__ lens, int max_len, int group,
-                                                         float scale, uint16_t* O, int64_t ldo) {
-  const int64_t s = blockIdx.x;
-  const int h = blockIdx.y, lane = threadIdx.x;
-  const int len = min(max(lens[s], 0), max_len);
-  constexpr int E = HD / 64;
-  float q[E], o[E];
-  for (int e = 0; e < E; ++e) q[e] = bf16_bits_to_f32(Q[s * ldq + h * HD + lane + 64 * e]), o[e] = 0.f;
-  float m = -INFINITY, l = 0.f;
-  for (int j = 0; j < len; ++j) {
-    const int page = table[s * ldt + (j >> g.shift)];
-    if (page < 0 || page >= g.pages) {
-      l = NAN;
-      break;
-    }
-    const uint8_t* blk = g.data + ((int64_t)page * g.heads + h / group) * g.block;
-    const int row = j & ((1 << g.shift) - 1);
-    float x = 0.f;
-    for (int e = 0; e < E; ++e) x = fmaf(q[e], kv_number<FMT, HD>(blk, 0, g.shift, row, lane + 64 * e), x);
-    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
-    x *= scale;
-    const float mn = fmaxf(m, x), base = mn == -INFINITY ? 0.f : mn;
-    const float f = expf(m - base), p = expf(x - base);
-    m = mn;
-    l = l * f + p;
-    for (int e = 0; e < E; ++e) o[e] = o[e] * f + p * kv_number<FMT, HD>(blk, 1, g.shift, row, lane + 64 * e);
+// Joins the parts of the rows that lie in several workgroups.  One workgroup of 256
+// threads per row and query head: weights of the parts first, then the outputs, two
+// parts (of head_dim 128; four of 64) per wave and load.
+template <int KEYS, int HD>
+__global__ __launch_bounds__(256) void paged_join_kernel(const float* __restrict__ part, PagedWork work, int kv_heads,
+                                                         int group, int cols, int per, uint16_t* __restrict__ O,
+                                                         int64_t ldo, int vec) {
+  __shared__ Count cnt;
+  __shared__ float wt[kMaxWg];
+  __shared__ float red[4];
+  __shared__ float acc[256 / (HD / 4)][HD];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int c = blockIdx.x % cols, row = blockIdx.x / cols % work.rows, s = blockIdx.x / cols / work.rows;
+  const int h = row % kv_heads, c0 = row / kv_heads * kCols;
+  if (c >= group - c0) return;
+  count_tiles<KEYS>(work, cnt, per);
+  const int64_t total = cnt.cum[255] * work.rows;
+  const int n = shares(total, work.wgs);
+  const int64_t tiles = (seq_len(work, s) + KEYS - 1) / KEYS;
+  if (tiles == 0) return;
+  const int bucket = s / per;
+  int64_t r0 = bucket ? cnt.cum[bucket - 1] : 0;
+  for (int i = bucket * per; i < s; ++i) r0 += (seq_len(work, i) + KEYS - 1) / KEYS;
+  r0 = r0 * work.rows + row * tiles;
+  const int64_t r1 = r0 + tiles;
+  // the shares of the row's first and last tile
+  auto owner = [&](int64_t u) {
+    int w = (int)(u * n / total);
+    while (w + 1 < n && share(total, n, w + 1) <= u) ++w;
+    while (w > 0 && share(total, n, w) > u) --w;
+    return w;
+  };
+  const int wa = owner(r0), wb = owner(r1 - 1);
+  if (wa == wb) return;
+  const int np = wb - wa + 1;
+  const int64_t stride = (int64_t)cols * (HD + 2);
+  const float* const p0 = part + (2 * (int64_t)wa + (share(total, n, wa) < r0)) * stride + c * (HD + 2);  // the first part
+  auto at = [&](int i) { return i ? part + 2 * (int64_t)(wa + i) * stride + c * (HD + 2) : p0; };
+  // weights
+  float top = -INFINITY;
+  for (int i = tid; i < np; i += 256) {
+    wt[i] = at(i)[HD];
+    top = fmaxf(top, wt[i]);
   }
-  for (int e = 0; e < E; ++e) O[s * ldo + h * HD + lane + 64 * e] = len > 0 ? f32_to_bf16_bits(o[e] / l) : (uint16_t)0;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  if (lane == 0) red[tid >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  __syncthreads();
+  float sum = 0.f;
+  for (int i = tid; i < np; i += 256) {
+    const float l = at(i)[HD + 1];
+    const float f = wt[i] == -INFINITY ? (l == 0.f ? 0.f : l) : __builtin_amdgcn_exp2f(wt[i] - top);
+    wt[i] = f;
+    sum += f * l;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  if (lane == 0) red[tid >> 6] = sum;
+  __syncthreads();
+  sum = (red[0] + red[1]) + (red[2] + red[3]);
+  // outputs
+  constexpr int T = HD / 4, NP = 256 / T;  // threads per part, parts at once
+  const int d = tid % T * 4, k = tid / T;
+  f4 a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = k; i < np; i += NP) {
+    const float2 v0 = *(const float2*)(at(i) + d), v1 = *(const float2*)(at(i) + d + 2);
+    a += f4{v0.x, v0.y, v1.x, v1.y} * wt[i];
+  }
+  *(f4*)&acc[k][d] = a;
+  __syncthreads();
+  if (tid < HD / 2) {
+    float y0 = 0.f, y1 = 0.f;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) y0 += acc[i][2 * tid], y1 += acc[i][2 * tid + 1];
+    const uint32_t two = pack_bf16(y0 / sum, y1 / sum);
+    uint16_t* const y = O + (int64_t)s * ldo + (h * group + c0 + c) * HD + 2 * tid;
+    if (vec)
+      *(uint32_t*)y = two;
+    else
+      y[0] = (uint16_t)two, y[1] = (uint16_t)(two >> 16);
+  }
 }
 
 }  // namespace
@@ -66,7 +672,13 @@ extern "C" {
 
 size_t duo_attention_paged_workspace_size(int64_t nseq, int64_t heads, int64_t kv_heads, int64_t head_dim,
                                           int64_t max_len) {
-  return 0;
+  if (nseq < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads || max_len < 1 || (head_dim != 64 && head_dim != 128))
+    return 0;
+  const int64_t group = heads / kv_heads, cols = std::min<int64_t>(group, kCols);
+  // parts: two per workgroup, and no more workgroups than tiles
+  const double tiles = (double)nseq * (double)(kv_heads * cdiv(group, kCols)) * (double)cdiv(max_len, kMinKeys);
+  const int64_t wgs = tiles < kMaxWg ? (int64_t)tiles : kMaxWg;
+  return align_up((size_t)(2 * wgs * cols * (head_dim + 2)) * sizeof(float));
 }
 
 duo_status duo_attention_paged(const void* Q, int64_t ldq, const duo_kv_cache* cache, const int32_t* table, int64_t ldt,
@@ -78,17 +690,36 @@ duo_status duo_attention_paged(const void* Q, int64_t ldq, const duo_kv_cache* c
   if (nseq < 0 || max_len < 0 || heads < 1 || heads > 65535 || heads % g.heads || !std::isfinite(scale) ||
       ldq < heads * hd || ldo < heads * hd || ldt < 0 || ldt < cdiv(max_len, cache->page_size))
     return DUO_ERR_INVALID_ARG;
-  if (nseq > INT32_MAX || max_len > INT32_MAX - 1024) return DUO_ERR_UNSUPPORTED;
+  const int64_t group = heads / g.heads, cols = std::min<int64_t>(group, kCols), rows = g.heads * cdiv(group, kCols);
+  if (nseq > INT32_MAX || max_len > INT32_MAX - 1024 || nseq * rows * cols > INT32_MAX) return DUO_ERR_UNSUPPORTED;
   if (nseq == 0) return DUO_OK;
   if (!Q || !O || !lens || (max_len > 0 && !table)) return DUO_ERR_INVALID_ARG;
   if (ldq % 8 || !aligned16(Q)) return DUO_ERR_UNSUPPORTED;
+  const size_t need = duo_attention_paged_workspace_size(nseq, heads, g.heads, hd, max_len);
+  if (need && (!ws || ws_bytes < need || reinterpret_cast<uintptr_t>(ws) % kAlign)) return DUO_ERR_WORKSPACE;
   if (duo_status d = device_ok(); d != DUO_OK) return d;
+  const hipStream_t s = (hipStream_t)stream;
+  // exp(x scale) = 2^(x cexp); a negative scale turns the queries' signs instead
+  const float cexp = (float)(std::fabs(scale) * 1.4426950408889634);
+  const uint32_t flip = scale < 0.0 ? 0x80008000u : 0u;
+  const int per = (int)cdiv(nseq, 256);
+  const int vec = ldo % 2 == 0 && reinterpret_cast<uintptr_t>(O) % 4 == 0;
   return kv_by_format(cache, [&](auto fmt, auto dim) -> duo_status {
     constexpr int FMT = decltype(fmt)::value, HD = decltype(dim)::value;
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(paged_plain_kernel<FMT, HD>), dim3((unsigned)nseq, (unsigned)heads), dim3(64), 0,
-                       (hipStream_t)stream, (const uint16_t*)Q, ldq, g, table, ldt, lens, (int)max_len,
-                       (int)(heads / g.heads), (float)scale, (uint16_t*)O, ldo);
+    using P = PagedGeo<FMT, HD>;
+    const double tiles = (double)nseq * (double)rows * (double)cdiv(max_len, P::KEYS);
+    const int wgs = (int)std::max(1.0, std::min(tiles, 256.0 * P::WGS));
+    const PagedWork w = {lens, (int)nseq, (int)max_len, (int)rows, wgs};
+    const auto kern = paged_kernel<FMT, HD>;
+    if (duo_status st = set_max_lds((const void*)kern, 4 * P::WAVE); st != DUO_OK) return st;
+    hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(256), 4 * P::WAVE, s, (const uint16_t*)Q, ldq, g, table, ldt, w,
+                       (int)group, (int)cols, per, cexp, flip, (uint16_t*)O, ldo, (float*)ws, vec);
     DUO_LAUNCH_CHECK();
+    if (max_len > P::KEYS && wgs > 1) {  // a row of one tile is never split
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(paged_join_kernel<P::KEYS, HD>), dim3((unsigned)(nseq * rows * cols)), dim3(256),
+                         0, s, (const float*)ws, w, g.heads, (int)group, (int)cols, per, (uint16_t*)O, ldo, vec);
+      DUO_LAUNCH_CHECK();
+    }
     return DUO_OK;
   });
 }
