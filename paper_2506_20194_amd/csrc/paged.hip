@@ -3,13 +3,13 @@
 //
 // The work is a list of tiles (32 cached tokens in 16 bits, 64 in 8 and 4) of rows,
 // a row being one sequence, one K/V head and up to 16 of its query heads.  Tiles of
-// all rows are counted through, and every workgroup takes an equal share of
-// consecutive tiles, wherever rows begin and end: sequences of any mix of lengths
-// load the CUs evenly, and no launch size depends on the lengths, which only the
-// device knows.  A workgroup's four waves take the tiles of a row in turn, each with
-// its own running maximum and sum, and join at the row's end; a row that lies in
-// one workgroup is finished there, the parts of one that does not go to the
-// workspace and are joined by a second launch.
+// all rows are counted through, with some more for what a row costs beside its
+// tiles, and every workgroup takes an equal share of the count, wherever rows begin
+// and end: sequences of any mix of lengths load the CUs evenly, and no launch size
+// depends on the lengths, which only the device knows.  A workgroup's four waves
+// take the tiles of a row in turn, each with its own running maximum and sum, and
+// join at the row's end; a row that lies in one share is finished there, the parts
+// of one that does not go to the workspace and are joined by a second launch.
 //
 // A wave computes transposed, with v_mfma_f32_16x16x32_bf16:
 //   S^T = K Q^T  (16 keys x 16 heads per instruction): a lane's scores belong to one
@@ -49,7 +49,8 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) % 16) == 
 
 constexpr int kCols = 16;       // query heads per row
 constexpr int kMaxWg = 1024;    // workgroups of a launch, at most
-constexpr int kMinTiles = 4;    // tiles per workgroup, at least
+constexpr int kRowCost = 4;     // what a row's start and end cost, in tiles
+constexpr int kMinShare = 8;    // smallest share, in tiles
 constexpr int kMinKeys = 32;    // tokens of the smallest tile
 
 template <int FMT, int HD>
@@ -68,30 +69,38 @@ struct PagedGeo {
   static constexpr int WGS = 4 * WAVE > 40960 ? 2 : FMT != DUO_KV_BF16 ? 3 : 4;  // workgroups per CU: LDS, registers
 };
 
-// What both launches need to know of the work.
+// The rows to do, and into how many shares at most.
 struct PagedWork {
   const int32_t* lens;
   int nseq, max_len, rows;  // rows per sequence
-  int wgs;
+  int per;                  // sequences per bucket of the count: ceil(nseq / 256)
 };
 
-// Tiles of all rows counted through.  cum[i]: tiles of one row of every sequence up to the
-// end of bucket i (`per` sequences each); *total of all of them, of one row each.
-struct Count {
-  int64_t cum[256];
-  int64_t wave[4];
+// A row that begins in a share and ends in another one: the join's task.  parts = 0: none.
+struct Task {
+  int seq, row, parts, pad;
 };
 
 __device__ inline int seq_len(const PagedWork& w, int s) { return min(max(w.lens[s], 0), w.max_len); }
 
-// 256 threads; ends with a barrier.
+// Tiles, and what counts for one row of them.
 template <int KEYS>
-__device__ inline void count_tiles(const PagedWork& w, Count& c, int per) {
+__device__ inline int tiles_of(int len) { return (len + KEYS - 1) / KEYS; }
+__device__ inline int cost_of(int tiles) { return tiles ? tiles + kRowCost : 0; }
+
+// cum[i]: cost of one row of every sequence up to the end of bucket i.  256 threads;
+// ends with a barrier.
+struct Count {
+  int64_t cum[256];
+  int64_t wave[4];
+};
+template <int KEYS>
+__device__ inline void count_rows(const PagedWork& w, Count& c) {
   const int tid = threadIdx.x, lane = tid & 63;
   int64_t n = 0;
-  for (int i = 0; i < per; ++i) {
-    const int64_t s = (int64_t)tid * per + i;
-    if (s < w.nseq) n += (seq_len(w, (int)s) + KEYS - 1) / KEYS;
+  for (int i = 0; i < w.per; ++i) {
+    const int64_t s = (int64_t)tid * w.per + i;
+    if (s < w.nseq) n += cost_of(tiles_of<KEYS>(seq_len(w, (int)s)));
   }
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -103,13 +112,6 @@ __device__ inline void count_tiles(const PagedWork& w, Count& c, int per) {
   for (int i = 0; i < tid >> 6; ++i) n += c.wave[i];
   c.cum[tid] = n;
   __syncthreads();
-}
-
-// First tile of workgroup i of n, of `total` tiles.
-__device__ inline int64_t share(int64_t total, int n, int i) { return total * i / n; }
-
-__device__ inline int shares(int64_t total, int wgs) {
-  return (int)max((int64_t)1, min((int64_t)wgs, (total + kMinTiles - 1) / kMinTiles));
 }
 
 // max over the four lanes that hold one column
@@ -163,7 +165,7 @@ __device__ __forceinline__ int v_at(int r, int c) {
 template <int FMT, int HD>
 __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
     const uint16_t* __restrict__ Q, int64_t ldq, KvGeo kv, const int32_t* __restrict__ table, int64_t ldt, PagedWork work,
-    int group, int cols, int per, float cexp, uint32_t flip, uint16_t* __restrict__ O, int64_t ldo,
+    int group, int cols, float cexp, uint32_t flip, uint16_t* __restrict__ O, int64_t ldo, Task* __restrict__ tasks,
     float* __restrict__ part, int vec) {
   using G = PagedGeo<FMT, HD>;
   constexpr int KEYS = G::KEYS, NB = G::NB, CK = G::CK, RB = G::RB, CH = G::CH, RPL = G::RPL, NL = G::NL, NS = G::NS;
@@ -181,44 +183,42 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
     if (seq_len(work, s) == 0)
       for (int e = tid; e < group * kv.heads * HD; e += 256) O[(int64_t)s * ldo + e] = 0;
 
-  count_tiles<KEYS>(work, cnt, per);
+  if (tid == 0 && tasks) tasks[blockIdx.x].parts = 0;
+
+  count_rows<KEYS>(work, cnt);
   const int64_t total = cnt.cum[255] * work.rows;
-  const int n = shares(total, work.wgs);
+  const int n = (int)min((int64_t)gridDim.x, (total + kMinShare - 1) / kMinShare);
   if ((int)blockIdx.x >= n) return;
-  int64_t u = share(total, n, blockIdx.x);
-  const int64_t u1 = share(total, n, blockIdx.x + 1);
-  if (u >= u1) return;
-  const int64_t first_u = u;
-  // the sequence of tile u: its bucket (the first whose end lies behind u), then one by one
-  int s = 0;
-  int64_t before = 0;  // tiles of the sequences before s, all rows
-  {
-    int lo = 0, hi = 255;
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      if (cnt.cum[mid] * work.rows > u) hi = mid; else lo = mid + 1;
-    }
-    s = lo * per;
-    before = lo ? cnt.cum[lo - 1] * work.rows : 0;
+  // share i of n: [total i / n, total (i + 1) / n)
+  int64_t u = total * blockIdx.x / n;
+  const int64_t u1 = total * (blockIdx.x + 1) / n;
+  // the sequence of u: its bucket (the first whose end lies behind u), then one by one
+  int lo = 0;
+  for (int hi = 255; lo < hi;) {
+    const int mid = (lo + hi) / 2;
+    if (cnt.cum[mid] * work.rows > u) hi = mid; else lo = mid + 1;
   }
+  int64_t before = lo ? cnt.cum[lo - 1] * work.rows : 0;  // cost of the sequences before s
   uint8_t* const sK = lsm + wave * G::WAVE;
   uint8_t* const sV = sK + G::ROWS;
   uint8_t* const sS = sV + G::ROWS;  // scales: [parity of the tile's turn][K, V]
 
-  for (; u < u1; ++s) {
+  for (int s = lo * work.per; u < u1; ++s) {
     const int len = __builtin_amdgcn_readfirstlane(seq_len(work, s));
-    const int64_t tiles = (len + KEYS - 1) / KEYS;
-    if (before + tiles * work.rows <= u) {
-      before += tiles * work.rows;
-      continue;
-    }
+    const int tiles = tiles_of<KEYS>(len), cost = cost_of(tiles);
+    const int64_t start = before;
+    before += (int64_t)cost * work.rows;
+    if (before <= u) continue;
     const int32_t* const pages = table + (int64_t)s * ldt;
     const int last_page = (len - 1) >> kv.shift;
-    for (; u < u1 && u < before + tiles * work.rows;) {
+    while (u < u1 && u < before) {
       // one row, or what of it is in this share
-      const int row = (int)((u - before) / tiles);
-      const int t0 = (int)((u - before) % tiles);
-      const int t1 = (int)min(tiles, t0 + (u1 - u));
+      const int row = (int)((u - start) / cost), at = (int)((u - start) % cost);
+      const int here = (int)min((int64_t)(cost - at), u1 - u);
+      const int t0 = max(at - kRowCost, 0), t1 = max(at + here - kRowCost, 0);
+      const int64_t row_end = u + (cost - at);
+      u += here;
+      if (t0 >= t1) continue;
       const int h = row % kv.heads, c0 = row / kv.heads * kCols;  // K/V head, first of its query heads
       const int nc = min(cols, group - c0);
       const uint16_t* const q = Q + (int64_t)s * ldq + (h * group + c0) * HD;
@@ -545,9 +545,14 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
         }
       }
       __syncthreads();
+      // a share has at most one row that began before it, and one that ends after it
       const bool whole = t0 == 0 && t1 == tiles;
-      const int64_t slot = 2 * (int64_t)blockIdx.x + (u != first_u);
-      float* const ps = part + slot * cols * (HD + 2);
+      float* const ps = part + (2 * (int64_t)blockIdx.x + (t0 == 0)) * cols * (HD + 2);
+      if (!whole && t0 == 0 && tid == 0) {
+        int last = (int)((row_end - 1) * n / total);  // the share of the row's last tile
+        while (total * (last + 1) / n < row_end) ++last;
+        tasks[blockIdx.x] = Task{s, row, last - (int)blockIdx.x + 1, 0};
+      }
       for (int e = tid; e < nc * (HD / 2); e += 256) {
         const int c = e / (HD / 2), d = e % (HD / 2) * 2;
         const float big = fmaxf(fmaxf(jm[0][c], jm[1][c]), fmaxf(jm[2][c], jm[3][c]));
@@ -574,96 +579,79 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
         }
       }
       __syncthreads();
-      u += t1 - t0;
     }
-    before += tiles * work.rows;
   }
 }
 
-// Joins the parts of the rows that lie in several workgroups.  One workgroup of 256
-// threads per row and query head: weights of the parts first, then the outputs, two
-// parts (of head_dim 128; four of 64) per wave and load.
-template <int KEYS, int HD>
-__global__ __launch_bounds__(256) void paged_join_kernel(const float* __restrict__ part, PagedWork work, int kv_heads,
-                                                         int group, int cols, int per, uint16_t* __restrict__ O,
+// Joins the parts of the rows that lie in several shares: one workgroup for two heads of
+// the row that begins in share blockIdx.x, if any does and ends in another: its own part
+// (the second of its two places), then the first places of the shares after it.
+template <int HD>
+__global__ __launch_bounds__(256) void paged_join_kernel(const Task* __restrict__ tasks, const float* __restrict__ part,
+                                                         int kv_heads, int group, int cols, uint16_t* __restrict__ O,
                                                          int64_t ldo, int vec) {
-  __shared__ Count cnt;
-  __shared__ float wt[kMaxWg];
-  __shared__ float red[4];
-  __shared__ float acc[256 / (HD / 4)][HD];
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int c = blockIdx.x % cols, row = blockIdx.x / cols % work.rows, s = blockIdx.x / cols / work.rows;
-  const int h = row % kv_heads, c0 = row / kv_heads * kCols;
-  if (c >= group - c0) return;
-  count_tiles<KEYS>(work, cnt, per);
-  const int64_t total = cnt.cum[255] * work.rows;
-  const int n = shares(total, work.wgs);
-  const int64_t tiles = (seq_len(work, s) + KEYS - 1) / KEYS;
-  if (tiles == 0) return;
-  const int bucket = s / per;
-  int64_t r0 = bucket ? cnt.cum[bucket - 1] : 0;
-  for (int i = bucket * per; i < s; ++i) r0 += (seq_len(work, i) + KEYS - 1) / KEYS;
-  r0 = r0 * work.rows + row * tiles;
-  const int64_t r1 = r0 + tiles;
-  // the shares of the row's first and last tile
-  auto owner = [&](int64_t u) {
-    int w = (int)(u * n / total);
-    while (w + 1 < n && share(total, n, w + 1) <= u) ++w;
-    while (w > 0 && share(total, n, w) > u) --w;
-    return w;
-  };
-  const int wa = owner(r0), wb = owner(r1 - 1);
-  if (wa == wb) return;
-  const int np = wb - wa + 1;
+  constexpr int T = HD / 4, NP = 128 / T;  // threads per part and head, parts at once
+  __shared__ float wt[2][kMaxWg];
+  __shared__ float red[2][2][2];
+  __shared__ float acc[2][NP][HD];
+  const Task task = tasks[blockIdx.x];
+  if (task.parts == 0) return;
+  const int tid = threadIdx.x & 127, j = threadIdx.x >> 7;  // j: which of the two heads
+  const int row = task.row, np = task.parts, h = row % kv_heads, c0 = row / kv_heads * kCols;
+  const int c = blockIdx.y * 2 + j, live = c < min(cols, group - c0);
   const int64_t stride = (int64_t)cols * (HD + 2);
-  const float* const p0 = part + (2 * (int64_t)wa + (share(total, n, wa) < r0)) * stride + c * (HD + 2);  // the first part
-  auto at = [&](int i) { return i ? part + 2 * (int64_t)(wa + i) * stride + c * (HD + 2) : p0; };
+  const float* const p0 = part + 2 * (int64_t)blockIdx.x * stride + (live ? c : 0) * (HD + 2);
+  auto at = [&](int i) { return p0 + (i ? 2 * i : 1) * stride; };
   // weights
   float top = -INFINITY;
-  for (int i = tid; i < np; i += 256) {
-    wt[i] = at(i)[HD];
-    top = fmaxf(top, wt[i]);
+  for (int i = tid; i < np; i += 128) {
+    wt[j][i] = at(i)[HD];
+    top = fmaxf(top, wt[j][i]);
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  if (lane == 0) red[tid >> 6] = top;
+  if (tid % 64 == 0) red[0][j][tid >> 6] = top;
   __syncthreads();
-  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  __syncthreads();
+  top = fmaxf(red[0][j][0], red[0][j][1]);
   float sum = 0.f;
-  for (int i = tid; i < np; i += 256) {
+  for (int i = tid; i < np; i += 128) {
     const float l = at(i)[HD + 1];
-    const float f = wt[i] == -INFINITY ? (l == 0.f ? 0.f : l) : __builtin_amdgcn_exp2f(wt[i] - top);
-    wt[i] = f;
+    const float f = wt[j][i] == -INFINITY ? (l == 0.f ? 0.f : l) : __builtin_amdgcn_exp2f(wt[j][i] - top);
+    wt[j][i] = f;
     sum += f * l;
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-  if (lane == 0) red[tid >> 6] = sum;
+  if (tid % 64 == 0) red[1][j][tid >> 6] = sum;
   __syncthreads();
-  sum = (red[0] + red[1]) + (red[2] + red[3]);
+  sum = red[1][j][0] + red[1][j][1];
   // outputs
-  constexpr int T = HD / 4, NP = 256 / T;  // threads per part, parts at once
   const int d = tid % T * 4, k = tid / T;
   f4 a = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
   for (int i = k; i < np; i += NP) {
     const float2 v0 = *(const float2*)(at(i) + d), v1 = *(const float2*)(at(i) + d + 2);
-    a += f4{v0.x, v0.y, v1.x, v1.y} * wt[i];
+    a += f4{v0.x, v0.y, v1.x, v1.y} * wt[j][i];
   }
-  *(f4*)&acc[k][d] = a;
+  *(f4*)&acc[j][k][d] = a;
   __syncthreads();
-  if (tid < HD / 2) {
+  if (tid < HD / 2 && live) {
     float y0 = 0.f, y1 = 0.f;
 #pragma unroll
-    for (int i = 0; i < NP; ++i) y0 += acc[i][2 * tid], y1 += acc[i][2 * tid + 1];
+    for (int i = 0; i < NP; ++i) y0 += acc[j][i][2 * tid], y1 += acc[j][i][2 * tid + 1];
     const uint32_t two = pack_bf16(y0 / sum, y1 / sum);
-    uint16_t* const y = O + (int64_t)s * ldo + (h * group + c0 + c) * HD + 2 * tid;
+    uint16_t* const y = O + (int64_t)task.seq * ldo + (h * group + c0 + c) * HD + 2 * tid;
     if (vec)
       *(uint32_t*)y = two;
     else
       y[0] = (uint16_t)two, y[1] = (uint16_t)(two >> 16);
   }
+}
+
+// Workgroups for rows of at most `tiles` tiles: no more than smallest shares.
+int64_t paged_wgs(double rows, int64_t tiles, int most) {
+  const double cost = tiles ? rows * (double)(tiles + kRowCost) / kMinShare : 1.0;
+  return cost < most ? std::max<int64_t>(1, (int64_t)std::ceil(cost)) : most;
 }
 
 }  // namespace
@@ -675,10 +663,9 @@ size_t duo_attention_paged_workspace_size(int64_t nseq, int64_t heads, int64_t k
   if (nseq < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads || max_len < 1 || (head_dim != 64 && head_dim != 128))
     return 0;
   const int64_t group = heads / kv_heads, cols = std::min<int64_t>(group, kCols);
-  // parts: two per workgroup, and no more workgroups than tiles
-  const double tiles = (double)nseq * (double)(kv_heads * cdiv(group, kCols)) * (double)cdiv(max_len, kMinKeys);
-  const int64_t wgs = tiles < kMaxWg ? (int64_t)tiles : kMaxWg;
-  return align_up((size_t)(2 * wgs * cols * (head_dim + 2)) * sizeof(float));
+  // one task and two parts per workgroup
+  const int64_t wgs = paged_wgs((double)nseq * (double)(kv_heads * cdiv(group, kCols)), cdiv(max_len, kMinKeys), kMaxWg);
+  return align_up(wgs * sizeof(Task)) + align_up((size_t)(2 * wgs * cols * (head_dim + 2)) * sizeof(float));
 }
 
 duo_status duo_attention_paged(const void* Q, int64_t ldq, const duo_kv_cache* cache, const int32_t* table, int64_t ldt,
@@ -702,22 +689,22 @@ duo_status duo_attention_paged(const void* Q, int64_t ldq, const duo_kv_cache* c
   // exp(x scale) = 2^(x cexp); a negative scale turns the queries' signs instead
   const float cexp = (float)(std::fabs(scale) * 1.4426950408889634);
   const uint32_t flip = scale < 0.0 ? 0x80008000u : 0u;
-  const int per = (int)cdiv(nseq, 256);
   const int vec = ldo % 2 == 0 && reinterpret_cast<uintptr_t>(O) % 4 == 0;
   return kv_by_format(cache, [&](auto fmt, auto dim) -> duo_status {
     constexpr int FMT = decltype(fmt)::value, HD = decltype(dim)::value;
     using P = PagedGeo<FMT, HD>;
-    const double tiles = (double)nseq * (double)rows * (double)cdiv(max_len, P::KEYS);
-    const int wgs = (int)std::max(1.0, std::min(tiles, 256.0 * P::WGS));
-    const PagedWork w = {lens, (int)nseq, (int)max_len, (int)rows, wgs};
+    const int64_t wgs = paged_wgs((double)nseq * (double)rows, cdiv(max_len, P::KEYS), 256 * P::WGS);
+    const PagedWork w = {lens, (int)nseq, (int)max_len, (int)rows, (int)cdiv(nseq, 256)};
+    Task* const tasks = (Task*)ws;
+    float* const part = (float*)((uint8_t*)ws + align_up(wgs * sizeof(Task)));
     const auto kern = paged_kernel<FMT, HD>;
     if (duo_status st = set_max_lds((const void*)kern, 4 * P::WAVE); st != DUO_OK) return st;
     hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(256), 4 * P::WAVE, s, (const uint16_t*)Q, ldq, g, table, ldt, w,
-                       (int)group, (int)cols, per, cexp, flip, (uint16_t*)O, ldo, (float*)ws, vec);
+                       (int)group, (int)cols, cexp, flip, (uint16_t*)O, ldo, max_len > 0 ? tasks : nullptr, part, vec);
     DUO_LAUNCH_CHECK();
     if (max_len > P::KEYS && wgs > 1) {  // a row of one tile is never split
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(paged_join_kernel<P::KEYS, HD>), dim3((unsigned)(nseq * rows * cols)), dim3(256),
-                         0, s, (const float*)ws, w, g.heads, (int)group, (int)cols, per, (uint16_t*)O, ldo, vec);
+      hipLaunchKernelGGL(paged_join_kernel<HD>, dim3((unsigned)wgs, (unsigned)cdiv(cols, 2)), dim3(256), 0, s,
+                         (const Task*)tasks, (const float*)part, g.heads, (int)group, (int)cols, (uint16_t*)O, ldo, vec);
       DUO_LAUNCH_CHECK();
     }
     return DUO_OK;
