@@ -16,13 +16,13 @@
 // they then stay below 2^8, which costs no accuracy in fp32 or bf16.
 //
 // Unseen keys get probability 0, and 0 times a value that is not finite would not be
-// 0: tiles in which some query does not see some key are searched for such values,
-// and where there are any they enter as zeros, and what is seen of them is counted with
-// two more products (see poison).
+// 0: in the steps where some query does not see some key such values enter as zeros,
+// and the queries that do see them get them added at the end.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
 
+#include "dma.h"
 #include "internal.h"
 #include "mfma.h"
 #include "pingpong.h"
@@ -99,11 +99,12 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
   constexpr int DB = HD / 32;           // 32-wide blocks of the output row
   constexpr int TILE = KB * CH;         // chunks per operand tile
   constexpr int NL = TILE / (64 * NW);  // 16-byte loads per thread, operand and tile
+  constexpr int RPL = 64 / CH;          // keys per wave-wide load
   constexpr int QB = 32 * NW;
   __shared__ u32x4 sm[2][2][TILE];      // [buffer][K, V]
   int head, block, s, qb;
   if (!place(blockIdx.x, a, &head, &block) || !find<QB>(a, block, &s, &qb)) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, half = lane >> 5;
   const int q_first = cut(a.cu_q[s], a.total_q), lq = cut(a.cu_q[s + 1], a.total_q) - q_first;
   const int k_first = cut(a.cu_k[s], a.total_k), lk = max(cut(a.cu_k[s + 1], a.total_k) - k_first, 0);
@@ -129,14 +130,17 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
   }
   const int seen = min(q0 + QB, lq) + off;  // keys that the block's last query sees
   const int nkb = (seen + KB - 1) / KB;     // <= 0: none
-  auto issue = [&](const uint16_t* src, int64_t ld, int kb, u32x4* dst, bool is_v) {
+  // this wave's part of tile kb of K (or V), keys past the last as the last
+  auto issue = [&](const uint16_t* src, int64_t ld, int kb, const u32x4* dst, bool is_v) __attribute__((always_inline)) {
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds_addr(dst + wave * NL * 64));
+    const uint16_t* const tile = src + (int64_t)kb * KB * ld;
+    const int left = lk - 1 - kb * KB;  // the last key's place in the tile
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int base = (wave * NL + i) * 64;  // wave-uniform destination
-      const int key = (base + lane) / CH, p = (base + lane) % CH;
-      const int64_t at = (int64_t)min(kb * KB + key, lk - 1) * ld;
-      __builtin_amdgcn_global_load_lds((const void*)(src + at + 8 * (is_v ? vswz(key, p) : kswz(key, p))),
-                                       (__attribute__((address_space(3))) void*)(dst + base), 16, 0, 0);
+      const int key = (wave * NL + i) * RPL + lane / CH, p = lane % CH;
+      const int row = left >= KB ? key : min(key, left);
+      const int c = is_v ? vswz(key, p) : kswz(key, p);
+      dma16(tile, (uint32_t)row * (uint32_t)(ld * 2) + 16 * c, to + i * 1024);
     }
   };
 
@@ -161,137 +165,196 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
     __builtin_memcpy((char*)&v + 8, &v1, 8);
     return v;
   };
-  auto key_of = [&](int b, int r) { return 32 * b + 8 * (r >> 2) + 4 * half + (r & 3); };
+  // Steps of 32 keys, two per tile.  This wave: steps of which its queries see a key, and of
+  // which they see every key.
+  const int nu = qw < lq && qw + 31 + off >= 0 ? min((qw + 31 + off) / 32 + 1, 2 * nkb) : 0;
+  const int nfull = max((qw + off + 1) / 32, 0);
+  auto key_of = [&](int r) { return 8 * (r >> 2) + 4 * half + (r & 3); };
+
+  f16x sa, sb;  // scores of an even and of an odd step
+  u32x4 pf[2];  // probabilities of a step
+  auto k_rows = [&](int u) { return (const u32x4*)sm[u >> 1 & 1][0] + (u & 1) * 32 * CH; };
+  auto v_rows = [&](int u) { return (const uint8_t*)sm[u >> 1 & 1][1] + (u & 1) * 32 * HD * 2; };
+  auto read_k = [&](const u32x4* sK, int c) { return sK[l32 * CH + kswz(l32, 2 * c + half)]; };
+  auto score = [&](int u, f16x& sc) __attribute__((always_inline)) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[r] = 0.f;
+#pragma unroll
+    for (int c = 0; c < KS; ++c) sc = mma32_bf16(read_k(k_rows(u), c), qa[c], sc);
+  };
+  // a new reference where the step's scores leave the old one's range: the factor of what is
+  // relative to the old one (1 elsewhere), and whether any lane has one
+  auto refer = [&](const f16x& sc, float* f) __attribute__((always_inline)) {
+    float mt = sc[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mt = fmaxf(mt, sc[r]);
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
+    mt = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+    const bool up = mt > m && !(mt * a.cexp <= mc + 8.f);
+    if (!__any(up)) return false;
+    const float mcn = up ? mt * a.cexp : mc;
+    *f = up ? m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - mcn) : 1.f;
+    m = up ? mt : m;
+    mc = mcn;
+    l *= *f;
+    return true;
+  };
+  auto scale_o = [&](float f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int d = 0; d < DB; ++d) asm volatile("s_nop 15" : "+v"(o[d]));  // the last products have been written
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] *= f;
+  };
+  // O += V^T P^T of step u
+  uint32_t poison = 0;
+  auto add = [&](int u) __attribute__((always_inline)) {
+    const uint8_t* sV = v_rows(u);
+    if (u < nfull) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[d] = mma32_bf16(read_v(sV, t, d), pf[t], o[d]);
+    } else {  // some query does not see some key: numbers that are not finite enter as zeros
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          u32x4 v = read_v(sV, t, d);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t bad = ((v[j] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;  // exponent all ones
+            poison |= bad;
+            v[j] &= ~((bad >> 15) * 0xffffu);
+          }
+          o[d] = mma32_bf16(v, pf[t], o[d]);
+        }
+    }
+  };
+  // Step u's probabilities, the values of the step before and the scores of the next are
+  // independent of each other.  Where all three are there and nothing is masked they are
+  // dealt out evenly: MFMAs of the one, LDS reads and vector instructions of the others.
+  auto fast = [&](auto place, f16x& sc, f16x& sn) __attribute__((always_inline)) {
+    constexpr int P = decltype(place)::value;  // the step's place in two tiles, as its LDS buffers go by it
+    float f = 1.f;
+    const bool moved = refer(sc, &f);
+    const float base = m == -INFINITY ? 0.f : mc;
+    const u32x4* sK = k_rows(P + 1);
+    const uint8_t* sV = v_rows(P + 3);
+    u32x4 pn[2];
+    float ls[2] = {0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sn[r] = 0.f;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int r = 8 * t + 2 * j;
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[r], a.cexp, -base));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[r + 1], a.cexp, -base));
+        ls[0] += p0;
+        ls[1] += p1;
+        pn[t][j] = pack_bf16(p0, p1);
+      }
+#pragma unroll
+      for (int i = 0; i < KS / 2; ++i) {
+        const int c = t * (KS / 2) + i;
+        sn = mma32_bf16(read_k(sK, c), qa[c], sn);
+        if (i < DB) o[i] = mma32_bf16(read_v(sV, t, i), pf[t], o[i]);
+      }
+    }
+    l += ls[0] + ls[1];
+    pf[0] = pn[0];
+    pf[1] = pn[1];
+    asm volatile("" : "+v"(pf[0]), "+v"(pf[1]), "+v"(l));  // computed here, not where they are used
+    __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+    for (int i = 0; i < DB + KS / 2; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, HD == 128 ? 4 : 8, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, HD == 128 ? 3 : 6, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (moved) scale_o(f);
+  };
+  auto slow = [&](int u, f16x& sc, f16x& sn) __attribute__((always_inline)) {
+    if (u > 0 && u <= nu) add(u - 1);
+    if (u < nu) {
+      const int see = qw + l32 + off - u * 32;
+      if (u >= nfull)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[r] = key_of(r) > see ? -INFINITY : sc[r];
+      float f;
+      if (refer(sc, &f)) scale_o(f);
+      const float base = m == -INFINITY ? 0.f : mc;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(sc[r], a.cexp, -base));
+        sc[r] = u >= nfull && key_of(r) > see ? 0.f : p;  // also where a scale of 0 makes -inf NaN
+        l += sc[r];
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) pf[t][j] = pack_bf16(sc[8 * t + 2 * j], sc[8 * t + 2 * j + 1]);
+      if (u + 1 < nu) score(u + 1, sn);
+    }
+  };
 
   if (nkb > 0) {
     issue(Kh, a.ldk, 0, sm[0][0], false);
+    issue(Kh, a.ldk, min(1, nkb - 1), sm[1][0], false);
     issue(Vh, a.ldv, 0, sm[0][1], true);
+    wait_vm<2 * NL>();
+    lds_barrier();
+    if (nu > 0) score(0, sa);
   }
-  for (int kb = 0; kb < nkb; ++kb) {
-    wait_vm<0>();   // this wave's part of the tiles landed
-    lds_barrier();  // every wave's; and every wave is done with the tiles before
-    if (kb + 1 < nkb) {
-      issue(Kh, a.ldk, kb + 1, sm[(kb + 1) & 1][0], false);
-      issue(Vh, a.ldv, kb + 1, sm[(kb + 1) & 1][1], true);
-    }
-    if (kb * KB > qw + 31 + off) continue;  // uniform per wave: every key lies above its queries
-    const u32x4* sK = sm[kb & 1][0];
-    const uint8_t* sV = (const uint8_t*)sm[kb & 1][1];
-    f16x sc[2];
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) sc[b][r] = 0.f;
-      const int key = 32 * b + l32;
-#pragma unroll
-      for (int c = 0; c < KS; ++c) sc[b] = mma32_bf16(sK[key * CH + kswz(key, 2 * c + half)], qa[c], sc[b]);
-    }
-    const bool masked = kb * KB + KB - 1 > qw + off;  // uniform per wave: some query does not see some key
-    const int see = qw + l32 + off - kb * KB;         // this lane's query sees keys 0 .. see of the tile
-    if (masked) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (key_of(b, r) > see) sc[b][r] = -INFINITY;
-    }
-    float mt = sc[0][0];
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mt = fmaxf(mt, sc[b][r]);
-    {
-      const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
-      mt = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
-    }
-    // a new reference where the scores leave the old one's range
-    if (__any(mt > m && !(mt * a.cexp <= mc + 8.f))) {
-      const bool up = mt > m && !(mt * a.cexp <= mc + 8.f);
-      const float mcn = up ? mt * a.cexp : mc;
-      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - mcn);
-      m = up ? mt : m;
-      mc = mcn;
-      l = m == -INFINITY ? l : l * f;
-#pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[d][r] *= f;
-    }
-    const float base = m == -INFINITY ? 0.f : mc;
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) sc[b][r] = __builtin_amdgcn_exp2f(fmaf(sc[b][r], a.cexp, -base));
-    bool poison = false;
-    if (masked) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (key_of(b, r) > see) sc[b][r] = 0.f;
-      uint32_t any = 0;
-#pragma unroll
-      for (int i = 0; i < TILE / 64; ++i) {
-        const u32x4 v = ((const u32x4*)sV)[i * 64 + lane];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) any |= ((v[j] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;  // exponent all ones
-      }
-      poison = __any(any != 0);
-    }
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) l += sc[b][r];
-    u32x4 pf[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) pf[t][j] = pack_bf16(sc[t >> 1][8 * (t & 1) + 2 * j], sc[t >> 1][8 * (t & 1) + 2 * j + 1]);
-    if (!poison) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int d = 0; d < DB; ++d) o[d] = mma32_bf16(read_v(sV, t, d), pf[t], o[d]);
-    } else {
-      // values that are not finite as zeros, and, for every output, how many of them its
-      // query sees (n) and their signs' sum (c): n of one sign give that infinity,
-      // both signs or NaN (which has none) give NaN
-#pragma unroll
-      for (int d = 0; d < DB; ++d) {
-        f16x n, c;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) n[r] = c[r] = 0.f;
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const u32x4 v = read_v(sV, t, d);
-          u32x4 fin, one, sign, sees;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            fin[j] = one[j] = sign[j] = sees[j] = 0;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const uint32_t x = v[j] >> (16 * e) & 0xffffu;
-              const bool bad = (x & 0x7f80u) == 0x7f80u;
-              fin[j] |= (bad ? 0u : x) << (16 * e);
-              one[j] |= (bad ? 0x3f80u : 0u) << (16 * e);
-              sign[j] |= ((x & 0x7fffu) == 0x7f80u ? 0x3f80u | (x & 0x8000u) : 0u) << (16 * e);
-              sees[j] |= (key_of(t >> 1, 8 * (t & 1) + 2 * j + e) <= see ? 0x3f80u : 0u) << (16 * e);
-            }
-          }
-          o[d] = mma32_bf16(fin, pf[t], o[d]);
-          n = mma32_bf16(one, sees, n);
-          c = mma32_bf16(sign, sees, c);
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (n[r] > 0.f) o[d][r] += c[r] == n[r] ? INFINITY : c[r] == -n[r] ? -INFINITY : NAN;
-      }
+  // K of the next tile and V of this one have landed, and every wave is done with K of
+  // this one and V of the one before, whose places the next ones take
+  auto turn = [&](int kb) __attribute__((always_inline)) {
+    wait_vm<0>();
+    lds_barrier();
+    if (kb + 2 < nkb) issue(Kh, a.ldk, kb + 2, sm[kb & 1][0], false);
+    if (kb + 1 < nkb) issue(Vh, a.ldv, kb + 1, sm[(kb + 1) & 1][1], true);
+  };
+  for (int kb = 0; kb < nkb;) {
+    slow(2 * kb, sa, sb);
+    turn(kb);
+    slow(2 * kb + 1, sb, sa);
+    for (++kb; (kb & 1) && 2 * kb + 4 < nu && 2 * kb + 3 < nfull; kb += 2) {
+      fast(std::integral_constant<int, 2>{}, sa, sb);
+      turn(kb);
+      fast(std::integral_constant<int, 3>{}, sb, sa);
+      fast(std::integral_constant<int, 0>{}, sa, sb);
+      turn(kb + 1);
+      fast(std::integral_constant<int, 1>{}, sb, sa);
     }
   }
+  if (nu > 0 && nu == 2 * nkb) add(nu - 1);
   // The compiler (ROCm 7.2) copied an accumulator at a loop's exit before its last
   // MFMA had written it; nothing may touch them until it has.
 #pragma unroll
   for (int d = 0; d < DB; ++d) asm volatile("s_nop 15" : "+v"(o[d]));
+  if (__any(poison != 0)) {
+    // what every query sees of the numbers left out (infinities and NaN add up as they do)
+    const int q = min(qw + l32, lq - 1);
+#pragma unroll 1
+    for (int j = nfull * 32; j < min(nu * 32, lk); ++j) {
+      const uint16_t* v = Vh + (int64_t)j * a.ldv + 4 * half;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float x = bf16_bits_to_f32(v[32 * d + 8 * (r >> 2) + (r & 3)]);
+          o[d][r] += j <= q + off && !(fabsf(x) < INFINITY) ? x : 0.f;
+        }
+    }
+  }
   const int q = qw + l32;
   if (q >= lq) return;
   const auto rl = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
@@ -299,22 +362,31 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
   const float inv = 1.0f / (__uint_as_float(rl[0]) + __uint_as_float(rl[1]));
   const bool none = q + off < 0;
   uint16_t* y0 = a.O + (int64_t)(q_first + q) * a.ldo + head * HD + 4 * half;
+  uint2 y[DB][4];
 #pragma unroll
   for (int d = 0; d < DB; ++d)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      uint16_t* yp = y0 + 32 * d + 8 * g;
-      const uint32_t u0 = none ? 0u : pack_bf16(o[d][4 * g] * inv, o[d][4 * g + 1] * inv);
-      const uint32_t u1 = none ? 0u : pack_bf16(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv);
-      if (a.vec) {
-        *(uint2*)yp = make_uint2(u0, u1);
-      } else {
-        yp[0] = (uint16_t)u0;
-        yp[1] = (uint16_t)(u0 >> 16);
-        yp[2] = (uint16_t)u1;
-        yp[3] = (uint16_t)(u1 >> 16);
-      }
+      y[d][g].x = none ? 0u : pack_bf16(o[d][4 * g] * inv, o[d][4 * g + 1] * inv);
+      y[d][g].y = none ? 0u : pack_bf16(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv);
     }
+  if (a.vec) {
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) *(uint2*)(y0 + 32 * d + 8 * g) = y[d][g];
+  } else {
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        uint16_t* yp = y0 + 32 * d + 8 * g;
+        yp[0] = (uint16_t)y[d][g].x;
+        yp[1] = (uint16_t)(y[d][g].x >> 16);
+        yp[2] = (uint16_t)y[d][g].y;
+        yp[3] = (uint16_t)(y[d][g].y >> 16);
+      }
+  }
 }
 
 }  // namespace
@@ -332,6 +404,7 @@ duo_status duo_attention_packed(const void* Q, int64_t ldq, const void* K, int64
     return DUO_ERR_INVALID_ARG;
   if (!cu_k && total_k != total_q) return DUO_ERR_INVALID_ARG;
   if (head_dim != 64 && head_dim != 128) return DUO_ERR_UNSUPPORTED;
+  if (ldk >= 1 << 24 || ldv >= 1 << 24) return DUO_ERR_UNSUPPORTED;  // a tile within 2^31 bytes
   if (total_q > (int64_t)1 << 30 || total_k > (int64_t)1 << 30 || nseq > (int64_t)1 << 30) return DUO_ERR_UNSUPPORTED;
   if (nseq == 0 || total_q == 0) return DUO_OK;
   if (!Q || !O || !cu_q || (total_k > 0 && (!K || !V))) return DUO_ERR_INVALID_ARG;

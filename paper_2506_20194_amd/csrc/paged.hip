@@ -36,6 +36,7 @@
 #include <cmath>
 
 #include "cache.h"
+#include "dma.h"
 #include "internal.h"
 #include "mfma.h"
 #include "pingpong.h"
@@ -175,7 +176,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
   extern __shared__ __attribute__((aligned(16))) uint8_t lsm[];
   __shared__ Count cnt;
   __shared__ float jm[4][kCols], jl[4][kCols];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
 
   // sequences without tokens
@@ -256,9 +257,11 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
         return out ? 0 : id;
       };
       // this wave's loads of tile t's K (which = 0) or V rows and scales; K first
-      auto issue = [&](int t, auto which_c, uint8_t* rows, uint8_t* scales) {
+      auto issue = [&](int t, auto which_c, const uint8_t* to_rows, const uint8_t* to_scales) __attribute__((always_inline)) {
         constexpr int which = decltype(which_c)::value;
         const int k0 = t * KEYS;
+        const uint32_t rows = __builtin_amdgcn_readfirstlane(lds_addr(to_rows));
+        const uint32_t scales = __builtin_amdgcn_readfirstlane(lds_addr(to_scales));
         if (which == 0 && k0 >> kv.shift >= win + 64) {  // four tiles never reach further than the next window
           pid = nid;
           win += 64;
@@ -285,8 +288,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
           for (int i = 0; i < NL; ++i) {
             const int r = i * RPL + lane / CH, b = i * RPL / 16;
             const uint8_t* at = base[b] + (rows_at + in[b] * RB);
-            __builtin_amdgcn_global_load_lds((const void*)(at + (uint32_t)((r & 15) * RB + chunk(r))),
-                                             (__attribute__((address_space(3))) void*)(rows + i * 1024), 16, 0, 0);
+            dma16(at, (uint32_t)((r & 15) * RB + chunk(r)), rows + i * 1024);
           }
           if constexpr (QUANT) {
 #pragma unroll
@@ -299,8 +301,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
                 const uint8_t* x = base[i * BPL + b] + (scales_at + in[i * BPL + b] * G::SB);
                 at = bl == b ? x : at;
               }
-              __builtin_amdgcn_global_load_lds((const void*)(at + (uint32_t)(lane * 4 % (16 * G::SB))),
-                                               (__attribute__((address_space(3))) void*)(scales + i * 256), 4, 0, 0);
+              dma4(at + lane * 4 % (16 * G::SB), scales + i * 256);
             }
           }
         } else {
@@ -315,16 +316,14 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
           for (int i = 0; i < NL; ++i) {
             const int r = i * RPL + lane / CH;
             const auto [b, in] = place(r);
-            __builtin_amdgcn_global_load_lds((const void*)(b + rows_at + in * RB + chunk(r)),
-                                             (__attribute__((address_space(3))) void*)(rows + i * 1024), 16, 0, 0);
+            dma16(b + rows_at + in * RB + chunk(r), rows + i * 1024);
           }
           if constexpr (QUANT) {
 #pragma unroll 1
             for (int i = 0; i < NS; ++i) {
               const int e = i * 256 + lane * 4;
               const auto [b, in] = place(e / G::SB);
-              __builtin_amdgcn_global_load_lds((const void*)(b + scales_at + in * G::SB + e % G::SB),
-                                               (__attribute__((address_space(3))) void*)(scales + i * 256), 4, 0, 0);
+              dma4(b + scales_at + in * G::SB + e % G::SB, scales + i * 256);
             }
           }
         }
