@@ -1,15 +1,18 @@
 // Causal attention over packed sequences of different lengths, with grouped heads, in
 // one pass over the keys with a running maximum and sum.
 //
-// One workgroup per (sequence, query head, block of 32 NW queries); wave w owns queries
-// 32 w .. 32 w + 31.  Everything is computed transposed, with v_mfma_f32_32x32x16_bf16
+// One workgroup per (sequence, K/V head, block of 32 NW rows), a row being a query and one
+// of the heads that read this K/V head, the heads of a query side by side: few queries
+// fill a block all the same, and a wave's 32 rows end at nearly the same key.  Wave w owns
+// rows 32 w .. 32 w + 31.  Everything is computed transposed, with v_mfma_f32_32x32x16_bf16
 // (lane l holds row l % 32 of A and column l % 32 of B, the 8 consecutive k of half
 // l / 32; accumulator element r sits at row 8 (r / 4) + 4 (l / 32) + r % 4, column
 // l % 32):
 //   S^T = K Q^T    a lane's 16 elements per block of 32 keys belong to one query;
 //   O^T = V^T P^T  P^T's fragments are the lane's own probabilities, V^T's take the
 //                  same keys from the row-major V tile with transposing LDS reads.
-// K and V tiles of 64 keys stream global -> LDS directly, two buffers each.
+// K and V tiles of 64 keys stream global -> LDS directly, two buffers each; a wave's step is
+// half a tile.
 //
 // Probabilities are taken relative to a running reference that is moved (and O and the
 // sum with it) only when a score exceeds it by more than 8 in the exponent of two:
@@ -40,7 +43,7 @@ struct PackedArgs {
   int64_t ldq, ldk, ldv, ldo;
   const int32_t *cu_q, *cu_k;
   int total_q, total_k, nseq, kv_heads, group;
-  int blocks;  // bound of the blocks of queries of one head
+  int blocks;  // bound of the blocks of rows of one K/V head
   float cexp;  // exp(s scale) = 2^(s cexp), with the queries' signs turned for a negative scale
   uint32_t flip;
   int vec;  // 8-byte stores of O
@@ -48,20 +51,16 @@ struct PackedArgs {
 
 __device__ inline int cut(int v, int total) { return min(max(v, 0), total); }
 
-// Of workgroup `id`: its query head, and which block of queries counted through all
+// Of workgroup `id`: its K/V head, and which block of rows counted through all
 // sequences.  Ids go round-robin over the XCDs: a K/V head lives on 8 / e of them, e =
-// gcd(kv_heads, 8), which take its blocks in turn, all heads of a group one after the
-// other, so that they share K and V in that L2.
-__device__ inline bool place(int id, const PackedArgs& a, int* head, int* block) {
-  const int x = id & 7, e = a.kv_heads & -a.kv_heads & 7 ? a.kv_heads & -a.kv_heads & 7 : 8, sh = 8 / e;
-  int j = id >> 3;
-  const int g = j % a.group;
-  j /= a.group;
+// gcd(kv_heads, 8), which take its blocks in turn and share K and V in their L2.
+__device__ inline bool place(int id, const PackedArgs& a, int* kv, int* block) {
+  const int low = a.kv_heads & -a.kv_heads & 7, e = low ? low : 8, sh = 8 / e;
+  const int x = id & 7, j = id >> 3;
   const int per = (a.blocks + sh - 1) / sh;  // blocks of one K/V head here
-  const int kv = j / per * e + x % e;
-  *head = kv * a.group + g;
+  *kv = j / per * e + x % e;
   *block = j % per * sh + x / e;
-  return kv < a.kv_heads && *block < a.blocks;
+  return *kv < a.kv_heads && *block < a.blocks;
 }
 
 // The sequence and the block within it (the last block first) of block b; false past the last.
@@ -71,7 +70,7 @@ __device__ inline bool find(const PackedArgs& a, int b, int* seq, int* qb) {
   for (int s0 = 0; s0 < a.nseq; s0 += 64) {
     const int s = s0 + lane;
     int n = 0;
-    if (s < a.nseq) n = (max(cut(a.cu_q[s + 1], a.total_q) - cut(a.cu_q[s], a.total_q), 0) + QB - 1) / QB;
+    if (s < a.nseq) n = (max(cut(a.cu_q[s + 1], a.total_q) - cut(a.cu_q[s], a.total_q), 0) * a.group + QB - 1) / QB;
     int up = n;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -86,7 +85,6 @@ __device__ inline bool find(const PackedArgs& a, int b, int* seq, int* qb) {
       return true;
     }
     b -= __builtin_amdgcn_readlane(up, 63);
-    if (b < 0) return false;
   }
   return false;
 }
@@ -102,16 +100,19 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
   constexpr int RPL = 64 / CH;          // keys per wave-wide load
   constexpr int QB = 32 * NW;
   __shared__ u32x4 sm[2][2][TILE];      // [buffer][K, V]
-  int head, block, s, qb;
-  if (!place(blockIdx.x, a, &head, &block) || !find<QB>(a, block, &s, &qb)) return;
+  int kv, block, s, qb;
+  if (!place(blockIdx.x, a, &kv, &block) || !find<QB>(a, block, &s, &qb)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, half = lane >> 5;
   const int q_first = cut(a.cu_q[s], a.total_q), lq = cut(a.cu_q[s + 1], a.total_q) - q_first;
   const int k_first = cut(a.cu_k[s], a.total_k), lk = max(cut(a.cu_k[s + 1], a.total_k) - k_first, 0);
   const int off = lk - lq;              // query i sees keys j <= i + off
-  const int q0 = qb * QB, qw = q0 + 32 * wave;
-  const uint16_t* const Kh = a.K + (int64_t)k_first * a.ldk + head / a.group * HD;
-  const uint16_t* const Vh = a.V + (int64_t)k_first * a.ldv + head / a.group * HD;
+  // row r of the sequence and K/V head: query r / group, head r % group of its group
+  const int rows = lq * a.group, row0 = qb * QB + 32 * wave, row = min(row0 + l32, rows - 1);
+  const int q = row / a.group, head = kv * a.group + row - q * a.group;
+  const int q_lo = row0 / a.group, q_hi = min(row0 + 31, rows - 1) / a.group;  // of this wave
+  const uint16_t* const Kh = a.K + (int64_t)k_first * a.ldk + kv * HD;
+  const uint16_t* const Vh = a.V + (int64_t)k_first * a.ldv + kv * HD;
   // chunk c of key row r sits at position kswz(r, c) (vswz) of its row: 16 consecutive
   // keys' chunks of a K fragment, and the four keys x 64 bytes that half a wave's
   // transposing read of V touches, cover the 64 banks once
@@ -120,15 +121,15 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
 
   u32x4 qa[KS];
   {
-    const uint16_t* q = a.Q + (int64_t)(q_first + min(qw + l32, lq - 1)) * a.ldq + head * HD;
+    const uint16_t* at = a.Q + (int64_t)(q_first + q) * a.ldq + head * HD;
 #pragma unroll
     for (int c = 0; c < KS; ++c) {
-      qa[c] = *(const u32x4*)(q + 8 * (2 * c + half));
+      qa[c] = *(const u32x4*)(at + 8 * (2 * c + half));
 #pragma unroll
       for (int j = 0; j < 4; ++j) qa[c][j] ^= a.flip;
     }
   }
-  const int seen = min(q0 + QB, lq) + off;  // keys that the block's last query sees
+  const int seen = min(qb * QB + QB - 1, rows - 1) / a.group + 1 + off;  // keys that the block's last query sees
   const int nkb = (seen + KB - 1) / KB;     // <= 0: none
   // this wave's part of tile kb of K (or V), keys past the last as the last
   auto issue = [&](const uint16_t* src, int64_t ld, int kb, const u32x4* dst, bool is_v) __attribute__((always_inline)) {
@@ -167,8 +168,8 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
   };
   // Steps of 32 keys, two per tile.  This wave: steps of which its queries see a key, and of
   // which they see every key.
-  const int nu = qw < lq && qw + 31 + off >= 0 ? min((qw + 31 + off) / 32 + 1, 2 * nkb) : 0;
-  const int nfull = max((qw + off + 1) / 32, 0);
+  const int nu = row0 < rows && q_hi + off >= 0 ? min((q_hi + off) / 32 + 1, 2 * nkb) : 0;
+  const int nfull = max((q_lo + off + 1) / 32, 0);
   auto key_of = [&](int r) { return 8 * (r >> 2) + 4 * half + (r & 3); };
 
   f16x sa, sb;  // scores of an even and of an odd step
@@ -285,7 +286,7 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
   auto slow = [&](int u, f16x& sc, f16x& sn) __attribute__((always_inline)) {
     if (u > 0 && u <= nu) add(u - 1);
     if (u < nu) {
-      const int see = qw + l32 + off - u * 32;
+      const int see = q + off - u * 32;
       if (u >= nfull)
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[r] = key_of(r) > see ? -INFINITY : sc[r];
@@ -342,7 +343,6 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
   for (int d = 0; d < DB; ++d) asm volatile("s_nop 15" : "+v"(o[d]));
   if (__any(poison != 0)) {
     // what every query sees of the numbers left out (infinities and NaN add up as they do)
-    const int q = min(qw + l32, lq - 1);
 #pragma unroll 1
     for (int j = nfull * 32; j < min(nu * 32, lk); ++j) {
       const uint16_t* v = Vh + (int64_t)j * a.ldv + 4 * half;
@@ -355,8 +355,7 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
         }
     }
   }
-  const int q = qw + l32;
-  if (q >= lq) return;
+  if (row0 + l32 >= rows) return;
   const auto rl = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
   // queries that see no key: 0; a sum of 0 (every score -inf) gives NaN
   const float inv = 1.0f / (__uint_as_float(rl[0]) + __uint_as_float(rl[1]));
@@ -409,14 +408,16 @@ duo_status duo_attention_packed(const void* Q, int64_t ldq, const void* K, int64
   if (nseq == 0 || total_q == 0) return DUO_OK;
   if (!Q || !O || !cu_q || (total_k > 0 && (!K || !V))) return DUO_ERR_INVALID_ARG;
   if (ldq % 8 || ldk % 8 || ldv % 8 || !aligned16(Q) || !aligned16(K) || !aligned16(V)) return DUO_ERR_UNSUPPORTED;
-  // 128 queries per workgroup; 64 when that would leave CUs without their two
+  // 128 rows per workgroup; 64 when that would leave CUs without their two
   // workgroups (512 in all)
-  auto bound = [&](int64_t qb) { return total_q / qb + std::min(nseq, total_q); };
-  const bool wide = (total_q / 128 + nseq / 2) * heads >= 512;
+  const int64_t group = heads / kv_heads;
+  if (total_q * group > INT32_MAX / 2) return DUO_ERR_UNSUPPORTED;
+  auto bound = [&](int64_t rows) { return total_q * group / rows + std::min(nseq, total_q); };
+  const bool wide = (total_q * group / 128 + nseq / 2) * kv_heads >= 512;
   const int64_t blocks = bound(wide ? 128 : 64);
   int64_t e = 1;
   while (e < 8 && kv_heads % (2 * e) == 0) e *= 2;
-  const int64_t wgs = 8 * (kv_heads / e) * cdiv(blocks, 8 / e) * (heads / kv_heads);
+  const int64_t wgs = 8 * (kv_heads / e) * cdiv(blocks, 8 / e);
   if (wgs > INT32_MAX) return DUO_ERR_UNSUPPORTED;
   if (duo_status d = device_ok(); d != DUO_OK) return d;
   PackedArgs a;
@@ -424,7 +425,7 @@ duo_status duo_attention_packed(const void* Q, int64_t ldq, const void* K, int64
   a.ldq = ldq, a.ldk = ldk, a.ldv = ldv, a.ldo = ldo;
   a.cu_q = cu_q, a.cu_k = cu_k ? cu_k : cu_q;
   a.total_q = (int)total_q, a.total_k = (int)total_k, a.nseq = (int)nseq;
-  a.kv_heads = (int)kv_heads, a.group = (int)(heads / kv_heads), a.blocks = (int)blocks;
+  a.kv_heads = (int)kv_heads, a.group = (int)group, a.blocks = (int)blocks;
   a.cexp = (float)(std::fabs(scale) * 1.4426950408889634);
   a.flip = scale < 0.0 ? 0x80008000u : 0u;
   a.vec = ldo % 4 == 0 && (reinterpret_cast<uintptr_t>(O) & 7) == 0;
