@@ -89,19 +89,42 @@ template <int KEYS>
 __device__ inline int tiles_of(int len) { return (len + KEYS - 1) / KEYS; }
 __device__ inline int cost_of(int tiles) { return tiles ? tiles + kRowCost : 0; }
 
-// cum[i]: cost of one row of every sequence up to the end of bucket i.  256 threads;
-// ends with a barrier.
+__device__ inline uint64_t div64(uint64_t a, uint32_t b) { return a >> 32 ? a / b : (uint32_t)a / b; }
+
+// The count cut into n shares as equal as whole numbers allow: share i begins at
+// i size + min(i, more).
+struct Shares {
+  int64_t size;
+  int more, n;
+  __device__ Shares(int64_t total, int most) {
+    n = (int)min((int64_t)most, (total + kMinShare - 1) / kMinShare);
+    size = n ? (int64_t)div64((uint64_t)total, (uint32_t)n) : 0;
+    more = (int)(total - size * n);
+  }
+  __device__ int64_t begin(int i) const { return i * size + min(i, more); }
+  __device__ int of(int64_t u) const {  // size < 2^31: fewer than 2^31 of anything in 2^10 shares
+    const int64_t cut = more * (size + 1);
+    return u < cut ? (int)div64((uint64_t)u, (uint32_t)size + 1) : more + (int)div64((uint64_t)(u - cut), (uint32_t)size);
+  }
+};
+
+// cost[i]: of one row of every sequence up to the end of bucket i; len: of the sequences,
+// where a bucket is one.  256 threads; ends with a barrier.
 struct Count {
-  int64_t cum[256];
   int64_t wave[4];
+  int64_t before;  // cost of the sequences before bucket `at`
+  int at;
+  int len[256];
 };
 template <int KEYS>
-__device__ inline void count_rows(const PagedWork& w, Count& c) {
+__device__ inline int64_t count_rows(const PagedWork& w, Count& c, int64_t* mine) {
   const int tid = threadIdx.x, lane = tid & 63;
   int64_t n = 0;
   for (int i = 0; i < w.per; ++i) {
     const int64_t s = (int64_t)tid * w.per + i;
-    if (s < w.nseq) n += cost_of(tiles_of<KEYS>(seq_len(w, (int)s)));
+    const int len = s < w.nseq ? seq_len(w, (int)s) : 0;
+    if (w.per == 1) c.len[tid] = len;
+    n += cost_of(tiles_of<KEYS>(len));
   }
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -110,9 +133,14 @@ __device__ inline void count_rows(const PagedWork& w, Count& c) {
   }
   if (lane == 63) c.wave[tid >> 6] = n;
   __syncthreads();
-  for (int i = 0; i < tid >> 6; ++i) n += c.wave[i];
-  c.cum[tid] = n;
-  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (i < tid >> 6) n += c.wave[i];
+    total += c.wave[i];
+  }
+  *mine = n;
+  return total;
 }
 
 // max over the four lanes that hold one column
@@ -179,33 +207,34 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
 
+  int64_t mine;
+  const int64_t total = count_rows<KEYS>(work, cnt, &mine) * work.rows;
+  const Shares shares(total, gridDim.x);
+  int64_t u = shares.begin(blockIdx.x);
+  const int64_t u1 = (int)blockIdx.x < shares.n ? shares.begin(blockIdx.x + 1) : u;
+  {
+    // the bucket that u lies in: the first whose end lies behind it
+    const int64_t upto = __shfl_up(mine, 1);
+    int64_t prev = lane ? upto : 0;
+    if (lane == 0)
+      for (int i = 0; i < wave; ++i) prev += cnt.wave[i];
+    if (prev * work.rows <= u && u < mine * work.rows) cnt.at = tid, cnt.before = prev * work.rows;
+  }
+  if (tid == 0 && tasks) tasks[blockIdx.x].parts = 0;
+  __syncthreads();
+  auto len_of = [&](int s) { return __builtin_amdgcn_readfirstlane(work.per == 1 ? cnt.len[s] : seq_len(work, s)); };
   // sequences without tokens
   for (int s = blockIdx.x; s < work.nseq; s += gridDim.x)
-    if (seq_len(work, s) == 0)
+    if (len_of(s) == 0)
       for (int e = tid; e < group * kv.heads * HD; e += 256) O[(int64_t)s * ldo + e] = 0;
-
-  if (tid == 0 && tasks) tasks[blockIdx.x].parts = 0;
-
-  count_rows<KEYS>(work, cnt);
-  const int64_t total = cnt.cum[255] * work.rows;
-  const int n = (int)min((int64_t)gridDim.x, (total + kMinShare - 1) / kMinShare);
-  if ((int)blockIdx.x >= n) return;
-  // share i of n: [total i / n, total (i + 1) / n)
-  int64_t u = total * blockIdx.x / n;
-  const int64_t u1 = total * (blockIdx.x + 1) / n;
-  // the sequence of u: its bucket (the first whose end lies behind u), then one by one
-  int lo = 0;
-  for (int hi = 255; lo < hi;) {
-    const int mid = (lo + hi) / 2;
-    if (cnt.cum[mid] * work.rows > u) hi = mid; else lo = mid + 1;
-  }
-  int64_t before = lo ? cnt.cum[lo - 1] * work.rows : 0;  // cost of the sequences before s
+  if (u >= u1) return;
+  int64_t before = cnt.before;  // cost of the sequences before s
   uint8_t* const sK = lsm + wave * G::WAVE;
   uint8_t* const sV = sK + G::ROWS;
   uint8_t* const sS = sV + G::ROWS;  // scales: [parity of the tile's turn][K, V]
 
-  for (int s = lo * work.per; u < u1; ++s) {
-    const int len = __builtin_amdgcn_readfirstlane(seq_len(work, s));
+  for (int s = cnt.at * work.per; u < u1; ++s) {
+    const int len = len_of(s);
     const int tiles = tiles_of<KEYS>(len), cost = cost_of(tiles);
     const int64_t start = before;
     before += (int64_t)cost * work.rows;
@@ -214,7 +243,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
     const int last_page = (len - 1) >> kv.shift;
     while (u < u1 && u < before) {
       // one row, or what of it is in this share
-      const int row = (int)((u - start) / cost), at = (int)((u - start) % cost);
+      const int row = (int)div64((uint64_t)(u - start), (uint32_t)cost), at = (int)(u - start - (int64_t)row * cost);
       const int here = (int)min((int64_t)(cost - at), u1 - u);
       const int t0 = max(at - kRowCost, 0), t1 = max(at + here - kRowCost, 0);
       const int64_t row_end = u + (cost - at);
@@ -226,36 +255,22 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
       const uint8_t* const block0 = kv.data + h * kv.block;
       const int64_t page_bytes = kv.heads * kv.block;
 
-      // Q^T's fragments, heads past the last as zeros; -bias sum(q) of every group
-      u32x4 qf[CK];
-      float qs[CK];
-#pragma unroll
-      for (int c = 0; c < CK; ++c) {
-        u32x4 v = {0u, 0u, 0u, 0u};
-        if (l16 < nc) v = *(const u32x4*)(q + l16 * HD + 32 * c + 8 * g);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] ^= flip;
-        if constexpr (QUANT) {
-          float t = 0.f;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) t += lo16(v[j]) + hi16(v[j]);
-          qs[c] = -BIAS * col_sum(t);
-        }
-        if constexpr (FMT == DUO_KV_I4)  // channels j and j + 4 together, as widen4 gives them
-          v = u32x4{(v[0] & 0xffffu) | v[2] << 16, v[0] >> 16 | (v[2] & 0xffff0000u), (v[1] & 0xffffu) | v[3] << 16,
-                    v[1] >> 16 | (v[3] & 0xffff0000u)};
-        qf[c] = v;
-      }
-
       // 64 pages of the table in one register, the next 64 in another
       bool bad = false;
-      int win = 0, pid = 0, nid = 0;
+      int t = t0 + wave;
+      int win = (t * KEYS >> kv.shift) & ~3;  // a tile's pages, four at most, lie in one window
       auto ids = [&](int p) {
         int id = pages[min(p + lane, last_page)];
         const bool out = id < 0 || id >= kv.pages;
         bad |= out;
         return out ? 0 : id;
       };
+      int pid = ids(win), nid = ids(win + 64);
+      u32x4 qf[CK];
+#pragma unroll
+      for (int c = 0; c < CK; ++c) qf[c] = *(const u32x4*)(q + min(l16, nc - 1) * HD + 32 * c + 8 * g);
+#pragma unroll
+      for (int c = 0; c < CK; ++c) asm volatile("" : "+v"(qf[c]));  // waited for here, and not behind the tiles
       // this wave's loads of tile t's K (which = 0) or V rows and scales; K first
       auto issue = [&](int t, auto which_c, const uint8_t* to_rows, const uint8_t* to_scales) __attribute__((always_inline)) {
         constexpr int which = decltype(which_c)::value;
@@ -336,13 +351,27 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
 #pragma unroll
       for (int d = 0; d < 2 * CK; ++d) o[d] = f4{0.f, 0.f, 0.f, 0.f};
 
-      int t = t0 + wave;
       if (t < t1) {
-        win = (t * KEYS >> kv.shift) & ~3;  // a tile's pages, four at most, lie in one window
-        pid = ids(win);
-        nid = ids(win + 64);
         issue(t, kK, sK, sS);
         issue(t, kV, sV, sS + NS * 256);
+      }
+      // Q^T's fragments, heads past the last as zeros; -bias sum(q) of every group
+      float qs[CK];
+#pragma unroll
+      for (int c = 0; c < CK; ++c) {
+        u32x4 v = qf[c];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = l16 < nc ? v[j] ^ flip : 0u;
+        if constexpr (QUANT) {
+          float t = 0.f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) t += lo16(v[j]) + hi16(v[j]);
+          qs[c] = -BIAS * col_sum(t);
+        }
+        if constexpr (FMT == DUO_KV_I4)  // channels j and j + 4 together, as widen4 gives them
+          v = u32x4{(v[0] & 0xffffu) | v[2] << 16, v[0] >> 16 | (v[2] & 0xffff0000u), (v[1] & 0xffffu) | v[3] << 16,
+                    v[1] >> 16 | (v[3] & 0xffff0000u)};
+        qf[c] = v;
       }
       for (uint8_t* sc = sS; t < t1; t += 4) {
         const bool more = t + 4 < t1;
@@ -548,9 +577,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
       const bool whole = t0 == 0 && t1 == tiles;
       float* const ps = part + (2 * (int64_t)blockIdx.x + (t0 == 0)) * cols * (HD + 2);
       if (!whole && t0 == 0 && tid == 0) {
-        int last = (int)((row_end - 1) * n / total);  // the share of the row's last tile
-        while (total * (last + 1) / n < row_end) ++last;
-        tasks[blockIdx.x] = Task{s, row, last - (int)blockIdx.x + 1, 0};
+        tasks[blockIdx.x] = Task{s, row, shares.of(row_end - 1) - (int)blockIdx.x + 1, 0};
       }
       for (int e = tid; e < nc * (HD / 2); e += 256) {
         const int c = e / (HD / 2), d = e % (HD / 2) * 2;

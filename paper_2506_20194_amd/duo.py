@@ -727,12 +727,48 @@ def duo_silu_mul(G, U, out=None):
 
 KV_FORMATS = {"bf16": DUO_KV_BF16, "int8": DUO_KV_I8, "int4": DUO_KV_I4}
 
+# These calls are a few microseconds of device work when a single token is served, so
+# their checks are written for speed: device indexes are compared as numbers and
+# pointers passed as such.
 
-def _ints(t, dtype, shape, name):
+
+def _on(index, name, *ts):
+    """All of ts on device `index` (>= 0: a HIP device)."""
+    if index < 0:
+        raise ValueError("duo: tensors must live on a CUDA (HIP) device")
+    for t in ts:
+        if t is not None and t.get_device() != index:
+            raise ValueError(f"duo: {name}: all tensors must be on one CUDA (HIP) device")
+
+
+def _rows(t, m, w, name):
+    """Row stride of an m x w bf16 matrix."""
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"duo: {name} must be bfloat16")
+    if t.shape != (m, w):
+        raise ValueError(f"duo: {name} has shape {tuple(t.shape)}, expected {(m, w)}")
+    ld, one = t.stride()
+    if one != 1 and w > 1:
+        raise ValueError(f"duo: {name} must have unit column stride")
+    return max(ld, w) if m <= 1 else ld
+
+
+def _ints(t, dtype, n, name):
+    """Pointer of a contiguous 1-d integer tensor of n entries."""
     if t.dtype != dtype:
         raise TypeError(f"duo: {name} must be {dtype}")
-    _shape(t, shape, name)
-    _contig(t, name)
+    if t.shape != (n,):
+        raise ValueError(f"duo: {name} has shape {tuple(t.shape)}, expected {(n,)}")
+    if not t.is_contiguous():
+        raise ValueError(f"duo: {name} must be contiguous")
+    return t.data_ptr()
+
+
+def _empty(m, w, like):
+    return torch.empty((m, w), dtype=torch.bfloat16, device=like.device)
+
+
+_raw_stream = torch._C._cuda_getCurrentRawStream  # of a device index; torch's current stream
 
 
 class KVCache:
@@ -740,7 +776,7 @@ class KVCache:
     kv_heads, bytes of a head's block; see include/duo.h for what a block
     holds).  fmt: "bf16", "int8" or "int4".  KVCache.empty allocates one."""
 
-    __slots__ = ("data", "page_size", "kv_heads", "head_dim", "fmt", "c")
+    __slots__ = ("data", "page_size", "kv_heads", "head_dim", "fmt", "c", "ref")
 
     def __init__(self, data, page_size, kv_heads, head_dim, fmt="bf16"):
         if fmt not in KV_FORMATS:
@@ -748,10 +784,13 @@ class KVCache:
         nbytes = kv_page_bytes(page_size, kv_heads, head_dim, fmt)
         if data.dtype != torch.uint8:
             raise TypeError("duo: a cache's data must be uint8")
-        _shape(data, (data.shape[0], kv_heads, nbytes // kv_heads), "data")
-        _contig(data, "data")
+        if data.dim() != 3 or data.shape[1:] != (kv_heads, nbytes // kv_heads):
+            raise ValueError(f"duo: data has shape {tuple(data.shape)}, expected (pages, {kv_heads}, {nbytes // kv_heads})")
+        if not data.is_contiguous():
+            raise ValueError("duo: data must be contiguous")
         self.data, self.page_size, self.kv_heads, self.head_dim, self.fmt = data, page_size, kv_heads, head_dim, fmt
         self.c = KvCache(data.data_ptr(), data.shape[0], page_size, kv_heads, head_dim, KV_FORMATS[fmt])
+        self.ref = ctypes.byref(self.c)
 
     @classmethod
     def empty(cls, pages, page_size, kv_heads, head_dim, fmt="bf16", device="cuda"):
@@ -768,47 +807,47 @@ class KVCache:
 
 
 def kv_page_bytes(page_size, kv_heads, head_dim, fmt="bf16") -> int:
-    n = int(lib().duo_kv_page_bytes(KV_FORMATS[fmt], page_size, kv_heads, head_dim))
+    n = lib().duo_kv_page_bytes(KV_FORMATS[fmt], page_size, kv_heads, head_dim)
     if n == 0:
         raise DuoError(DUO_ERR_UNSUPPORTED, "duo_kv_page_bytes")
     return n
 
 
 def duo_rope_at(X, heads, head_dim, pos, theta=1e4, out=None):
-    """Rows of X rotated by the angles of the positions pos (m int32); out may be X."""
-    m = X.shape[0]
-    if X.shape[1] != heads * head_dim:
-        raise ValueError("duo: X must be heads * head_dim wide")
-    Y = torch.empty((m, X.shape[1]), dtype=torch.bfloat16, device=X.device) if out is None else out
-    _same_device(X, pos, Y)
-    _shape(Y, X.shape, "out")
-    _ints(pos, torch.int32, (m,), "pos")
-    _check(lib().duo_rope_at(_ptr(X), m, heads, head_dim, _bf16_rows(X, "X"), _ptr(pos), float(theta), _ptr(Y),
-                             _bf16_rows(Y, "out"), _stream(X.device)), "duo_rope_at")
+    """Rows of X (m x heads*head_dim) rotated by the angles of the positions pos (m
+    int32); out may be X."""
+    m, w = X.shape[0], heads * head_dim
+    Y = _empty(m, w, X) if out is None else out
+    dev = X.get_device()
+    _on(dev, "duo_rope_at", pos, Y)
+    st = lib().duo_rope_at(X.data_ptr(), m, heads, head_dim, _rows(X, m, w, "X"), _ints(pos, torch.int32, m, "pos"), theta,
+                           Y.data_ptr(), _rows(Y, m, w, "out"), _raw_stream(dev))
+    if st:
+        raise DuoError(st, "duo_rope_at")
     return Y
 
 
 def duo_kv_write(cache, K, V, slots):
     """Rows of K and V (m x kv_heads*head_dim bf16) into their slots (m int64)."""
     m, w = K.shape[0], cache.kv_heads * cache.head_dim
-    _same_device(cache.data, K, V, slots)
-    _shape(K, (m, w), "K")
-    _shape(V, (m, w), "V")
-    _ints(slots, torch.int64, (m,), "slots")
-    _check(lib().duo_kv_write(ctypes.byref(cache.c), _ptr(K), _bf16_rows(K, "K"), _ptr(V), _bf16_rows(V, "V"),
-                              _ptr(slots), m, _stream(K.device)), "duo_kv_write")
+    dev = K.get_device()
+    _on(dev, "duo_kv_write", V, slots, cache.data)
+    st = lib().duo_kv_write(cache.ref, K.data_ptr(), _rows(K, m, w, "K"), V.data_ptr(), _rows(V, m, w, "V"),
+                            _ints(slots, torch.int64, m, "slots"), m, _raw_stream(dev))
+    if st:
+        raise DuoError(st, "duo_kv_write")
 
 
 def duo_kv_read(cache, slots, out=None):
     """(K, V) bf16 rows at the slots (m int64); out: a pair to write into."""
-    shape = (slots.shape[0], cache.kv_heads * cache.head_dim)
-    K, V = out if out is not None else (torch.empty(shape, dtype=torch.bfloat16, device=slots.device) for _ in "KV")
-    _same_device(cache.data, K, V, slots)
-    _shape(K, shape, "K")
-    _shape(V, shape, "V")
-    _ints(slots, torch.int64, shape[:1], "slots")
-    _check(lib().duo_kv_read(ctypes.byref(cache.c), _ptr(slots), shape[0], _ptr(K), _bf16_rows(K, "K"), _ptr(V),
-                             _bf16_rows(V, "V"), _stream(slots.device)), "duo_kv_read")
+    m, w = slots.shape[0], cache.kv_heads * cache.head_dim
+    K, V = (_empty(m, w, slots), _empty(m, w, slots)) if out is None else out
+    dev = slots.get_device()
+    _on(dev, "duo_kv_read", K, V, cache.data)
+    st = lib().duo_kv_read(cache.ref, _ints(slots, torch.int64, m, "slots"), m, K.data_ptr(), _rows(K, m, w, "K"),
+                           V.data_ptr(), _rows(V, m, w, "V"), _raw_stream(dev))
+    if st:
+        raise DuoError(st, "duo_kv_read")
     return K, V
 
 
@@ -817,25 +856,22 @@ def duo_attention_packed(Q, K, V, cu_q, heads, kv_heads, head_dim, cu_k=None, sc
     total_k x kv_heads*head_dim, cu_q and cu_k (None: cu_q) the sequences' first
     rows, nseq + 1 int32 each.  scale: None for head_dim^-1/2.  Rows of the result
     that lie in no sequence are not written."""
-    n = cu_q.shape[0] - 1
-    O = torch.empty((Q.shape[0], heads * head_dim), dtype=torch.bfloat16, device=Q.device) if out is None else out
-    _same_device(Q, K, V, cu_q, cu_k, O)
-    _shape(Q, (Q.shape[0], heads * head_dim), "Q")
-    _shape(K, (K.shape[0], kv_heads * head_dim), "K")
-    _shape(V, K.shape, "V")
-    _shape(O, Q.shape, "out")
-    _ints(cu_q, torch.int32, (n + 1,), "cu_q")
-    if cu_k is not None:
-        _ints(cu_k, torch.int32, (n + 1,), "cu_k")
-    _check(lib().duo_attention_packed(_ptr(Q), _bf16_rows(Q, "Q"), _ptr(K), _bf16_rows(K, "K"), _ptr(V),
-                                      _bf16_rows(V, "V"), _ptr(cu_q), Q.shape[0], _ptr(cu_k), K.shape[0], n, heads,
-                                      kv_heads, head_dim, head_dim ** -0.5 if scale is None else float(scale), _ptr(O),
-                                      _bf16_rows(O, "out"), _stream(Q.device)), "duo_attention_packed")
+    n, tq, tk, w, wk = cu_q.shape[0] - 1, Q.shape[0], K.shape[0], heads * head_dim, kv_heads * head_dim
+    O = _empty(tq, w, Q) if out is None else out
+    dev = Q.get_device()
+    _on(dev, "duo_attention_packed", K, V, cu_q, cu_k, O)
+    st = lib().duo_attention_packed(
+        Q.data_ptr(), _rows(Q, tq, w, "Q"), K.data_ptr(), _rows(K, tk, wk, "K"), V.data_ptr(), _rows(V, tk, wk, "V"),
+        _ints(cu_q, torch.int32, n + 1, "cu_q"), tq, None if cu_k is None else _ints(cu_k, torch.int32, n + 1, "cu_k"), tk,
+        n, heads, kv_heads, head_dim, head_dim ** -0.5 if scale is None else scale, O.data_ptr(), _rows(O, tq, w, "out"),
+        _raw_stream(dev))
+    if st:
+        raise DuoError(st, "duo_attention_packed")
     return O
 
 
 def attention_paged_workspace(nseq, heads, kv_heads, head_dim, max_len, device):
-    n = int(lib().duo_attention_paged_workspace_size(nseq, heads, kv_heads, head_dim, max_len))
+    n = lib().duo_attention_paged_workspace_size(nseq, heads, kv_heads, head_dim, max_len)
     return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
 
 
@@ -843,24 +879,27 @@ def duo_attention_paged(Q, cache, table, lens, heads, max_len=None, scale=None, 
     """Attention of one query per sequence (Q: nseq x heads*head_dim) over its
     first lens[s] cached tokens, whose pages are row s of table (both int32).
     max_len: a bound of lens known to the caller (None: all that table holds)."""
-    n = Q.shape[0]
-    O = torch.empty((n, heads * cache.head_dim), dtype=torch.bfloat16, device=Q.device) if out is None else out
-    if max_len is None:
-        max_len = table.shape[1] * cache.page_size
-    if ws is None:
-        ws = attention_paged_workspace(n, heads, cache.kv_heads, cache.head_dim, max_len, Q.device)
-    _same_device(Q, cache.data, table, lens, O, ws)
-    _shape(Q, (n, heads * cache.head_dim), "Q")
-    _shape(O, Q.shape, "out")
-    _ints(lens, torch.int32, (n,), "lens")
+    n, hd = Q.shape[0], cache.head_dim
+    w = heads * hd
+    O = _empty(n, w, Q) if out is None else out
     if table.dtype != torch.int32:
         raise TypeError("duo: table must be torch.int32")
-    _shape(table, (n, table.shape[1]), "table")
-    if max_len > table.shape[1] * cache.page_size:
+    if table.dim() != 2 or table.shape[0] != n:
+        raise ValueError(f"duo: table has shape {tuple(table.shape)}, expected {n} rows")
+    most = table.shape[1] * cache.page_size
+    if max_len is None:
+        max_len = most
+    elif max_len > most:
         raise ValueError("duo: table holds fewer than max_len tokens")
-    _check(lib().duo_attention_paged(_ptr(Q), _bf16_rows(Q, "Q"), ctypes.byref(cache.c), _ptr(table), _ld(table),
-                                     _ptr(lens), n, max_len, heads,
-                                     cache.head_dim ** -0.5 if scale is None else float(scale), _ptr(O),
-                                     _bf16_rows(O, "out"), _ptr(ws), ws.numel(), _stream(Q.device)),
-           "duo_attention_paged")
+    if ws is None:
+        ws = attention_paged_workspace(n, heads, cache.kv_heads, hd, max_len, Q.device)
+    dev = Q.get_device()
+    _on(dev, "duo_attention_paged", table, lens, O, ws, cache.data)
+    ldt = _ld(table) if n > 1 or table.stride(1) != 1 else table.shape[1]
+    st = lib().duo_attention_paged(
+        Q.data_ptr(), _rows(Q, n, w, "Q"), cache.ref, table.data_ptr(), ldt, _ints(lens, torch.int32, n, "lens"), n,
+        max_len, heads, hd ** -0.5 if scale is None else scale, O.data_ptr(), _rows(O, n, w, "out"), ws.data_ptr(),
+        ws.numel(), _raw_stream(dev))
+    if st:
+        raise DuoError(st, "duo_attention_paged")
     return O
