@@ -533,7 +533,7 @@ typedef struct {
   void* data;
   int64_t num_pages;
   int32_t page_size;
-  int32_t kv_heads;
+  int32_t kv_heads; /* at most 4096 */
   int32_t head_dim; /* 64 or 128 */
   int32_t format;
 } duo_kv_cache;

@@ -8,7 +8,8 @@
 
 namespace duo {
 
-constexpr int kKvGroup = 32;  // channels per scale
+constexpr int kKvGroup = 32;       // channels per scale
+constexpr int kMaxKvHeads = 4096;  // a page within 2^32 bytes
 
 // Bytes of a cached row and of its scales, most of a code, and what is added to it.
 template <int FMT>

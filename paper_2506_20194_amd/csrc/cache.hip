@@ -231,7 +231,7 @@ duo_status kv_geo(const duo_kv_cache* c, KvGeo* g) {
 extern "C" {
 
 size_t duo_kv_page_bytes(int32_t format, int32_t page_size, int32_t kv_heads, int32_t head_dim) {
-  if (kv_heads < 1 || kv_heads > 65535 || (head_dim != 64 && head_dim != 128)) return 0;
+  if (kv_heads < 1 || kv_heads > kMaxKvHeads || (head_dim != 64 && head_dim != 128)) return 0;
   if (page_size < 16 || page_size > 256 || (page_size & (page_size - 1))) return 0;
   int row;
   switch (format) {

@@ -191,7 +191,12 @@ __device__ __forceinline__ int v_at(int r, int c) {
     return c ^ (r >> 4 & 1);
 }
 
-template <int FMT, int HD>
+// PAIR (8 and 4 bits, at most 8 heads): the columns that would stay empty take the second
+// half of the tile's keys.  A block of keys of each half is multiplied with the queries in
+// its half of the columns, both into one accumulator, and what follows for a score
+// (scales, maximum, exponential, rounding), the larger part of the vector work, is done
+// for two keys at once; the halves of a column's pair meet at the join.
+template <int FMT, int HD, bool PAIR>
 __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
     const uint16_t* __restrict__ Q, int64_t ldq, KvGeo kv, const int32_t* __restrict__ table, int64_t ldt, PagedWork work,
     int group, int cols, float cexp, uint32_t flip, uint16_t* __restrict__ O, int64_t ldo, Task* __restrict__ tasks,
@@ -200,12 +205,15 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
   constexpr int KEYS = G::KEYS, NB = G::NB, CK = G::CK, RB = G::RB, CH = G::CH, RPL = G::RPL, NL = G::NL, NS = G::NS;
   constexpr int NK = NL + NS;  // loads per operand and tile
   constexpr bool QUANT = FMT != DUO_KV_BF16;
+  constexpr int XB = PAIR ? NB / 2 : NB;  // blocks of 16 keys in a lane's scores
+  static_assert(QUANT || !PAIR, "");
   constexpr float BIAS = FMT == DUO_KV_I8 ? 128.f : 136.f;
   extern __shared__ __attribute__((aligned(16))) uint8_t lsm[];
   __shared__ Count cnt;
   __shared__ float jm[4][kCols], jl[4][kCols];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
+  const int col = PAIR ? l16 & 7 : l16, half = PAIR ? l16 >> 3 : 0;  // this lane's head, and half of the keys
 
   int64_t mine;
   const int64_t total = count_rows<KEYS>(work, cnt, &mine) * work.rows;
@@ -253,7 +261,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
       const int nc = min(cols, group - c0);
       const uint16_t* const q = Q + (int64_t)s * ldq + (h * group + c0) * HD;
       const uint8_t* const block0 = kv.data + h * kv.block;
-      const int64_t page_bytes = kv.heads * kv.block;
+      const uint32_t page_bytes = (uint32_t)(kv.heads * kv.block);
 
       // 64 pages of the table in one register, the next 64 in another
       bool bad = false;
@@ -268,7 +276,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
       int pid = ids(win), nid = ids(win + 64);
       u32x4 qf[CK];
 #pragma unroll
-      for (int c = 0; c < CK; ++c) qf[c] = *(const u32x4*)(q + min(l16, nc - 1) * HD + 32 * c + 8 * g);
+      for (int c = 0; c < CK; ++c) qf[c] = *(const u32x4*)(q + min(col, nc - 1) * HD + 32 * c + 8 * g);
 #pragma unroll
       for (int c = 0; c < CK; ++c) asm volatile("" : "+v"(qf[c]));  // waited for here, and not behind the tiles
       // this wave's loads of tile t's K (which = 0) or V rows and scales; K first
@@ -288,15 +296,28 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
           const int p = lane % CH;
           return 16 * (which ? v_at<FMT, CH>(r, p) : k_at<FMT, CH>(r, p));
         };
-        if (k0 + KEYS <= len && RPL <= 16) {
-          // whole tile: each group of 16 keys lies in one page, the same for all lanes
+        if (k0 + KEYS <= len && 1 << kv.shift >= KEYS) {
+          // whole tile in one page: its rows and scales are runs of bytes
+          const int id = __builtin_amdgcn_readlane(pid, (k0 >> kv.shift) - win);
+          const uint8_t* const at = block0 + (uint64_t)(uint32_t)id * page_bytes;
+          const int in = k0 & mask;
+          uint32_t off[NL];
+#pragma unroll
+          for (int i = 0; i < NL; ++i) off[i] = lane / CH * RB + chunk(i * RPL + lane / CH);
+          dma16_run<NL>(at + (rows_at + in * RB), off, rows);
+          if constexpr (QUANT) {
+#pragma unroll
+            for (int i = 0; i < NS; ++i) dma4(at + (scales_at + in * G::SB + 256 * i), lane * 4, scales + i * 256);
+          }
+        } else if (k0 + KEYS <= len && RPL <= 16) {
+          // whole tile in several pages: each group of 16 keys lies in one, the same for all lanes
           const uint8_t* base[NB];
           int in[NB];
 #pragma unroll
           for (int b = 0; b < NB; ++b) {
             const int key = k0 + 16 * b;
             const int id = __builtin_amdgcn_readlane(pid, (key >> kv.shift) - win);
-            base[b] = block0 + id * page_bytes;
+            base[b] = block0 + (uint64_t)(uint32_t)id * page_bytes;
             in[b] = key & mask;
           }
 #pragma unroll
@@ -325,7 +346,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
           auto place = [&](int r) {
             const int key = min(k0 + r, len - 1);
             const int id = __shfl(pid, (key >> kv.shift) - win);
-            return std::make_pair(block0 + id * page_bytes, key & mask);
+            return std::make_pair(block0 + (uint64_t)(uint32_t)id * page_bytes, key & mask);
           };
 #pragma unroll 1
           for (int i = 0; i < NL; ++i) {
@@ -357,11 +378,12 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
       }
       // Q^T's fragments, heads past the last as zeros; -bias sum(q) of every group
       float qs[CK];
+      u32x4 qh[CK];  // of the second half's columns
 #pragma unroll
       for (int c = 0; c < CK; ++c) {
         u32x4 v = qf[c];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = l16 < nc ? v[j] ^ flip : 0u;
+        for (int j = 0; j < 4; ++j) v[j] = col < nc ? v[j] ^ flip : 0u;
         if constexpr (QUANT) {
           float t = 0.f;
 #pragma unroll
@@ -371,7 +393,8 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
         if constexpr (FMT == DUO_KV_I4)  // channels j and j + 4 together, as widen4 gives them
           v = u32x4{(v[0] & 0xffffu) | v[2] << 16, v[0] >> 16 | (v[2] & 0xffff0000u), (v[1] & 0xffffu) | v[3] << 16,
                     v[1] >> 16 | (v[3] & 0xffff0000u)};
-        qf[c] = v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) qf[c][j] = half ? 0u : v[j], qh[c][j] = half ? v[j] : 0u;
       }
       for (uint8_t* sc = sS; t < t1; t += 4) {
         const bool more = t + 4 < t1;
@@ -380,7 +403,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
         // ---- scores
-        float x[NB][4];
+        float x[XB][4];
         if constexpr (!QUANT) {
           u32x4 kf[NB][CK];
 #pragma unroll
@@ -413,17 +436,19 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
           }
           wait_lds<0>();
           if (more) issue(t + 4, kK, sK, sn);
+          auto widen = [](const uint2& v) { return FMT == DUO_KV_I8 ? widen8(v.x, v.y) : widen4(v.x); };
 #pragma unroll
-          for (int b = 0; b < NB; ++b) {
+          for (int b = 0; b < XB; ++b) {
             uint32_t ks[2 * CK];  // scales of the lane's four keys
 #pragma unroll
-            for (int j = 0; j < 2 * CK; j += 4) *(u32x4*)&ks[j] = *(const u32x4*)(sc + (16 * b + 4 * g) * G::SB + 4 * j);
+            for (int j = 0; j < 2 * CK; j += 4)
+              *(u32x4*)&ks[j] = *(const u32x4*)(sc + (32 * half + 16 * b + 4 * g) * G::SB + 4 * j);
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[b][r] = 0.f;
 #pragma unroll
             for (int c = 0; c < CK; ++c) {
-              const u32x4 kf = FMT == DUO_KV_I8 ? widen8(kr[b][c].x, kr[b][c].y) : widen4(kr[b][c].x);
-              const f4 a = mma_bf16(kf, qf[c], f4{qs[c], qs[c], qs[c], qs[c]});
+              f4 a = mma_bf16(widen(kr[b][c]), qf[c], f4{qs[c], qs[c], qs[c], qs[c]});
+              if constexpr (PAIR) a = mma_bf16(widen(kr[b + XB][c]), qh[c], a);
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
                 const uint32_t w = ks[(r * CK + c) / 2];
@@ -433,17 +458,14 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
           }
         }
         // ---- probabilities relative to the running maximum
-        const int left = len - t * KEYS;  // tokens of the row from this tile on
-        const bool tail = left < KEYS;
-        if (tail)
+        const int left = len - t * KEYS - 32 * half - 4 * g;  // tokens of the row from this lane's first key on
 #pragma unroll
-          for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < XB; ++b)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (16 * b + 4 * g + r >= left) x[b][r] = -INFINITY;
+          for (int r = 0; r < 4; ++r) x[b][r] = 16 * b + r < left ? x[b][r] : -INFINITY;
         float mt = x[0][0];
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < XB; ++b)
 #pragma unroll
           for (int r = 0; r < 4; ++r) mt = fmaxf(mt, x[b][r]);
         mt = col_max(mt);
@@ -461,17 +483,11 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
         }
         const float base = m == -INFINITY ? 0.f : mc;
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < XB; ++b)
 #pragma unroll
           for (int r = 0; r < 4; ++r) x[b][r] = __builtin_amdgcn_exp2f(fmaf(x[b][r], cexp, -base));
-        if (tail)
 #pragma unroll
-          for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (16 * b + 4 * g + r >= left) x[b][r] = 0.f;
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < XB; ++b)
 #pragma unroll
           for (int r = 0; r < 4; ++r) l += x[b][r];
         // ---- times V
@@ -522,32 +538,45 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
           if (more) issue(t + 4, kV, sV, sn + NS * 256);
           const uint32_t nb = pack_bf16(-BIAS, -BIAS);
           const u32x4 bias = {nb, nb, nb, nb};
-#pragma unroll
-          for (int st = 0; st < 2; ++st) {
+          // probabilities times scales of the 32 keys of blocks 2 st and 2 st + 1, by groups of channels
+          auto weigh = [&](int st, u32x4 (&pf)[CK]) __attribute__((always_inline)) {
             uint32_t vs[2][2 * CK];
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
               for (int j = 0; j < 2 * CK; j += 4)
-                *(u32x4*)&vs[b][j] = *(const u32x4*)(sc + NS * 256 + (32 * st + 16 * b + 4 * g) * G::SB + 4 * j);
+                *(u32x4*)&vs[b][j] =
+                    *(const u32x4*)(sc + NS * 256 + (32 * (PAIR ? half : st) + 16 * b + 4 * g) * G::SB + 4 * j);
 #pragma unroll
             for (int c = 0; c < CK; ++c) {
               float p[8];
 #pragma unroll
               for (int e = 0; e < 8; ++e) {
-                const int b = 2 * st + (e >> 2), r = e & 3;
+                const int r = e & 3;
                 const uint32_t w = vs[e >> 2][(r * CK + c) / 2];
-                p[e] = x[b][r] * ((r * CK + c) & 1 ? hi16(w) : lo16(w));
+                p[e] = x[(PAIR ? 0 : 2 * st) + (e >> 2)][r] * ((r * CK + c) & 1 ? hi16(w) : lo16(w));
               }
-              u32x4 pf;
 #pragma unroll
               for (int j = 0; j < 4; ++j)
-                pf[j] = FMT == DUO_KV_I8 ? pack_bf16(p[2 * j], p[2 * j + 1]) : pack_bf16(p[j], p[j + 4]);
+                pf[c][j] = FMT == DUO_KV_I8 ? pack_bf16(p[2 * j], p[2 * j + 1]) : pack_bf16(p[j], p[j + 4]);
+            }
+          };
+          u32x4 pf[CK];
+          if constexpr (PAIR) weigh(0, pf);
+#pragma unroll
+          for (int st = 0; st < 2; ++st) {
+            if constexpr (!PAIR) weigh(st, pf);
+#pragma unroll
+            for (int c = 0; c < CK; ++c) {
+              u32x4 ph = pf[c];
+              if constexpr (PAIR)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) ph[j] = half == st ? ph[j] : 0u;
 #pragma unroll
               for (int d = 2 * c; d < 2 * c + 2; ++d) {
                 const u32x4 vf = FMT == DUO_KV_I8 ? widen8((uint32_t)vr[st][d][0], (uint32_t)vr[st][d][1])
                                                   : widen4((uint32_t)vr[0][d][st]);
-                o[d] = mma_bf16(vf, pf, mma_bf16(bias, pf, o[d]));
+                o[d] = mma_bf16(vf, ph, mma_bf16(bias, ph, o[d]));
               }
             }
           }
@@ -561,7 +590,12 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
       l = col_sum(l);
       if (g == 0) jm[wave][l16] = mc, jl[wave][l16] = l;
       __syncthreads();
-      const float top = fmaxf(fmaxf(jm[0][l16], jm[1][l16]), fmaxf(jm[2][l16], jm[3][l16]));
+      auto largest = [&](int c) {
+        float v = fmaxf(fmaxf(jm[0][c], jm[1][c]), fmaxf(jm[2][c], jm[3][c]));
+        if constexpr (PAIR) v = fmaxf(v, fmaxf(fmaxf(jm[0][c + 8], jm[1][c + 8]), fmaxf(jm[2][c + 8], jm[3][c + 8])));
+        return v;
+      };
+      const float top = largest(col);
       {
         const float f = mc == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - top);
         float* y = (float*)sK + l16 * G::OLD + 4 * g;
@@ -581,13 +615,14 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
       }
       for (int e = tid; e < nc * (HD / 2); e += 256) {
         const int c = e / (HD / 2), d = e % (HD / 2) * 2;
-        const float big = fmaxf(fmaxf(jm[0][c], jm[1][c]), fmaxf(jm[2][c], jm[3][c]));
+        const float big = largest(c);
         float sum = 0.f, v0 = 0.f, v1 = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const float f = jm[w][c] == -INFINITY ? (jl[w][c] == 0.f ? 0.f : jl[w][c]) : __builtin_amdgcn_exp2f(jm[w][c] - big);
-          sum += jl[w][c] * f;
-          const float* y = (const float*)(lsm + w * G::WAVE) + c * G::OLD + d;
+        for (int i = 0; i < (PAIR ? 8 : 4); ++i) {
+          const int w = i & 3, k = c + 8 * (i >> 2);
+          const float f = jm[w][k] == -INFINITY ? (jl[w][k] == 0.f ? 0.f : jl[w][k]) : __builtin_amdgcn_exp2f(jm[w][k] - big);
+          sum += jl[w][k] * f;
+          const float* y = (const float*)(lsm + w * G::WAVE) + k * G::OLD + d;
           v0 += y[0];
           v1 += y[1];
         }
@@ -713,7 +748,8 @@ duo_status duo_attention_paged(const void* Q, int64_t ldq, const duo_kv_cache* c
   if (duo_status d = device_ok(); d != DUO_OK) return d;
   const hipStream_t s = (hipStream_t)stream;
   // exp(x scale) = 2^(x cexp); a negative scale turns the queries' signs instead
-  const float cexp = (float)(std::fabs(scale) * 1.4426950408889634);
+  // (never 0: the scores of tokens past the end, -inf, have to stay that)
+  const float cexp = std::max((float)(std::fabs(scale) * 1.4426950408889634), 1.4e-45f);
   const uint32_t flip = scale < 0.0 ? 0x80008000u : 0u;
   const int vec = ldo % 2 == 0 && reinterpret_cast<uintptr_t>(O) % 4 == 0;
   return kv_by_format(cache, [&](auto fmt, auto dim) -> duo_status {
@@ -723,7 +759,8 @@ duo_status duo_attention_paged(const void* Q, int64_t ldq, const duo_kv_cache* c
     const PagedWork w = {lens, (int)nseq, (int)max_len, (int)rows, (int)cdiv(nseq, 256)};
     Task* const tasks = (Task*)ws;
     float* const part = (float*)((uint8_t*)ws + align_up(wgs * sizeof(Task)));
-    const auto kern = paged_kernel<FMT, HD>;
+    constexpr bool Q8 = FMT != DUO_KV_BF16;
+    const auto kern = Q8 && cols <= 8 ? paged_kernel<FMT, HD, Q8> : paged_kernel<FMT, HD, false>;
     if (duo_status st = set_max_lds((const void*)kern, 4 * P::WAVE); st != DUO_OK) return st;
     hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(256), 4 * P::WAVE, s, (const uint16_t*)Q, ldq, g, table, ldt, w,
                        (int)group, (int)cols, cexp, flip, (uint16_t*)O, ldo, max_len > 0 ? tasks : nullptr, part, vec);
