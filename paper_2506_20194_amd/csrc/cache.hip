@@ -7,7 +7,7 @@
 // x and s have eight significant bits, so a quotient that is no half integer is at
 // least 2^-16 (relative) away from one, and x / s in fp32 rounds to the code of the
 // exact quotient, ties included where the division is exact at them.  The kernel
-// forms x (1/s) and corrects it by its exact remainder once, which is exact at ties.
+// forms x (1/s) and corrects it once by its remainder, which is exact at ties.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -79,116 +79,176 @@ __global__ __launch_bounds__(256) void rope_at_kernel(const uint16_t* X, int64_t
 }
 
 // ---------------------------------------------------------------------------
-// writing
+// writing and reading
 // ---------------------------------------------------------------------------
 
-// One thread per 8 channels of one row of K (which = 0) or V; the four threads of a
-// group of 32 agree on its scale.
+// Both directions: blockIdx.y is a head's K (even) or V, a thread takes 8 channels of
+// kTok tokens, whose slots and rows are all loaded before the first is used.  Bound: HBM;
+// a CU has some 80 vector instructions per 8 channels in the time of their bytes.
+constexpr int kTok = 4;
+
+// Where the row of slot `slot` begins in the cache, and its scales (which: 0 K, 1 V).
+template <int FMT, int HD>
+struct KvRow {
+  uint8_t *codes, *scales;
+  __device__ KvRow(const KvGeo& g, int64_t slot, int h, int which) {
+    const uint32_t page = (uint32_t)(slot >> g.shift), row = (uint32_t)slot & ((1u << g.shift) - 1);
+    uint8_t* const blk = g.data + h * g.block + (uint64_t)page * (uint32_t)(g.heads * g.block);
+    codes = blk + kv_rows_at<FMT, HD>(which, g.shift) + row * KvFmt<FMT>::row(HD);
+    scales = blk + kv_scales_at<FMT, HD>(which, g.shift) + row * KvFmt<FMT>::scales(HD);
+  }
+};
+
+// The codes of a group of 32 channels, eight per thread and four threads in a row, with what
+// is added to them (8 bits: in bytes of q.x, q.y; 4 bits: in q.x), and the scale.
+template <int FMT>
+__device__ __forceinline__ uint2 kv_encode(const u32x4& x, uint16_t* scale) {
+  typedef unsigned short u16v2 __attribute__((ext_vector_type(2)));
+  u16v2 most2 = {0, 0};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    u16v2 v;
+    const uint32_t a = x[j] & 0x7fff7fffu;
+    __builtin_memcpy(&v, &a, 4);
+    most2 = __builtin_elementwise_max(most2, v);
+  }
+  uint32_t mag = most2[0] > most2[1] ? most2[0] : most2[1];
+  mag = max(mag, (uint32_t)__shfl_xor((int)mag, 1));
+  mag = max(mag, (uint32_t)__shfl_xor((int)mag, 2));
+  constexpr int most = KvFmt<FMT>::most, bias = KvFmt<FMT>::bias;
+  // max |x| / q is never within 2^-17 of halfway between two bf16 numbers, so the product
+  // rounds as the quotient does
+  const uint16_t sb = f32_to_bf16_bits(bf16_bits_to_f32((uint16_t)mag) * (1.0f / most));
+  const float s = bf16_bits_to_f32(sb);
+  const bool some = mag < 0x7f80u && s >= 1.1754943508222875e-38f;
+  *scale = some ? sb : mag < 0x7f80u ? 0 : 0x7fc0u;
+  const float inv = some ? __builtin_amdgcn_rcpf(s) : 0.f, div = some ? s : 0.f;
+  uint32_t code[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float v = some ? __uint_as_float(j & 1 ? x[j >> 1] & 0xffff0000u : x[j >> 1] << 16) : 0.f;
+    const float q = v * inv;
+    // + 1.5 2^23: the nearest whole number, ties to even, in the low bits; it lies within
+    // the codes, as s is at most 2^-8 too small
+    code[j] = __float_as_uint(fmaf(fmaf(-q, div, v), inv, q) + (12582912.0f + bias));
+  }
+  uint2 q = {0, 0};
+  if constexpr (FMT == DUO_KV_I8) {
+    auto bytes = [&](int j) {
+      return __builtin_amdgcn_perm(__builtin_amdgcn_perm(code[j + 3], code[j + 2], 0x0c0c0400u),
+                                   __builtin_amdgcn_perm(code[j + 1], code[j], 0x0c0c0400u), 0x05040100u);
+    };
+    q.x = bytes(0);
+    q.y = bytes(4);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q.x |= (code[j] & 15u) << (4 * j);
+  }
+  return q;
+}
+
 template <int FMT, int HD>
 __global__ __launch_bounds__(256) void kv_write_kernel(const uint16_t* __restrict__ K, int64_t ldk,
                                                        const uint16_t* __restrict__ V, int64_t ldv,
-                                                       const int64_t* __restrict__ slots, int64_t m, KvGeo g) {
-  constexpr int C = HD / 8;  // threads per row
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int c = (int)(id % C);
-  const int64_t r = id / C;
-  const int which = (int)(r % 2), h = (int)(r / 2 % g.heads);
-  const int64_t t = r / 2 / g.heads;
-  const bool in = t < m;
-  const int64_t slot = in ? slots[t] : -1;
-  const bool ok = slot >= 0 && slot < g.pages << g.shift;
-  const uint16_t* src = (which ? V + (in ? t : 0) * ldv : K + (in ? t : 0) * ldk) + h * HD + 8 * c;
-  const u32x4 x = in ? *(const u32x4*)src : u32x4{0u, 0u, 0u, 0u};
-  const int64_t page = ok ? slot >> g.shift : 0;
-  const int row = ok ? (int)(slot & ((1 << g.shift) - 1)) : 0;
-  uint8_t* blk = g.data + (page * g.heads + h) * g.block;
-  uint8_t* dst = blk + kv_rows_at<FMT, HD>(which, g.shift) + row * KvFmt<FMT>::row(HD);
-  if constexpr (FMT == DUO_KV_BF16) {
-    if (ok) *(u32x4*)(dst + 16 * c) = x;
-  } else {
-    uint32_t mag = 0;
+                                                       const int64_t* __restrict__ slots, int m, KvGeo g) {
+  constexpr int C = HD / 8, T = 256 / C;  // threads per row, tokens at once
+  const int which = blockIdx.y & 1, h = blockIdx.y >> 1;
+  const int c = threadIdx.x % C, t0 = blockIdx.x * (T * kTok) + threadIdx.x / C;
+  const uint16_t* const src = (which ? V : K) + h * HD + 8 * c;
+  const int64_t ld = which ? ldv : ldk;
+  int64_t slot[kTok];
+  u32x4 x[kTok];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) mag = max(mag, max(x[j] & 0x7fffu, x[j] >> 16 & 0x7fffu));
-    mag = max(mag, (uint32_t)__shfl_xor((int)mag, 1));
-    mag = max(mag, (uint32_t)__shfl_xor((int)mag, 2));
-    constexpr int most = KvFmt<FMT>::most, bias = KvFmt<FMT>::bias;
-    const bool fin = mag < 0x7f80u;
-    uint16_t sb = f32_to_bf16_bits(bf16_bits_to_f32((uint16_t)mag) / (float)most);
-    float s = bf16_bits_to_f32(sb);
-    const bool some = fin && s >= 1.1754943508222875e-38f;
-    if (!some) sb = fin ? 0 : 0x7fc0u;
-    const float inv = some ? 1.0f / s : 0.f;
-    s = some ? s : 0.f;
-    uint32_t code[8];
+  for (int i = 0; i < kTok; ++i) {
+    const int t = min(t0 + i * T, m - 1);
+    slot[i] = t0 + i * T < m ? slots[t] : -1;
+    x[i] = *(const u32x4*)(src + t * ld);
+  }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float v = some ? bf16_bits_to_f32((uint16_t)(x[j >> 1] >> (16 * (j & 1)))) : 0.f;
-      const float q = v * inv;
-      const float n = rintf(fmaf(fmaf(-q, s, v), inv, q));
-      code[j] = (uint32_t)((int)fminf(fmaxf(n, (float)-most), (float)most) + bias);
-    }
-    if (ok) {
-      if constexpr (FMT == DUO_KV_I8) {
-        uint2 w;
-        w.x = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
-        w.y = code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24;
-        *(uint2*)(dst + 8 * c) = w;
-      } else {
-        uint32_t w = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w |= code[j] << (4 * j);
-        *(uint32_t*)(dst + 4 * c) = w;
+  for (int i = 0; i < kTok; ++i) {
+    const bool ok = slot[i] >= 0 && slot[i] < g.pages << g.shift;
+    const KvRow<FMT, HD> row(g, ok ? slot[i] : 0, h, which);
+    if constexpr (FMT == DUO_KV_BF16) {
+      if (ok) *(u32x4*)(row.codes + 16 * c) = x[i];
+    } else {
+      uint16_t s;
+      const uint2 q = kv_encode<FMT>(x[i], &s);
+      if (ok) {
+        if constexpr (FMT == DUO_KV_I8)
+          *(uint2*)(row.codes + 8 * c) = q;
+        else
+          *(uint32_t*)(row.codes + 4 * c) = q.x;
+        if (c % 4 == 0) *(uint16_t*)(row.scales + c / 4 * 2) = s;
       }
-      if (c % 4 == 0)
-        *(uint16_t*)(blk + kv_scales_at<FMT, HD>(which, g.shift) + row * KvFmt<FMT>::scales(HD) + c / 4 * 2) = sb;
     }
   }
 }
 
-// ---------------------------------------------------------------------------
-// reading
-// ---------------------------------------------------------------------------
 template <int FMT, int HD>
-__global__ __launch_bounds__(256) void kv_read_kernel(KvGeo g, const int64_t* __restrict__ slots, int64_t m,
+__global__ __launch_bounds__(256) void kv_read_kernel(KvGeo g, const int64_t* __restrict__ slots, int m,
                                                       uint16_t* __restrict__ K, int64_t ldk, uint16_t* __restrict__ V,
                                                       int64_t ldv) {
-  constexpr int C = HD / 8;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int c = (int)(id % C);
-  const int64_t r = id / C;
-  const int which = (int)(r % 2), h = (int)(r / 2 % g.heads);
-  const int64_t t = r / 2 / g.heads;
-  if (t >= m) return;
-  const int64_t slot = slots[t];
-  u32x4 y = {0u, 0u, 0u, 0u};
-  if (slot >= 0 && slot < g.pages << g.shift) {
-    const int row = (int)(slot & ((1 << g.shift) - 1));
-    const uint8_t* blk = g.data + ((slot >> g.shift) * g.heads + h) * g.block;
-    const uint8_t* src = blk + kv_rows_at<FMT, HD>(which, g.shift) + row * KvFmt<FMT>::row(HD);
+  constexpr int C = HD / 8, T = 256 / C;
+  const int which = blockIdx.y & 1, h = blockIdx.y >> 1;
+  const int c = threadIdx.x % C, t0 = blockIdx.x * (T * kTok) + threadIdx.x / C;
+  uint16_t* const dst = (which ? V : K) + h * HD + 8 * c;
+  const int64_t ld = which ? ldv : ldk;
+  int64_t slot[kTok];
+#pragma unroll
+  for (int i = 0; i < kTok; ++i) slot[i] = slots[min(t0 + i * T, m - 1)];
+  u32x4 y[kTok];
+  uint2 q[kTok];
+  float s[kTok];
+#pragma unroll
+  for (int i = 0; i < kTok; ++i) {
+    const bool ok = slot[i] >= 0 && slot[i] < g.pages << g.shift;
+    const KvRow<FMT, HD> row(g, ok ? slot[i] : 0, h, which);
     if constexpr (FMT == DUO_KV_BF16) {
-      y = *(const u32x4*)(src + 16 * c);
+      y[i] = *(const u32x4*)(row.codes + 16 * c);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[i][j] = ok ? y[i][j] : 0u;
     } else {
-      const float s = bf16_bits_to_f32(
-          *(const uint16_t*)(blk + kv_scales_at<FMT, HD>(which, g.shift) + row * KvFmt<FMT>::scales(HD) + c / 4 * 2));
-      uint2 w;
+      const float v = bf16_bits_to_f32(*(const uint16_t*)(row.scales + c / 4 * 2));
       if constexpr (FMT == DUO_KV_I8)
-        w = *(const uint2*)(src + 8 * c);
+        q[i] = *(const uint2*)(row.codes + 8 * c);
       else
-        w.x = *(const uint32_t*)(src + 4 * c);
-      float v[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint32_t n = FMT == DUO_KV_I8 ? ((j < 4 ? w.x : w.y) >> (8 * (j & 3)) & 255u) : (w.x >> (4 * j) & 15u);
-        const float p = (float)((int)n - KvFmt<FMT>::bias) * s;
-        // a code times a scale near bf16's end may round past it; NaN stays NaN
-        v[j] = fabsf(p) > 3.3895313892515355e38f ? copysignf(3.3895313892515355e38f, p) : p;
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+        q[i].x = *(const uint32_t*)(row.codes + 4 * c);
+      s[i] = ok ? v : 0.f;
     }
   }
-  *(u32x4*)((which ? V + t * ldv : K + t * ldk) + h * HD + 8 * c) = y;
+#pragma unroll
+  for (int i = 0; i < kTok; ++i) {
+    if (t0 + i * T >= m) break;
+    if constexpr (FMT != DUO_KV_BF16) {
+      constexpr float bias = KvFmt<FMT>::bias;
+      float v[8];  // codes with their bias
+      if constexpr (FMT == DUO_KV_I8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (float)((j < 4 ? q[i].x : q[i].y) >> (8 * (j & 3)) & 255u);
+      } else {
+        const uint32_t even = q[i].x & 0x0f0f0f0fu, odd = q[i].x >> 4 & 0x0f0f0f0fu;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (float)((j & 1 ? odd : even) >> (8 * (j >> 1)) & 255u);
+      }
+      if (__any(s[i] > 6.6e35f)) {  // a code times a scale near bf16's end may round past it
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float p = (v[j] - bias) * s[i];  // NaN stays NaN
+          v[j] = fabsf(p) > 3.3895313892515355e38f ? copysignf(3.3895313892515355e38f, p) : p;
+        }
+      } else {  // n s - bias s is exact in fp32
+        const float off = s[i] * -bias;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = fmaf(v[j], s[i], off);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[i][j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+    }
+    *(u32x4*)(dst + (t0 + i * T) * ld) = y[i];
+  }
 }
+
+dim3 kv_grid(int64_t m, int hd, int heads) { return dim3((unsigned)cdiv(m, 256 / (hd / 8) * kTok), 2 * heads); }
 
 // Common checks of duo_kv_write and duo_kv_read.
 duo_status rows_ok(const duo_kv_cache* c, const void* K, int64_t ldk, const void* V, int64_t ldv, const int64_t* slots,
@@ -200,7 +260,7 @@ duo_status rows_ok(const duo_kv_cache* c, const void* K, int64_t ldk, const void
   if (m == 0) return DUO_OK;
   if (!K || !V || !slots) return DUO_ERR_INVALID_ARG;
   if (ldk % 8 || ldv % 8 || !aligned16(K) || !aligned16(V)) return DUO_ERR_UNSUPPORTED;
-  if (m > INT32_MAX || cdiv(m * 2 * w / 8, 256) > INT32_MAX) return DUO_ERR_UNSUPPORTED;
+  if (m > (int64_t)1 << 30) return DUO_ERR_UNSUPPORTED;
   return DUO_OK;
 }
 
@@ -279,8 +339,8 @@ duo_status duo_kv_write(const duo_kv_cache* cache, const void* K, int64_t ldk, c
   if (duo_status d = device_ok(); d != DUO_OK) return d;
   return kv_by_format(cache, [&](auto fmt, auto hd) -> duo_status {
     constexpr int FMT = decltype(fmt)::value, HD = decltype(hd)::value;
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_write_kernel<FMT, HD>), dim3((unsigned)cdiv(m * 2 * g.heads * (HD / 8), 256)),
-                       dim3(256), 0, (hipStream_t)stream, (const uint16_t*)K, ldk, (const uint16_t*)V, ldv, slots, m, g);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_write_kernel<FMT, HD>), kv_grid(m, HD, g.heads), dim3(256), 0,
+                       (hipStream_t)stream, (const uint16_t*)K, ldk, (const uint16_t*)V, ldv, slots, (int)m, g);
     DUO_LAUNCH_CHECK();
     return DUO_OK;
   });
@@ -294,8 +354,8 @@ duo_status duo_kv_read(const duo_kv_cache* cache, const int64_t* slots, int64_t 
   if (duo_status d = device_ok(); d != DUO_OK) return d;
   return kv_by_format(cache, [&](auto fmt, auto hd) -> duo_status {
     constexpr int FMT = decltype(fmt)::value, HD = decltype(hd)::value;
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_read_kernel<FMT, HD>), dim3((unsigned)cdiv(m * 2 * g.heads * (HD / 8), 256)),
-                       dim3(256), 0, (hipStream_t)stream, g, slots, m, (uint16_t*)K, ldk, (uint16_t*)V, ldv);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_read_kernel<FMT, HD>), kv_grid(m, HD, g.heads), dim3(256), 0,
+                       (hipStream_t)stream, g, slots, (int)m, (uint16_t*)K, ldk, (uint16_t*)V, ldv);
     DUO_LAUNCH_CHECK();
     return DUO_OK;
   });
