@@ -9,7 +9,8 @@
 // depends on the lengths, which only the device knows.  A workgroup's four waves
 // take the tiles of a row in turn, each with its own running maximum and sum, and
 // join at the row's end; a row that lies in one share is finished there, the parts
-// of one that does not go to the workspace and are joined by a second launch.
+// of one that does not go to the workspace and are joined by a second launch.  Where rows
+// are many, short ones go four to a workgroup, one for each wave.
 //
 // A wave computes transposed, with v_mfma_f32_16x16x32_bf16:
 //   S^T = K Q^T  (16 keys x 16 heads per instruction): a lane's scores belong to one
@@ -50,8 +51,9 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) % 16) == 
 
 constexpr int kCols = 16;       // query heads per row
 constexpr int kMaxWg = 1024;    // workgroups of a launch, at most
-constexpr int kRowCost = 4;     // what a row's start and end cost, in tiles
+constexpr int kRowCost = 10;    // what a row's start and end cost, in tiles
 constexpr int kMinShare = 8;    // smallest share, in tiles
+constexpr int kShort = 4;       // tiles of a row that one wave does alone where rows are many
 constexpr int kMinKeys = 32;    // tokens of the smallest tile
 
 template <int FMT, int HD>
@@ -75,6 +77,7 @@ struct PagedWork {
   const int32_t* lens;
   int nseq, max_len, rows;  // rows per sequence
   int per;                  // sequences per bucket of the count: ceil(nseq / 256)
+  int many;                 // rows enough for every share: short ones go four to a workgroup
 };
 
 // A row that begins in a share and ends in another one: the join's task.  parts = 0: none.
@@ -87,7 +90,18 @@ __device__ inline int seq_len(const PagedWork& w, int s) { return min(max(w.lens
 // Tiles, and what counts for one row of them.
 template <int KEYS>
 __device__ inline int tiles_of(int len) { return (len + KEYS - 1) / KEYS; }
-__device__ inline int cost_of(int tiles) { return tiles ? tiles + kRowCost : 0; }
+
+// The rows of a sequence of `tiles` tiles: `units` of `cost` each.  A unit is a row, or four
+// rows, one for each wave, where they are short and many.
+struct Units {
+  int tiles, cost, units;
+  bool quad;
+  __device__ Units(int tiles, const PagedWork& w) : tiles(tiles) {
+    quad = w.many && tiles <= kShort;
+    units = tiles == 0 ? 0 : quad ? (w.rows + 3) / 4 : w.rows;
+    cost = (quad ? 4 * tiles : tiles) + kRowCost;
+  }
+};
 
 __device__ inline uint64_t div64(uint64_t a, uint32_t b) { return a >> 32 ? a / b : (uint32_t)a / b; }
 
@@ -108,13 +122,13 @@ struct Shares {
   }
 };
 
-// cost[i]: of one row of every sequence up to the end of bucket i; len: of the sequences,
-// where a bucket is one.  256 threads; ends with a barrier.
+// *mine: cost of the sequences up to the end of this thread's bucket; the result: of all.
+// 256 threads; ends with a barrier.
 struct Count {
   int64_t wave[4];
   int64_t before;  // cost of the sequences before bucket `at`
   int at;
-  int len[256];
+  int len[256];    // of the sequences, where a bucket is one
 };
 template <int KEYS>
 __device__ inline int64_t count_rows(const PagedWork& w, Count& c, int64_t* mine) {
@@ -124,7 +138,8 @@ __device__ inline int64_t count_rows(const PagedWork& w, Count& c, int64_t* mine
     const int64_t s = (int64_t)tid * w.per + i;
     const int len = s < w.nseq ? seq_len(w, (int)s) : 0;
     if (w.per == 1) c.len[tid] = len;
-    n += cost_of(tiles_of<KEYS>(len));
+    const Units x(tiles_of<KEYS>(len), w);
+    n += (int64_t)x.cost * x.units;
   }
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -155,6 +170,11 @@ __device__ __forceinline__ float col_sum(float v) {
   v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
   const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// The value of the lane eight places on, within groups of sixteen lanes.
+__device__ __forceinline__ float ror8(float v) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x128, 0xf, 0xf, false));
 }
 
 __device__ __forceinline__ float lo16(uint32_t v) { return __uint_as_float(v << 16); }
@@ -216,7 +236,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
   const int col = PAIR ? l16 & 7 : l16, half = PAIR ? l16 >> 3 : 0;  // this lane's head, and half of the keys
 
   int64_t mine;
-  const int64_t total = count_rows<KEYS>(work, cnt, &mine) * work.rows;
+  const int64_t total = count_rows<KEYS>(work, cnt, &mine);
   const Shares shares(total, gridDim.x);
   int64_t u = shares.begin(blockIdx.x);
   const int64_t u1 = (int)blockIdx.x < shares.n ? shares.begin(blockIdx.x + 1) : u;
@@ -226,7 +246,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
     int64_t prev = lane ? upto : 0;
     if (lane == 0)
       for (int i = 0; i < wave; ++i) prev += cnt.wave[i];
-    if (prev * work.rows <= u && u < mine * work.rows) cnt.at = tid, cnt.before = prev * work.rows;
+    if (prev <= u && u < mine) cnt.at = tid, cnt.before = prev;
   }
   if (tid == 0 && tasks) tasks[blockIdx.x].parts = 0;
   __syncthreads();
@@ -243,19 +263,30 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
 
   for (int s = cnt.at * work.per; u < u1; ++s) {
     const int len = len_of(s);
-    const int tiles = tiles_of<KEYS>(len), cost = cost_of(tiles);
+    const Units x(tiles_of<KEYS>(len), work);
+    const int tiles = x.tiles, cost = x.cost;
     const int64_t start = before;
-    before += (int64_t)cost * work.rows;
+    before += (int64_t)cost * x.units;
     if (before <= u) continue;
     const int32_t* const pages = table + (int64_t)s * ldt;
     const int last_page = (len - 1) >> kv.shift;
     while (u < u1 && u < before) {
       // one row, or what of it is in this share
-      const int row = (int)div64((uint64_t)(u - start), (uint32_t)cost), at = (int)(u - start - (int64_t)row * cost);
+      int row = (int)div64((uint64_t)(u - start), (uint32_t)cost);
+      const int at = (int)(u - start - (int64_t)row * cost);
       const int here = (int)min((int64_t)(cost - at), u1 - u);
-      const int t0 = max(at - kRowCost, 0), t1 = max(at + here - kRowCost, 0);
+      int t0 = max(at - kRowCost, 0), t1 = max(at + here - kRowCost, 0);
       const int64_t row_end = u + (cost - at);
       u += here;
+      int t = t0 + wave, step = 4;  // this wave's tiles
+      if (x.quad) {  // whole in the share that it begins in
+        if (at > 0) continue;
+        row = 4 * row + wave;
+        if (row >= work.rows) continue;
+        t = t0 = 0;
+        t1 = tiles;
+        step = 1;
+      }
       if (t0 >= t1) continue;
       const int h = row % kv.heads, c0 = row / kv.heads * kCols;  // K/V head, first of its query heads
       const int nc = min(cols, group - c0);
@@ -265,7 +296,6 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
 
       // 64 pages of the table in one register, the next 64 in another
       bool bad = false;
-      int t = t0 + wave;
       int win = (t * KEYS >> kv.shift) & ~3;  // a tile's pages, four at most, lie in one window
       auto ids = [&](int p) {
         int id = pages[min(p + lane, last_page)];
@@ -396,8 +426,8 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
 #pragma unroll
         for (int j = 0; j < 4; ++j) qf[c][j] = half ? 0u : v[j], qh[c][j] = half ? v[j] : 0u;
       }
-      for (uint8_t* sc = sS; t < t1; t += 4) {
-        const bool more = t + 4 < t1;
+      for (uint8_t* sc = sS; t < t1; t += step) {
+        const bool more = t + step < t1;
         uint8_t* const sn = sc == sS ? sS + 2 * NS * 256 : sS;  // the next tile's scales
         wait_vm<NK>();  // K of this tile
         asm volatile("" ::: "memory");
@@ -412,7 +442,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
             for (int c = 0; c < CK; ++c)
               kf[b][c] = *(const u32x4*)(sK + (16 * b + l16) * RB + 16 * k_at<FMT, CH>(16 * b + l16, 4 * c + g));
           wait_lds<0>();
-          if (more) issue(t + 4, kK, sK, sn);
+          if (more) issue(t + step, kK, sK, sn);
 #pragma unroll
           for (int b = 0; b < NB; ++b) {
             f4 a = {0.f, 0.f, 0.f, 0.f};
@@ -435,7 +465,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
             }
           }
           wait_lds<0>();
-          if (more) issue(t + 4, kK, sK, sn);
+          if (more) issue(t + step, kK, sK, sn);
           auto widen = [](const uint2& v) { return FMT == DUO_KV_I8 ? widen8(v.x, v.y) : widen4(v.x); };
 #pragma unroll
           for (int b = 0; b < XB; ++b) {
@@ -510,7 +540,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
             __builtin_memcpy((char*)&vf[d] + 8, &b, 8);
           }
           wait_lds<0>();
-          if (more) issue(t + 4, kV, sV, sn + NS * 256);
+          if (more) issue(t + step, kV, sV, sn + NS * 256);
           const u32x4 pf = {pack_bf16(x[0][0], x[0][1]), pack_bf16(x[0][2], x[0][3]), pack_bf16(x[1][0], x[1][1]),
                             pack_bf16(x[1][2], x[1][3])};
 #pragma unroll
@@ -535,7 +565,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
             }
           }
           wait_lds<0>();
-          if (more) issue(t + 4, kV, sV, sn + NS * 256);
+          if (more) issue(t + step, kV, sV, sn + NS * 256);
           const uint32_t nb = pack_bf16(-BIAS, -BIAS);
           const u32x4 bias = {nb, nb, nb, nb};
           // probabilities times scales of the 32 keys of blocks 2 st and 2 st + 1, by groups of channels
@@ -588,6 +618,38 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
       for (int d = 0; d < 2 * CK; ++d) asm volatile("s_nop 7" : "+v"(o[d]));  // the last products have been written
       if (__any(bad)) l = NAN;
       l = col_sum(l);
+      if (x.quad) {
+        // alone: the halves of the keys joined in registers, and written
+        if constexpr (PAIR) {
+          const float mo = ror8(mc), top = fmaxf(mc, mo);
+          // a half without a finite score holds zeros, or NaN that has to stay
+          const float f = mc == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - top);
+          l = mc == -INFINITY ? l : l * f;
+          l += ror8(l);
+#pragma unroll
+          for (int d = 0; d < 2 * CK; ++d)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float v = o[d][r] * f;
+              o[d][r] = v + ror8(v);
+            }
+        }
+        if (half == 0 && col < nc) {
+          uint16_t* const y = O + (int64_t)s * ldo + (h * group + c0 + col) * HD + 4 * g;
+#pragma unroll
+          for (int d = 0; d < 2 * CK; ++d) {
+            const uint32_t y0 = pack_bf16(o[d][0] / l, o[d][1] / l), y1 = pack_bf16(o[d][2] / l, o[d][3] / l);
+            if (vec) {
+              *(uint32_t*)(y + 16 * d) = y0;
+              *(uint32_t*)(y + 16 * d + 2) = y1;
+            } else {
+              y[16 * d] = (uint16_t)y0, y[16 * d + 1] = (uint16_t)(y0 >> 16);
+              y[16 * d + 2] = (uint16_t)y1, y[16 * d + 3] = (uint16_t)(y1 >> 16);
+            }
+          }
+        }
+        continue;
+      }
       if (g == 0) jm[wave][l16] = mc, jl[wave][l16] = l;
       __syncthreads();
       auto largest = [&](int c) {
@@ -756,7 +818,7 @@ duo_status duo_attention_paged(const void* Q, int64_t ldq, const duo_kv_cache* c
     constexpr int FMT = decltype(fmt)::value, HD = decltype(dim)::value;
     using P = PagedGeo<FMT, HD>;
     const int64_t wgs = paged_wgs((double)nseq * (double)rows, cdiv(max_len, P::KEYS), 256 * P::WGS);
-    const PagedWork w = {lens, (int)nseq, (int)max_len, (int)rows, (int)cdiv(nseq, 256)};
+    const PagedWork w = {lens, (int)nseq, (int)max_len, (int)rows, (int)cdiv(nseq, 256), nseq * rows >= 2 * 256 * P::WGS};
     Task* const tasks = (Task*)ws;
     float* const part = (float*)((uint8_t*)ws + align_up(wgs * sizeof(Task)));
     constexpr bool Q8 = FMT != DUO_KV_BF16;

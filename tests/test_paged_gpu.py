@@ -288,3 +288,14 @@ def test_refusals(duo_lib):
         duo_lib.KVCache.empty(4, 24, 2, 64, "int8")
     with pytest.raises(TypeError):
         duo_lib.duo_kv_write(cache, Q[:, :128].contiguous(), Q[:, :128].contiguous(), n)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("nseq,heads,kv,hd", [(120, 16, 16, 128), (330, 5, 5, 64), (210, 96, 8, 128), (200, 64, 8, 64)])
+def test_many_short_rows(duo_lib, nseq, heads, kv, hd, fmt):
+    """Rows (sequences times K/V heads) in the thousands, where short ones are done by
+    single waves, with longer and empty ones between them."""
+    say("paged many short rows", nseq, heads, kv, hd, fmt)
+    lens = [(1, 0, 63, 64, 65, 128, 129, 200, 256, 257, 31, 17)[i % 12] for i in range(nseq)]
+    lens[7], lens[-1] = 700, 5
+    run(duo_lib, lens, heads, kv, hd, 32, fmt, pad=8)
