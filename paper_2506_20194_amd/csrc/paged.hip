@@ -69,7 +69,9 @@ struct PagedGeo {
   static constexpr int WAVE = 2 * (ROWS + 2 * NS * 256);   // LDS of a wave; scales have two buffers
   static constexpr int OLD = HD + 4;                       // row stride of the join's fp32 outputs
   static_assert(kCols * OLD * 4 <= WAVE, "the join uses a wave's tile space");
-  static constexpr int WGS = 4 * WAVE > 40960 ? 2 : FMT != DUO_KV_BF16 ? 3 : 4;  // workgroups per CU: LDS, registers
+  // Workgroups per CU: two where LDS holds no more, or (4 bits, head_dim 128) the registers: with
+  // three some of them are spilled in the loop (8 sequences of up to 131072 tokens 66 us; 52).
+  static constexpr int WGS = 4 * WAVE >= 40960 ? 2 : FMT != DUO_KV_BF16 ? 3 : 4;
 };
 
 // The rows to do, and into how many shares at most.
