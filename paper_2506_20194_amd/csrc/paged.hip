@@ -716,7 +716,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const Task* __restrict_
                                                          int kv_heads, int group, int cols, uint16_t* __restrict__ O,
                                                          int64_t ldo, int vec) {
   constexpr int T = HD / 4, NP = 128 / T;  // threads per part and head, parts at once
-  __shared__ float wt[2][kMaxWg];
+  __shared__ float wt[2][kMaxWg], ls[2][kMaxWg];
   __shared__ float red[2][2][2];
   __shared__ float acc[2][NP][HD];
   const Task task = tasks[blockIdx.x];
@@ -727,11 +727,23 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const Task* __restrict_
   const int64_t stride = (int64_t)cols * (HD + 2);
   const float* const p0 = part + 2 * (int64_t)blockIdx.x * stride + (live ? c : 0) * (HD + 2);
   auto at = [&](int i) { return p0 + (i ? 2 * i : 1) * stride; };
-  // weights
+  // the first parts' outputs are on their way while the weights are found
+  const int d = tid % T * 4, k = tid / T;
+  constexpr int EARLY = 4;
+  f4 first[EARLY];
+  auto load = [&](int i) {
+    const float2 v0 = *(const float2*)(at(i) + d), v1 = *(const float2*)(at(i) + d + 2);
+    return f4{v0.x, v0.y, v1.x, v1.y};
+  };
+#pragma unroll
+  for (int i = 0; i < EARLY; ++i) first[i] = load(min(k + i * NP, np - 1));
+  // weights: exp of each part's maximum relative to the largest, and the sum of all
   float top = -INFINITY;
   for (int i = tid; i < np; i += 128) {
-    wt[j][i] = at(i)[HD];
-    top = fmaxf(top, wt[j][i]);
+    const float2 ml = *(const float2*)(at(i) + HD);
+    wt[j][i] = ml.x;
+    ls[j][i] = ml.y;
+    top = fmaxf(top, ml.x);
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
@@ -740,8 +752,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const Task* __restrict_
   top = fmaxf(red[0][j][0], red[0][j][1]);
   float sum = 0.f;
   for (int i = tid; i < np; i += 128) {
-    const float l = at(i)[HD + 1];
-    const float f = wt[j][i] == -INFINITY ? (l == 0.f ? 0.f : l) : __builtin_amdgcn_exp2f(wt[j][i] - top);
+    const float m = wt[j][i], l = ls[j][i];
+    const float f = m == -INFINITY ? (l == 0.f ? 0.f : l) : __builtin_amdgcn_exp2f(m - top);
     wt[j][i] = f;
     sum += f * l;
   }
@@ -750,14 +762,12 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const Task* __restrict_
   if (tid % 64 == 0) red[1][j][tid >> 6] = sum;
   __syncthreads();
   sum = red[1][j][0] + red[1][j][1];
-  // outputs
-  const int d = tid % T * 4, k = tid / T;
   f4 a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < EARLY; ++i)
+    if (k + i * NP < np) a += first[i] * wt[j][k + i * NP];
 #pragma unroll 4
-  for (int i = k; i < np; i += NP) {
-    const float2 v0 = *(const float2*)(at(i) + d), v1 = *(const float2*)(at(i) + d + 2);
-    a += f4{v0.x, v0.y, v1.x, v1.y} * wt[j][i];
-  }
+  for (int i = k + EARLY * NP; i < np; i += NP) a += load(i) * wt[j][i];
   *(f4*)&acc[j][k][d] = a;
   __syncthreads();
   if (tid < HD / 2 && live) {
