@@ -23,6 +23,7 @@
 // and the queries that do see them get them added at the end.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "dma.h"
@@ -63,14 +64,20 @@ __device__ inline bool place(int id, const PackedArgs& a, int* kv, int* block) {
   return *kv < a.kv_heads && *block < a.blocks;
 }
 
-// The sequence and the block within it (the last block first) of block b; false past the last.
+// A sequence's first rows and their numbers, and which block of it (the last one first).
+struct Found {
+  int q_first, lq, k_first, lk, qb;
+};
+
+// The sequence and the block within it of block b; false past the last.
 template <int QB>
-__device__ inline bool find(const PackedArgs& a, int b, int* seq, int* qb) {
+__device__ inline bool find(const PackedArgs& a, int b, Found* f) {
   const int lane = threadIdx.x & 63;
   for (int s0 = 0; s0 < a.nseq; s0 += 64) {
-    const int s = s0 + lane;
-    int n = 0;
-    if (s < a.nseq) n = (max(cut(a.cu_q[s + 1], a.total_q) - cut(a.cu_q[s], a.total_q), 0) * a.group + QB - 1) / QB;
+    const int s = min(s0 + lane, a.nseq - 1);
+    const int q0 = cut(a.cu_q[s], a.total_q), q1 = cut(a.cu_q[s + 1], a.total_q);
+    const int k0 = cut(a.cu_k[s], a.total_k), k1 = cut(a.cu_k[s + 1], a.total_k);
+    const int n = s0 + lane < a.nseq ? (max(q1 - q0, 0) * a.group + QB - 1) / QB : 0;
     int up = n;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -80,8 +87,8 @@ __device__ inline bool find(const PackedArgs& a, int b, int* seq, int* qb) {
     const uint64_t past = __ballot(up > b);
     if (past) {
       const int l = __ffsll((unsigned long long)past) - 1;
-      *seq = s0 + l;
-      *qb = __builtin_amdgcn_readlane(up, l) - 1 - b;
+      auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+      *f = Found{of(q0), of(q1 - q0), of(k0), max(of(k1 - k0), 0), of(up) - 1 - b};
       return true;
     }
     b -= __builtin_amdgcn_readlane(up, 63);
@@ -100,12 +107,12 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
   constexpr int RPL = 64 / CH;          // keys per wave-wide load
   constexpr int QB = 32 * NW;
   __shared__ u32x4 sm[2][2][TILE];      // [buffer][K, V]
-  int kv, block, s, qb;
-  if (!place(blockIdx.x, a, &kv, &block) || !find<QB>(a, block, &s, &qb)) return;
+  int kv, block;
+  Found f;
+  if (!place(blockIdx.x, a, &kv, &block) || !find<QB>(a, block, &f)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, half = lane >> 5;
-  const int q_first = cut(a.cu_q[s], a.total_q), lq = cut(a.cu_q[s + 1], a.total_q) - q_first;
-  const int k_first = cut(a.cu_k[s], a.total_k), lk = max(cut(a.cu_k[s + 1], a.total_k) - k_first, 0);
+  const int q_first = f.q_first, lq = f.lq, k_first = f.k_first, lk = f.lk, qb = f.qb;
   const int off = lk - lq;              // query i sees keys j <= i + off
   // row r of the sequence and K/V head: query r / group, head r % group of its group
   const int rows = lq * a.group, row0 = qb * QB + 32 * wave, row = min(row0 + l32, rows - 1);
@@ -208,6 +215,21 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[d][r] *= f;
   };
+  // probabilities of a step, and their sum
+  auto probabilities = [&](const f16x& sc, u32x4 (&p)[2]) __attribute__((always_inline)) {
+    const float base = m == -INFINITY ? 0.f : mc;
+    float sum = 0.f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[8 * t + 2 * j], a.cexp, -base));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[8 * t + 2 * j + 1], a.cexp, -base));
+        sum += p0 + p1;
+        p[t][j] = pack_bf16(p0, p1);
+      }
+    return sum;
+  };
   // O += V^T P^T of step u
   uint32_t poison = 0;
   auto add = [&](int u) __attribute__((always_inline)) {
@@ -238,13 +260,11 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
   // dealt out evenly: MFMAs of the one, LDS reads and vector instructions of the others.
   auto fast = [&](auto place, f16x& sc, f16x& sn) __attribute__((always_inline)) {
     constexpr int P = decltype(place)::value;  // the step's place in two tiles, as its LDS buffers go by it
-    float f = 1.f;
-    const bool moved = refer(sc, &f);
-    const float base = m == -INFINITY ? 0.f : mc;
+    const float base = mc;
     const u32x4* sK = k_rows(P + 1);
     const uint8_t* sV = v_rows(P + 3);
     u32x4 pn[2];
-    float ls[2] = {0.f, 0.f};
+    float ls[2] = {0.f, 0.f}, most = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) sn[r] = 0.f;
     __builtin_amdgcn_sched_barrier(0);
@@ -257,6 +277,7 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
         const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[r + 1], a.cexp, -base));
         ls[0] += p0;
         ls[1] += p1;
+        most = fmaxf(most, fmaxf(p0, p1));
         pn[t][j] = pack_bf16(p0, p1);
       }
 #pragma unroll
@@ -266,10 +287,8 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
         if (i < DB) o[i] = mma32_bf16(read_v(sV, t, i), pf[t], o[i]);
       }
     }
-    l += ls[0] + ls[1];
-    pf[0] = pn[0];
-    pf[1] = pn[1];
-    asm volatile("" : "+v"(pf[0]), "+v"(pf[1]), "+v"(l));  // computed here, not where they are used
+    float sum = ls[0] + ls[1];
+    asm volatile("" : "+v"(pn[0]), "+v"(pn[1]), "+v"(sum), "+v"(most));  // computed here, not where they are used
     __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
 #pragma unroll
     for (int i = 0; i < DB + KS / 2; ++i) {
@@ -278,10 +297,18 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
       __builtin_amdgcn_sched_group_barrier(0x002, HD == 128 ? 4 : 8, 0);
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-      __builtin_amdgcn_sched_group_barrier(0x002, HD == 128 ? 3 : 6, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, HD == 128 ? 4 : 8, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (moved) scale_o(f);
+    // scores that leave the reference's range (or have none yet): once more, with another
+    if (__any(most > 256.f || m == -INFINITY)) {
+      float f = 1.f;
+      if (refer(sc, &f)) scale_o(f);
+      sum = probabilities(sc, pn);
+    }
+    l += sum;
+    pf[0] = pn[0];
+    pf[1] = pn[1];
   };
   auto slow = [&](int u, f16x& sc, f16x& sn) __attribute__((always_inline)) {
     if (u > 0 && u <= nu) add(u - 1);
@@ -292,17 +319,7 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
         for (int r = 0; r < 16; ++r) sc[r] = key_of(r) > see ? -INFINITY : sc[r];
       float f;
       if (refer(sc, &f)) scale_o(f);
-      const float base = m == -INFINITY ? 0.f : mc;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(sc[r], a.cexp, -base));
-        sc[r] = u >= nfull && key_of(r) > see ? 0.f : p;  // also where a scale of 0 makes -inf NaN
-        l += sc[r];
-      }
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) pf[t][j] = pack_bf16(sc[8 * t + 2 * j], sc[8 * t + 2 * j + 1]);
+      l += probabilities(sc, pf);
       if (u + 1 < nu) score(u + 1, sn);
     }
   };
@@ -327,6 +344,7 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
     slow(2 * kb, sa, sb);
     turn(kb);
     slow(2 * kb + 1, sb, sa);
+    // two tiles at a time, the odd one first, so that places in LDS are known when compiled
     for (++kb; (kb & 1) && 2 * kb + 4 < nu && 2 * kb + 3 < nfull; kb += 2) {
       fast(std::integral_constant<int, 2>{}, sa, sb);
       turn(kb);
@@ -426,7 +444,8 @@ duo_status duo_attention_packed(const void* Q, int64_t ldq, const void* K, int64
   a.cu_q = cu_q, a.cu_k = cu_k ? cu_k : cu_q;
   a.total_q = (int)total_q, a.total_k = (int)total_k, a.nseq = (int)nseq;
   a.kv_heads = (int)kv_heads, a.group = (int)group, a.blocks = (int)blocks;
-  a.cexp = (float)(std::fabs(scale) * 1.4426950408889634);
+  // never 0: the scores of keys that are not seen, -inf, have to stay that
+  a.cexp = std::max((float)(std::fabs(scale) * 1.4426950408889634), 1.4e-45f);
   a.flip = scale < 0.0 ? 0x80008000u : 0u;
   a.vec = ldo % 4 == 0 && (reinterpret_cast<uintptr_t>(O) & 7) == 0;
   auto go = [&](auto kern, int nw) {
