@@ -47,7 +47,7 @@ struct PackedArgs {
   int blocks;  // bound of the blocks of rows of one K/V head
   float cexp;  // exp(s scale) = 2^(s cexp), with the queries' signs turned for a negative scale
   uint32_t flip;
-  int vec;  // 8-byte stores of O
+  int vec;  // 16-byte stores of O
 };
 
 __device__ inline int cut(int v, int total) { return min(max(v, 0), total); }
@@ -231,29 +231,53 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
     return sum;
   };
   // O += V^T P^T of step u
-  uint32_t poison = 0;
+  typedef short s16v2 __attribute__((ext_vector_type(2)));
+  typedef unsigned short u16v2 __attribute__((ext_vector_type(2)));
+  bool poison = false;
   auto add = [&](int u) __attribute__((always_inline)) {
     const uint8_t* sV = v_rows(u);
-    if (u < nfull) {
+    u32x4 v[2][DB];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int d = 0; d < DB; ++d) v[t][d] = read_v(sV, t, d);
+    if (u >= nfull) {
+      // some query does not see some key: are there numbers that are not finite?  As 16-bit
+      // integers those are the largest, signed for one sign and unsigned for the other.
+      s16v2 most_s = {0, 0};
+      u16v2 most_u = {0, 0};
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int d = 0; d < DB; ++d) o[d] = mma32_bf16(read_v(sV, t, d), pf[t], o[d]);
-    } else {  // some query does not see some key: numbers that are not finite enter as zeros
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          u32x4 v = read_v(sV, t, d);
+        for (int d = 0; d < DB; ++d)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const uint32_t bad = ((v[j] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;  // exponent all ones
-            poison |= bad;
-            v[j] &= ~((bad >> 15) * 0xffffu);
+            s16v2 x;
+            u16v2 y;
+            const uint32_t w = v[t][d][j];
+            __builtin_memcpy(&x, &w, 4);
+            __builtin_memcpy(&y, &w, 4);
+            most_s = __builtin_elementwise_max(most_s, x);
+            most_u = __builtin_elementwise_max(most_u, y);
           }
-          o[d] = mma32_bf16(v, pf[t], o[d]);
-        }
+      if (__any(most_s[0] >= 0x7f80 || most_s[1] >= 0x7f80 || most_u[0] >= 0xff80 || most_u[1] >= 0xff80)) {
+        poison = true;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t w = v[t][d][j];
+              const uint32_t lo = (w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+              v[t][d][j] = w & ~(lo | hi);
+            }
+      }
     }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int d = 0; d < DB; ++d) o[d] = mma32_bf16(v[t][d], pf[t], o[d]);
   };
   // Step u's probabilities, the values of the step before and the scores of the next are
   // independent of each other.  Where all three are there and nothing is masked they are
@@ -318,7 +342,7 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[r] = key_of(r) > see ? -INFINITY : sc[r];
       float f;
-      if (refer(sc, &f)) scale_o(f);
+      if (refer(sc, &f) && u > 0) scale_o(f);
       l += probabilities(sc, pf);
       if (u + 1 < nu) score(u + 1, sn);
     }
@@ -359,7 +383,7 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
   // MFMA had written it; nothing may touch them until it has.
 #pragma unroll
   for (int d = 0; d < DB; ++d) asm volatile("s_nop 15" : "+v"(o[d]));
-  if (__any(poison != 0)) {
+  if (poison) {
     // what every query sees of the numbers left out (infinities and NaN add up as they do)
 #pragma unroll 1
     for (int j = nfull * 32; j < min(nu * 32, lk); ++j) {
@@ -373,12 +397,10 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
         }
     }
   }
-  if (row0 + l32 >= rows) return;
   const auto rl = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
   // queries that see no key: 0; a sum of 0 (every score -inf) gives NaN
   const float inv = 1.0f / (__uint_as_float(rl[0]) + __uint_as_float(rl[1]));
   const bool none = q + off < 0;
-  uint16_t* y0 = a.O + (int64_t)(q_first + q) * a.ldo + head * HD + 4 * half;
   uint2 y[DB][4];
 #pragma unroll
   for (int d = 0; d < DB; ++d)
@@ -388,11 +410,25 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
       y[d][g].y = none ? 0u : pack_bf16(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv);
     }
   if (a.vec) {
+    // through this wave's part of LDS, so that a row is written at once, 16 bytes per lane;
+    // chunk c of row r at c ^ (r % CH)
+    lds_barrier();  // every wave is done with the tiles
+    uint8_t* const st = (uint8_t*)sm + wave * (32 * HD * 2);
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) *(uint2*)(y0 + 32 * d + 8 * g) = y[d][g];
-  } else {
+      for (int g = 0; g < 4; ++g)
+        *(uint2*)(st + l32 * HD * 2 + ((4 * d + g) ^ (l32 & (CH - 1))) * 16 + 8 * half) = y[d][g];
+    wait_lds<0>();
+#pragma unroll
+    for (int i = 0; i < 32 / RPL; ++i) {
+      const int r = i * RPL + lane / CH, c = lane % CH;
+      if (row0 + r >= rows) break;
+      const int qr = (row0 + r) / a.group, h = kv * a.group + (row0 + r) - qr * a.group;
+      *(u32x4*)(a.O + (int64_t)(q_first + qr) * a.ldo + h * HD + 8 * c) = *(const u32x4*)(st + r * HD * 2 + (c ^ (r & (CH - 1))) * 16);
+    }
+  } else if (row0 + l32 < rows) {
+    uint16_t* y0 = a.O + (int64_t)(q_first + q) * a.ldo + head * HD + 4 * half;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -447,7 +483,7 @@ duo_status duo_attention_packed(const void* Q, int64_t ldq, const void* K, int64
   // never 0: the scores of keys that are not seen, -inf, have to stay that
   a.cexp = std::max((float)(std::fabs(scale) * 1.4426950408889634), 1.4e-45f);
   a.flip = scale < 0.0 ? 0x80008000u : 0u;
-  a.vec = ldo % 4 == 0 && (reinterpret_cast<uintptr_t>(O) & 7) == 0;
+  a.vec = ldo % 8 == 0 && aligned16(O);
   auto go = [&](auto kern, int nw) {
     hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(64 * nw), 0, (hipStream_t)stream, a);
   };
