@@ -572,12 +572,17 @@ duo_status duo_kv_read(const duo_kv_cache* cache, const int64_t* slots, int64_t 
  *   Offsets are taken as within [0, total] (larger ones as total, a sequence whose
  *   end lies before its start as empty); rows of O in no sequence are left alone.
  *   scale finite.  heads % kv_heads == 0, head_dim 64 or 128; Q, K, V 16-byte
- *   aligned with ldq, ldk, ldv % 8 == 0 (else DUO_ERR_UNSUPPORTED).  No scratch
- *   memory. */
+ *   aligned with ldq, ldk, ldv % 8 == 0 and ldk, ldv < 2^24 (else
+ *   DUO_ERR_UNSUPPORTED).  Few queries on long sequences are split over the keys and
+ *   joined (by the sizes alone: results are deterministic).  Workspace:
+ *   duo_attention_packed_workspace_size with the same sizes; 0 where nothing is
+ *   split (ws may then be NULL). */
+size_t duo_attention_packed_workspace_size(int64_t total_q, int64_t total_k, int64_t nseq, int64_t heads,
+                                           int64_t kv_heads, int64_t head_dim);
 duo_status duo_attention_packed(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
                                 const int32_t* cu_q, int64_t total_q, const int32_t* cu_k, int64_t total_k,
                                 int64_t nseq, int64_t heads, int64_t kv_heads, int64_t head_dim, double scale, void* O,
-                                int64_t ldo, void* stream);
+                                int64_t ldo, void* ws, size_t ws_bytes, void* stream);
 
 /* duo_attention_paged - attention of one query per sequence over its cached tokens:
  *   row s of Q (nseq x heads*head_dim, ldq) against the first lens[s] tokens of

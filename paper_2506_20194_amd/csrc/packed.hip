@@ -18,6 +18,9 @@
 // sum with it) only when a score exceeds it by more than 8 in the exponent of two:
 // they then stay below 2^8, which costs no accuracy in fp32 or bf16.
 //
+// Few rows on long sequences: the keys of a block are split over workgroups, and a second
+// launch joins the parts.
+//
 // Unseen keys get probability 0, and 0 times a value that is not finite would not be
 // 0: in the steps where some query does not see some key such values enter as zeros,
 // and the queries that do see them get them added at the end.
@@ -25,6 +28,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "dma.h"
 #include "internal.h"
@@ -48,6 +52,10 @@ struct PackedArgs {
   float cexp;  // exp(s scale) = 2^(s cexp), with the queries' signs turned for a negative scale
   uint32_t flip;
   int vec;  // 16-byte stores of O
+  // SPLIT: parts of a block's keys, and each part's outputs (rows x head_dim, not normalised)
+  // and references and sums (rows x 2)
+  int parts;
+  float *po, *pml;
 };
 
 __device__ inline int cut(int v, int total) { return min(max(v, 0), total); }
@@ -96,7 +104,7 @@ __device__ inline bool find(const PackedArgs& a, int b, Found* f) {
   return false;
 }
 
-template <int HD, int NW>
+template <int HD, int NW, bool SPLIT>
 __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
   constexpr int KB = 64;                // keys per tile
   constexpr int CH = HD / 8;            // 16-byte chunks per key row
@@ -109,6 +117,7 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
   __shared__ u32x4 sm[2][2][TILE];      // [buffer][K, V]
   int kv, block;
   Found f;
+  const int part = SPLIT ? blockIdx.y : 0;
   if (!place(blockIdx.x, a, &kv, &block) || !find<QB>(a, block, &f)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, half = lane >> 5;
@@ -137,7 +146,10 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
     }
   }
   const int seen = min(qb * QB + QB - 1, rows - 1) / a.group + 1 + off;  // keys that the block's last query sees
-  const int nkb = (seen + KB - 1) / KB;     // <= 0: none
+  const int tiles = (seen + KB - 1) / KB;   // <= 0: none
+  // this workgroup's: all of them, or a part that begins with an even one
+  const int each = SPLIT ? max((tiles + a.parts - 1) / a.parts + 1 & ~1, 2) : 0;
+  const int kb0 = part * each, nkb = SPLIT ? min(tiles, kb0 + each) : tiles;
   // this wave's part of tile kb of K (or V), keys past the last as the last
   auto issue = [&](const uint16_t* src, int64_t ld, int kb, const u32x4* dst, bool is_v) __attribute__((always_inline)) {
     const uint32_t to = __builtin_amdgcn_readfirstlane(lds_addr(dst + wave * NL * 64));
@@ -175,7 +187,8 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
   };
   // Steps of 32 keys, two per tile.  This wave: steps of which its queries see a key, and of
   // which they see every key.
-  const int nu = row0 < rows && q_hi + off >= 0 ? min((q_hi + off) / 32 + 1, 2 * nkb) : 0;
+  const int nu = row0 < rows && q_hi + off >= 0 ? min((q_hi + off) / 32 + 1, 2 * nkb) : 0;  // up to step nu
+  const int u0 = 2 * kb0;
   const int nfull = max((q_lo + off + 1) / 32, 0);
   auto key_of = [&](int r) { return 8 * (r >> 2) + 4 * half + (r & 3); };
 
@@ -244,8 +257,8 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
     if (u >= nfull) {
       // some query does not see some key: are there numbers that are not finite?  As 16-bit
       // integers those are the largest, signed for one sign and unsigned for the other.
-      s16v2 most_s = {0, 0};
-      u16v2 most_u = {0, 0};
+      s16v2 ms[4] = {};
+      u16v2 mu[4] = {};
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -257,9 +270,11 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
             const uint32_t w = v[t][d][j];
             __builtin_memcpy(&x, &w, 4);
             __builtin_memcpy(&y, &w, 4);
-            most_s = __builtin_elementwise_max(most_s, x);
-            most_u = __builtin_elementwise_max(most_u, y);
+            ms[j] = __builtin_elementwise_max(ms[j], x);
+            mu[j] = __builtin_elementwise_max(mu[j], y);
           }
+      const s16v2 most_s = __builtin_elementwise_max(__builtin_elementwise_max(ms[0], ms[1]), __builtin_elementwise_max(ms[2], ms[3]));
+      const u16v2 most_u = __builtin_elementwise_max(__builtin_elementwise_max(mu[0], mu[1]), __builtin_elementwise_max(mu[2], mu[3]));
       if (__any(most_s[0] >= 0x7f80 || most_s[1] >= 0x7f80 || most_u[0] >= 0xff80 || most_u[1] >= 0xff80)) {
         poison = true;
 #pragma unroll
@@ -335,26 +350,26 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
     pf[1] = pn[1];
   };
   auto slow = [&](int u, f16x& sc, f16x& sn) __attribute__((always_inline)) {
-    if (u > 0 && u <= nu) add(u - 1);
+    if (u > u0 && u <= nu) add(u - 1);
     if (u < nu) {
       const int see = q + off - u * 32;
       if (u >= nfull)
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[r] = key_of(r) > see ? -INFINITY : sc[r];
       float f;
-      if (refer(sc, &f) && u > 0) scale_o(f);
+      if (refer(sc, &f) && u > u0) scale_o(f);
       l += probabilities(sc, pf);
       if (u + 1 < nu) score(u + 1, sn);
     }
   };
 
-  if (nkb > 0) {
-    issue(Kh, a.ldk, 0, sm[0][0], false);
-    issue(Kh, a.ldk, min(1, nkb - 1), sm[1][0], false);
-    issue(Vh, a.ldv, 0, sm[0][1], true);
+  if (nkb > kb0) {
+    issue(Kh, a.ldk, kb0, sm[0][0], false);
+    issue(Kh, a.ldk, min(kb0 + 1, nkb - 1), sm[1][0], false);
+    issue(Vh, a.ldv, kb0, sm[0][1], true);
     wait_vm<2 * NL>();
     lds_barrier();
-    if (nu > 0) score(0, sa);
+    if (nu > u0) score(u0, sa);
   }
   // K of the next tile and V of this one have landed, and every wave is done with K of
   // this one and V of the one before, whose places the next ones take
@@ -364,7 +379,7 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
     if (kb + 2 < nkb) issue(Kh, a.ldk, kb + 2, sm[kb & 1][0], false);
     if (kb + 1 < nkb) issue(Vh, a.ldv, kb + 1, sm[(kb + 1) & 1][1], true);
   };
-  for (int kb = 0; kb < nkb;) {
+  for (int kb = kb0; kb < nkb;) {
     slow(2 * kb, sa, sb);
     turn(kb);
     slow(2 * kb + 1, sb, sa);
@@ -378,7 +393,7 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
       fast(std::integral_constant<int, 1>{}, sb, sa);
     }
   }
-  if (nu > 0 && nu == 2 * nkb) add(nu - 1);
+  if (nu > u0 && nu == 2 * nkb) add(nu - 1);
   // The compiler (ROCm 7.2) copied an accumulator at a loop's exit before its last
   // MFMA had written it; nothing may touch them until it has.
 #pragma unroll
@@ -386,7 +401,7 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
   if (poison) {
     // what every query sees of the numbers left out (infinities and NaN add up as they do)
 #pragma unroll 1
-    for (int j = nfull * 32; j < min(nu * 32, lk); ++j) {
+    for (int j = max(nfull, u0) * 32; j < min(nu * 32, lk); ++j) {
       const uint16_t* v = Vh + (int64_t)j * a.ldv + 4 * half;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
@@ -398,6 +413,18 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
     }
   }
   const auto rl = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+  if constexpr (SPLIT) {
+    const int64_t at = (((int64_t)kv * a.blocks + block) * a.parts + part) * QB + 32 * wave + l32;
+    if (half == 0) *(float2*)(a.pml + 2 * at) = make_float2(mc, __uint_as_float(rl[0]) + __uint_as_float(rl[1]));
+    float* y = a.po + at * HD + 4 * half;
+    if (nu > u0)
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *(f4*)(y + 32 * d + 8 * g) = f4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
+    return;
+  }
   // queries that see no key: 0; a sum of 0 (every score -inf) gives NaN
   const float inv = 1.0f / (__uint_as_float(rl[0]) + __uint_as_float(rl[1]));
   const bool none = q + off < 0;
@@ -442,14 +469,77 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
   }
 }
 
+// Joins the parts of a block's rows: HD / 4 threads per row, blockIdx.y counts the rows of a
+// block by the 1024 / HD that a workgroup takes.
+template <int HD, int QB>
+__global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
+  constexpr int T = HD / 4;
+  int kv, block;
+  Found f;
+  if (!place(blockIdx.x, a, &kv, &block) || !find<QB>(a, block, &f)) return;
+  const int local = blockIdx.y * (256 / T) + threadIdx.x / T, row = f.qb * QB + local, d = threadIdx.x % T * 4;
+  if (row >= f.lq * a.group) return;
+  const int q = row / a.group, head = kv * a.group + row - q * a.group;
+  const int64_t at = ((int64_t)kv * a.blocks + block) * a.parts * QB + local;
+  float top = -INFINITY;
+#pragma unroll 4
+  for (int i = 0; i < a.parts; ++i) top = fmaxf(top, a.pml[2 * (at + (int64_t)i * QB)]);
+  float sum = 0.f;
+  f4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = 0; i < a.parts; ++i) {
+    const float2 ml = *(const float2*)(a.pml + 2 * (at + (int64_t)i * QB));
+    if (ml.x == -INFINITY && ml.y == 0.f) continue;  // nothing seen, and nothing written
+    const float w = ml.x == -INFINITY ? ml.y : __builtin_amdgcn_exp2f(ml.x - top);
+    sum += w * ml.y;
+    y += *(const f4*)(a.po + (at + (int64_t)i * QB) * HD + d) * w;
+  }
+  const bool none = q + f.lk - f.lq < 0;
+  const uint2 two = none ? make_uint2(0, 0) : make_uint2(pack_bf16(y[0] / sum, y[1] / sum), pack_bf16(y[2] / sum, y[3] / sum));
+  uint16_t* const o = a.O + (int64_t)(f.q_first + q) * a.ldo + head * HD + d;
+  if (a.vec) {
+    *(uint2*)o = two;
+  } else {
+    o[0] = (uint16_t)two.x, o[1] = (uint16_t)(two.x >> 16);
+    o[2] = (uint16_t)two.y, o[3] = (uint16_t)(two.y >> 16);
+  }
+}
+
+// How a call is cut: rows per workgroup, a bound of the blocks of a K/V head, parts of their keys.
+struct Plan {
+  int rows;
+  int64_t blocks, parts;
+};
+Plan packed_plan(int64_t total_q, int64_t total_k, int64_t nseq, int64_t group, int64_t kv_heads) {
+  // 128 rows per workgroup; 64 when that would leave CUs without their two workgroups (512
+  // in all)
+  auto bound = [&](int64_t rows) { return total_q * group / rows + std::min(nseq, total_q); };
+  if ((total_q * group / 128 + nseq / 2) * kv_heads >= 512) return {128, bound(128), 1};
+  // Few rows on long sequences leave most CUs idle, so their keys are split too: as many
+  // parts as fill the CUs, of 256 keys at least (on average over the sequences).
+  const int64_t blocks = bound(64), wgs = blocks * kv_heads;
+  const int64_t parts = std::min(512 / wgs, total_k / nseq / 256);
+  return {64, blocks, wgs <= 256 && parts >= 2 ? std::min<int64_t>(parts, 64) : 1};
+}
+
 }  // namespace
 
 extern "C" {
 
+size_t duo_attention_packed_workspace_size(int64_t total_q, int64_t total_k, int64_t nseq, int64_t heads,
+                                           int64_t kv_heads, int64_t head_dim) {
+  if (total_q < 1 || total_k < 1 || nseq < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads ||
+      (head_dim != 64 && head_dim != 128) || heads > 65535 || total_q * (heads / kv_heads) > INT32_MAX / 2)
+    return 0;
+  const Plan p = packed_plan(total_q, total_k, nseq, heads / kv_heads, kv_heads);
+  if (p.parts == 1) return 0;
+  return align_up((size_t)(p.blocks * kv_heads * p.parts * p.rows * (head_dim + 2)) * sizeof(float));
+}
+
 duo_status duo_attention_packed(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
                                 const int32_t* cu_q, int64_t total_q, const int32_t* cu_k, int64_t total_k,
                                 int64_t nseq, int64_t heads, int64_t kv_heads, int64_t head_dim, double scale, void* O,
-                                int64_t ldo, void* stream) {
+                                int64_t ldo, void* ws, size_t ws_bytes, void* stream) {
   if (nseq < 0 || total_q < 0 || total_k < 0 || heads < 1 || kv_heads < 1 || head_dim < 1 || heads > 65535 ||
       kv_heads > heads || heads % kv_heads || !std::isfinite(scale))
     return DUO_ERR_INVALID_ARG;
@@ -462,13 +552,12 @@ duo_status duo_attention_packed(const void* Q, int64_t ldq, const void* K, int64
   if (nseq == 0 || total_q == 0) return DUO_OK;
   if (!Q || !O || !cu_q || (total_k > 0 && (!K || !V))) return DUO_ERR_INVALID_ARG;
   if (ldq % 8 || ldk % 8 || ldv % 8 || !aligned16(Q) || !aligned16(K) || !aligned16(V)) return DUO_ERR_UNSUPPORTED;
-  // 128 rows per workgroup; 64 when that would leave CUs without their two
-  // workgroups (512 in all)
   const int64_t group = heads / kv_heads;
   if (total_q * group > INT32_MAX / 2) return DUO_ERR_UNSUPPORTED;
-  auto bound = [&](int64_t rows) { return total_q * group / rows + std::min(nseq, total_q); };
-  const bool wide = (total_q * group / 128 + nseq / 2) * kv_heads >= 512;
-  const int64_t blocks = bound(wide ? 128 : 64);
+  const size_t need = duo_attention_packed_workspace_size(total_q, total_k, nseq, heads, kv_heads, head_dim);
+  if (need && (!ws || ws_bytes < need || reinterpret_cast<uintptr_t>(ws) % kAlign)) return DUO_ERR_WORKSPACE;
+  const Plan plan = packed_plan(total_q, total_k, nseq, group, kv_heads);
+  const int64_t blocks = plan.blocks;
   int64_t e = 1;
   while (e < 8 && kv_heads % (2 * e) == 0) e *= 2;
   const int64_t wgs = 8 * (kv_heads / e) * cdiv(blocks, 8 / e);
@@ -484,15 +573,27 @@ duo_status duo_attention_packed(const void* Q, int64_t ldq, const void* K, int64
   a.cexp = std::max((float)(std::fabs(scale) * 1.4426950408889634), 1.4e-45f);
   a.flip = scale < 0.0 ? 0x80008000u : 0u;
   a.vec = ldo % 8 == 0 && aligned16(O);
-  auto go = [&](auto kern, int nw) {
-    hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(64 * nw), 0, (hipStream_t)stream, a);
+  a.parts = (int)plan.parts;
+  const int64_t rows = blocks * kv_heads * plan.parts * plan.rows;
+  a.po = (float*)ws;
+  a.pml = a.po + (need ? rows * head_dim : 0);
+  const hipStream_t st = (hipStream_t)stream;
+  auto go = [&](auto hd) -> duo_status {
+    constexpr int HD = decltype(hd)::value;
+    const dim3 grid((unsigned)wgs, (unsigned)plan.parts);
+    if (plan.parts > 1) {
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(packed_kernel<HD, 2, true>), grid, dim3(128), 0, st, a);
+      DUO_LAUNCH_CHECK();
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(packed_join_kernel<HD, 64>), dim3((unsigned)wgs, HD / 16), dim3(256), 0, st, a);
+    } else if (plan.rows == 128) {
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(packed_kernel<HD, 4, false>), grid, dim3(256), 0, st, a);
+    } else {
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(packed_kernel<HD, 2, false>), grid, dim3(128), 0, st, a);
+    }
+    DUO_LAUNCH_CHECK();
+    return DUO_OK;
   };
-  if (head_dim == 128)
-    wide ? go(packed_kernel<128, 4>, 4) : go(packed_kernel<128, 2>, 2);
-  else
-    wide ? go(packed_kernel<64, 4>, 4) : go(packed_kernel<64, 2>, 2);
-  DUO_LAUNCH_CHECK();
-  return DUO_OK;
+  return head_dim == 128 ? go(std::integral_constant<int, 128>{}) : go(std::integral_constant<int, 64>{});
 }
 
 }  // extern "C"

@@ -31,7 +31,7 @@ EXPORTED = (
     "duo_act_sparsify", "duo_linear", "duo_rope", "duo_attention", "duo_silu_mul", "duo_act_order",
     "duo_permute", "duo_permute_mask", "duo_dsc_workspace_size", "duo_dsc_layout", "duo_dsc_pack",
     "duo_dsc_gemv", "duo_dsc_gemv_noalloc", "duo_hessian_status", "duo_rope_at", "duo_kv_page_bytes", "duo_kv_write",
-    "duo_kv_read", "duo_attention_packed", "duo_attention_paged_workspace_size", "duo_attention_paged",
+    "duo_kv_read", "duo_attention_packed", "duo_attention_packed_workspace_size", "duo_attention_paged_workspace_size", "duo_attention_paged",
 )
 PROF = dict(gram=0, hessian=1, chol=2, score=3, sweep=4, inblock=5, trail=6, select=7, decode=8)
 DUO_BOP_ACT_SPARSIFY, DUO_BOP_LINEAR, DUO_BOP_ATTENTION = 0, 1, 2
@@ -146,7 +146,10 @@ def lib():
         L.duo_kv_read.restype = I32
         L.duo_kv_read.argtypes = [KV, P, I64, P, I64, P, I64, P]
         L.duo_attention_packed.restype = I32
-        L.duo_attention_packed.argtypes = [P, I64, P, I64, P, I64, P, I64, P, I64, I64, I64, I64, I64, F64, P, I64, P]
+        L.duo_attention_packed.argtypes = [P, I64, P, I64, P, I64, P, I64, P, I64, I64, I64, I64, I64, F64, P, I64, P,
+                                           SZ, P]
+        L.duo_attention_packed_workspace_size.restype = SZ
+        L.duo_attention_packed_workspace_size.argtypes = [I64, I64, I64, I64, I64, I64]
         L.duo_attention_paged_workspace_size.restype = SZ
         L.duo_attention_paged_workspace_size.argtypes = [I64, I64, I64, I64, I64]
         L.duo_attention_paged.restype = I32
@@ -851,7 +854,13 @@ def duo_kv_read(cache, slots, out=None):
     return K, V
 
 
-def duo_attention_packed(Q, K, V, cu_q, heads, kv_heads, head_dim, cu_k=None, scale=None, out=None):
+def attention_packed_workspace(total_q, total_k, nseq, heads, kv_heads, head_dim, device):
+    """A workspace tensor, or None where none is needed."""
+    n = lib().duo_attention_packed_workspace_size(total_q, total_k, nseq, heads, kv_heads, head_dim)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def duo_attention_packed(Q, K, V, cu_q, heads, kv_heads, head_dim, cu_k=None, scale=None, out=None, ws=None):
     """Causal attention of packed sequences: Q total_q x heads*head_dim, K and V
     total_k x kv_heads*head_dim, cu_q and cu_k (None: cu_q) the sequences' first
     rows, nseq + 1 int32 each.  scale: None for head_dim^-1/2.  Rows of the result
@@ -859,12 +868,14 @@ def duo_attention_packed(Q, K, V, cu_q, heads, kv_heads, head_dim, cu_k=None, sc
     n, tq, tk, w, wk = cu_q.shape[0] - 1, Q.shape[0], K.shape[0], heads * head_dim, kv_heads * head_dim
     O = _empty(tq, w, Q) if out is None else out
     dev = Q.get_device()
-    _on(dev, "duo_attention_packed", K, V, cu_q, cu_k, O)
+    if ws is None:
+        ws = attention_packed_workspace(tq, tk, n, heads, kv_heads, head_dim, Q.device)
+    _on(dev, "duo_attention_packed", K, V, cu_q, cu_k, O, ws)
     st = lib().duo_attention_packed(
         Q.data_ptr(), _rows(Q, tq, w, "Q"), K.data_ptr(), _rows(K, tk, wk, "K"), V.data_ptr(), _rows(V, tk, wk, "V"),
         _ints(cu_q, torch.int32, n + 1, "cu_q"), tq, None if cu_k is None else _ints(cu_k, torch.int32, n + 1, "cu_k"), tk,
         n, heads, kv_heads, head_dim, head_dim ** -0.5 if scale is None else scale, O.data_ptr(), _rows(O, tq, w, "out"),
-        _raw_stream(dev))
+        None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _raw_stream(dev))
     if st:
         raise DuoError(st, "duo_attention_packed")
     return O

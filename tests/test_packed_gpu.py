@@ -90,6 +90,40 @@ def test_rows_without_keys(duo_lib, lq, lk, hd):
 
 
 @pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("heads,kv,lq,lk", [(4, 2, [1], [5000]), (8, 8, [3, 40], [4097, 600]), (16, 2, [9, 1, 0, 70], [900, 8200, 3, 130]),
+                                            (1, 1, [64], [2048]), (2, 1, [130], [1100]), (4, 4, [5, 300], [2, 3000])])
+def test_split_over_keys(duo_lib, heads, kv, lq, lk, hd):
+    say("split over keys", heads, kv, lq, lk, hd)
+    assert duo_lib.attention_packed_workspace(sum(lq), sum(lk), len(lq), heads, kv, hd, DEV) is not None
+    run(duo_lib, lq, lk, heads, kv, hd)
+    run(duo_lib, lq, lk, heads, kv, hd, scale=-0.2, pad=8)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_split_unseen_and_infinite(duo_lib, hd):
+    """Parts that see nothing, and numbers that are not finite: unseen ones have no
+    influence, a seen one has, whichever part holds it."""
+    say("split, numbers that are not finite", hd)
+    heads, kv, lq, lk = 4, 2, 6, 3000
+    Q, K, V = bf((lq, heads * hd), 1), bf((lk, kv * hd), 2), bf((lk, kv * hd), 3)
+    clean = [f64(t) for t in (Q, K, V)]
+    V[lk - 1], K[lk - 2] = float("nan"), float("inf")   # seen by the last query, and by the last two
+    V[700, 5] = float("inf")                            # seen by all: channel 5 of the first group
+    V[800, hd] = float("nan")
+    dev = [t.to(DEV) for t in (Q, K, V)]
+    ws = duo_lib.attention_packed_workspace(lq, lk, 1, heads, kv, hd, DEV)
+    ws.fill_(255)
+    O = f64(duo_lib.duo_attention_packed(*dev, cu([lq]).to(DEV), heads, kv, hd, cu_k=cu([lk]).to(DEV), ws=ws)).reshape(lq, heads, hd)
+    ref, tol = S.attend(clean[0].reshape(lq, heads, hd), clean[1].reshape(lk, kv, hd), clean[2].reshape(lk, kv, hd), hd ** -0.5,
+                        S.causal(lq, lk))
+    assert not np.isfinite(O[4:]).any()
+    assert (O[:4, :2, 5] == np.inf).all() and np.isnan(O[:4, 2:, 0]).all()
+    ok = np.ones((4, heads, hd), dtype=bool)
+    ok[:, :2, 5] = ok[:, 2:, 0] = False
+    assert (np.abs(O[:4] - ref[:4]) <= tol[:4])[ok].all()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
 def test_strides_and_scale(duo_lib, hd):
     say("strides, scale", hd)
     run(duo_lib, [100, 33], None, 4, 2, hd, scale=0.3, pad=8)

@@ -82,8 +82,8 @@ def test_attention_packed(codes):
     L, OK, E, UNS, NODEV = codes
 
     def call(Q=FAKE, ldq=256, K=FAKE, ldk=128, V=FAKE, ldv=128, cq=FAKE, tq=10, ck=FAKE, tk=20, n=2, h=4, kv=2, hd=64, sc=0.1,
-             O=FAKE, ldo=256):
-        return L.duo_attention_packed(Q, ldq, K, ldk, V, ldv, cq, tq, ck, tk, n, h, kv, hd, sc, O, ldo, None)
+             O=FAKE, ldo=256, ws=None, wsb=0):
+        return L.duo_attention_packed(Q, ldq, K, ldk, V, ldv, cq, tq, ck, tk, n, h, kv, hd, sc, O, ldo, ws, wsb, None)
 
     assert call() == NODEV
     assert call(ck=None, tk=10) == NODEV
@@ -95,9 +95,24 @@ def test_attention_packed(codes):
                 dict(sc=float("inf")), dict(ldq=255), dict(ldk=127), dict(ldv=127), dict(ldo=255)):
         assert call(**bad) == E, bad
     for odd in (dict(hd=32), dict(ldq=260), dict(ldk=132), dict(ldv=130), dict(Q=ctypes.c_void_p(FAKE.value + 2)),
-                dict(K=ctypes.c_void_p(FAKE.value + 8)), dict(V=ctypes.c_void_p(FAKE.value + 4)), dict(tq=1 << 31),
+                dict(K=ctypes.c_void_p(FAKE.value + 8)), dict(V=ctypes.c_void_p(FAKE.value + 4)), dict(ldk=1 << 24), dict(tq=1 << 31),
                 dict(tk=1 << 31)):
         assert call(**odd) == UNS, odd
+
+
+def test_attention_packed_workspace(codes, duo_lib):
+    """Nothing but few queries on long sequences is split and needs scratch memory."""
+    L, OK, E, UNS, NODEV = codes
+    size = L.duo_attention_packed_workspace_size
+    assert size(10, 20, 2, 4, 2, 64) == size(100000, 100000, 10, 32, 32, 128) == size(10, 100000, 0, 4, 2, 64) == 0
+    assert size(1, 100000, 1, 4, 3, 64) == size(1, 100000, 1, 4, 2, 32) == size(0, 100000, 1, 4, 2, 64) == 0
+    need = size(1, 100000, 1, 4, 2, 64)
+    assert 0 < need < 1 << 26
+    call = lambda ws, wsb: L.duo_attention_packed(FAKE, 256, FAKE, 128, FAKE, 128, FAKE, 1, FAKE, 100000, 1, 4, 2, 64, 0.1, FAKE,
+                                                  256, ws, wsb, None)
+    assert call(WS, need) == NODEV
+    for ws, wsb in ((None, 0), (WS, need - 1), (ctypes.c_void_p(WS.value + 64), BIG)):
+        assert call(ws, wsb) == duo_lib.DUO_ERR_WORKSPACE
 
 
 def test_attention_paged(codes, duo_lib):
