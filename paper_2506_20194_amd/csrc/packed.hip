@@ -48,6 +48,8 @@ struct PackedArgs {
   int64_t ldq, ldk, ldv, ldo;
   const int32_t *cu_q, *cu_k;
   int total_q, total_k, nseq, kv_heads, group;
+  uint32_t by_group;  // for by(): a row's query
+  int by_shift;
   int blocks;  // bound of the blocks of rows of one K/V head
   float cexp;  // exp(s scale) = 2^(s cexp), with the queries' signs turned for a negative scale
   uint32_t flip;
@@ -57,6 +59,10 @@ struct PackedArgs {
   int parts;
   float *po, *pml;
 };
+
+// n / group for 0 <= n < 2^31: with 2^(s-1) < group <= 2^s and by_group = ceil(2^(31+s) / group),
+// by_group group is at most 2^s more than 2^(31+s), which never carries a quotient up.
+__device__ inline int by(int n, const PackedArgs& a) { return (int)(__umulhi(2u * (uint32_t)n, a.by_group) >> a.by_shift); }
 
 __device__ inline int cut(int v, int total) { return min(max(v, 0), total); }
 
@@ -86,12 +92,17 @@ __device__ inline bool find(const PackedArgs& a, int b, Found* f) {
     const int q0 = cut(a.cu_q[s], a.total_q), q1 = cut(a.cu_q[s + 1], a.total_q);
     const int k0 = cut(a.cu_k[s], a.total_k), k1 = cut(a.cu_k[s + 1], a.total_k);
     const int n = s0 + lane < a.nseq ? (max(q1 - q0, 0) * a.group + QB - 1) / QB : 0;
+    // running sum over the lanes: within rows of 16, then over the rows
     int up = n;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(up, o);
-      if (lane >= o) up += v;
-    }
+#define DUO_UP(o) up += __builtin_amdgcn_update_dpp(0, up, 0x110 + o, 0xf, 0xf, true)
+    DUO_UP(1);
+    DUO_UP(2);
+    DUO_UP(4);
+    DUO_UP(8);
+#undef DUO_UP
+    const int r0 = __builtin_amdgcn_readlane(up, 15), r1 = r0 + __builtin_amdgcn_readlane(up, 31);
+    const int r2 = r1 + __builtin_amdgcn_readlane(up, 47);
+    up += lane < 16 ? 0 : lane < 32 ? r0 : lane < 48 ? r1 : r2;
     const uint64_t past = __ballot(up > b);
     if (past) {
       const int l = __ffsll((unsigned long long)past) - 1;
@@ -125,8 +136,8 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
   const int off = lk - lq;              // query i sees keys j <= i + off
   // row r of the sequence and K/V head: query r / group, head r % group of its group
   const int rows = lq * a.group, row0 = qb * QB + 32 * wave, row = min(row0 + l32, rows - 1);
-  const int q = row / a.group, head = kv * a.group + row - q * a.group;
-  const int q_lo = row0 / a.group, q_hi = min(row0 + 31, rows - 1) / a.group;  // of this wave
+  const int q = by(row, a), head = kv * a.group + row - q * a.group;
+  const int q_lo = by(row0, a), q_hi = by(min(row0 + 31, rows - 1), a);  // of this wave
   const uint16_t* const Kh = a.K + (int64_t)k_first * a.ldk + kv * HD;
   const uint16_t* const Vh = a.V + (int64_t)k_first * a.ldv + kv * HD;
   // chunk c of key row r sits at position kswz(r, c) (vswz) of its row: 16 consecutive
@@ -135,17 +146,7 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
   auto kswz = [](int key, int c) { return CH == 16 ? c ^ (key & 15) : c ^ ((key >> 1) & 7); };
   auto vswz = [](int key, int c) { return CH == 16 ? c ^ (4 * (key & 3)) : c ^ (4 * ((key >> 1) & 1)); };
 
-  u32x4 qa[KS];
-  {
-    const uint16_t* at = a.Q + (int64_t)(q_first + q) * a.ldq + head * HD;
-#pragma unroll
-    for (int c = 0; c < KS; ++c) {
-      qa[c] = *(const u32x4*)(at + 8 * (2 * c + half));
-#pragma unroll
-      for (int j = 0; j < 4; ++j) qa[c][j] ^= a.flip;
-    }
-  }
-  const int seen = min(qb * QB + QB - 1, rows - 1) / a.group + 1 + off;  // keys that the block's last query sees
+  const int seen = by(min(qb * QB + QB - 1, rows - 1), a) + 1 + off;  // keys that the block's last query sees
   const int tiles = (seen + KB - 1) / KB;   // <= 0: none
   // this workgroup's: all of them, or a part that begins with an even one
   const int each = SPLIT ? max((tiles + a.parts - 1) / a.parts + 1 & ~1, 2) : 0;
@@ -163,6 +164,21 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
       dma16(tile, (uint32_t)row * (uint32_t)(ld * 2) + 16 * c, to + i * 1024);
     }
   };
+
+  // the first keys and the queries are on their way together
+  if (nkb > kb0) issue(Kh, a.ldk, kb0, sm[0][0], false);
+  u32x4 qa[KS];
+  {
+    const uint16_t* at = a.Q + (int64_t)(q_first + q) * a.ldq + head * HD;
+#pragma unroll
+    for (int c = 0; c < KS; ++c) qa[c] = *(const u32x4*)(at + 8 * (2 * c + half));
+#pragma unroll
+    for (int c = 0; c < KS; ++c) {
+      asm volatile("" : "+v"(qa[c]));  // waited for here, and not behind the loads that follow
+#pragma unroll
+      for (int j = 0; j < 4; ++j) qa[c][j] ^= a.flip;
+    }
+  }
 
   float m = -INFINITY, mc = -INFINITY, l = 0.f;  // reference, times cexp; sum of this half's keys
   f16x o[DB];
@@ -364,7 +380,6 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
   };
 
   if (nkb > kb0) {
-    issue(Kh, a.ldk, kb0, sm[0][0], false);
     issue(Kh, a.ldk, min(kb0 + 1, nkb - 1), sm[1][0], false);
     issue(Vh, a.ldv, kb0, sm[0][1], true);
     wait_vm<2 * NL>();
@@ -426,33 +441,32 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
     return;
   }
   // queries that see no key: 0; a sum of 0 (every score -inf) gives NaN
-  const float inv = 1.0f / (__uint_as_float(rl[0]) + __uint_as_float(rl[1]));
-  const bool none = q + off < 0;
+  const float inv = q + off < 0 ? 0.f : 1.0f / (__uint_as_float(rl[0]) + __uint_as_float(rl[1]));
   uint2 y[DB][4];
 #pragma unroll
   for (int d = 0; d < DB; ++d)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      y[d][g].x = none ? 0u : pack_bf16(o[d][4 * g] * inv, o[d][4 * g + 1] * inv);
-      y[d][g].y = none ? 0u : pack_bf16(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv);
+      y[d][g].x = pack_bf16(o[d][4 * g] * inv, o[d][4 * g + 1] * inv);
+      y[d][g].y = pack_bf16(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv);
     }
   if (a.vec) {
-    // through this wave's part of LDS, so that a row is written at once, 16 bytes per lane;
-    // chunk c of row r at c ^ (r % CH)
-    lds_barrier();  // every wave is done with the tiles
-    uint8_t* const st = (uint8_t*)sm + wave * (32 * HD * 2);
+    // through this wave's part of LDS, where the last K tiles were (every wave was done with
+    // them at the last turn), so that a row is written at once, 16 bytes per lane; chunk c of
+    // row r at c ^ (r % CH)
+    uint8_t* const st = (uint8_t*)sm[wave / (NW / 2)][0] + wave % (NW / 2) * (32 * HD * 2);
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
         *(uint2*)(st + l32 * HD * 2 + ((4 * d + g) ^ (l32 & (CH - 1))) * 16 + 8 * half) = y[d][g];
     wait_lds<0>();
+    uint16_t* const O0 = a.O + (int64_t)q_first * a.ldo + 8 * (lane % CH);
 #pragma unroll
     for (int i = 0; i < 32 / RPL; ++i) {
-      const int r = i * RPL + lane / CH, c = lane % CH;
-      if (row0 + r >= rows) break;
-      const int qr = (row0 + r) / a.group, h = kv * a.group + (row0 + r) - qr * a.group;
-      *(u32x4*)(a.O + (int64_t)(q_first + qr) * a.ldo + h * HD + 8 * c) = *(const u32x4*)(st + r * HD * 2 + (c ^ (r & (CH - 1))) * 16);
+      const int r = i * RPL + lane / CH, qr = by(row0 + r, a), h = kv * a.group + (row0 + r) - qr * a.group;
+      const u32x4 v = *(const u32x4*)(st + r * HD * 2 + (lane % CH ^ (r & (CH - 1))) * 16);
+      if (row0 + r < rows) *(u32x4*)(O0 + qr * a.ldo + h * HD) = v;
     }
   } else if (row0 + l32 < rows) {
     uint16_t* y0 = a.O + (int64_t)(q_first + q) * a.ldo + head * HD + 4 * half;
@@ -479,7 +493,7 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
   if (!place(blockIdx.x, a, &kv, &block) || !find<QB>(a, block, &f)) return;
   const int local = blockIdx.y * (256 / T) + threadIdx.x / T, row = f.qb * QB + local, d = threadIdx.x % T * 4;
   if (row >= f.lq * a.group) return;
-  const int q = row / a.group, head = kv * a.group + row - q * a.group;
+  const int q = by(row, a), head = kv * a.group + row - q * a.group;
   const int64_t at = ((int64_t)kv * a.blocks + block) * a.parts * QB + local;
   float top = -INFINITY;
 #pragma unroll 4
@@ -569,6 +583,9 @@ duo_status duo_attention_packed(const void* Q, int64_t ldq, const void* K, int64
   a.cu_q = cu_q, a.cu_k = cu_k ? cu_k : cu_q;
   a.total_q = (int)total_q, a.total_k = (int)total_k, a.nseq = (int)nseq;
   a.kv_heads = (int)kv_heads, a.group = (int)group, a.blocks = (int)blocks;
+  a.by_shift = 0;
+  while ((int64_t)1 << a.by_shift < group) ++a.by_shift;
+  a.by_group = (uint32_t)((((uint64_t)1 << (31 + a.by_shift)) + group - 1) / group);
   // never 0: the scores of keys that are not seen, -inf, have to stay that
   a.cexp = std::max((float)(std::fabs(scale) * 1.4426950408889634), 1.4e-45f);
   a.flip = scale < 0.0 ? 0x80008000u : 0u;
