@@ -25,25 +25,22 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) % 16) == 
 // ---------------------------------------------------------------------------
 // rotation by positions
 // ---------------------------------------------------------------------------
-constexpr int kMaxHalf = 128;
-
-// Turns per position of every pair, theta^(-2i/head_dim) / 2 pi, computed on the host.
-struct Turns {
-  double f[kMaxHalf];
-};
+constexpr int kMaxHalf = 128;  // pairs
 
 // A workgroup takes `per` tokens; the cosines and sines of a token are computed once
-// (the angle in turns and its fraction in fp64, the rest in fp32) and shared by all
-// of its heads through LDS.  V: pairs per access (8 in 16-byte accesses, or 1).
+// (the frequency theta^(-2i/head_dim) = 2^(i step), the angle in turns and its fraction in
+// fp64, the rest in fp32) and shared by all of its heads through LDS.  The frequencies are
+// computed here: a table of them among the arguments (1 KB) made the launch, which bounds a
+// small call, 4.0 us instead of 3.5.  V: pairs per access (8 in 16-byte accesses, or 1).
 template <int V>
 __global__ __launch_bounds__(256) void rope_at_kernel(const uint16_t* X, int64_t ldx, int64_t m, int heads, int half,
-                                                      const int32_t* __restrict__ pos, Turns turns, uint16_t* Y,
+                                                      const int32_t* __restrict__ pos, double step, uint16_t* Y,
                                                       int64_t ldy, int per) {
   extern __shared__ float2 cs[];  // [token][pair]: cosine, sine
   const int64_t t0 = (int64_t)blockIdx.x * per;
   const int nt = (int)min((int64_t)per, m - t0);
   for (int e = threadIdx.x; e < nt * half; e += 256) {
-    const double turn = (double)pos[t0 + e / half] * turns.f[e % half];
+    const double turn = (double)pos[t0 + e / half] * (exp2(e % half * step) * 0.15915494309189535);
     const float a = (float)((turn - rint(turn)) * 6.283185307179586);
     float sn, cn;
     sincosf(a, &sn, &cn);
@@ -314,8 +311,7 @@ duo_status duo_rope_at(const void* X, int64_t m, int64_t heads, int64_t head_dim
   if (m > INT32_MAX) return DUO_ERR_UNSUPPORTED;
   if (duo_status d = device_ok(); d != DUO_OK) return d;
   const int half = (int)head_dim / 2;
-  Turns tr;
-  for (int i = 0; i < half; ++i) tr.f[i] = std::pow(theta, -2.0 * i / (double)head_dim) / 6.283185307179586;
+  const double step = -2.0 / (double)head_dim * std::log2(theta);
   const bool vec = half % 8 == 0 && ldx % 8 == 0 && ldy % 8 == 0 && aligned16(X) && aligned16(Y);
   const int64_t items = heads * (half / (vec ? 8 : 1));  // of one token
   const int per = (int)std::max<int64_t>(1, 256 / items);
@@ -323,10 +319,10 @@ duo_status duo_rope_at(const void* X, int64_t m, int64_t heads, int64_t head_dim
   const size_t lds = (size_t)per * half * sizeof(float2);
   if (vec)
     hipLaunchKernelGGL(rope_at_kernel<8>, grid, dim3(256), lds, (hipStream_t)stream, (const uint16_t*)X, ldx, m,
-                       (int)heads, half, pos, tr, (uint16_t*)Y, ldy, per);
+                       (int)heads, half, pos, step, (uint16_t*)Y, ldy, per);
   else
     hipLaunchKernelGGL(rope_at_kernel<1>, grid, dim3(256), lds, (hipStream_t)stream, (const uint16_t*)X, ldx, m,
-                       (int)heads, half, pos, tr, (uint16_t*)Y, ldy, per);
+                       (int)heads, half, pos, step, (uint16_t*)Y, ldy, per);
   DUO_LAUNCH_CHECK();
   return DUO_OK;
 }

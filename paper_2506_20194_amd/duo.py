@@ -10,6 +10,7 @@ missing or no gfx950 device is present the calls raise.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -768,7 +769,7 @@ def _ints(t, dtype, n, name):
 
 
 def _empty(m, w, like):
-    return torch.empty((m, w), dtype=torch.bfloat16, device=like.device)
+    return torch.empty(m, w, dtype=torch.bfloat16, device=like.device)
 
 
 _raw_stream = torch._C._cuda_getCurrentRawStream  # of a device index; torch's current stream
@@ -787,12 +788,13 @@ class KVCache:
         nbytes = kv_page_bytes(page_size, kv_heads, head_dim, fmt)
         if data.dtype != torch.uint8:
             raise TypeError("duo: a cache's data must be uint8")
-        if data.dim() != 3 or data.shape[1:] != (kv_heads, nbytes // kv_heads):
+        pages = data.shape[0] if data.dim() == 3 else 0
+        if data.shape != (pages, kv_heads, nbytes // kv_heads):
             raise ValueError(f"duo: data has shape {tuple(data.shape)}, expected (pages, {kv_heads}, {nbytes // kv_heads})")
         if not data.is_contiguous():
             raise ValueError("duo: data must be contiguous")
         self.data, self.page_size, self.kv_heads, self.head_dim, self.fmt = data, page_size, kv_heads, head_dim, fmt
-        self.c = KvCache(data.data_ptr(), data.shape[0], page_size, kv_heads, head_dim, KV_FORMATS[fmt])
+        self.c = KvCache(data.data_ptr(), pages, page_size, kv_heads, head_dim, KV_FORMATS[fmt])
         self.ref = ctypes.byref(self.c)
 
     @classmethod
@@ -809,6 +811,8 @@ class KVCache:
         return table[seq, pos // self.page_size].long() * self.page_size + pos % self.page_size
 
 
+# Sizes go by their arguments alone; a program asks for the same few again and again.
+@functools.lru_cache(maxsize=256)
 def kv_page_bytes(page_size, kv_heads, head_dim, fmt="bf16") -> int:
     n = lib().duo_kv_page_bytes(KV_FORMATS[fmt], page_size, kv_heads, head_dim)
     if n == 0:
@@ -854,9 +858,14 @@ def duo_kv_read(cache, slots, out=None):
     return K, V
 
 
+@functools.lru_cache(maxsize=256)
+def _packed_bytes(total_q, total_k, nseq, heads, kv_heads, head_dim):
+    return lib().duo_attention_packed_workspace_size(total_q, total_k, nseq, heads, kv_heads, head_dim)
+
+
 def attention_packed_workspace(total_q, total_k, nseq, heads, kv_heads, head_dim, device):
     """A workspace tensor, or None where none is needed."""
-    n = lib().duo_attention_packed_workspace_size(total_q, total_k, nseq, heads, kv_heads, head_dim)
+    n = _packed_bytes(total_q, total_k, nseq, heads, kv_heads, head_dim)
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
 
@@ -881,9 +890,13 @@ def duo_attention_packed(Q, K, V, cu_q, heads, kv_heads, head_dim, cu_k=None, sc
     return O
 
 
+@functools.lru_cache(maxsize=256)
+def _paged_bytes(nseq, heads, kv_heads, head_dim, max_len):
+    return max(lib().duo_attention_paged_workspace_size(nseq, heads, kv_heads, head_dim, max_len), 256)
+
+
 def attention_paged_workspace(nseq, heads, kv_heads, head_dim, max_len, device):
-    n = lib().duo_attention_paged_workspace_size(nseq, heads, kv_heads, head_dim, max_len)
-    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+    return torch.empty(_paged_bytes(nseq, heads, kv_heads, head_dim, max_len), dtype=torch.uint8, device=device)
 
 
 def duo_attention_paged(Q, cache, table, lens, heads, max_len=None, scale=None, out=None, ws=None):

@@ -18,6 +18,8 @@ BIG = 10 ** 12
 @pytest.fixture()
 def codes(duo_lib):
     d = duo_lib
+    if torch.cuda.device_count():
+        pytest.skip("valid arguments with made-up addresses would be launched")
     return d.lib(), d.DUO_OK, d.DUO_ERR_INVALID_ARG, d.DUO_ERR_UNSUPPORTED, d.DUO_ERR_NO_DEVICE
 
 
@@ -155,6 +157,8 @@ def test_paged_workspace_never_falls(duo_lib, heads, kv, hd):
 
 def test_binding_refuses_host_tensors(duo_lib):
     d = duo_lib
+    if torch.cuda.device_count():
+        pytest.skip("valid arguments with made-up addresses would be launched")
     cache = d.KVCache(torch.zeros((2, 1, d.kv_page_bytes(16, 1, 64)), dtype=torch.uint8), 16, 1, 64)
     x = torch.zeros((3, 64), dtype=torch.bfloat16)
     i = torch.zeros(3, dtype=torch.int64)
@@ -172,6 +176,8 @@ def test_binding_refuses_host_tensors(duo_lib):
 
 def test_cache_object(duo_lib):
     d = duo_lib
+    if torch.cuda.device_count():
+        pytest.skip("valid arguments with made-up addresses would be launched")
     cache = d.KVCache(torch.zeros((5, 2, d.kv_page_bytes(32, 2, 64, "int4") // 2), dtype=torch.uint8), 32, 2, 64, "int4")
     table = torch.tensor([[3, 1], [0, 4]], dtype=torch.int32)
     s = cache.slots(table, torch.tensor([0, 0, 1]), torch.tensor([31, 32, 63]))
