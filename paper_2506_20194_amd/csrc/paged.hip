@@ -78,7 +78,7 @@ struct PagedGeo {
 struct PagedWork {
   const int32_t* lens;
   int nseq, max_len, rows;  // rows per sequence
-  int per;                  // sequences per bucket of the count: ceil(nseq / 256)
+  int per;                  // sequences per bucket of the count: ceil(nseq / 64)
   int many;                 // rows enough for every share: short ones go four to a workgroup
 };
 
@@ -124,40 +124,37 @@ struct Shares {
   }
 };
 
-// *mine: cost of the sequences up to the end of this thread's bucket; the result: of all.
-// 256 threads; ends with a barrier.
-struct Count {
-  int64_t wave[4];
-  int64_t before;  // cost of the sequences before bucket `at`
-  int at;
-  int len[256];    // of the sequences, where a bucket is one
-};
+__device__ inline int64_t lane64(int64_t v, int l) {
+  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), l) << 32 |
+                   (uint32_t)__builtin_amdgcn_readlane((int)v, l));
+}
+
+// Cost of the sequences up to the end of this lane's bucket of `per`.  Every wave counts for
+// itself: no barrier, and no wave waits for another.  *len: this lane's sequence, where a
+// bucket is one.
 template <int KEYS>
-__device__ inline int64_t count_rows(const PagedWork& w, Count& c, int64_t* mine) {
-  const int tid = threadIdx.x, lane = tid & 63;
+__device__ inline int64_t count_rows(const PagedWork& w, int* len) {
+  const int lane = threadIdx.x & 63;
   int64_t n = 0;
+  *len = 0;
+#pragma unroll 4
   for (int i = 0; i < w.per; ++i) {
-    const int64_t s = (int64_t)tid * w.per + i;
-    const int len = s < w.nseq ? seq_len(w, (int)s) : 0;
-    if (w.per == 1) c.len[tid] = len;
-    const Units x(tiles_of<KEYS>(len), w);
+    const int64_t s = (int64_t)lane * w.per + i;
+    *len = s < w.nseq ? seq_len(w, (int)s) : 0;
+    const Units x(tiles_of<KEYS>(*len), w);
     n += (int64_t)x.cost * x.units;
   }
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t up = __shfl_up(n, o);
-    if (lane >= o) n += up;
-  }
-  if (lane == 63) c.wave[tid >> 6] = n;
-  __syncthreads();
-  int64_t total = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (i < tid >> 6) n += c.wave[i];
-    total += c.wave[i];
-  }
-  *mine = n;
-  return total;
+  // running sum over the lanes: within rows of 16, then over the rows
+#define DUO_UP(o)                                                                                        \
+  n += (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_update_dpp(0, (int)(n >> 32), 0x110 + o, 0xf, 0xf, true) << 32 | \
+                 (uint32_t)__builtin_amdgcn_update_dpp(0, (int)n, 0x110 + o, 0xf, 0xf, true))
+  DUO_UP(1);
+  DUO_UP(2);
+  DUO_UP(4);
+  DUO_UP(8);
+#undef DUO_UP
+  const int64_t r0 = lane64(n, 15), r1 = r0 + lane64(n, 31), r2 = r1 + lane64(n, 47);
+  return n + (lane < 16 ? 0 : lane < 32 ? r0 : lane < 48 ? r1 : r2);
 }
 
 // max over the four lanes that hold one column
@@ -231,39 +228,33 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
   static_assert(QUANT || !PAIR, "");
   constexpr float BIAS = FMT == DUO_KV_I8 ? 128.f : 136.f;
   extern __shared__ __attribute__((aligned(16))) uint8_t lsm[];
-  __shared__ Count cnt;
   __shared__ float jm[4][kCols], jl[4][kCols];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
   const int col = PAIR ? l16 & 7 : l16, half = PAIR ? l16 >> 3 : 0;  // this lane's head, and half of the keys
 
-  int64_t mine;
-  const int64_t total = count_rows<KEYS>(work, cnt, &mine);
-  const Shares shares(total, gridDim.x);
+  int my_len;
+  const int64_t upto = count_rows<KEYS>(work, &my_len);
+  const Shares shares(lane64(upto, 63), gridDim.x);
   int64_t u = shares.begin(blockIdx.x);
   const int64_t u1 = (int)blockIdx.x < shares.n ? shares.begin(blockIdx.x + 1) : u;
-  {
-    // the bucket that u lies in: the first whose end lies behind it
-    const int64_t upto = __shfl_up(mine, 1);
-    int64_t prev = lane ? upto : 0;
-    if (lane == 0)
-      for (int i = 0; i < wave; ++i) prev += cnt.wave[i];
-    if (prev <= u && u < mine) cnt.at = tid, cnt.before = prev;
-  }
   if (tid == 0 && tasks) tasks[blockIdx.x].parts = 0;
-  __syncthreads();
-  auto len_of = [&](int s) { return __builtin_amdgcn_readfirstlane(work.per == 1 ? cnt.len[s] : seq_len(work, s)); };
+  auto len_of = [&](int s) {
+    return work.per == 1 ? __builtin_amdgcn_readlane(my_len, s) : __builtin_amdgcn_readfirstlane(seq_len(work, s));
+  };
   // sequences without tokens
   for (int s = blockIdx.x; s < work.nseq; s += gridDim.x)
     if (len_of(s) == 0)
       for (int e = tid; e < group * kv.heads * HD; e += 256) O[(int64_t)s * ldo + e] = 0;
   if (u >= u1) return;
-  int64_t before = cnt.before;  // cost of the sequences before s
+  // the bucket that u lies in: the first whose end lies behind it
+  const int at_bucket = __ffsll((unsigned long long)__ballot(upto > u)) - 1;
+  int64_t before = at_bucket ? lane64(upto, at_bucket - 1) : 0;  // cost of the sequences before s
   uint8_t* const sK = lsm + wave * G::WAVE;
   uint8_t* const sV = sK + G::ROWS;
   uint8_t* const sS = sV + G::ROWS;  // scales: [parity of the tile's turn][K, V]
 
-  for (int s = cnt.at * work.per; u < u1; ++s) {
+  for (int s = at_bucket * work.per; u < u1; ++s) {
     const int len = len_of(s);
     const Units x(tiles_of<KEYS>(len), work);
     const int tiles = x.tiles, cost = x.cost;
@@ -830,7 +821,7 @@ duo_status duo_attention_paged(const void* Q, int64_t ldq, const duo_kv_cache* c
     constexpr int FMT = decltype(fmt)::value, HD = decltype(dim)::value;
     using P = PagedGeo<FMT, HD>;
     const int64_t wgs = paged_wgs((double)nseq * (double)rows, cdiv(max_len, P::KEYS), 256 * P::WGS);
-    const PagedWork w = {lens, (int)nseq, (int)max_len, (int)rows, (int)cdiv(nseq, 256), nseq * rows >= 2 * 256 * P::WGS};
+    const PagedWork w = {lens, (int)nseq, (int)max_len, (int)rows, (int)cdiv(nseq, 64), nseq * rows >= 2 * 256 * P::WGS};
     Task* const tasks = (Task*)ws;
     float* const part = (float*)((uint8_t*)ws + align_up(wgs * sizeof(Task)));
     constexpr bool Q8 = FMT != DUO_KV_BF16;
