@@ -42,6 +42,8 @@ namespace {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) % 16) == 0; }
 
+constexpr int NW = 4, QB = 32 * NW;  // waves of a workgroup, rows of a block
+
 struct PackedArgs {
   const uint16_t *Q, *K, *V;
   uint16_t* O;
@@ -84,7 +86,6 @@ struct Found {
 };
 
 // The sequence and the block within it of block b; false past the last.
-template <int QB>
 __device__ inline bool find(const PackedArgs& a, int b, Found* f) {
   const int lane = threadIdx.x & 63;
   for (int s0 = 0; s0 < a.nseq; s0 += 64) {
@@ -115,8 +116,8 @@ __device__ inline bool find(const PackedArgs& a, int b, Found* f) {
   return false;
 }
 
-template <int HD, int NW, bool SPLIT>
-__global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
+template <int HD, bool SPLIT>
+__global__ __launch_bounds__(64 * NW, 2) void packed_kernel(PackedArgs a) {
   constexpr int KB = 64;                // keys per tile
   constexpr int CH = HD / 8;            // 16-byte chunks per key row
   constexpr int KS = HD / 16;           // MFMA steps over head_dim
@@ -124,12 +125,11 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
   constexpr int TILE = KB * CH;         // chunks per operand tile
   constexpr int NL = TILE / (64 * NW);  // 16-byte loads per thread, operand and tile
   constexpr int RPL = 64 / CH;          // keys per wave-wide load
-  constexpr int QB = 32 * NW;
   __shared__ u32x4 sm[2][2][TILE];      // [buffer][K, V]
   int kv, block;
   Found f;
   const int part = SPLIT ? blockIdx.y : 0;
-  if (!place(blockIdx.x, a, &kv, &block) || !find<QB>(a, block, &f)) return;
+  if (!place(blockIdx.x, a, &kv, &block) || !find(a, block, &f)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, half = lane >> 5;
   const int q_first = f.q_first, lq = f.lq, k_first = f.k_first, lk = f.lk, qb = f.qb;
@@ -485,12 +485,12 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void packed_kernel(PackedArgs a) {
 
 // Joins the parts of a block's rows: HD / 4 threads per row, blockIdx.y counts the rows of a
 // block by the 1024 / HD that a workgroup takes.
-template <int HD, int QB>
+template <int HD>
 __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
   constexpr int T = HD / 4;
   int kv, block;
   Found f;
-  if (!place(blockIdx.x, a, &kv, &block) || !find<QB>(a, block, &f)) return;
+  if (!place(blockIdx.x, a, &kv, &block) || !find(a, block, &f)) return;
   const int local = blockIdx.y * (256 / T) + threadIdx.x / T, row = f.qb * QB + local, d = threadIdx.x % T * 4;
   if (row >= f.lq * a.group) return;
   const int q = by(row, a), head = kv * a.group + row - q * a.group;
@@ -519,21 +519,19 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
   }
 }
 
-// How a call is cut: rows per workgroup, a bound of the blocks of a K/V head, parts of their keys.
+// How a call is cut: a bound of the blocks of a K/V head, parts of their keys.
 struct Plan {
-  int rows;
   int64_t blocks, parts;
 };
 Plan packed_plan(int64_t total_q, int64_t total_k, int64_t nseq, int64_t group, int64_t kv_heads) {
-  // 128 rows per workgroup; 64 when that would leave CUs without their two workgroups (512
-  // in all)
-  auto bound = [&](int64_t rows) { return total_q * group / rows + std::min(nseq, total_q); };
-  if ((total_q * group / 128 + nseq / 2) * kv_heads >= 512) return {128, bound(128), 1};
+  const int64_t blocks = total_q * group / QB + std::min(nseq, total_q), wgs = blocks * kv_heads;
   // Few rows on long sequences leave most CUs idle, so their keys are split too: as many
-  // parts as fill the CUs, of 256 keys at least (on average over the sequences).
-  const int64_t blocks = bound(64), wgs = blocks * kv_heads;
-  const int64_t parts = std::min(512 / wgs, total_k / nseq / 256);
-  return {64, blocks, wgs <= 256 && parts >= 2 ? std::min<int64_t>(parts, 64) : 1};
+  // parts as fill the CUs (two workgroups on each), of 512 keys at least (on average over the
+  // sequences).  One query on 16384 keys, 64 heads on 8: 238 us whole, 33 split, 44 with
+  // parts of 256 keys; 256 queries there 261 and 166; where nothing is split for shortness, 512
+  // queries on 512 keys, 32 heads on 8: 15 us, and 20 in parts of 256.
+  const int64_t parts = std::min<int64_t>({512 / wgs, total_k / nseq / 512, 64});
+  return {blocks, parts >= 2 ? parts : 1};
 }
 
 }  // namespace
@@ -547,7 +545,7 @@ size_t duo_attention_packed_workspace_size(int64_t total_q, int64_t total_k, int
     return 0;
   const Plan p = packed_plan(total_q, total_k, nseq, heads / kv_heads, kv_heads);
   if (p.parts == 1) return 0;
-  return align_up((size_t)(p.blocks * kv_heads * p.parts * p.rows * (head_dim + 2)) * sizeof(float));
+  return align_up((size_t)(p.blocks * kv_heads * p.parts * QB * (head_dim + 2)) * sizeof(float));
 }
 
 duo_status duo_attention_packed(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
@@ -591,7 +589,7 @@ duo_status duo_attention_packed(const void* Q, int64_t ldq, const void* K, int64
   a.flip = scale < 0.0 ? 0x80008000u : 0u;
   a.vec = ldo % 8 == 0 && aligned16(O);
   a.parts = (int)plan.parts;
-  const int64_t rows = blocks * kv_heads * plan.parts * plan.rows;
+  const int64_t rows = blocks * kv_heads * plan.parts * QB;
   a.po = (float*)ws;
   a.pml = a.po + (need ? rows * head_dim : 0);
   const hipStream_t st = (hipStream_t)stream;
@@ -599,13 +597,11 @@ duo_status duo_attention_packed(const void* Q, int64_t ldq, const void* K, int64
     constexpr int HD = decltype(hd)::value;
     const dim3 grid((unsigned)wgs, (unsigned)plan.parts);
     if (plan.parts > 1) {
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(packed_kernel<HD, 2, true>), grid, dim3(128), 0, st, a);
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(packed_kernel<HD, true>), grid, dim3(64 * NW), 0, st, a);
       DUO_LAUNCH_CHECK();
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(packed_join_kernel<HD, 64>), dim3((unsigned)wgs, HD / 16), dim3(256), 0, st, a);
-    } else if (plan.rows == 128) {
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(packed_kernel<HD, 4, false>), grid, dim3(256), 0, st, a);
+      hipLaunchKernelGGL(packed_join_kernel<HD>, dim3((unsigned)wgs, QB * HD / 1024), dim3(256), 0, st, a);
     } else {
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(packed_kernel<HD, 2, false>), grid, dim3(128), 0, st, a);
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(packed_kernel<HD, false>), grid, dim3(64 * NW), 0, st, a);
     }
     DUO_LAUNCH_CHECK();
     return DUO_OK;
