@@ -566,11 +566,13 @@ duo_status duo_kv_read(const duo_kv_cache* cache, const int64_t* slots, int64_t 
  *   and a query that sees no key (lk < lq) gets 0.  Keys and values that a query
  *   does not see have no influence on it, whatever they hold.  Scores, maxima,
  *   sums and O are fp32, in one pass over the keys; the probabilities are rounded
- *   to bf16 before the product with V, relative to the largest score so far.
+ *   to bf16 before the product with V, relative to a running reference that the
+ *   scores exceed by a factor of 2^8 at most.
  *   Q total_q x heads*head_dim (ldq), K and V total_k x kv_heads*head_dim (ldk,
  *   ldv), O total_q x heads*head_dim (ldo, not overlapping the inputs), bf16.
  *   Offsets are taken as within [0, total] (larger ones as total, a sequence whose
- *   end lies before its start as empty); rows of O in no sequence are left alone.
+ *   end lies before its start as empty); rows of O in no sequence are left alone,
+ *   and where sequences overlap (offsets that fall) some of theirs may be too.
  *   scale finite.  heads % kv_heads == 0, head_dim 64 or 128; Q, K, V 16-byte
  *   aligned with ldq, ldk, ldv % 8 == 0 and ldk, ldv < 2^24 (else
  *   DUO_ERR_UNSUPPORTED).  Few queries on long sequences are split over the keys and
@@ -594,9 +596,10 @@ duo_status duo_attention_packed(const void* Q, int64_t ldq, const void* K, int64
  *   Scores are exact products of bf16 queries and cached codes summed in fp32,
  *   times the group's scale; probabilities, in 8 and 4 bits times the scale of V,
  *   are rounded to bf16 before the product with V.  Long sequences are split over
- *   their length and joined; where is a matter of the sizes alone (nseq, max_len,
- *   heads), so results are deterministic.  ldt * page_size >= max_len.  Workspace: duo_attention_paged_workspace_size
- *   with the same sizes (it never falls with a larger max_len or nseq). */
+ *   their length and joined; where is a matter of nseq, max_len, heads and the
+ *   lengths alone, so results are deterministic.  ldt * page_size >= max_len.
+ *   Workspace: duo_attention_paged_workspace_size with the same sizes (it never
+ *   falls with a larger max_len or nseq). */
 size_t duo_attention_paged_workspace_size(int64_t nseq, int64_t heads, int64_t kv_heads, int64_t head_dim,
                                           int64_t max_len);
 duo_status duo_attention_paged(const void* Q, int64_t ldq, const duo_kv_cache* cache, const int32_t* table, int64_t ldt,

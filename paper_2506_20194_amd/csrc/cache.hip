@@ -32,6 +32,8 @@ constexpr int kMaxHalf = 128;  // pairs
 // fp64, the rest in fp32) and shared by all of its heads through LDS.  The frequencies are
 // computed here: a table of them among the arguments (1 KB) made the launch, which bounds a
 // small call, 4.0 us instead of 3.5.  V: pairs per access (8 in 16-byte accesses, or 1).
+// Bound: HBM; 32768 rows of 64 heads of 128 take 186 us, 5.7 TB/s read and written (a large copy
+// reaches 4.95); 64 rows 5.4 us, the launch.
 template <int V>
 __global__ __launch_bounds__(256) void rope_at_kernel(const uint16_t* X, int64_t ldx, int64_t m, int heads, int half,
                                                       const int32_t* __restrict__ pos, double step, uint16_t* Y,
@@ -81,7 +83,10 @@ __global__ __launch_bounds__(256) void rope_at_kernel(const uint16_t* X, int64_t
 
 // Both directions: blockIdx.y is a head's K (even) or V, a thread takes 8 channels of
 // kTok tokens, whose slots and rows are all loaded before the first is used.  Bound: HBM;
-// a CU has some 80 vector instructions per 8 channels in the time of their bytes.
+// a CU has some 80 vector instructions per 8 channels in the time of their bytes, which is
+// why the codes are made without a division and both formats' bias rides on an addition.
+// Eight heads of 128: 131072 tokens of 4 bits read in 137 us (5.0 TB/s; a token per thread
+// with heads in the grid's first axis, 231); 16411 tokens written and read back in 8 bits in 45.
 constexpr int kTok = 4;
 
 // Where the row of slot `slot` begins in the cache, and its scales (which: 0 K, 1 V).

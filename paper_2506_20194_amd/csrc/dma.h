@@ -16,10 +16,10 @@ __device__ __forceinline__ uint32_t lds_addr(const void* p) {
 
 // 16 or 4 bytes per lane from base + off; base and lds are the same for all lanes.
 __device__ __forceinline__ void dma16(const void* base, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
 __device__ __forceinline__ void dma4(const void* base, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
 // N (2, 4 or 8) loads of 16 bytes per lane from consecutive KiB: load i from base + 1024 i +
 // off[i] to lds + 1024 i (the instruction's offset counts for both sides).
@@ -29,7 +29,7 @@ __device__ __forceinline__ void dma16_run(const uint8_t* base, const uint32_t (&
   if constexpr (N == 2)
     asm volatile(
         "s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\t"
-        "global_load_lds_dwordx4 %2, %3 offset:1024" ::"s"(lds), "v"(off[0]), "v"(off[1]), "s"(base) : "memory");
+        "global_load_lds_dwordx4 %2, %3 offset:1024" ::"s"(lds), "v"(off[0]), "v"(off[1]), "s"(base) : "memory", "m0");
   else
 #pragma unroll
     for (int i = 0; i < N; i += 4)
@@ -37,7 +37,7 @@ __device__ __forceinline__ void dma16_run(const uint8_t* base, const uint32_t (&
           "s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\t"
           "global_load_lds_dwordx4 %2, %5 offset:1024\n\tglobal_load_lds_dwordx4 %3, %5 offset:2048\n\t"
           "global_load_lds_dwordx4 %4, %5 offset:3072" ::"s"(lds + 1024 * i),
-          "v"(off[i]), "v"(off[i + 1]), "v"(off[i + 2]), "v"(off[i + 3]), "s"(base + 1024 * i) : "memory");
+          "v"(off[i]), "v"(off[i + 1]), "v"(off[i + 2]), "v"(off[i + 3]), "s"(base + 1024 * i) : "memory", "m0");
 }
 // The same from an address per lane.
 __device__ __forceinline__ void dma16(const void* at, uint32_t lds) {

@@ -31,6 +31,12 @@
 // -bias sum(q) of the group for S and gets -bias sum(p) from one more MFMA for O.  A
 // score is the sum of its groups' products times their scales, in fp32; the scale
 // of V goes into the probability before that is rounded to bf16.
+//
+// Bound: HBM where there is enough to read: 64 sequences of 8192 tokens, 64 heads of 128 on 8,
+// 355 us in 16 bits (6.0 TB/s), 206 in 8 (5.5), 121 in 4 (5.0, where the vector work on the
+// codes shows).  Short of that what a launch and a row begin with: lengths, page numbers
+// and the first K are three trips to memory, 4 us, and the join's launch takes another 4 to 5
+// (one request of 1777 tokens, 32 heads: 12 us).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -51,9 +57,17 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) % 16) == 
 
 constexpr int kCols = 16;       // query heads per row
 constexpr int kMaxWg = 1024;    // workgroups of a launch, at most
-constexpr int kRowCost = 10;    // what a row's start and end cost, in tiles
-constexpr int kMinShare = 8;    // smallest share, in tiles
-constexpr int kShort = 4;       // tiles of a row that one wave does alone where rows are many
+// What a row's start and end cost, in tiles.  Eight sequences of 1 to 131072 tokens in 4 bits, 64
+// heads on 8: 73 us with 4, 55 with 8, 51 with 10 and 14; 48 of up to 8192 in 8 bits: 51, 46, 47, 47.
+constexpr int kRowCost = 10;
+// Smallest share, in tiles: one sequence of 4096 tokens in 4 bits 13.3 us, 17.3 with 16; with 4
+// as with 8, for twice the parts.
+constexpr int kMinShare = 8;
+// Tiles of a row that one wave does alone where rows are many: 512 sequences of 100 tokens in 4
+// bits, 64 heads on 8, 68 us with 0, 32 with 4 and 8; 128 of 256 tokens in 16 bits, 32 on 8, 26 us
+// with 0 and 4, 33 with 8.  Where rows are few four waves on one are shorter: 4 sequences of 250 tokens
+// in 8 bits, 64 on 8, 11 us, and 16 with a wave alone.
+constexpr int kShort = 4;
 constexpr int kMinKeys = 32;    // tokens of the smallest tile
 
 template <int FMT, int HD>
@@ -214,7 +228,8 @@ __device__ __forceinline__ int v_at(int r, int c) {
 // half of the tile's keys.  A block of keys of each half is multiplied with the queries in
 // its half of the columns, both into one accumulator, and what follows for a score
 // (scales, maximum, exponential, rounding), the larger part of the vector work, is done
-// for two keys at once; the halves of a column's pair meet at the join.
+// for two keys at once; the halves of a column's pair meet at the join.  64 sequences of 8192
+// tokens, 64 heads on 8: 214 us without and 206 with in 8 bits, 133 and 121 in 4.
 template <int FMT, int HD, bool PAIR>
 __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
     const uint16_t* __restrict__ Q, int64_t ldq, KvGeo kv, const int32_t* __restrict__ table, int64_t ldt, PagedWork work,
