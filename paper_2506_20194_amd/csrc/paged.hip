@@ -36,7 +36,7 @@
 // 355 us in 16 bits (6.0 TB/s), 206 in 8 (5.5), 121 in 4 (5.0, where the vector work on the
 // codes shows).  Short of that what a launch and a row begin with: lengths, page numbers
 // and the first K are three trips to memory, 4 us, and the join's launch takes another 4 to 5
-// (one request of 1777 tokens, 32 heads: 12 us).
+// (one request of 1777 tokens, 32 heads: 10 and 4 us).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
