@@ -104,7 +104,7 @@ def attend(Q, K, V, scale, seen, extra=0.0):
     O = np.zeros((lq, H, hd))
     bound = np.zeros((lq, H, hd))
     if not len(K):
-        return O, bound
+        return O, bound + 1e-37
     for h in range(H):
         k, v = K[:, h // (H // Hk)], V[:, h // (H // Hk)]
         S = np.where(seen, Q[:, h] @ k.T * scale, -np.inf)
