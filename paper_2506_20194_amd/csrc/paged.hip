@@ -379,8 +379,8 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
             }
           }
         } else {
-          // the row's last tile: rows past its end are taken from its last token,
-          // whose numbers its result holds anyway
+          // the row's last tile: rows past its end are taken from its last token, and
+          // neither their scores nor (below) their values enter
           auto place = [&](int r) {
             const int key = min(k0 + r, len - 1);
             const int id = __shfl(pid, (key >> kv.shift) - win);
@@ -549,6 +549,19 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
           }
           wait_lds<0>();
           if (more) issue(t + step, kV, sV, sn + NS * 256);
+          if (t * KEYS + KEYS > len) {
+            // copies of the last token behind the row's end: their probability is 0, and 0 times
+            // an infinite value would be NaN (codes are finite, and a scale that is not is NaN)
+            int rest = left;
+            asm volatile("" : "+v"(rest));  // compared here: the scores' comparisons would be kept for it in the loop
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int key = 16 * (j >> 1) + 2 * (j & 1);  // the register's two keys: this one and the next
+              const uint32_t keep = (key < rest ? 0xffffu : 0u) | (key + 1 < rest ? 0xffff0000u : 0u);
+#pragma unroll
+              for (int d = 0; d < 2 * CK; ++d) vf[d][j] &= keep;
+            }
+          }
           const u32x4 pf = {pack_bf16(x[0][0], x[0][1]), pack_bf16(x[0][2], x[0][3]), pack_bf16(x[1][0], x[1][1]),
                             pack_bf16(x[1][2], x[1][3])};
 #pragma unroll
