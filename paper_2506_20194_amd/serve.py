@@ -30,7 +30,8 @@ class Step:
     """The tokens of one step: sequence s goes from before[s] cached tokens to
     before[s] + new[s] (Python ints).  table: int32, row s holds the pages of
     sequence s, enough for its new length.  The token rows of the step are the
-    sequences' new tokens one behind the other."""
+    sequences' new tokens one behind the other.  A sequence that needs a page which
+    the cache does not have gets NaN for them; the table is read on the device only."""
 
     def __init__(self, cache, table, before, new):
         if len(before) != len(new) or len(new) != table.shape[0]:
@@ -51,6 +52,11 @@ class Step:
             self.lens = torch.tensor(after, dtype=torch.int32).to(dev)
             return
         self.cu_q = self._offsets(new).to(dev)
+        # token rows of sequences whose tokens do not all have a page; duo_kv_write skips such
+        # tokens and duo_kv_read gives zeros for them, which attention would take for keys
+        need = torch.arange(table.shape[1]) * cache.page_size < torch.tensor(after, dtype=torch.int64)[:, None]
+        outside = (table < 0) | (table >= cache.data.shape[0])
+        self.lost = (outside & need.to(dev)).any(1)[seq.to(dev)][:, None]
         # the whole sequences, where the chunk's own rows of K and V are not all of them
         self.cu_k, self.all_slots = None, self.slots
         if any(before):
@@ -93,7 +99,8 @@ def attention(x, weights, cfg, cache, step, p_x=None):
         return duo.duo_attention_paged(q, cache, step.table, step.lens, heads, max_len=step.max_len)
     if step.cu_k is not None or cache.fmt != "bf16":
         k, v = duo.duo_kv_read(cache, step.all_slots)
-    return duo.duo_attention_packed(q, k, v, step.cu_q, heads, kv, hd, cu_k=step.cu_k)
+    a = duo.duo_attention_packed(q, k, v, step.cu_q, heads, kv, hd, cu_k=step.cu_k)
+    return a.masked_fill_(step.lost, float("nan"))  # as duo_attention_paged does by itself
 
 
 def run_block(h, weights, cfg, cache, step, p_x=None):
