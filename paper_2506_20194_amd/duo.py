@@ -772,7 +772,10 @@ def _empty(m, w, like):
     return torch.empty(m, w, dtype=torch.bfloat16, device=like.device)
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream  # of a device index; torch's current stream
+# Torch's current stream on a device index.  The short way is missing in a torch without CUDA
+# (HIP), where this module is still imported: host-side checks and sizes need no device.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 class KVCache:
