@@ -14,6 +14,10 @@ __device__ __forceinline__ uint32_t lds_addr(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
 
+// m0 says where in LDS the loads go, and is named as changed.  The compiler warns that it may not keep
+// what it has in m0 itself across such a block: nothing else in the kernels that use this file may
+// need m0 (tests/test_dma_listing_cpu.py looks at what was compiled).
+//
 // 16 or 4 bytes per lane from base + off; base and lds are the same for all lanes.
 __device__ __forceinline__ void dma16(const void* base, uint32_t off, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
@@ -41,10 +45,10 @@ __device__ __forceinline__ void dma16_run(const uint8_t* base, const uint32_t (&
 }
 // The same from an address per lane.
 __device__ __forceinline__ void dma16(const void* at, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(at) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(at) : "memory", "m0");
 }
 __device__ __forceinline__ void dma4(const void* at, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(at) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(at) : "memory", "m0");
 }
 
 }  // namespace duo
