@@ -1,5 +1,6 @@
 """The loads into LDS that the compiler does not see (dma.h), in what it makes of the
-kernels that use them: m0 belongs to those blocks alone."""
+kernels that use them: m0 belongs to those blocks alone, and no load takes its scalar
+address from a register that a vector instruction may just have written."""
 
 import concurrent.futures
 import os
@@ -58,4 +59,9 @@ def test_blocks(listings, name):
             if code.startswith("global_load_lds"):
                 loads += 1
                 assert re.fullmatch(r"s_mov_b32 m0, \w+", block[0]), block
+                address = code.split(",")[1].split()[0]
+                if address == "off":
+                    assert block[1] == "s_nop 0", block
+                else:
+                    assert block[1].startswith(f"s_mov_b64 {address},"), block
     assert loads > 50
