@@ -262,7 +262,7 @@ duo_status rows_ok(const duo_kv_cache* c, const void* K, int64_t ldk, const void
   if (m == 0) return DUO_OK;
   if (!K || !V || !slots) return DUO_ERR_INVALID_ARG;
   if (ldk % 8 || ldv % 8 || !aligned16(K) || !aligned16(V)) return DUO_ERR_UNSUPPORTED;
-  if (m > (int64_t)1 << 30) return DUO_ERR_UNSUPPORTED;
+  if (m >= (int64_t)1 << 30) return DUO_ERR_UNSUPPORTED;  // fewer than 2^32 work items (kv_grid)
   return DUO_OK;
 }
 
@@ -314,14 +314,16 @@ duo_status duo_rope_at(const void* X, int64_t m, int64_t heads, int64_t head_dim
   if (m == 0) return DUO_OK;
   if (!X || !Y || !pos || (X == Y && ldx != ldy)) return DUO_ERR_INVALID_ARG;
   if (m > INT32_MAX) return DUO_ERR_UNSUPPORTED;
-  if (duo_status d = device_ok(); d != DUO_OK) return d;
   const int half = (int)head_dim / 2;
   const double step = -2.0 / (double)head_dim * std::log2(theta);
   const bool vec = half % 8 == 0 && ldx % 8 == 0 && ldy % 8 == 0 && aligned16(X) && aligned16(Y);
   const int64_t items = heads * (half / (vec ? 8 : 1));  // of one token
-  const int per = (int)std::max<int64_t>(1, 256 / items);
+  // an access per thread, and more where a launch would pass 2^32 work items
+  const int per = (int)std::max<int64_t>({1, 256 / items, cdiv(m, kMaxGrid)});
   const dim3 grid((unsigned)cdiv(m, per));
   const size_t lds = (size_t)per * half * sizeof(float2);
+  if (lds > 65536) return DUO_ERR_UNSUPPORTED;  // more rows than memory holds
+  if (duo_status d = device_ok(); d != DUO_OK) return d;
   if (vec)
     hipLaunchKernelGGL(rope_at_kernel<8>, grid, dim3(256), lds, (hipStream_t)stream, (const uint16_t*)X, ldx, m,
                        (int)heads, half, pos, step, (uint16_t*)Y, ldy, per);

@@ -25,6 +25,7 @@ constexpr int kTokBlk = 32;       // tokens per packed operand row (one MFMA K s
 constexpr int kMaxK = 32768;      // per-token selection keeps a token in registers
 constexpr int kMaxBlock = 128;    // sweep block width limit
 constexpr size_t kAlign = 256;
+constexpr int64_t kMaxGrid = UINT32_MAX / 256;  // workgroups of 256 in an axis: a launch has fewer than 2^32 work items there
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f4;

@@ -581,7 +581,7 @@ duo_status duo_attention_packed(const void* Q, int64_t ldq, const void* K, int64
   int64_t e = 1;
   while (e < 8 && kv_heads % (2 * e) == 0) e *= 2;
   const int64_t wgs = 8 * (kv_heads / e) * cdiv(blocks, 8 / e);
-  if (wgs > INT32_MAX) return DUO_ERR_UNSUPPORTED;
+  if (wgs > kMaxGrid) return DUO_ERR_UNSUPPORTED;
   if (duo_status d = device_ok(); d != DUO_OK) return d;
   PackedArgs a;
   a.Q = (const uint16_t*)Q, a.K = (const uint16_t*)K, a.V = (const uint16_t*)V, a.O = (uint16_t*)O;
