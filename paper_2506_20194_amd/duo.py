@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import operator
 import os
 
 import torch
@@ -781,9 +782,12 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
 class KVCache:
     """A paged key-value cache over `data`, a contiguous uint8 tensor (pages,
     kv_heads, bytes of a head's block; see include/duo.h for what a block
-    holds).  fmt: "bf16", "int8" or "int4".  KVCache.empty allocates one."""
+    holds).  fmt: "bf16", "int8" or "int4".  KVCache.empty allocates one.  What it is
+    of cannot be changed: a larger pool, say, is another KVCache."""
 
-    __slots__ = ("data", "page_size", "kv_heads", "head_dim", "fmt", "c", "ref")
+    __slots__ = ("_data", "_page_size", "_kv_heads", "_head_dim", "_fmt", "c", "ref")
+    # read only, as the calls go by c, the description that was made of them
+    data, page_size, kv_heads, head_dim, fmt = (property(operator.attrgetter(n)) for n in __slots__[:5])
 
     def __init__(self, data, page_size, kv_heads, head_dim, fmt="bf16"):
         if fmt not in KV_FORMATS:
@@ -796,7 +800,7 @@ class KVCache:
             raise ValueError(f"duo: data has shape {tuple(data.shape)}, expected (pages, {kv_heads}, {nbytes // kv_heads})")
         if not data.is_contiguous():
             raise ValueError("duo: data must be contiguous")
-        self.data, self.page_size, self.kv_heads, self.head_dim, self.fmt = data, page_size, kv_heads, head_dim, fmt
+        self._data, self._page_size, self._kv_heads, self._head_dim, self._fmt = data, page_size, kv_heads, head_dim, fmt
         self.c = KvCache(data.data_ptr(), pages, page_size, kv_heads, head_dim, KV_FORMATS[fmt])
         self.ref = ctypes.byref(self.c)
 
