@@ -747,7 +747,7 @@ def _on(index, name, *ts):
 
 
 def _rows(t, m, w, name):
-    """Row stride of an m x w bf16 matrix."""
+    """Row stride of an m x w bf16 matrix (w for a single row, which has none to speak of)."""
     if t.dtype != torch.bfloat16:
         raise TypeError(f"duo: {name} must be bfloat16")
     if t.shape != (m, w):
@@ -755,7 +755,7 @@ def _rows(t, m, w, name):
     ld, one = t.stride()
     if one != 1 and w > 1:
         raise ValueError(f"duo: {name} must have unit column stride")
-    return max(ld, w) if m <= 1 else ld
+    return w if m <= 1 else ld
 
 
 def _ints(t, dtype, n, name):
