@@ -14,14 +14,16 @@ __device__ __forceinline__ uint32_t lds_addr(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
 
-// m0 says where in LDS the loads go, and is named as changed.  The compiler warns that it may not keep
-// what it has in m0 itself across such a block: nothing else in the kernels that use this file may
-// need m0 (tests/test_dma_listing_cpu.py looks at what was compiled).
+// m0 says where in LDS the loads go, and is named as changed.  The compiler warns (400 times, silenced
+// here) that it may not keep what it has in m0 itself across such a block: nothing else in the kernels
+// that use this file may need m0, and tests/test_dma_listing_cpu.py looks at what was compiled.
 //
 // A scalar address is moved here, by a scalar instruction: a load needs five wait states behind a
 // vector instruction that wrote its address (a lane read, such as brings back a spilled register),
 // and the compiler inserts none for loads that it does not see.  The move is also the one
 // wait state that a load needs behind a write of m0.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 #define DUO_DMA_TO "s_mov_b32 m0, %1\n\ts_mov_b64 %0, %2\n\t"
 
 // 16 or 4 bytes per lane from base + off; base and lds are the same for all lanes.
@@ -63,5 +65,6 @@ __device__ __forceinline__ void dma16(const void* at, uint32_t lds) {
 __device__ __forceinline__ void dma4(const void* at, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(at) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 }  // namespace duo
