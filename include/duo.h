@@ -494,7 +494,8 @@ duo_status duo_silu_mul(const void* G, const void* U, int64_t m, int64_t n, int6
  * other, a paged key-value cache in 16, 8 or 4 bits, and attention with grouped
  * heads over both.  As in the harness above activations are bf16, token-major,
  * arithmetic fp32, everything stream ordered and argument errors found before
- * anything is enqueued.  Numbers that these calls read on the device (positions,
+ * anything is enqueued; what would take a launch of 2^32 work items or more in an axis
+ * is DUO_ERR_UNSUPPORTED.  Numbers that these calls read on the device (positions,
  * slots, pages, lengths, offsets) cannot be checked on the host: one that points
  * outside what the call was given is skipped as each call says, and no access
  * outside is made.
@@ -567,7 +568,8 @@ duo_status duo_kv_read(const duo_kv_cache* cache, const int64_t* slots, int64_t 
  *   does not see have no influence on it, whatever they hold.  Scores, maxima,
  *   sums and O are fp32, in one pass over the keys; the probabilities are rounded
  *   to bf16 before the product with V, relative to a running reference that the
- *   scores exceed by a factor of 2^8 at most.
+ *   scores exceed by a factor of 2^8 at most (sums are fp32: values times keys have
+ *   to stay below 2^119).
  *   Q total_q x heads*head_dim (ldq), K and V total_k x kv_heads*head_dim (ldk,
  *   ldv), O total_q x heads*head_dim (ldo, not overlapping the inputs), bf16.
  *   Offsets are taken as within [0, total] (larger ones as total, a sequence whose
@@ -595,7 +597,8 @@ duo_status duo_attention_packed(const void* Q, int64_t ldq, const void* K, int64
  *   no influence.  O: nseq x heads*head_dim bf16 (ldo, not overlapping Q).
  *   Scores are exact products of bf16 queries and cached codes summed in fp32,
  *   times the group's scale; probabilities, in 8 and 4 bits times the scale of V,
- *   are rounded to bf16 before the product with V.  Long sequences are split over
+ *   are rounded to bf16 before the product with V (sums are fp32: values times tokens
+ *   have to stay below 2^127, in 8 bits 2^126, in 4 bits 2^123).  Long sequences are split over
  *   their length and joined; where is a matter of nseq, max_len, heads and the
  *   lengths alone, so results are deterministic.  ldt * page_size >= max_len.
  *   Workspace: duo_attention_paged_workspace_size with the same sizes (it never

@@ -86,7 +86,8 @@ __global__ __launch_bounds__(256) void rope_at_kernel(const uint16_t* X, int64_t
 // a CU has some 80 vector instructions per 8 channels in the time of their bytes, which is
 // why the codes are made without a division and both formats' bias rides on an addition.
 // Eight heads of 128: 131072 tokens of 4 bits read in 137 us (5.0 TB/s; a token per thread
-// with heads in the grid's first axis, 231); 16411 tokens written and read back in 8 bits in 45.
+// with heads in the grid's first axis, 231) and written in 140 (4.9), of 8 bits in 162 and 165 (5.1,
+// 5.0), of 16 bits 210 both ways (5.1); 16411 tokens written and read back in 8 bits in 45.
 constexpr int kTok = 4;
 
 // Where the row of slot `slot` begins in the cache, and its scales (which: 0 K, 1 V).
