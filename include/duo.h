@@ -510,6 +510,16 @@ duo_status duo_silu_mul(const void* G, const void* U, int64_t m, int64_t n, int6
 duo_status duo_rope_at(const void* X, int64_t m, int64_t heads, int64_t head_dim, int64_t ldx, const int32_t* pos,
                        double theta, void* Y, int64_t ldy, void* stream);
 
+/* duo_head_norm_rope - duo_rope_at with a norm of every head before the rotation: a
+ *   head x becomes x / sqrt(mean(x^2) + eps) * gain (mean over its head_dim numbers)
+ *   and is then rotated; fp32, one rounding.  gain: head_dim numbers of gain_dtype
+ *   (DUO_BF16 or DUO_F32) for all heads, or NULL for ones (gain_dtype is not looked
+ *   at then).  eps >= 0; squares have to stay below fp32's range (|x| < 2^60).
+ *   The rest as duo_rope_at. */
+duo_status duo_head_norm_rope(const void* X, int64_t m, int64_t heads, int64_t head_dim, int64_t ldx, const int32_t* pos,
+                              const void* gain, int32_t gain_dtype, double eps, double theta, void* Y, int64_t ldy,
+                              void* stream);
+
 /*
  * The cache.  Pages of page_size tokens (16, 32, 64, 128 or 256); in a page each
  * K/V head has one block of bytes, at data + (page * kv_heads + head) * block:
@@ -556,6 +566,22 @@ duo_status duo_kv_write(const duo_kv_cache* cache, const void* K, int64_t ldk, c
  *   duo_kv_write. */
 duo_status duo_kv_read(const duo_kv_cache* cache, const int64_t* slots, int64_t m, void* K, int64_t ldk, void* V,
                        int64_t ldv, void* stream);
+
+/* duo_kv_append - the new tokens of a step on their way into the cache, in one
+ *   launch: row t of K is rotated by the angles of position pos[t] (m int32) and
+ *   written into slot slots[t] with row t of V, and rows of Q (heads heads of the
+ *   cache's head_dim; heads = 0 for none) are rotated into Y (which may equal Q).
+ *   With eps >= 0 the heads of K and Q are normed first, times k_gain and q_gain
+ *   (as duo_head_norm_rope, both of gain_dtype; NULL for ones); eps < 0: no norms
+ *   (and no gains).  What is stored is, bit for bit, what duo_rope_at or
+ *   duo_head_norm_rope followed by duo_kv_write store: 8- and 4-bit codes are
+ *   those of the key rounded to bf16.  Slots, alignment and strides as
+ *   duo_kv_write (a skipped slot's query is rotated all the same); ldq and ldy are
+ *   multiples of 8, Q and Y 16-byte aligned. */
+duo_status duo_kv_append(const duo_kv_cache* cache, const void* K, int64_t ldk, const void* V, int64_t ldv,
+                         const int64_t* slots, const int32_t* pos, int64_t m, double theta, double eps, const void* k_gain,
+                         const void* Q, int64_t ldq, int64_t heads, const void* q_gain, int32_t gain_dtype, void* Y,
+                         int64_t ldy, void* stream);
 
 /* duo_attention_packed - causal attention of nseq sequences of different lengths,
  *   packed one behind the other, with grouped heads: query head h reads K/V head

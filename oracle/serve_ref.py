@@ -37,6 +37,13 @@ def rope_at(x, heads, head_dim, pos, theta):
     return np.stack((x[:, :, 0] * c - x[:, :, 1] * s, x[:, :, 1] * c + x[:, :, 0] * s), 2).reshape(len(x), -1)
 
 
+def head_norm(x, heads, head_dim, gain=None, eps=1e-5):
+    """Every head of the rows x divided by its root mean square, times gain."""
+    h = np.asarray(x, dtype=np.float64).reshape(-1, heads, head_dim)
+    h = h / np.sqrt((h * h).mean(-1, keepdims=True) + eps)
+    return (h if gain is None else h * np.asarray(gain, dtype=np.float64)).reshape(len(x), -1)
+
+
 def quantize(x, fmt):
     """(codes, scales) of rows x (m, kv, hd): integer codes without what is added
     to them, and float64 scales (m, kv, hd / 32)."""

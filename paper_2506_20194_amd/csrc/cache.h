@@ -64,4 +64,71 @@ duo_status kv_by_format(const duo_kv_cache* c, const F& f) {
   return with(std::integral_constant<int, DUO_KV_I4>{});
 }
 
+// Where the row of slot `slot` begins in the cache, and its scales (which: 0 K, 1 V).
+template <int FMT, int HD>
+struct KvRow {
+  uint8_t *codes, *scales;
+  __device__ KvRow(const KvGeo& g, int64_t slot, int h, int which) {
+    const uint32_t page = (uint32_t)(slot >> g.shift), row = (uint32_t)slot & ((1u << g.shift) - 1);
+    uint8_t* const blk = g.data + h * g.block + (uint64_t)page * (uint32_t)(g.heads * g.block);
+    codes = blk + kv_rows_at<FMT, HD>(which, g.shift) + row * KvFmt<FMT>::row(HD);
+    scales = blk + kv_scales_at<FMT, HD>(which, g.shift) + row * KvFmt<FMT>::scales(HD);
+  }
+};
+
+// A group of 32 channels of one token and head has one scale,
+//   s = bf16(max |x| / q),  code = rint(x / s),  q = 127 (8 bits) or 7 (4 bits).
+// x and s have eight significant bits, so a quotient that is no half integer is at
+// least 2^-16 (relative) away from one, and x / s in fp32 rounds to the code of the
+// exact quotient, ties included where the division is exact at them.  kv_encode
+// forms x (1/s) and corrects it once by its remainder, which is exact at ties.
+//
+// The codes of a group of 32 channels, eight per thread and four threads in a row, with what
+// is added to them (8 bits: in bytes of q.x, q.y; 4 bits: in q.x), and the scale.
+template <int FMT>
+__device__ __forceinline__ uint2 kv_encode(const u32x4& x, uint16_t* scale) {
+  typedef unsigned short u16v2 __attribute__((ext_vector_type(2)));
+  u16v2 most2 = {0, 0};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    u16v2 v;
+    const uint32_t a = x[j] & 0x7fff7fffu;
+    __builtin_memcpy(&v, &a, 4);
+    most2 = __builtin_elementwise_max(most2, v);
+  }
+  uint32_t mag = most2[0] > most2[1] ? most2[0] : most2[1];
+  mag = max(mag, (uint32_t)__shfl_xor((int)mag, 1));
+  mag = max(mag, (uint32_t)__shfl_xor((int)mag, 2));
+  constexpr int most = KvFmt<FMT>::most, bias = KvFmt<FMT>::bias;
+  // max |x| / q is never within 2^-17 of halfway between two bf16 numbers, so the product
+  // rounds as the quotient does
+  const uint16_t sb = f32_to_bf16_bits(bf16_bits_to_f32((uint16_t)mag) * (1.0f / most));
+  const float s = bf16_bits_to_f32(sb);
+  const bool some = mag < 0x7f80u && s >= 1.1754943508222875e-38f;
+  *scale = some ? sb : mag < 0x7f80u ? 0 : 0x7fc0u;
+  const float inv = some ? __builtin_amdgcn_rcpf(s) : 0.f, div = some ? s : 0.f;
+  uint32_t code[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float v = some ? __uint_as_float(j & 1 ? x[j >> 1] & 0xffff0000u : x[j >> 1] << 16) : 0.f;
+    const float q = v * inv;
+    // + 1.5 2^23: the nearest whole number, ties to even, in the low bits; it lies within
+    // the codes, as s is at most 2^-8 too small
+    code[j] = __float_as_uint(fmaf(fmaf(-q, div, v), inv, q) + (12582912.0f + bias));
+  }
+  uint2 q = {0, 0};
+  if constexpr (FMT == DUO_KV_I8) {
+    auto bytes = [&](int j) {
+      return __builtin_amdgcn_perm(__builtin_amdgcn_perm(code[j + 3], code[j + 2], 0x0c0c0400u),
+                                   __builtin_amdgcn_perm(code[j + 1], code[j], 0x0c0c0400u), 0x05040100u);
+    };
+    q.x = bytes(0);
+    q.y = bytes(4);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q.x |= (code[j] & 15u) << (4 * j);
+  }
+  return q;
+}
+
 }  // namespace duo

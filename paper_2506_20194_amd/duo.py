@@ -33,7 +33,7 @@ EXPORTED = (
     "duo_act_sparsify", "duo_linear", "duo_rope", "duo_attention", "duo_silu_mul", "duo_act_order",
     "duo_permute", "duo_permute_mask", "duo_dsc_workspace_size", "duo_dsc_layout", "duo_dsc_pack",
     "duo_dsc_gemv", "duo_dsc_gemv_noalloc", "duo_hessian_status", "duo_rope_at", "duo_kv_page_bytes", "duo_kv_write",
-    "duo_kv_read", "duo_attention_packed", "duo_attention_packed_workspace_size", "duo_attention_paged_workspace_size", "duo_attention_paged",
+    "duo_kv_read", "duo_head_norm_rope", "duo_kv_append", "duo_attention_packed", "duo_attention_packed_workspace_size", "duo_attention_paged_workspace_size", "duo_attention_paged",
 )
 PROF = dict(gram=0, hessian=1, chol=2, score=3, sweep=4, inblock=5, trail=6, select=7, decode=8)
 DUO_BOP_ACT_SPARSIFY, DUO_BOP_LINEAR, DUO_BOP_ATTENTION = 0, 1, 2
@@ -145,6 +145,10 @@ def lib():
         L.duo_kv_page_bytes.argtypes = [I32, I32, I32, I32]
         L.duo_kv_write.restype = I32
         L.duo_kv_write.argtypes = [KV, P, I64, P, I64, P, I64, P]
+        L.duo_head_norm_rope.restype = I32
+        L.duo_head_norm_rope.argtypes = [P, I64, I64, I64, I64, P, P, I32, F64, F64, P, I64, P]
+        L.duo_kv_append.restype = I32
+        L.duo_kv_append.argtypes = [P, P, I64, P, I64, P, P, I64, F64, F64, P, P, I64, I64, P, I32, P, I64, P]
         L.duo_kv_read.restype = I32
         L.duo_kv_read.argtypes = [KV, P, I64, P, I64, P, I64, P]
         L.duo_attention_packed.restype = I32
@@ -746,6 +750,15 @@ def _on(index, name, *ts):
             raise ValueError(f"duo: {name}: all tensors must be on one CUDA (HIP) device")
 
 
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _current(index, name):
+    """Device `index` is the current one, where a launch goes to."""
+    if index != _device():
+        raise ValueError(f"duo: {name}: the tensors' device must be the current one")
+
+
 def _rows(t, m, w, name):
     """Row stride of an m x w bf16 matrix (w for a single row, which has none to speak of)."""
     if t.dtype != torch.bfloat16:
@@ -863,6 +876,70 @@ def duo_kv_read(cache, slots, out=None):
     if st:
         raise DuoError(st, "duo_kv_read")
     return K, V
+
+
+def _gain(t, n, name):
+    """Pointer and dtype code of a head's gains (None: ones)."""
+    if t is None:
+        return None, DUO_BF16
+    code = _dtype(t)
+    if t.shape != (n,):
+        raise ValueError(f"duo: {name} has shape {tuple(t.shape)}, expected {(n,)}")
+    if not t.is_contiguous():
+        raise ValueError(f"duo: {name} must be contiguous")
+    return t.data_ptr(), code
+
+
+def duo_head_norm_rope(X, heads, head_dim, pos, gain=None, eps=1e-5, theta=1e4, out=None):
+    """duo_rope_at with every head divided by its root mean square before, times gain
+    (head_dim numbers, bf16 or fp32; None: ones); out may be X."""
+    m, w = X.shape[0], heads * head_dim
+    Y = _empty(m, w, X) if out is None else out
+    dev = X.get_device()
+    _on(dev, "duo_head_norm_rope", pos, gain, Y)
+    _current(dev, "duo_head_norm_rope")
+    gp, code = _gain(gain, head_dim, "gain")
+    st = lib().duo_head_norm_rope(X.data_ptr(), m, heads, head_dim, _rows(X, m, w, "X"), _ints(pos, torch.int32, m, "pos"), gp,
+                                  code, eps, theta, Y.data_ptr(), _rows(Y, m, w, "out"), _raw_stream(dev))
+    if st:
+        raise DuoError(st, "duo_head_norm_rope")
+    return Y
+
+
+def duo_kv_append(cache, K, V, slots, pos, theta=1e4, eps=None, k_gain=None, Q=None, q_gain=None, out=None):
+    """Rows of K (m x kv_heads*head_dim bf16) rotated by the positions pos (m int32) and
+    written into their slots (m int64) with the rows of V; eps: their heads (and
+    those of Q) normed before, with the gains k_gain and q_gain (both bf16 or both fp32;
+    None: ones).  Q: rows of queries that are rotated beside them and returned (out:
+    where to, may be Q)."""
+    m, hd = K.shape[0], cache.head_dim
+    w, wq = cache.kv_heads * hd, 0 if Q is None else Q.shape[1]
+    if wq % hd:
+        raise ValueError(f"duo: Q's width {wq} is no multiple of the cache's head_dim {hd}")
+    if Q is None and (out is not None or q_gain is not None):
+        raise ValueError("duo: out and q_gain belong to Q, which is not given")
+    if eps is None and (k_gain is not None or q_gain is not None):
+        raise ValueError("duo: gains belong to a norm, whose eps is not given")
+    if eps is not None and eps < 0:
+        raise ValueError("duo: eps must not be negative")
+    Y = _empty(m, wq, Q) if out is None and Q is not None else out
+    dev = K.get_device()
+    _on(dev, "duo_kv_append", V, slots, pos, cache.data, k_gain, q_gain, Q, Y)
+    _current(dev, "duo_kv_append")
+    kg, code = _gain(k_gain, hd, "k_gain")
+    qg, code_q = _gain(q_gain, hd, "q_gain")
+    if kg is None:
+        code = code_q
+    elif qg is not None and code != code_q:
+        raise TypeError("duo: k_gain and q_gain must have one dtype")
+    st = lib().duo_kv_append(
+        cache.ref, K.data_ptr(), _rows(K, m, w, "K"), V.data_ptr(), _rows(V, m, w, "V"), _ints(slots, torch.int64, m, "slots"),
+        _ints(pos, torch.int32, m, "pos"), m, theta, -1.0 if eps is None else eps, kg, None if Q is None else Q.data_ptr(),
+        0 if Q is None else _rows(Q, m, wq, "Q"), wq // hd, qg, code, None if Q is None else Y.data_ptr(),
+        0 if Q is None else _rows(Y, m, wq, "out"), _raw_stream(dev))
+    if st:
+        raise DuoError(st, "duo_kv_append")
+    return Y
 
 
 @functools.lru_cache(maxsize=256)
