@@ -635,6 +635,32 @@ duo_status duo_attention_paged(const void* Q, int64_t ldq, const duo_kv_cache* c
                                const int32_t* lens, int64_t nseq, int64_t max_len, int64_t heads, double scale, void* O,
                                int64_t ldo, void* ws, size_t ws_bytes, void* stream);
 
+/* duo_attention_chunk - attention of new tokens of nseq sequences (chunks of prompts,
+ *   drafts, single tokens, in any mix) over the pages, where their own keys and values
+ *   already are (duo_kv_append, duo_kv_write).  Sequence s has the rows cu_q[s] ..
+ *   cu_q[s+1] - 1 of Q and O (nseq + 1 int32) and lens[s] tokens in the cache, the
+ *   new ones among them and last: query i of n is at position p = lens[s] - n + i
+ *   and sees the tokens j <= p; with a window > 0 of those the ones with
+ *   j > p - window or j < sinks (window 0: none, and sinks do not matter).
+ *   Scores, probabilities, pages and lengths as duo_attention_paged; a query that
+ *   sees no token (p < 0) gets 0, one that sees a token in a page outside the
+ *   cache NaN.  What a query does not see has no influence on it, whatever it holds,
+ *   and entries of table for pages that no query of a sequence sees (behind its
+ *   window) are not used.  Offsets as duo_attention_packed: rows of O in no sequence
+ *   are left alone.  max_q: a bound of the new tokens of a sequence, if the caller
+ *   knows one (else total_q); how the work is cut goes by it, results are right with
+ *   any.  Everything is split by the sizes and the lengths alone: results are
+ *   deterministic.  Q 16-byte aligned, ldq % 8 == 0 (else DUO_ERR_UNSUPPORTED); O must
+ *   not overlap Q.  total_q * heads, nseq and max_len at most 2^30.
+ *   Workspace: duo_attention_chunk_workspace_size with the same sizes (it never falls
+ *   with a larger total_q, nseq or max_len). */
+size_t duo_attention_chunk_workspace_size(int64_t total_q, int64_t nseq, int64_t heads, int64_t kv_heads, int64_t head_dim,
+                                          int64_t max_len);
+duo_status duo_attention_chunk(const void* Q, int64_t ldq, int64_t total_q, const duo_kv_cache* cache, const int32_t* table,
+                               int64_t ldt, const int32_t* lens, const int32_t* cu_q, int64_t nseq, int64_t max_q,
+                               int64_t max_len, int64_t heads, int64_t window, int64_t sinks, double scale, void* O,
+                               int64_t ldo, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -103,24 +103,66 @@ struct PagedWork {
 };
 
 // A row that begins in a share and ends in another one: the join's task.  parts = 0: none.
+// For chunks seq is the sequence's first row of Q, and cols the columns of this row.
 struct Task {
-  int seq, row, parts, pad;
+  int seq, row, parts, cols;
+};
+
+// What new tokens add to a call (CHUNK below).  A column is then a pair of one of a sequence's
+// new tokens and a query head of the K/V head's group, the heads of a token side by side, and
+// a row up to kCols (with PAIR 8) of them; all rows of a sequence have the tiles that any of its
+// new tokens sees: those of the sinks, then from the window of the first of them on.
+template <bool CHUNK>
+struct ChunkArgs {};
+template <>
+struct ChunkArgs<true> {
+  const int32_t* cu_q;
+  int total_q;
+  int window, sinks;  // window: 0 for none
+  int64_t most;       // columns of the sequences that are done here, at most
+  uint32_t by_group;  // see by()
+  int by_shift;
+};
+// n / group for 0 <= n < 2^31: by_group = ceil(2^(31+s) / group) with 2^(s-1) < group <= 2^s
+__device__ inline int by(int n, const ChunkArgs<true>& a) { return (int)(__umulhi(2u * (uint32_t)n, a.by_group) >> a.by_shift); }
+
+// One sequence: its tokens, its new ones (1, the only query, without CHUNK) and their first row
+// in Q, its tiles: the first `sinks`, then those from `from` on.
+struct Seq {
+  int len, lq, q0, tiles, sinks, from;
 };
 
 __device__ inline int seq_len(const PagedWork& w, int s) { return min(max(w.lens[s], 0), w.max_len); }
+__device__ inline int within(int v, int most) { return min(max(v, 0), most); }
 
 // Tiles, and what counts for one row of them.
 template <int KEYS>
 __device__ inline int tiles_of(int len) { return (len + KEYS - 1) / KEYS; }
+
+// A sequence as it counts: len, lq and q0 as loaded.
+template <int KEYS>
+__device__ inline Seq seq_tiles(int len, int lq, int q0, const ChunkArgs<false>&) {
+  const int n = tiles_of<KEYS>(len);
+  return Seq{len, lq, q0, n, 0, 0};
+}
+template <int KEYS>
+__device__ inline Seq seq_tiles(int len, int lq, int q0, const ChunkArgs<true>& c) {
+  Seq s{len, lq, q0, 0, 0, 0};
+  const int first = c.window ? max(max(len - lq, 0) - c.window + 1, 0) : 0;  // of the first query's window
+  s.sinks = tiles_of<KEYS>(min(c.sinks, first));
+  s.from = max(first / KEYS, s.sinks);
+  s.tiles = lq == 0 || len == 0 ? 0 : s.sinks + tiles_of<KEYS>(len) - s.from;
+  return s;
+}
 
 // The rows of a sequence of `tiles` tiles: `units` of `cost` each.  A unit is a row, or four
 // rows, one for each wave, where they are short and many.
 struct Units {
   int tiles, cost, units;
   bool quad;
-  __device__ Units(int tiles, const PagedWork& w) : tiles(tiles) {
+  __device__ Units(int tiles, int rows, const PagedWork& w) : tiles(tiles) {
     quad = w.many && tiles <= kShort;
-    units = tiles == 0 ? 0 : quad ? (w.rows + 3) / 4 : w.rows;
+    units = tiles == 0 ? 0 : quad ? (rows + 3) / 4 : rows;
     cost = (quad ? 4 * tiles : tiles) + kRowCost;
   }
 };
@@ -149,19 +191,35 @@ __device__ inline int64_t lane64(int64_t v, int l) {
                    (uint32_t)__builtin_amdgcn_readlane((int)v, l));
 }
 
+// Sequence s as loaded, and the rows that it has.
+__device__ inline void load_seq(const PagedWork& w, const ChunkArgs<false>&, int s, Seq* q) {
+  q->len = seq_len(w, s), q->lq = 1, q->q0 = s;
+}
+__device__ inline void load_seq(const PagedWork& w, const ChunkArgs<true>& c, int s, Seq* q) {
+  const int a = within(c.cu_q[s], c.total_q), b = within(c.cu_q[s + 1], c.total_q);
+  q->len = seq_len(w, s), q->lq = max(b - a, 0), q->q0 = a;
+}
+template <int COLS>
+__device__ inline int rows_of(const PagedWork& w, const ChunkArgs<false>&, int, int, int) { return w.rows; }
+template <int COLS>
+__device__ inline int rows_of(const PagedWork&, const ChunkArgs<true>& c, int lq, int group, int kv_heads) {
+  const int64_t n = (int64_t)lq * group;
+  return n > c.most ? 0 : (int)((n + COLS - 1) / COLS) * kv_heads;
+}
+
 // Cost of the sequences up to the end of this lane's bucket of `per`.  Every wave counts for
-// itself: no barrier, and no wave waits for another.  *len: this lane's sequence, where a
+// itself: no barrier, and no wave waits for another.  *q: this lane's sequence, where a
 // bucket is one.
-template <int KEYS>
-__device__ inline int64_t count_rows(const PagedWork& w, int* len) {
+template <int KEYS, int COLS, class C>
+__device__ inline int64_t count_rows(const PagedWork& w, const C& c, int group, int kv_heads, Seq* q) {
   const int lane = threadIdx.x & 63;
   int64_t n = 0;
-  *len = 0;
 #pragma unroll 4
   for (int i = 0; i < w.per; ++i) {
     const int64_t s = (int64_t)lane * w.per + i;
-    *len = s < w.nseq ? seq_len(w, (int)s) : 0;
-    const Units x(tiles_of<KEYS>(*len), w);
+    *q = Seq{};
+    if (s < w.nseq) load_seq(w, c, (int)s, q);
+    const Units x(seq_tiles<KEYS>(q->len, q->lq, q->q0, c).tiles, rows_of<COLS>(w, c, q->lq, group, kv_heads), w);
     n += (int64_t)x.cost * x.units;
   }
   // running sum over the lanes: within rows of 16, then over the rows
@@ -236,11 +294,18 @@ __device__ __forceinline__ int v_at(int r, int c) {
 // (scales, maximum, exponential, rounding), the larger part of the vector work, is done
 // for two keys at once; the halves of a column's pair meet at the join.  64 sequences of 8192
 // tokens, 64 heads on 8: 214 us without and 206 with in 8 bits, 133 and 121 in 4.
-template <int FMT, int HD, bool PAIR>
+//
+// CHUNK: new tokens of each sequence instead of one query (see ChunkArgs).  A tile that some
+// column does not see whole has its scores masked; a page outside the cache makes the scores of
+// its keys NaN, so that those who see them become NaN and nobody else.  Probabilities of keys that
+// are not seen are 0, and what V holds there must not meet them if it is not finite: in 8 and 4 bits
+// their weights are set to 0 after the scale, in 16 bits such numbers enter as zeros and are added
+// for those columns that see them.
+template <int FMT, int HD, bool PAIR, bool CHUNK>
 __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
     const uint16_t* __restrict__ Q, int64_t ldq, KvGeo kv, const int32_t* __restrict__ table, int64_t ldt, PagedWork work,
     int group, int cols, float cexp, uint32_t flip, uint16_t* __restrict__ O, int64_t ldo, Task* __restrict__ tasks,
-    float* __restrict__ part, int vec) {
+    float* __restrict__ part, int vec, ChunkArgs<CHUNK> ch) {
   using G = PagedGeo<FMT, HD>;
   constexpr int KEYS = G::KEYS, NB = G::NB, CK = G::CK, RB = G::RB, CH = G::CH, RPL = G::RPL, NL = G::NL, NS = G::NS;
   constexpr int NK = NL + NS;  // loads per operand and tile
@@ -254,19 +319,43 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
   const int l16 = lane & 15, g = lane >> 4;
   const int col = PAIR ? l16 & 7 : l16, half = PAIR ? l16 >> 3 : 0;  // this lane's head, and half of the keys
 
-  int my_len;
-  const int64_t upto = count_rows<KEYS>(work, &my_len);
+  constexpr int COLS = PAIR ? 8 : kCols;  // of a row (CHUNK)
+  Seq mine;
+  const int64_t upto = count_rows<KEYS, COLS>(work, ch, group, kv.heads, &mine);
   const Shares shares(lane64(upto, 63), gridDim.x);
   int64_t u = shares.begin(blockIdx.x);
   const int64_t u1 = (int)blockIdx.x < shares.n ? shares.begin(blockIdx.x + 1) : u;
   if (tid == 0 && tasks) tasks[blockIdx.x].parts = 0;
   auto len_of = [&](int s) {
-    return work.per == 1 ? __builtin_amdgcn_readlane(my_len, s) : __builtin_amdgcn_readfirstlane(seq_len(work, s));
+    return work.per == 1 ? __builtin_amdgcn_readlane(mine.len, s) : __builtin_amdgcn_readfirstlane(seq_len(work, s));
+  };
+  auto seq_of = [&](int s) {
+    Seq q{};
+    if constexpr (CHUNK) {
+      if (work.per == 1) {
+        q.len = __builtin_amdgcn_readlane(mine.len, s), q.lq = __builtin_amdgcn_readlane(mine.lq, s);
+        q.q0 = __builtin_amdgcn_readlane(mine.q0, s);
+      } else {
+        load_seq(work, ch, s, &q);
+        q.len = __builtin_amdgcn_readfirstlane(q.len), q.lq = __builtin_amdgcn_readfirstlane(q.lq);
+        q.q0 = __builtin_amdgcn_readfirstlane(q.q0);
+      }
+    } else {
+      q.len = len_of(s), q.lq = 1, q.q0 = s;
+    }
+    return seq_tiles<KEYS>(q.len, q.lq, q.q0, ch);
   };
   // sequences without tokens
   for (int s = blockIdx.x; s < work.nseq; s += gridDim.x)
-    if (len_of(s) == 0)
-      for (int e = tid; e < group * kv.heads * HD; e += 256) O[(int64_t)s * ldo + e] = 0;
+    if (len_of(s) == 0) {
+      if constexpr (CHUNK) {
+        const Seq q = seq_of(s);
+        for (int i = 0; i < q.lq; ++i)
+          for (int e = tid; e < group * kv.heads * HD; e += 256) O[(int64_t)(q.q0 + i) * ldo + e] = 0;
+      } else {
+        for (int e = tid; e < group * kv.heads * HD; e += 256) O[(int64_t)s * ldo + e] = 0;
+      }
+    }
   if (u >= u1) return;
   // the bucket that u lies in: the first whose end lies behind it
   const int at_bucket = __ffsll((unsigned long long)__ballot(upto > u)) - 1;
@@ -276,8 +365,9 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
   uint8_t* const sS = sV + G::ROWS;  // scales: [parity of the tile's turn][K, V]
 
   for (int s = at_bucket * work.per; u < u1; ++s) {
-    const int len = len_of(s);
-    const Units x(tiles_of<KEYS>(len), work);
+    const Seq seq = seq_of(s);
+    const int len = seq.len, seq_rows = rows_of<COLS>(work, ch, seq.lq, group, kv.heads);
+    const Units x(seq.tiles, seq_rows, work);
     const int tiles = x.tiles, cost = x.cost;
     const int64_t start = before;
     before += (int64_t)cost * x.units;
@@ -296,43 +386,80 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
       if (x.quad) {  // whole in the share that it begins in
         if (at > 0) continue;
         row = 4 * row + wave;
-        if (row >= work.rows) continue;
+        if (row >= seq_rows) continue;
         t = t0 = 0;
         t1 = tiles;
         step = 1;
       }
       if (t0 >= t1) continue;
-      const int h = row % kv.heads, c0 = row / kv.heads * kCols;  // K/V head, first of its query heads
-      const int nc = min(cols, group - c0);
-      const uint16_t* const q = Q + (int64_t)s * ldq + (h * group + c0) * HD;
+      const int h = row % kv.heads, c0 = row / kv.heads * COLS;  // K/V head, first of its query heads (columns)
+      const int nc = CHUNK ? min(COLS, seq.lq * group - c0) : min(cols, group - c0);
+      // where column c's numbers begin in rows of Q or O, and its position (CHUNK)
+      auto column = [&](int c, int64_t ld) {
+        if constexpr (CHUNK) {
+          const int i = by(c0 + c, ch);
+          return (int64_t)(seq.q0 + i) * ld + (h * group + c0 + c - i * group) * HD;
+        } else {
+          return (int64_t)s * ld + (h * group + c0 + c) * HD;
+        }
+      };
+      auto position = [&](int c) {
+        if constexpr (CHUNK)
+          return len - seq.lq + by(c0 + c, ch);
+        else
+          return len - 1;
+      };
+      const int my_pos = position(min(col, nc - 1)), pos_lo = position(0), pos_hi = position(nc - 1);
+      int my_from = 0;  // this column's window begins here
+      if constexpr (CHUNK) my_from = ch.window ? my_pos - ch.window + 1 : 0;
+      auto place_of = [&](int t) { return CHUNK && t >= seq.sinks ? t - seq.sinks + seq.from : t; };  // tile t of the row
       const uint8_t* const block0 = kv.data + h * kv.block;
       const uint32_t page_bytes = (uint32_t)(kv.heads * kv.block);
 
       // 64 pages of the table in one register, the next 64 in another
       bool bad = false;
-      int win = (t * KEYS >> kv.shift) & ~3;  // a tile's pages, four at most, lie in one window
+      uint64_t lost = 0, lost_next = 0;  // CHUNK: which pages of the two registers are outside the cache
+      uint32_t tile_lost = 0;            // of the tile issued last: which of its runs of 16 keys
+      int win = (place_of(t) * KEYS >> kv.shift) & ~3;  // a tile's pages, four at most, lie in one window
       auto ids = [&](int p) {
         int id = pages[min(p + lane, last_page)];
         const bool out = id < 0 || id >= kv.pages;
-        bad |= out;
+        if constexpr (CHUNK)
+          lost_next = __ballot(out);
+        else
+          bad |= out;
         return out ? 0 : id;
       };
-      int pid = ids(win), nid = ids(win + 64);
+      int pid = ids(win);
+      lost = lost_next;
+      int nid = ids(win + 64);
       u32x4 qf[CK];
 #pragma unroll
-      for (int c = 0; c < CK; ++c) qf[c] = *(const u32x4*)(q + min(col, nc - 1) * HD + 32 * c + 8 * g);
+      for (int c = 0; c < CK; ++c) qf[c] = *(const u32x4*)(Q + column(min(col, nc - 1), ldq) + 32 * c + 8 * g);
 #pragma unroll
       for (int c = 0; c < CK; ++c) asm volatile("" : "+v"(qf[c]));  // waited for here, and not behind the tiles
       // this wave's loads of tile t's K (which = 0) or V rows and scales; K first
       auto issue = [&](int t, auto which_c, const uint8_t* to_rows, const uint8_t* to_scales) __attribute__((always_inline)) {
         constexpr int which = decltype(which_c)::value;
-        const int k0 = t * KEYS;
+        const int k0 = place_of(t) * KEYS;
         const uint32_t rows = __builtin_amdgcn_readfirstlane(lds_addr(to_rows));
         const uint32_t scales = __builtin_amdgcn_readfirstlane(lds_addr(to_scales));
         if (which == 0 && k0 >> kv.shift >= win + 64) {  // four tiles never reach further than the next window
+          if (CHUNK && k0 >> kv.shift >= win + 128) {  // but the first after the sinks may
+            win = (k0 >> kv.shift & ~3) - 64;
+            nid = ids(win + 64);
+          }
           pid = nid;
+          lost = lost_next;
           win += 64;
           nid = ids(win + 64);
+        }
+        if constexpr (CHUNK && which == 0) {
+          tile_lost = 0;
+          if (lost)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+              if (k0 + 16 * b < len) tile_lost |= (uint32_t)(lost >> (((k0 + 16 * b) >> kv.shift) - win) & 1) << b;
         }
         const int rows_at = kv_rows_at<FMT, HD>(which, kv.shift), scales_at = kv_scales_at<FMT, HD>(which, kv.shift);
         const int mask = (1 << kv.shift) - 1;
@@ -442,6 +569,13 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
       }
       for (uint8_t* sc = sS; t < t1; t += step) {
         const bool more = t + step < t1;
+        const int k0 = place_of(t) * KEYS;
+        // does every column see every key?
+        bool whole_tile = true;
+        const uint32_t lost_here = tile_lost;
+        if constexpr (CHUNK)
+          whole_tile = k0 + KEYS - 1 <= pos_lo && !lost_here &&
+                       (!ch.window || k0 > pos_hi - ch.window || k0 + KEYS <= ch.sinks);
         uint8_t* const sn = sc == sS ? sS + 2 * NS * 256 : sS;  // the next tile's scales
         wait_vm<NK>();  // K of this tile
         asm volatile("" ::: "memory");
@@ -502,11 +636,29 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
           }
         }
         // ---- probabilities relative to the running maximum
-        const int left = len - t * KEYS - 32 * half - 4 * g;  // tokens of the row from this lane's first key on
+        const int left = len - k0 - 32 * half - 4 * g;  // tokens of the row from this lane's first key on
+        uint32_t seen = 0xffffu;  // CHUNK: which of the lane's keys, four bits for each b, this column sees
+        if constexpr (CHUNK) {
+          if (!whole_tile) {
+            seen = 0;
+            const int key0 = k0 + 32 * half + 4 * g;
 #pragma unroll
-        for (int b = 0; b < XB; ++b)
+            for (int b = 0; b < XB; ++b)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) x[b][r] = 16 * b + r < left ? x[b][r] : -INFINITY;
+              for (int r = 0; r < 4; ++r) {
+                const int key = key0 + 16 * b + r;
+                const bool see = key <= my_pos && (key >= my_from || key < ch.sinks);
+                seen |= (see ? 1u : 0u) << (4 * b + r);
+                const float v = lost_here >> (b + 2 * half) & 1 ? NAN : x[b][r];
+                x[b][r] = see ? v : -INFINITY;
+              }
+          }
+        } else {
+#pragma unroll
+          for (int b = 0; b < XB; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[b][r] = 16 * b + r < left ? x[b][r] : -INFINITY;
+        }
         float mt = x[0][0];
 #pragma unroll
         for (int b = 0; b < XB; ++b)
@@ -554,8 +706,45 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
             __builtin_memcpy((char*)&vf[d] + 8, &b, 8);
           }
           wait_lds<0>();
+          if constexpr (CHUNK) {
+            if (!whole_tile) {
+              // infinities and NaN in keys that some column may not see
+              uint32_t most = 0;
+#pragma unroll
+              for (int d = 0; d < 2 * CK; ++d)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  const uint32_t w = vf[d][j] & 0x7fff7fffu;
+                  most = max(most, max(w & 0xffffu, w >> 16));
+                }
+              if (__any(most >= 0x7f80u)) {
+#pragma unroll
+                for (int d = 0; d < 2 * CK; ++d)
+#pragma unroll
+                  for (int j = 0; j < 4; ++j) {
+                    const uint32_t w = vf[d][j];
+                    vf[d][j] = w & ~(((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u));
+                  }
+#pragma unroll
+                for (int d = 0; d < 2 * CK; ++d) asm volatile("s_nop 7" : "+v"(o[d]));
+#pragma unroll 1
+                for (int key = 0; key < KEYS; ++key) {
+                  const int k = k0 + key;
+                  const bool see = k <= my_pos && (k >= my_from || k < ch.sinks);
+#pragma unroll
+                  for (int d = 0; d < 2 * CK; ++d) {
+                    const uint2 v = *(const uint2*)(sV + key * RB + 16 * v_at<FMT, CH>(key, 2 * d + (g >> 1)) + 8 * (g & 1));
+                    const float w[4] = {lo16(v.x), hi16(v.x), lo16(v.y), hi16(v.y)};
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[d][r] += see && !(fabsf(w[r]) < INFINITY) ? w[r] : 0.f;
+                  }
+                }
+                wait_lds<0>();
+              }
+            }
+          }
           if (more) issue(t + step, kV, sV, sn + NS * 256);
-          if (t * KEYS + KEYS > len) {
+          if (!CHUNK && k0 + KEYS > len) {
             // copies of the last token behind the row's end: their probability is 0, and 0 times
             // an infinite value would be NaN (codes are finite, and a scale that is not is NaN)
             int rest = left;
@@ -596,7 +785,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
           const uint32_t nb = pack_bf16(-BIAS, -BIAS);
           const u32x4 bias = {nb, nb, nb, nb};
           // probabilities times scales of the 32 keys of blocks 2 st and 2 st + 1, by groups of channels
-          auto weigh = [&](int st, u32x4 (&pf)[CK]) __attribute__((always_inline)) {
+          auto weigh = [&](int st, u32x4 (&pf)[CK], bool whole) __attribute__((always_inline)) {
             uint32_t vs[2][2 * CK];
 #pragma unroll
             for (int b = 0; b < 2; ++b)
@@ -612,6 +801,8 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
                 const int r = e & 3;
                 const uint32_t w = vs[e >> 2][(r * CK + c) / 2];
                 p[e] = x[(PAIR ? 0 : 2 * st) + (e >> 2)][r] * ((r * CK + c) & 1 ? hi16(w) : lo16(w));
+                if constexpr (CHUNK)
+                  if (!whole) p[e] = seen >> (4 * ((PAIR ? 0 : 2 * st) + (e >> 2)) + r) & 1 ? p[e] : 0.f;
               }
 #pragma unroll
               for (int j = 0; j < 4; ++j)
@@ -619,10 +810,16 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
             }
           };
           u32x4 pf[CK];
-          if constexpr (PAIR) weigh(0, pf);
+          auto weights = [&](int st) __attribute__((always_inline)) {
+            if (!CHUNK || whole_tile)
+              weigh(st, pf, true);
+            else
+              weigh(st, pf, false);
+          };
+          if constexpr (PAIR) weights(0);
 #pragma unroll
           for (int st = 0; st < 2; ++st) {
-            if constexpr (!PAIR) weigh(st, pf);
+            if constexpr (!PAIR) weights(st);
 #pragma unroll
             for (int c = 0; c < CK; ++c) {
               u32x4 ph = pf[c];
@@ -645,6 +842,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
       for (int d = 0; d < 2 * CK; ++d) asm volatile("s_nop 7" : "+v"(o[d]));  // the last products have been written
       if (__any(bad)) l = NAN;
       l = col_sum(l);
+      if (CHUNK && my_pos < 0) mc = 0.f, l = 1.f;  // sees nothing: zeros over something
       if (x.quad) {
         // alone: the halves of the keys joined in registers, and written
         if constexpr (PAIR) {
@@ -662,7 +860,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
             }
         }
         if (half == 0 && col < nc) {
-          uint16_t* const y = O + (int64_t)s * ldo + (h * group + c0 + col) * HD + 4 * g;
+          uint16_t* const y = O + column(col, ldo) + 4 * g;
 #pragma unroll
           for (int d = 0; d < 2 * CK; ++d) {
             const uint32_t y0 = pack_bf16(o[d][0] / l, o[d][1] / l), y1 = pack_bf16(o[d][2] / l, o[d][3] / l);
@@ -700,7 +898,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
       const bool whole = t0 == 0 && t1 == tiles;
       float* const ps = part + (2 * (int64_t)blockIdx.x + (t0 == 0)) * cols * (HD + 2);
       if (!whole && t0 == 0 && tid == 0) {
-        tasks[blockIdx.x] = Task{s, row, shares.of(row_end - 1) - (int)blockIdx.x + 1, 0};
+        tasks[blockIdx.x] = Task{CHUNK ? seq.q0 : s, row, shares.of(row_end - 1) - (int)blockIdx.x + 1, nc};
       }
       for (int e = tid; e < nc * (HD / 2); e += 256) {
         const int c = e / (HD / 2), d = e % (HD / 2) * 2;
@@ -716,7 +914,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
           v1 += y[1];
         }
         if (whole) {
-          uint16_t* const y = O + (int64_t)s * ldo + (h * group + c0 + c) * HD + d;
+          uint16_t* const y = O + column(c, ldo) + d;
           const uint32_t two = pack_bf16(v0 / sum, v1 / sum);
           if (vec)
             *(uint32_t*)y = two;
@@ -736,10 +934,10 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
 // Joins the parts of the rows that lie in several shares: one workgroup for two heads of
 // the row that begins in share blockIdx.x, if any does and ends in another: its own part
 // (the second of its two places), then the first places of the shares after it.
-template <int HD>
+template <int HD, bool CHUNK>
 __global__ __launch_bounds__(256) void paged_join_kernel(const Task* __restrict__ tasks, const float* __restrict__ part,
                                                          int kv_heads, int group, int cols, uint16_t* __restrict__ O,
-                                                         int64_t ldo, int vec) {
+                                                         int64_t ldo, int vec, ChunkArgs<CHUNK> ch) {
   constexpr int T = HD / 4, NP = 128 / T;  // threads per part and head, parts at once
   __shared__ float wt[2][kMaxWg], ls[2][kMaxWg];
   __shared__ float red[2][2][2];
@@ -747,8 +945,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const Task* __restrict_
   const Task task = tasks[blockIdx.x];
   if (task.parts == 0) return;
   const int tid = threadIdx.x & 127, j = threadIdx.x >> 7;  // j: which of the two heads
-  const int row = task.row, np = task.parts, h = row % kv_heads, c0 = row / kv_heads * kCols;
-  const int c = blockIdx.y * 2 + j, live = c < min(cols, group - c0);
+  const int row = task.row, np = task.parts, h = row % kv_heads, c0 = row / kv_heads * (CHUNK ? cols : kCols);
+  const int c = blockIdx.y * 2 + j, live = c < (CHUNK ? task.cols : min(cols, group - c0));
   const int64_t stride = (int64_t)cols * (HD + 2);
   const float* const p0 = part + 2 * (int64_t)blockIdx.x * stride + (live ? c : 0) * (HD + 2);
   auto at = [&](int i) { return p0 + (i ? 2 * i : 1) * stride; };
@@ -800,7 +998,13 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const Task* __restrict_
 #pragma unroll
     for (int i = 0; i < NP; ++i) y0 += acc[j][i][2 * tid], y1 += acc[j][i][2 * tid + 1];
     const uint32_t two = pack_bf16(y0 / sum, y1 / sum);
-    uint16_t* const y = O + (int64_t)task.seq * ldo + (h * group + c0 + c) * HD + 2 * tid;
+    int64_t at_row = task.seq, in_row = h * group + c0 + c;
+    if constexpr (CHUNK) {
+      const int i = by(c0 + c, ch);
+      at_row += i;
+      in_row -= i * group;
+    }
+    uint16_t* const y = O + at_row * ldo + in_row * HD + 2 * tid;
     if (vec)
       *(uint32_t*)y = two;
     else
@@ -859,14 +1063,86 @@ duo_status duo_attention_paged(const void* Q, int64_t ldq, const duo_kv_cache* c
     Task* const tasks = (Task*)ws;
     float* const part = (float*)((uint8_t*)ws + align_up(wgs * sizeof(Task)));
     constexpr bool Q8 = FMT != DUO_KV_BF16;
-    const auto kern = Q8 && cols <= 8 ? paged_kernel<FMT, HD, Q8> : paged_kernel<FMT, HD, false>;
+    const auto kern = Q8 && cols <= 8 ? paged_kernel<FMT, HD, Q8, false> : paged_kernel<FMT, HD, false, false>;
     if (duo_status st = set_max_lds((const void*)kern, 4 * P::WAVE); st != DUO_OK) return st;
     hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(256), 4 * P::WAVE, s, (const uint16_t*)Q, ldq, g, table, ldt, w,
-                       (int)group, (int)cols, cexp, flip, (uint16_t*)O, ldo, max_len > 0 ? tasks : nullptr, part, vec);
+                       (int)group, (int)cols, cexp, flip, (uint16_t*)O, ldo, max_len > 0 ? tasks : nullptr, part, vec,
+                       ChunkArgs<false>{});
     DUO_LAUNCH_CHECK();
     if (max_len > P::KEYS && wgs > 1) {  // a row of one tile is never split
-      hipLaunchKernelGGL(paged_join_kernel<HD>, dim3((unsigned)wgs, (unsigned)cdiv(cols, 2)), dim3(256), 0, s,
-                         (const Task*)tasks, (const float*)part, g.heads, (int)group, (int)cols, (uint16_t*)O, ldo, vec);
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(paged_join_kernel<HD, false>), dim3((unsigned)wgs, (unsigned)cdiv(cols, 2)), dim3(256),
+                         0, s, (const Task*)tasks, (const float*)part, g.heads, (int)group, (int)cols, (uint16_t*)O, ldo, vec,
+                         ChunkArgs<false>{});
+      DUO_LAUNCH_CHECK();
+    }
+    return DUO_OK;
+  });
+}
+
+size_t duo_attention_chunk_workspace_size(int64_t total_q, int64_t nseq, int64_t heads, int64_t kv_heads, int64_t head_dim,
+                                          int64_t max_len) {
+  if (total_q < 1 || nseq < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads || max_len < 1 ||
+      (head_dim != 64 && head_dim != 128))
+    return 0;
+  const double rows = (double)kv_heads * ((double)total_q * (double)(heads / kv_heads) / 8 + (double)nseq);
+  const int64_t wgs = paged_wgs(rows, cdiv(max_len, kMinKeys), kMaxWg);
+  return align_up(wgs * sizeof(Task)) + align_up((size_t)(2 * wgs * kCols * (head_dim + 2)) * sizeof(float));
+}
+
+duo_status duo_attention_chunk(const void* Q, int64_t ldq, int64_t total_q, const duo_kv_cache* cache, const int32_t* table,
+                               int64_t ldt, const int32_t* lens, const int32_t* cu_q, int64_t nseq, int64_t max_q,
+                               int64_t max_len, int64_t heads, int64_t window, int64_t sinks, double scale, void* O,
+                               int64_t ldo, void* ws, size_t ws_bytes, void* stream) {
+  KvGeo g;
+  if (duo_status e = kv_geo(cache, &g); e != DUO_OK) return e;
+  const int hd = cache->head_dim;
+  if (total_q < 0 || nseq < 0 || max_q < 0 || max_len < 0 || window < 0 || sinks < 0 || heads < 1 || heads > 65535 ||
+      heads % g.heads || !std::isfinite(scale) || ldq < heads * hd || ldo < heads * hd || ldt < 0 ||
+      ldt < cdiv(max_len, cache->page_size))
+    return DUO_ERR_INVALID_ARG;
+  const int64_t group = heads / g.heads;
+  if (nseq > (int64_t)1 << 30 || max_len > (int64_t)1 << 30 || total_q > ((int64_t)1 << 30) / heads) return DUO_ERR_UNSUPPORTED;
+  // rows times tiles within what shares are counted in
+  if ((double)g.heads * ((double)total_q * (double)group / 8 + (double)nseq) * ((double)max_len / kMinKeys + 1 + kRowCost) > 1e12)
+    return DUO_ERR_UNSUPPORTED;
+  if (nseq == 0 || total_q == 0) return DUO_OK;
+  if (!Q || !O || !lens || !cu_q || (max_len > 0 && !table)) return DUO_ERR_INVALID_ARG;
+  if (ldq % 8 || !aligned16(Q)) return DUO_ERR_UNSUPPORTED;
+  const size_t need = duo_attention_chunk_workspace_size(total_q, nseq, heads, g.heads, hd, max_len);
+  if (need && (!ws || ws_bytes < need || reinterpret_cast<uintptr_t>(ws) % kAlign)) return DUO_ERR_WORKSPACE;
+  if (duo_status d = device_ok(); d != DUO_OK) return d;
+  const hipStream_t s = (hipStream_t)stream;
+  const float cexp = std::max((float)(std::fabs(scale) * 1.4426950408889634), 1.4e-45f);
+  const uint32_t flip = scale < 0.0 ? 0x80008000u : 0u;
+  const int vec = ldo % 2 == 0 && reinterpret_cast<uintptr_t>(O) % 4 == 0;
+  ChunkArgs<true> ch;
+  ch.cu_q = cu_q, ch.total_q = (int)total_q;
+  ch.window = window <= max_len ? (int)window : 0;  // a longer one hides nothing
+  ch.sinks = (int)std::min(sinks, max_len);
+  ch.most = INT64_MAX;
+  ch.by_shift = 0;
+  while ((int64_t)1 << ch.by_shift < group) ++ch.by_shift;
+  ch.by_group = (uint32_t)((((uint64_t)1 << (31 + ch.by_shift)) + group - 1) / group);
+  return kv_by_format(cache, [&](auto fmt, auto dim) -> duo_status {
+    constexpr int FMT = decltype(fmt)::value, HD = decltype(dim)::value;
+    using P = PagedGeo<FMT, HD>;
+    constexpr bool Q8 = FMT != DUO_KV_BF16;
+    const bool pair = Q8 && std::min(max_q, total_q) * group <= 8;
+    const int cols = pair ? 8 : kCols;
+    const double rows = (double)g.heads * ((double)total_q * (double)group / cols + (double)nseq);
+    const int64_t wgs = paged_wgs(rows, cdiv(max_len, P::KEYS), 256 * P::WGS);
+    const PagedWork w = {lens, (int)nseq, (int)max_len, 0, (int)cdiv(nseq, 64),
+                         g.heads * (total_q * group / cols) >= 2 * 256 * P::WGS};
+    Task* const tasks = (Task*)ws;
+    float* const part = (float*)((uint8_t*)ws + align_up(wgs * sizeof(Task)));
+    const auto kern = pair ? paged_kernel<FMT, HD, Q8, true> : paged_kernel<FMT, HD, false, true>;
+    if (duo_status st = set_max_lds((const void*)kern, 4 * P::WAVE); st != DUO_OK) return st;
+    hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(256), 4 * P::WAVE, s, (const uint16_t*)Q, ldq, g, table, ldt, w,
+                       (int)group, cols, cexp, flip, (uint16_t*)O, ldo, max_len > 0 ? tasks : nullptr, part, vec, ch);
+    DUO_LAUNCH_CHECK();
+    if (max_len > P::KEYS && wgs > 1) {  // a row of one tile is never split
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(paged_join_kernel<HD, true>), dim3((unsigned)wgs, (unsigned)cols / 2), dim3(256), 0, s,
+                         (const Task*)tasks, (const float*)part, g.heads, (int)group, cols, (uint16_t*)O, ldo, vec, ch);
       DUO_LAUNCH_CHECK();
     }
     return DUO_OK;

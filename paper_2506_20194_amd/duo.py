@@ -34,6 +34,7 @@ EXPORTED = (
     "duo_permute", "duo_permute_mask", "duo_dsc_workspace_size", "duo_dsc_layout", "duo_dsc_pack",
     "duo_dsc_gemv", "duo_dsc_gemv_noalloc", "duo_hessian_status", "duo_rope_at", "duo_kv_page_bytes", "duo_kv_write",
     "duo_kv_read", "duo_head_norm_rope", "duo_kv_append", "duo_attention_packed", "duo_attention_packed_workspace_size", "duo_attention_paged_workspace_size", "duo_attention_paged",
+    "duo_attention_chunk_workspace_size", "duo_attention_chunk",
 )
 PROF = dict(gram=0, hessian=1, chol=2, score=3, sweep=4, inblock=5, trail=6, select=7, decode=8)
 DUO_BOP_ACT_SPARSIFY, DUO_BOP_LINEAR, DUO_BOP_ATTENTION = 0, 1, 2
@@ -160,6 +161,10 @@ def lib():
         L.duo_attention_paged_workspace_size.argtypes = [I64, I64, I64, I64, I64]
         L.duo_attention_paged.restype = I32
         L.duo_attention_paged.argtypes = [P, I64, KV, P, I64, P, I64, I64, I64, F64, P, I64, P, SZ, P]
+        L.duo_attention_chunk_workspace_size.restype = SZ
+        L.duo_attention_chunk_workspace_size.argtypes = [I64] * 6
+        L.duo_attention_chunk.restype = I32
+        L.duo_attention_chunk.argtypes = [P, I64, I64, P, P, I64, P, P, I64, I64, I64, I64, I64, I64, F64, P, I64, P, SZ, P]
         L.duo_profile_enable.restype = I32
         L.duo_profile_enable.argtypes = [I32]
         L.duo_profile_read.restype = I32
@@ -1010,4 +1015,52 @@ def duo_attention_paged(Q, cache, table, lens, heads, max_len=None, scale=None, 
         ws.numel(), _raw_stream(dev))
     if st:
         raise DuoError(st, "duo_attention_paged")
+    return O
+
+
+@functools.lru_cache(maxsize=256)
+def _chunk_bytes(total_q, nseq, heads, kv_heads, head_dim, max_len):
+    return max(lib().duo_attention_chunk_workspace_size(total_q, nseq, heads, kv_heads, head_dim, max_len), 256)
+
+
+def attention_chunk_workspace(total_q, nseq, heads, kv_heads, head_dim, max_len, device):
+    return torch.empty(_chunk_bytes(total_q, nseq, heads, kv_heads, head_dim, max_len), dtype=torch.uint8, device=device)
+
+
+def duo_attention_chunk(Q, cache, table, lens, cu_q, heads, window=None, sinks=0, max_q=None, max_len=None, scale=None,
+                        out=None, ws=None):
+    """Attention of the new tokens of a batch of sequences over the paged cache, which
+    holds their keys and values already: rows cu_q[s] .. cu_q[s+1] - 1 of Q (total_q x
+    heads*head_dim; nseq + 1 int32) are the last of the lens[s] tokens whose pages are
+    row s of table (both int32).  A query at position p sees the tokens up to p; with a
+    window those after p - window and the first `sinks` ones.  max_q, max_len: bounds
+    of a sequence's new and of all its tokens known to the caller.  Rows of the
+    result that lie in no sequence are not written."""
+    n, tq, hd = cu_q.shape[0] - 1, Q.shape[0], cache.head_dim
+    w = heads * hd
+    O = _empty(tq, w, Q) if out is None else out
+    if table.dtype != torch.int32:
+        raise TypeError("duo: table must be torch.int32")
+    if table.dim() != 2 or table.shape[0] != n:
+        raise ValueError(f"duo: table has shape {tuple(table.shape)}, expected {n} rows")
+    if window is not None and window < 1:
+        raise ValueError("duo: a window holds the token itself at least (None: no window)")
+    most = table.shape[1] * cache.page_size
+    if max_len is None:
+        max_len = most
+    elif max_len > most:
+        raise ValueError("duo: table holds fewer than max_len tokens")
+    if ws is None:
+        ws = attention_chunk_workspace(tq, n, heads, cache.kv_heads, hd, max_len, Q.device)
+    dev = Q.get_device()
+    _on(dev, "duo_attention_chunk", table, lens, cu_q, O, ws, cache.data)
+    _current(dev, "duo_attention_chunk")
+    ldt = _ld(table) if n > 1 or table.stride(1) != 1 else table.shape[1]
+    st = lib().duo_attention_chunk(
+        Q.data_ptr(), _rows(Q, tq, w, "Q"), tq, cache.ref, table.data_ptr(), ldt, _ints(lens, torch.int32, n, "lens"),
+        _ints(cu_q, torch.int32, n + 1, "cu_q"), n, tq if max_q is None else max_q, max_len, heads, window or 0, sinks,
+        hd ** -0.5 if scale is None else scale, O.data_ptr(), _rows(O, tq, w, "out"), ws.data_ptr(), ws.numel(),
+        _raw_stream(dev))
+    if st:
+        raise DuoError(st, "duo_attention_chunk")
     return O
