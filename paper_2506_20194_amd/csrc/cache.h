@@ -131,4 +131,20 @@ __device__ __forceinline__ uint2 kv_encode(const u32x4& x, uint16_t* scale) {
   return q;
 }
 
+// Attention of chunks (duo_attention_chunk), checked: the part of it that sequences with more
+// than `least` rows (new tokens times heads of a group) take, and its workspace.
+struct ChunkCall {
+  const void* Q;
+  void* O;
+  int64_t ldq, ldo, total_q, nseq, max_len, heads, ldt;
+  const duo_kv_cache* cache;
+  KvGeo geo;
+  const int32_t *table, *lens, *cu_q;
+  int window, sinks;
+  float cexp;
+  uint32_t flip;
+};
+size_t chunk_rows_ws_bytes(int64_t total_q, int64_t nseq, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t max_len);
+duo_status chunk_rows_run(const ChunkCall& c, int64_t least, void* ws, hipStream_t s);
+
 }  // namespace duo

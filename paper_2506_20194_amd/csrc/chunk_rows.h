@@ -1,0 +1,817 @@
+// Attention of new tokens over the paged cache where a sequence has many rows: the kernel of
+// chunks (duo_attention_chunk), by whose side the paged kernel does the sequences of few rows.
+// Included by the one file that compiles it, behind dma.h, pingpong.h and mfma.h.
+//
+// A block is up to 128 rows of one sequence and K/V head, a row being a new token and one of the
+// heads that read this K/V head, the heads of a token side by side; wave w owns the rows 32 w
+// .. 32 w + 31.  As in the packed kernel everything is computed transposed on 32-wide MFMA tiles
+// (S^T = K Q^T, O^T = V^T P^T with P^T's fragments the lane's own probabilities and V^T's from
+// transposing LDS reads), in steps of 32 keys, with a running reference that moves only when
+// a score exceeds it by a factor of 2^8, and probabilities rounded to bf16 for the product with V.
+//
+// Tiles are 64 keys of the pages: a wave brings 16 of them, which lie in one page whatever its
+// size.  A block's tiles are those of the sinks, then those from its first query's window on.  Keys
+// behind the end are copies of the last one.  In 16 bits rows go global -> LDS directly.  In 8 and 4
+// bits the codes do, to a place of the wave's own, and a turn later the wave turns them into
+// bf16 numbers, rounded as duo_kv_read rounds them, in the tile that all waves read: once for
+// 128 rows, where the paged kernel, which multiplies the codes themselves, pays for scales in every
+// product.  (Rounding K and V adds about 0.0015 of the output's root mean square to an error of 0.0018.)
+//
+// Blocks cost what they have of keys, and something for their start and end; the count of all
+// blocks is cut into equal shares, one per workgroup, neighbours on one XCD.  A share's end that lies
+// near a block's end is moved there; a block in several shares is joined by a second launch.  All of
+// that follows from the lengths, on the device: no atomics, equal results every time.
+#pragma once
+
+#include "cache.h"
+
+namespace duo {
+
+using namespace pp;
+
+constexpr int kRowsQB = 128;     // rows of a block
+constexpr int kRowsWg = 512;     // workgroups at most: two on each CU
+constexpr int kRowsCost = 256;   // what a block's start and end cost, in keys
+constexpr int kRowsMin = 256;    // smallest share, in keys
+constexpr int kRowsSnap = 512;   // a share's end moves to a block's end that is no further than this
+
+struct RowsArgs {
+  const uint16_t* Q;
+  uint16_t* O;
+  int64_t ldq, ldo;
+  KvGeo kv;
+  const int32_t* table;
+  int64_t ldt;
+  const int32_t *lens, *cu_q;
+  int total_q, nseq, max_len, group;
+  int hg, nsub, qpb;  // heads of a block and such parts of a group, queries of a block
+  uint32_t by_hg;     // see by()
+  int by_shift;
+  int window, sinks;
+  int per;        // sequences per bucket of the count
+  int64_t least;  // sequences with no more rows than this are not done here
+  float cexp;     // exp(s scale) = 2^(s cexp), with the queries' signs turned for a negative scale
+  uint32_t flip;
+  int vec;        // 16-byte stores of O
+  struct RowsTask* tasks;
+  float *po, *pml;  // two places per share: outputs (rows x head_dim, not normalised), references and sums
+};
+
+// A block that begins in a share and ends in another one.
+struct RowsTask {
+  int parts, q0, head0, heads, rows, pos0;
+};
+
+// n / hg for 0 <= n < 2^31: by_hg = ceil(2^(31+s) / hg) with 2^(s-1) < hg <= 2^s
+__device__ inline int by(int n, const RowsArgs& a) { return (int)(__umulhi(2u * (uint32_t)n, a.by_hg) >> a.by_shift); }
+
+__device__ inline uint64_t rows_div(uint64_t a, uint64_t b) { return (a | b) >> 32 ? a / b : (uint32_t)a / (uint32_t)b; }
+
+// A sequence as the count sees it: block n costs min(first + (n + 1) qpb, most) keys, and kRowsCost.
+struct RowsSeq {
+  int q0, lq, len, nb;
+  int first, most, linear;  // tokens before the first new one; most keys of a block; blocks below it
+
+  __device__ RowsSeq(const RowsArgs& a, int s) {
+    const bool in = s < a.nseq;
+    const int x = in ? min(max(a.cu_q[s], 0), a.total_q) : 0, y = in ? min(max(a.cu_q[s + 1], 0), a.total_q) : 0;
+    q0 = x, lq = max(y - x, 0), len = in ? min(max(a.lens[s], 0), a.max_len) : 0;
+    nb = (int64_t)lq * a.group > a.least ? (lq + a.qpb - 1) / a.qpb : 0;
+    first = max(len - lq, 0);
+    most = a.window ? (int)min((int64_t)a.window + a.sinks + a.qpb + 192, (int64_t)INT32_MAX - 4096) : INT32_MAX;
+    linear = most < first ? 0 : min((most - first) / a.qpb, nb);
+  }
+  __device__ int cost(int n, const RowsArgs& a) const {
+    return (n < linear ? first + (n + 1) * a.qpb : most) + kRowsCost;
+  }
+  __device__ int64_t upto(int n, const RowsArgs& a) const {  // of the first n blocks
+    const int64_t m = min(n, linear);
+    return m * (first + kRowsCost) + m * (m + 1) / 2 * a.qpb + (int64_t)(n - m) * ((int64_t)most + kRowsCost);
+  }
+};
+
+__device__ inline int64_t lane_of(int64_t v, int l) {
+  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), l) << 32 |
+                   (uint32_t)__builtin_amdgcn_readlane((int)v, l));
+}
+
+// The same in all lanes, and known to be.
+__device__ inline int same(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ inline int64_t same(int64_t v) {
+  return (int64_t)((uint64_t)(uint32_t)same((int)(v >> 32)) << 32 | (uint32_t)same((int)v));
+}
+
+// The same number, as one that the compiler knows nothing of: what follows from it is worked out here.
+__device__ __forceinline__ int anew(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// Where the count stands: a block, and how far into it.
+struct RowsAt {
+  int s, hs, qb;     // sequence, K/V head and part of its group, block of queries
+  int64_t at;        // into the block
+};
+
+template <int FMT, int HD>
+struct RowsGeo {
+  static constexpr bool QUANT = FMT != DUO_KV_BF16;
+  static constexpr int KB = 64, CH = HD / 8, TILE = KB * CH;  // keys of a tile, 16-byte chunks per row, of a tile
+  static constexpr int RB = KvFmt<FMT>::row(HD);
+  static constexpr int NL = QUANT ? 1 + (16 * RB > 1024) : 16 * RB / 1024;  // loads of 16 rows
+  static constexpr int STAGE = QUANT ? NL * 1024 : 0;                       // of a wave and operand
+  static constexpr int LDS = 4 * TILE * 16 + 8 * STAGE;
+};
+
+template <int FMT, int HD>
+__global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
+  using G = RowsGeo<FMT, HD>;
+  constexpr int KB = G::KB, CH = G::CH, TILE = G::TILE, RB = G::RB, NL = G::NL, QB = kRowsQB;
+  constexpr int KS = HD / 16, DB = HD / 32;  // MFMA steps over head_dim, 32-wide blocks of the output row
+  constexpr int RPL = 64 / CH;               // rows of bf16 per wave-wide access
+  extern __shared__ __attribute__((aligned(16))) uint8_t lsm[];
+  u32x4* const sm = (u32x4*)lsm;  // [buffer][K, V][tile]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int nhs = a.kv.heads * a.nsub;
+
+  // ---- the count, and this workgroup's share of it
+  RowsSeq mine(a, a.per == 1 ? lane : a.nseq);
+  int64_t upto = 0;
+  if (a.per == 1)
+    upto = mine.upto(mine.nb, a) * nhs;
+  else
+    for (int i = 0; i < a.per; ++i) {
+      const RowsSeq q(a, (int)min((int64_t)lane * a.per + i, (int64_t)a.nseq));
+      upto += q.upto(q.nb, a) * nhs;
+    }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t v = __shfl_up(upto, o);
+    upto += lane >= o ? v : 0;
+  }
+  const int64_t total = lane_of(upto, 63);
+  const int shares = (int)min((int64_t)gridDim.x, (total + kRowsMin - 1) / kRowsMin);
+  const int64_t size = same(shares ? (int64_t)rows_div(total, shares) : 0);
+  const int more = (int)(total - size * shares);
+  auto begin = [&](int i) { return i * size + min(i, more); };
+  auto share_of = [&](int64_t u) {
+    const int64_t cut = more * (size + 1);
+    return u < cut ? (int)rows_div(u, size + 1) : more + (int)rows_div(u - cut, size);
+  };
+  // workgroups (a multiple of eight) go round-robin over the XCDs, neighbouring shares to one
+  const int share = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
+  if (tid == 0) a.tasks[share].parts = 0;
+  if (share >= shares) return;
+  auto load_seq = [&](int s) {
+    RowsSeq q(a, s);
+    q.q0 = same(q.q0), q.lq = same(q.lq), q.len = same(q.len), q.nb = same(q.nb);
+    q.first = same(q.first), q.most = same(q.most), q.linear = same(q.linear);
+    return q;
+  };
+  auto seq_of = [&](int s) {
+    if (a.per > 1) return load_seq(s);
+    RowsSeq q = mine;
+    q.q0 = __builtin_amdgcn_readlane(mine.q0, s), q.lq = __builtin_amdgcn_readlane(mine.lq, s);
+    q.len = __builtin_amdgcn_readlane(mine.len, s), q.nb = __builtin_amdgcn_readlane(mine.nb, s);
+    q.first = __builtin_amdgcn_readlane(mine.first, s), q.most = __builtin_amdgcn_readlane(mine.most, s);
+    q.linear = __builtin_amdgcn_readlane(mine.linear, s);
+    return q;
+  };
+  auto locate = [&](int64_t u) {  // u < total
+    const int bucket = __ffsll((unsigned long long)__ballot(upto > u)) - 1;
+    if (bucket) u -= lane_of(upto, bucket - 1);
+    RowsAt p;
+    for (p.s = bucket * a.per;; ++p.s) {
+      const RowsSeq q = seq_of(p.s);
+      const int64_t each = q.upto(q.nb, a);
+      if (u >= each * nhs) {
+        u -= each * nhs;
+        continue;
+      }
+      p.hs = same((int)rows_div(u, each));
+      u = same(u - p.hs * each);
+      int lo = 0, hi = q.nb - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (same((int)(q.upto(mid, a) <= u)))
+          lo = mid;
+        else
+          hi = mid - 1;
+      }
+      p.qb = lo;
+      p.at = same(u - q.upto(lo, a));
+      return p;
+    }
+  };
+  auto near = [](int c) { return min(kRowsSnap, c / 2); };
+  auto snapped = [&](int64_t u) {
+    if (u >= total) return total;
+    const RowsAt p = locate(u);
+    const int c = seq_of(p.s).cost(p.qb, a);
+    return same(p.at <= near(c) ? u - p.at : c - p.at <= near(c) ? u - p.at + c : u);
+  };
+  int64_t u = snapped(same(begin(share)));
+  const int64_t u1 = snapped(same(begin(share + 1)));
+  if (u >= u1) return;
+  RowsAt p = locate(u);
+  RowsSeq q = seq_of(p.s);  // of the next block
+
+  while (u < u1) {
+    const int cost = q.cost(p.qb, a);
+    const int64_t block = u - p.at;  // where it begins
+    const int from_at = same((int)p.at), to_at = same((int)min((int64_t)cost, u1 - block));
+    const int kvh = same(p.hs / a.nsub), sub = same(p.hs - kvh * a.nsub);
+    const int heads = same(min(a.hg, a.group - sub * a.hg)), head0 = kvh * a.group + sub * a.hg;
+    const int qi0 = same(p.qb * a.qpb), rows = same(min(a.qpb, q.lq - qi0) * a.hg);
+    const int len = same(q.len), pos0 = same(len - q.lq + qi0);  // position of the block's first query
+    const int32_t* const pages = a.table + same((int64_t)p.s * a.ldt);
+    const int seq_q0 = same(q.q0);
+    // on to the next block
+    u = same(block + to_at);
+    p.at = 0;
+    if (to_at == cost && ++p.qb == q.nb) {
+      p.qb = 0;
+      if (++p.hs == nhs) {
+        p.hs = 0;
+        while (u < u1) {
+          q = load_seq(++p.s);
+          if (q.nb) break;
+        }
+      }
+    }
+    // the block's tiles: `sinks` first ones, then those from `from` on; here: [t0, t0 + n)
+    const int pos_end = same(pos0 + by(rows - 1, a));  // of its last query
+    const int first = same(a.window ? max(pos0 - a.window + 1, 0) : 0);
+    const int sinks = same((min(a.sinks, first) + KB - 1) / KB), from = same(max(first / KB, sinks));
+    const int tiles = same(pos_end < 0 ? 0 : sinks + (pos_end + KB) / KB - from);
+    auto tile_at = [&](int x) { return min(max((x - kRowsCost + KB - 1) / KB, 0), tiles); };
+    const int t0 = same(tile_at(from_at)), n = same(tile_at(to_at) - t0);
+    const bool whole = n == tiles;
+    if (n == 0 && !(tiles == 0 && from_at == 0)) continue;
+    auto place = [&](int t) { return t < sinks ? t : t - sinks + from; };  // t: of all the block's tiles
+    lds_barrier();  // every wave is done with the block before
+    // the lane's number anew for every block: what is worked out from it would be kept, for all parts of
+    // this loop at once, in more registers than there are
+    const int ln = anew(lane), half = ln >> 5;
+    // chunk c of key r sits at position kswz(r, c) (vswz) of its row in a tile
+    auto kswz = [](int key, int c) { return CH == 16 ? c ^ (key & 15) : c ^ ((key >> 1) & 7); };
+    auto vswz = [](int key, int c) { return CH == 16 ? c ^ (4 * (key & 3)) : c ^ (4 * ((key >> 1) & 1)); };
+    // transposing read of 16 keys x 32 channels: lane i of each 16 addresses key i / 4, 4 values at 4 (i % 4)
+    auto v_at = [&](int x, int d) {
+      const int tj = (x & 15) >> 2;
+      return (4 * (x >> 5) + tj) * HD * 2 + vswz(tj, 4 * d + 2 * ((x >> 4) & 1)) * 16 + (x & 3) * 8;
+    };
+    typedef __attribute__((address_space(3))) s16v4 lds4;
+    auto read_v = [&](const uint8_t* sV, int t, int d, int x) {
+      const int at = v_at(x, d);
+      const s16v4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(sV + at + (16 * t) * HD * 2));
+      const s16v4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(sV + at + (16 * t + 8) * HD * 2));
+      u32x4 v;
+      __builtin_memcpy(&v, &v0, 8);
+      __builtin_memcpy((char*)&v + 8, &v1, 8);
+      return v;
+    };
+    auto k_rows = [&](int u) { return sm + ((u >> 1 & 1) * 2) * TILE + (u & 1) * 32 * CH; };
+    auto v_rows = [&](int u) { return (const uint8_t*)(sm + ((u >> 1 & 1) * 2 + 1) * TILE) + (u & 1) * 32 * HD * 2; };
+    auto read_k = [&](const u32x4* sK, int c, int x) { return sK[(x & 31) * CH + kswz(x & 31, 2 * c + (x >> 5))]; };
+
+    // ---- pages
+    const int last_page = (len - 1) >> a.kv.shift, page_mask = (1 << a.kv.shift) - 1;
+    const uint8_t* const block0 = a.kv.data + kvh * a.kv.block;
+    const uint32_t page_bytes = (uint32_t)(a.kv.heads * a.kv.block);
+    int win = n ? (place(t0) * KB >> a.kv.shift) & ~3 : 0;
+    auto ids = [&](int pg) {
+      const int v = pages[min(pg + lane, last_page)];
+      return v < 0 || v >= a.kv.pages ? 0 : v;
+    };
+    int pid = 0, nid = 0;
+    bool lost = false;  // some query sees a token in a page outside the cache
+    if (n) {
+      pid = ids(win);
+      nid = ids(win + 64);
+      const int p1 = min(place(t0 + n - 1) * KB + KB - 1, pos_end) >> a.kv.shift;
+      for (int pg = place(t0) * KB >> a.kv.shift; pg <= p1;) {
+        int v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = pages[min(pg + 64 * j + lane, last_page)];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int i = pg + 64 * j + lane, k = i << a.kv.shift;
+          lost |= i <= p1 && (v[j] < 0 || v[j] >= a.kv.pages) && (k + page_mask >= first || k < a.sinks);
+        }
+        pg += 256;
+        if (pg << a.kv.shift >= a.sinks) pg = max(pg, first >> a.kv.shift);
+      }
+      lost = __any(lost);
+    }
+    // first of this wave's 16 keys of tile t, as far as there are any
+    auto run_of = [&](int t) { return min(place(t) * KB + 16 * wave, (len - 1) & ~15); };
+    auto page_of = [&](int t) {  // tiles in order
+      const int pg = run_of(t) >> a.kv.shift;
+      if (pg >= win + 64) {
+        if (pg >= win + 128) {  // the first tile behind the sinks
+          win = (pg & ~3) - 64;
+          nid = ids(win + 64);
+        }
+        pid = nid;
+        win += 64;
+        nid = ids(win + 64);
+      }
+      return __builtin_amdgcn_readlane(pid, pg - win);
+    };
+    // this wave's 16 rows of tile t, which lie in page id: where they begin, rows past the last as the last
+    auto rows_at = [&](int t, int id, int which) {
+      return block0 + (uint64_t)(uint32_t)id * page_bytes + kv_rows_at<FMT, HD>(which, a.kv.shift) + (run_of(t) & page_mask) * RB;
+    };
+    auto issue = [&](int t, int id, auto which_c, const void* to) __attribute__((always_inline)) {
+      constexpr int which = decltype(which_c)::value;
+      const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_addr(to));
+      const uint8_t* const at = rows_at(t, id, which);
+      const int left = len - 1 - run_of(t), x = anew(lane);
+      uint32_t off[NL];
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        if constexpr (!G::QUANT) {
+          const int r = i * RPL + x / CH, c = x % CH;
+          off[i] = min(r, left) * RB + 16 * (which ? vswz(r, c) : kswz(r, c));
+        } else {  // bytes in order (16 rows of 32 bytes fill half a load: the others again)
+          const int e = (i * 1024 + x * 16) % (16 * RB);
+          off[i] = min(e / RB, left) * RB + e % RB;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < NL; ++i) dma16(at, off[i], lds + i * 1024);
+    };
+    constexpr std::integral_constant<int, 0> kK{};
+    constexpr std::integral_constant<int, 1> kV{};
+    // 8 and 4 bits: a thread takes a key of its wave's sixteen and HD / 4 channels, the scale of which
+    // it loads with the codes
+    uint8_t* const stage = lsm + 4 * TILE * 16 + wave * 2 * G::STAGE;  // codes of K, then of V
+    const int ckey = ln >> 2, cpart = ln & 3;
+    uint16_t ks = 0, vs = 0;
+    auto scale_of = [&](int t, int id, int which) {
+      const uint8_t* const s = block0 + (uint64_t)(uint32_t)id * page_bytes + kv_scales_at<FMT, HD>(which, a.kv.shift) +
+                               ((run_of(t) & page_mask) + min(ckey, len - 1 - run_of(t))) * KvFmt<FMT>::scales(HD);
+      return *(const uint16_t*)(s + (HD == 128 ? cpart : cpart >> 1) * 2);
+    };
+    auto convert = [&](const uint8_t* codes, uint16_t scale, u32x4* tile, bool is_v) __attribute__((always_inline)) {
+      if constexpr (G::QUANT) {
+        constexpr int NC = HD / 4;  // channels
+        constexpr float bias = KvFmt<FMT>::bias;
+        const float s = bf16_bits_to_f32(scale), off = s * -bias;
+        const uint8_t* const at = codes + ckey * RB + cpart * (RB / 4);
+        uint32_t w[RB / 16];
+#pragma unroll
+        for (int i = 0; i < RB / 16; i += 2) {
+          const uint2 two = *(const uint2*)(at + 4 * i);
+          w[i] = two.x, w[i + 1] = two.y;
+        }
+        const bool big = __any(s > 6.6e35f);  // a code times a scale near bf16's end may round past it
+#pragma unroll
+        for (int j = 0; j < NC / 8; ++j) {
+          float v[8];
+          if constexpr (FMT == DUO_KV_I8) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (float)(w[2 * j + (e >> 2)] >> (8 * (e & 3)) & 255u);
+          } else {
+            const uint32_t even = w[j] & 0x0f0f0f0fu, odd = w[j] >> 4 & 0x0f0f0f0fu;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (float)((e & 1 ? odd : even) >> (8 * (e >> 1)) & 255u);
+          }
+          if (big) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float x = (v[e] - bias) * s;  // NaN stays NaN
+              v[e] = fabsf(x) > 3.3895313892515355e38f ? copysignf(3.3895313892515355e38f, x) : x;
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e], s, off);
+          }
+          const int key = 16 * wave + ckey, c = cpart * (NC / 8) + j;
+          tile[key * CH + (is_v ? vswz(key, c) : kswz(key, c))] =
+              u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+        }
+      }
+    };
+    auto tile_of = [&](int i, int which) { return sm + ((i & 1) * 2 + which) * TILE; };  // i: of the tiles here
+    auto mine_of = [&](int i, int which) { return tile_of(i, which) + wave * 16 * CH; };
+
+    // ---- the first tiles and the queries are on their way together
+    const int row0 = 32 * wave;
+    struct Row {
+      int qi, head;
+    };
+    auto row_of = [&](int x) {
+      const int row = min(row0 + (x & 31), rows - 1), qi = by(row, a);
+      return Row{qi, row - qi * a.hg};
+    };
+    const int pos_lo = pos0 + by(min(row0, rows - 1), a), pos_hi = pos0 + by(min(row0 + 31, rows - 1), a);  // of this wave
+    int id_v = 0;  // page of the tile whose V comes next
+    if (n) {
+      const int id0 = page_of(t0), id1 = n > 1 ? page_of(t0 + 1) : 0;
+      id_v = id1;
+      if constexpr (!G::QUANT) {
+        issue(t0, id0, kK, mine_of(0, 0));
+        if (n > 1) issue(t0 + 1, id1, kK, mine_of(1, 0));
+        issue(t0, id0, kV, mine_of(0, 1));
+      } else {
+        uint8_t* const k1 = (uint8_t*)tile_of(1, 1) + wave * G::STAGE;  // the second K's codes: V's second tile comes later
+        uint16_t ks1 = 0;
+        issue(t0, id0, kK, stage);
+        issue(t0, id0, kV, stage + G::STAGE);
+        ks = scale_of(t0, id0, 0), vs = scale_of(t0, id0, 1);
+        if (n > 1) {
+          issue(t0 + 1, id1, kK, k1);
+          ks1 = scale_of(t0 + 1, id1, 0);
+        }
+        wait_vm<0>();
+        asm volatile("" ::: "memory");
+        convert(stage, ks, tile_of(0, 0), false);
+        convert(stage + G::STAGE, vs, tile_of(0, 1), true);
+        if (n > 1) convert(k1, ks1, tile_of(1, 0), false);
+        wait_lds<0>();
+        if (n > 2) {
+          const int id2 = page_of(t0 + 2);
+          issue(t0 + 2, id2, kK, stage);
+          ks = scale_of(t0 + 2, id2, 0);
+          id_v = id2;
+        }
+        if (n > 1) {
+          issue(t0 + 1, id1, kV, stage + G::STAGE);
+          vs = scale_of(t0 + 1, id1, 1);
+        }
+      }
+    }
+    u32x4 qa[KS];
+    {
+      const Row w = row_of(ln);
+      const uint16_t* const at = a.Q + (int64_t)(seq_q0 + qi0 + w.qi) * a.ldq + (int64_t)(head0 + min(w.head, heads - 1)) * HD;
+#pragma unroll
+      for (int c = 0; c < KS; ++c) qa[c] = *(const u32x4*)(at + 8 * (2 * c + half));
+#pragma unroll
+      for (int c = 0; c < KS; ++c) {
+        asm volatile("" : "+v"(qa[c]));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) qa[c][j] ^= a.flip;
+      }
+    }
+    float m = -INFINITY, mc = -INFINITY, l = 0.f;  // reference, times cexp; sum of this half's keys
+    f16x o[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+    // Steps of 32 keys, two per tile, counted from t0.  This wave: steps up to nu have keys that its
+    // queries see, those in [f0, f1) are seen whole by all of them.
+    const int shift = 2 * (sinks - from - t0);  // of a step behind the sinks, from its keys' number / 32
+    const int nu = row0 >= rows || pos_hi < 0 ? 0 : min(max((pos_hi >> 5) + 1 + shift, 0), 2 * n);
+    const int f0 = lost ? 2 * n : !a.window ? 0 : max((max(pos_hi - a.window + 1, 0) + 31) / 32, 2 * from) + shift;
+    const int f1 = lost ? 2 * n : max(pos_lo + 1, 0) / 32 + shift;
+    auto first_key = [&](int u) { return place(t0 + (u >> 1)) * KB + (u & 1) * 32; };
+    const int fast_end = same(min(nu - 4, f1 - 3));  // of two tiles' first step
+    const uint32_t nf = (uint32_t)same(max(f1 - f0, 0));
+    auto masked = [&](int u) { return (uint32_t)(u - f0) >= nf; };
+    // of the query at position pos
+    const int back = a.window ? a.window : INT32_MAX / 2;
+    auto sees = [&](int pos, int key) { return key <= pos && (key > pos - back || key < a.sinks); };
+
+    f16x sa, sb;  // scores of an even and of an odd step
+    u32x4 pf[2];  // probabilities of a step
+    auto score = [&](int u, f16x& sc) __attribute__((always_inline)) {
+      const int x = anew(lane);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[r] = 0.f;
+#pragma unroll
+      for (int c = 0; c < KS; ++c) sc = mma32_bf16(read_k(k_rows(u), c, x), qa[c], sc);
+    };
+    // a new reference where the step's scores leave the old one's range: the factor of what is
+    // relative to the old one (1 elsewhere), and whether any lane has one
+    auto refer = [&](const f16x& sc, float* f) __attribute__((always_inline)) {
+      float mt = sc[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) mt = fmaxf(mt, sc[r]);
+      const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
+      mt = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+      const bool up = mt > m && !(mt * a.cexp <= mc + 8.f);
+      if (!__any(up)) return false;
+      const float mcn = up ? mt * a.cexp : mc;
+      *f = up ? m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - mcn) : 1.f;
+      m = up ? mt : m;
+      mc = mcn;
+      l *= *f;
+      return true;
+    };
+    auto written = [&]() __attribute__((always_inline)) {  // the last products have been
+#pragma unroll
+      for (int d = 0; d < DB; ++d) asm volatile("s_nop 15" : "+v"(o[d]));
+    };
+    auto scale_o = [&](float f) __attribute__((always_inline)) {
+      written();
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] *= f;
+    };
+    auto probabilities = [&](const f16x& sc, u32x4 (&p)[2]) __attribute__((always_inline)) {
+      const float base = m == -INFINITY ? 0.f : mc;
+      float sum = 0.f;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[8 * t + 2 * j], a.cexp, -base));
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[8 * t + 2 * j + 1], a.cexp, -base));
+          sum += p0 + p1;
+          p[t][j] = pack_bf16(p0, p1);
+        }
+      return sum;
+    };
+    // O += V^T P^T of step u
+    auto add = [&](int u) __attribute__((always_inline)) {
+      const uint8_t* const sV = v_rows(u);
+      const int lx = anew(lane);
+      u32x4 v[2][DB];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int d = 0; d < DB; ++d) v[t][d] = read_v(sV, t, d, lx);
+      if (masked(u)) {
+        // some query may not see some key, and 0 times a number that is not finite would not be 0:
+        // such numbers enter as zeros and are added for those who see them
+        uint32_t most = 0;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t w = v[t][d][j] & 0x7fff7fffu;
+              most = max(most, max(w & 0xffffu, w >> 16));
+            }
+        if (__any(most >= 0x7f80u)) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const uint32_t w = v[t][d][j];
+                v[t][d][j] = w & ~(((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u));
+              }
+          written();
+          const int k0 = first_key(u), pos = pos0 + row_of(lx).qi;
+#pragma unroll 1
+          for (int key = 0; key < 32; ++key) {
+            const bool see = sees(pos, k0 + key);
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+              for (int g = 0; g < 4; ++g) {
+                const uint2 w = *(const uint2*)(sV + key * HD * 2 + vswz(key, 4 * d + g) * 16 + 8 * (lx >> 5));
+                const float x[4] = {__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+                                    __uint_as_float(w.y & 0xffff0000u)};
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[d][4 * g + r] += see && !(fabsf(x[r]) < INFINITY) ? x[r] : 0.f;
+              }
+          }
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[d] = mma32_bf16(v[t][d], pf[t], o[d]);
+    };
+    // Step u's probabilities, the values of the step before and the scores of the next, dealt out
+    // evenly where nothing is masked: MFMAs of the one, LDS reads and vector instructions of the others.
+    auto fast = [&](auto where, f16x& sc, f16x& sn) __attribute__((always_inline)) {
+      constexpr int W = decltype(where)::value;  // the step's place in two tiles, as its LDS buffers go by it
+      const float base = mc;
+      const u32x4* const sK = k_rows(W + 1);
+      const uint8_t* const sV = v_rows(W + 3);
+      u32x4 pn[2];
+      float ls[2] = {0.f, 0.f}, most = 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sn[r] = 0.f;
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int r = 8 * t + 2 * j;
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[r], a.cexp, -base));
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[r + 1], a.cexp, -base));
+          ls[0] += p0;
+          ls[1] += p1;
+          most = fmaxf(most, fmaxf(p0, p1));
+          pn[t][j] = pack_bf16(p0, p1);
+        }
+#pragma unroll
+        for (int i = 0; i < KS / 2; ++i) {
+          const int c = t * (KS / 2) + i;
+          sn = mma32_bf16(read_k(sK, c, ln), qa[c], sn);
+          if (i < DB) o[i] = mma32_bf16(read_v(sV, t, i, ln), pf[t], o[i]);
+        }
+      }
+      float sum = ls[0] + ls[1];
+      asm volatile("" : "+v"(pn[0]), "+v"(pn[1]), "+v"(sum), "+v"(most));  // computed here, not where they are used
+      __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+      for (int i = 0; i < DB + KS / 2; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, HD == 128 ? 4 : 8, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, HD == 128 ? 4 : 8, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      // scores that leave the reference's range (or have none yet): once more, with another
+      if (__any(most > 256.f || m == -INFINITY)) {
+        float f = 1.f;
+        if (refer(sc, &f)) scale_o(f);
+        sum = probabilities(sc, pn);
+      }
+      l += sum;
+      pf[0] = pn[0];
+      pf[1] = pn[1];
+    };
+    auto slow = [&](int u, f16x& sc, f16x& sn) __attribute__((always_inline)) {
+      if (u > 0 && u <= nu) add(u - 1);
+      if (u < nu) {
+        if (masked(u)) {
+          const int x = anew(lane), k0 = first_key(u), pos = pos0 + row_of(x).qi;
+          bool gone[2] = {false, false};  // of the step's two runs of 16 keys
+          if (lost)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int id = pages[min(k0 + 16 * i, len - 1) >> a.kv.shift];
+              gone[i] = id < 0 || id >= a.kv.pages;
+            }
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int key = k0 + 8 * (r >> 2) + 4 * (x >> 5) + (r & 3);
+            sc[r] = !sees(pos, key) ? -INFINITY : gone[r >> 3] ? NAN : sc[r];
+          }
+        }
+        float f;
+        if (refer(sc, &f) && u > 0) scale_o(f);
+        l += probabilities(sc, pf);
+        if (u + 1 < nu) score(u + 1, sn);
+      }
+    };
+    // K of the next tile and V of this one are in LDS, and every wave is done with K of this one and V
+    // of the one before, whose places the next ones take
+    auto turn = [&](int i) __attribute__((always_inline)) {
+      wait_vm<0>();
+      lds_barrier();
+      if constexpr (!G::QUANT) {
+        int id = 0;
+        if (i + 2 < n) {
+          id = page_of(t0 + i + 2);
+          issue(t0 + i + 2, id, kK, mine_of(i, 0));
+        }
+        if (i + 1 < n) issue(t0 + i + 1, id_v, kV, mine_of(i + 1, 1));
+        id_v = id;
+      } else {
+        if (i + 2 < n) convert(stage, ks, tile_of(i, 0), false);
+        if (i + 1 < n) convert(stage + G::STAGE, vs, tile_of(i + 1, 1), true);
+        wait_lds<0>();
+        int id = 0;
+        if (i + 3 < n) {
+          id = page_of(t0 + i + 3);
+          issue(t0 + i + 3, id, kK, stage);
+          ks = scale_of(t0 + i + 3, id, 0);
+        }
+        if (i + 2 < n) {
+          issue(t0 + i + 2, id_v, kV, stage + G::STAGE);
+          vs = scale_of(t0 + i + 2, id_v, 1);
+        }
+        id_v = id;
+      }
+    };
+    if (n) {
+      if constexpr (!G::QUANT) wait_vm<0>();
+      lds_barrier();
+      if (nu > 0) score(0, sa);
+    }
+    for (int i = 0; i < n;) {
+      slow(2 * i, sa, sb);
+      turn(i);
+      slow(2 * i + 1, sb, sa);
+      // two tiles at a time, the odd one first, so that places in LDS are known when compiled
+      for (++i; (i & 1) && 2 * i - 1 >= f0 && 2 * i < fast_end; i += 2) {
+        fast(std::integral_constant<int, 2>{}, sa, sb);
+        turn(i);
+        fast(std::integral_constant<int, 3>{}, sb, sa);
+        fast(std::integral_constant<int, 0>{}, sa, sb);
+        turn(i + 1);
+        fast(std::integral_constant<int, 1>{}, sb, sa);
+      }
+    }
+    if (nu > 0 && nu == 2 * n) add(nu - 1);
+    written();
+    // ---- out
+    const int le = anew(lane);
+    const auto rl = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    const float sum = __uint_as_float(rl[0]) + __uint_as_float(rl[1]);
+    if (!whole) {
+      const int64_t at = (2 * (int64_t)share + (t0 == 0)) * QB;
+      if (t0 == 0 && tid == 0) {
+        const int64_t end = block + min(kRowsCost + (tiles - 1) * KB + 1, cost - near(cost));
+        a.tasks[share] = RowsTask{share_of(end - 1) - share + 1, seq_q0 + qi0, head0, heads, rows, pos0};
+      }
+      if (row0 + (le & 31) < rows) {
+        if (le < 32) *(float2*)(a.pml + 2 * (at + row0 + (le & 31))) = make_float2(mc, sum);
+        float* const y = a.po + (at + row0 + (le & 31)) * HD + 4 * (le >> 5);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+            *(f4*)(y + 32 * d + 8 * g) = f4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
+      }
+      continue;
+    }
+    // queries that see no key: 0; a sum of 0 (every score -inf) gives NaN
+    const Row w = row_of(le);
+    const float inv = pos0 + w.qi < 0 ? 0.f : 1.0f / sum;
+    uint2 y[DB][4];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        y[d][g].x = pack_bf16(o[d][4 * g] * inv, o[d][4 * g + 1] * inv);
+        y[d][g].y = pack_bf16(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv);
+      }
+    if (a.vec) {
+      // through this wave's part of LDS, where K tiles were (every wave was done with them at the
+      // last turn), so that a row is written at once, 16 bytes per lane; chunk c of row r at
+      // c ^ (r % CH)
+      uint8_t* const st = (uint8_t*)tile_of(wave / 2, 0) + wave % 2 * (32 * HD * 2);
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *(uint2*)(st + (le & 31) * HD * 2 + ((4 * d + g) ^ ((le & 31) & (CH - 1))) * 16 + 8 * (le >> 5)) = y[d][g];
+      wait_lds<0>();
+#pragma unroll
+      for (int i = 0; i < 32 / RPL; ++i) {
+        const int r = i * RPL + le / CH, qr = by(min(row0 + r, rows - 1), a), h = row0 + r - qr * a.hg;
+        const u32x4 v = *(const u32x4*)(st + r * HD * 2 + (le % CH ^ (r & (CH - 1))) * 16);
+        if (row0 + r < rows && h < heads)
+          *(u32x4*)(a.O + (int64_t)(seq_q0 + qi0 + qr) * a.ldo + (int64_t)(head0 + h) * HD + 8 * (le % CH)) = v;
+      }
+    } else if (row0 + (le & 31) < rows && w.head < heads) {
+      uint16_t* const y0 = a.O + (int64_t)(seq_q0 + qi0 + w.qi) * a.ldo + (int64_t)(head0 + w.head) * HD + 4 * (le >> 5);
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          uint16_t* yp = y0 + 32 * d + 8 * g;
+          yp[0] = (uint16_t)y[d][g].x;
+          yp[1] = (uint16_t)(y[d][g].x >> 16);
+          yp[2] = (uint16_t)y[d][g].y;
+          yp[3] = (uint16_t)(y[d][g].y >> 16);
+        }
+    }
+  }
+}
+
+// Joins the parts of the block that begins in share blockIdx.x, if it ends in another one: its own
+// part (the second of its two places), then the first places of the shares after it.  HD / 4 threads
+// per row, blockIdx.y counts the rows by the 1024 / HD that a workgroup takes.
+template <int HD>
+__global__ __launch_bounds__(256) void rows_join_kernel(RowsArgs a) {
+  constexpr int T = HD / 4;
+  const RowsTask task = a.tasks[blockIdx.x];
+  const int row = blockIdx.y * (256 / T) + threadIdx.x / T, d = threadIdx.x % T * 4;
+  if (task.parts == 0 || row >= task.rows) return;
+  const int qi = by(row, a), h = row - qi * a.hg;
+  auto place = [&](int i) { return (2 * ((int64_t)blockIdx.x + i) + (i == 0)) * kRowsQB + row; };
+  float top = -INFINITY;
+#pragma unroll 4
+  for (int i = 0; i < task.parts; ++i) top = fmaxf(top, a.pml[2 * place(i)]);
+  float sum = 0.f;
+  f4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = 0; i < task.parts; ++i) {
+    const float2 ml = *(const float2*)(a.pml + 2 * place(i));
+    const f4 v = *(const f4*)(a.po + place(i) * HD + d);
+    // a part without a finite score holds zeros, or NaN that has to stay
+    const float w = ml.x == -INFINITY ? ml.y : __builtin_amdgcn_exp2f(ml.x - top);
+    sum += w * ml.y;
+    y += v * w;
+  }
+  if (h >= task.heads) return;
+  const bool none = task.pos0 + qi < 0;
+  const uint2 two = none ? make_uint2(0, 0) : make_uint2(pack_bf16(y[0] / sum, y[1] / sum), pack_bf16(y[2] / sum, y[3] / sum));
+  uint16_t* const o = a.O + (int64_t)(task.q0 + qi) * a.ldo + (int64_t)(task.head0 + h) * HD + d;
+  if (a.vec) {
+    *(uint2*)o = two;
+  } else {
+    o[0] = (uint16_t)two.x, o[1] = (uint16_t)(two.x >> 16);
+    o[2] = (uint16_t)two.y, o[3] = (uint16_t)(two.y >> 16);
+  }
+}
+
+}  // namespace duo

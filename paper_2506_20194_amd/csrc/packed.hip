@@ -52,6 +52,8 @@
 #include "mfma.h"
 #include "pingpong.h"
 
+#include "chunk_rows.h"
+
 using namespace duo;
 using namespace duo::pp;
 
@@ -551,7 +553,61 @@ Plan packed_plan(int64_t total_q, int64_t total_k, int64_t nseq, int64_t group, 
   return {blocks, parts >= 2 ? parts : 1};
 }
 
+// Workgroups of rows_kernel, a multiple of eight: no more than the smallest shares of all that the
+// sizes allow.
+int64_t rows_wgs(int64_t total_q, int64_t nseq, int64_t group, int64_t kv_heads, int64_t max_len) {
+  const int64_t nsub = cdiv(group, kRowsQB), qpb = kRowsQB / cdiv(group, nsub);
+  const double blocks = (double)(kv_heads * nsub) * (double)(total_q / qpb + std::min(nseq, total_q));
+  const double shares = blocks * (double)(max_len + qpb + kRowsCost) / kRowsMin + 1;
+  return shares < kRowsWg ? rup((int64_t)shares, 8) : kRowsWg;
+}
+
 }  // namespace
+
+namespace duo {
+
+size_t chunk_rows_ws_bytes(int64_t total_q, int64_t nseq, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t max_len) {
+  const int64_t wgs = rows_wgs(total_q, nseq, heads / kv_heads, kv_heads, max_len);
+  return align_up(wgs * sizeof(RowsTask)) + align_up((size_t)(2 * wgs * kRowsQB * (head_dim + 2)) * sizeof(float));
+}
+
+duo_status chunk_rows_run(const ChunkCall& c, int64_t least, void* ws, hipStream_t s) {
+  RowsArgs a = {};
+  a.Q = (const uint16_t*)c.Q, a.O = (uint16_t*)c.O;
+  a.ldq = c.ldq, a.ldo = c.ldo;
+  a.kv = c.geo;
+  a.table = c.table, a.ldt = c.ldt, a.lens = c.lens, a.cu_q = c.cu_q;
+  a.total_q = (int)c.total_q, a.nseq = (int)c.nseq, a.max_len = (int)c.max_len;
+  a.group = (int)(c.heads / c.geo.heads);
+  a.nsub = (int)cdiv(a.group, kRowsQB), a.hg = (int)cdiv(a.group, a.nsub), a.qpb = kRowsQB / a.hg;
+  while ((1 << a.by_shift) < a.hg) ++a.by_shift;
+  a.by_hg = (uint32_t)((((uint64_t)1 << (31 + a.by_shift)) + a.hg - 1) / a.hg);
+  a.window = c.window, a.sinks = c.sinks;
+  a.per = (int)cdiv(c.nseq, 64);
+  a.least = least;
+  a.cexp = c.cexp, a.flip = c.flip;
+  a.vec = c.ldo % 8 == 0 && aligned16(c.O);
+  const int hd = c.cache->head_dim;
+  const int64_t wgs = rows_wgs(c.total_q, c.nseq, a.group, c.geo.heads, c.max_len);
+  a.tasks = (RowsTask*)ws;
+  a.po = (float*)((uint8_t*)ws + align_up(wgs * sizeof(RowsTask)));
+  a.pml = a.po + 2 * wgs * kRowsQB * hd;
+  return kv_by_format(c.cache, [&](auto fmt, auto dim) -> duo_status {
+    constexpr int FMT = decltype(fmt)::value, HD = decltype(dim)::value;
+    constexpr int lds = RowsGeo<FMT, HD>::LDS;
+    const auto kern = rows_kernel<FMT, HD>;
+    if (duo_status st = set_max_lds((const void*)kern, lds); st != DUO_OK) return st;
+    hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(256), lds, s, a);
+    DUO_LAUNCH_CHECK();
+    if (wgs > 1) {
+      hipLaunchKernelGGL(rows_join_kernel<HD>, dim3((unsigned)wgs, kRowsQB * HD / 1024), dim3(256), 0, s, a);
+      DUO_LAUNCH_CHECK();
+    }
+    return DUO_OK;
+  });
+}
+
+}  // namespace duo
 
 extern "C" {
 

@@ -75,6 +75,9 @@ constexpr int kMinShare = 8;
 // in 8 bits, 64 on 8, 11 us, and 16 with a wave alone.
 constexpr int kShort = 4;
 constexpr int kMinKeys = 32;    // tokens of the smallest tile
+// Chunks: sequences of no more rows (new tokens times heads of a group) are done here, the others by
+// chunk_rows_run.
+constexpr int kFewRows = 32;
 
 template <int FMT, int HD>
 struct PagedGeo {
@@ -1086,7 +1089,8 @@ size_t duo_attention_chunk_workspace_size(int64_t total_q, int64_t nseq, int64_t
     return 0;
   const double rows = (double)kv_heads * ((double)total_q * (double)(heads / kv_heads) / 8 + (double)nseq);
   const int64_t wgs = paged_wgs(rows, cdiv(max_len, kMinKeys), kMaxWg);
-  return align_up(wgs * sizeof(Task)) + align_up((size_t)(2 * wgs * kCols * (head_dim + 2)) * sizeof(float));
+  return align_up(wgs * sizeof(Task)) + align_up((size_t)(2 * wgs * kCols * (head_dim + 2)) * sizeof(float)) +
+         chunk_rows_ws_bytes(total_q, nseq, heads, kv_heads, head_dim, max_len);
 }
 
 duo_status duo_attention_chunk(const void* Q, int64_t ldq, int64_t total_q, const duo_kv_cache* cache, const int32_t* table,
@@ -1119,7 +1123,15 @@ duo_status duo_attention_chunk(const void* Q, int64_t ldq, int64_t total_q, cons
   ch.cu_q = cu_q, ch.total_q = (int)total_q;
   ch.window = window <= max_len ? (int)window : 0;  // a longer one hides nothing
   ch.sinks = (int)std::min(sinks, max_len);
-  ch.most = INT64_MAX;
+  const bool many = std::min(max_q, total_q) * group > kFewRows, few = !many || nseq > 1;
+  ch.most = many ? kFewRows : INT64_MAX;
+  if (many) {
+    const ChunkCall c = {Q, O, ldq, ldo, total_q, nseq, max_len, heads, ldt, cache, g, table, lens, cu_q, ch.window, ch.sinks,
+                         cexp, flip};
+    uint8_t* const rows_ws = (uint8_t*)ws + (need - chunk_rows_ws_bytes(total_q, nseq, heads, g.heads, hd, max_len));
+    if (duo_status st = chunk_rows_run(c, few ? kFewRows : 0, rows_ws, s); st != DUO_OK) return st;
+    if (!few) return DUO_OK;
+  }
   ch.by_shift = 0;
   while ((int64_t)1 << ch.by_shift < group) ++ch.by_shift;
   ch.by_group = (uint32_t)((((uint64_t)1 << (31 + ch.by_shift)) + group - 1) / group);
