@@ -9,13 +9,22 @@
 // transposing LDS reads), in steps of 32 keys, with a running reference that moves only when
 // a score exceeds it by a factor of 2^8, and probabilities rounded to bf16 for the product with V.
 //
-// Tiles are 64 keys of the pages: a wave brings 16 of them, which lie in one page whatever its
-// size.  A block's tiles are those of the sinks, then those from its first query's window on.  Keys
-// behind the end are copies of the last one.  In 16 bits rows go global -> LDS directly.  In 8 and 4
-// bits the codes do, to a place of the wave's own, and a turn later the wave turns them into
-// bf16 numbers, rounded as duo_kv_read rounds them, in the tile that all waves read: once for
-// 128 rows, where the paged kernel, which multiplies the codes themselves, pays for scales in every
-// product.  (Rounding K and V adds about 0.0015 of the output's root mean square to an error of 0.0018.)
+// Tiles are 64 keys of the pages: a wave brings 16 of them (a run), which lie in one page whatever
+// its size.  A block's tiles are those of the sinks, then those from its first query's window on.  Keys
+// behind the end are copies of the last one.  In 16 bits rows go global -> LDS directly.
+//
+// In 8 and 4 bits the codes do, to a place of the wave's own, and a turn later the wave makes
+// numbers of them in the tile that all waves read: once for 128 rows, where the paged kernel, which
+// multiplies the codes themselves, pays for scales in every product.  The numbers are fp16 and so is
+// everything that they meet: a code of 4 bits times a scale (three bits times eight) is exact in it, one
+// of 8 bits is rounded to 2^-12 of itself (bf16 would cost 2^-9: an error of the output of 0.0031 and, in
+// 4 bits, 0.0048 of its root mean square, where the plain form has 0.0017).  fp16's range is made to
+// do by powers of two: a key whose largest number is outside 2^-3 .. 2^15 is brought to 2^14, and its
+// scores take the power back; a row of Q likewise; and a token's values, whose power goes into the
+// exponent of its probabilities (the running reference is then one of p |V|, not of p) and out of
+// their sum again.  None of that happens with numbers of ordinary size, so the steps that are dealt out
+// go without it.  What is lost: a token's numbers below 2^-28 of its largest are rounded at 2^-39 of
+// that.
 //
 // Blocks cost what they have of keys, and something for their start and end; the count of all
 // blocks is cut into equal shares, one per workgroup, neighbours on one XCD.  A share's end that lies
@@ -113,6 +122,43 @@ struct RowsAt {
   int64_t at;        // into the block
 };
 
+// Two numbers, and products of tiles, in bf16 or fp16.
+template <bool F16>
+__device__ __forceinline__ uint32_t pack_two(float lo, float hi) {
+  if constexpr (!F16) return pack_bf16(lo, hi);
+  typedef _Float16 f16v2 __attribute__((ext_vector_type(2)));
+  const f16v2 v = __builtin_convertvector(f32v2{lo, hi}, f16v2);  // round to nearest even
+  uint32_t u;
+  __builtin_memcpy(&u, &v, 4);
+  return u;
+}
+template <bool F16>
+__device__ __forceinline__ float low_of(uint32_t w) {
+  if constexpr (!F16) return __uint_as_float(w << 16);
+  const uint16_t h = (uint16_t)w;
+  _Float16 v;
+  __builtin_memcpy(&v, &h, 2);
+  return (float)v;
+}
+template <bool F16>
+__device__ __forceinline__ float high_of(uint32_t w) {
+  return F16 ? low_of<F16>(w >> 16) : __uint_as_float(w & 0xffff0000u);
+}
+template <bool F16>
+__device__ __forceinline__ f16x mma32(const u32x4& a, const u32x4& b, f16x c) {
+  if constexpr (!F16) return mma32_bf16(a, b, c);
+  typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+  f16x8 av, bv;
+  __builtin_memcpy(&av, &a, 16);
+  __builtin_memcpy(&bv, &b, 16);
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(av, bv, c, 0, 0, 0);
+}
+// The power of two that a group of numbers of at most `top` is divided by to fit fp16: 0 where they do.
+__device__ __forceinline__ int power_of(float top) {
+  const int e = (int)(__float_as_uint(top) >> 23) - 127;
+  return top == 0.f || e == 128 || (e >= -3 && e < 15) ? 0 : e - 14;
+}
+
 template <int FMT, int HD>
 struct RowsGeo {
   static constexpr bool QUANT = FMT != DUO_KV_BF16;
@@ -127,6 +173,7 @@ template <int FMT, int HD>
 __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   using G = RowsGeo<FMT, HD>;
   constexpr int KB = G::KB, CH = G::CH, TILE = G::TILE, RB = G::RB, NL = G::NL, QB = kRowsQB;
+  constexpr bool F16 = G::QUANT;
   constexpr int KS = HD / 16, DB = HD / 32;  // MFMA steps over head_dim, 32-wide blocks of the output row
   constexpr int RPL = 64 / CH;               // rows of bf16 per wave-wide access
   extern __shared__ __attribute__((aligned(16))) uint8_t lsm[];
@@ -344,21 +391,54 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     };
     constexpr std::integral_constant<int, 0> kK{};
     constexpr std::integral_constant<int, 1> kV{};
-    // 8 and 4 bits: a thread takes a key of its wave's sixteen and HD / 4 channels, the scale of which
-    // it loads with the codes
+    // ---- 8 and 4 bits
     uint8_t* const stage = lsm + 4 * TILE * 16 + wave * 2 * G::STAGE;  // codes of K, then of V
-    const int ckey = ln >> 2, cpart = ln & 3;
-    uint16_t ks = 0, vs = 0;
-    auto scale_of = [&](int t, int id, int which) {
-      const uint8_t* const s = block0 + (uint64_t)(uint32_t)id * page_bytes + kv_scales_at<FMT, HD>(which, a.kv.shift) +
-                               ((run_of(t) & page_mask) + min(ckey, len - 1 - run_of(t))) * KvFmt<FMT>::scales(HD);
-      return *(const uint16_t*)(s + (HD == 128 ? cpart : cpart >> 1) * 2);
+    // a lane looks after the scales of one key of the tile
+    struct Scales {
+      uint32_t w[HD / 64];
     };
-    auto convert = [&](const uint8_t* codes, uint16_t scale, u32x4* tile, bool is_v) __attribute__((always_inline)) {
+    auto lane_run = [&](int t, int x) { return min(place(t) * KB + (x & 48), (len - 1) & ~15); };
+    auto lane_page = [&](int t) { return __shfl(pid, (lane_run(t, lane) >> a.kv.shift) - win); };  // after page_of(t)
+    auto scales_of = [&](int t, int id, int which) {
+      const int x = anew(lane), run = lane_run(t, x);
+      const uint32_t* const s = (const uint32_t*)(block0 + (uint64_t)(uint32_t)id * page_bytes + kv_scales_at<FMT, HD>(which, a.kv.shift) +
+                                                  ((run & page_mask) + min(x & 15, len - 1 - run)) * KvFmt<FMT>::scales(HD));
+      Scales r;
+      if constexpr (HD == 128) {
+        const uint2 v = *(const uint2*)s;
+        r.w[0] = v.x, r.w[HD / 64 - 1] = v.y;
+      } else {
+        r.w[0] = *s;
+      }
+      return r;
+    };
+    // the largest number that the key's codes can stand for (a scale that is NaN aside)
+    auto most_of = [&](const Scales& s) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < HD / 64; ++i) {
+        const uint32_t lo = s.w[i] & 0xffffu, hi = s.w[i] >> 16;
+        m = max(m, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+      }
+      if constexpr (G::QUANT) return __uint_as_float(m << 16) * KvFmt<FMT>::most;
+      return 0.f;
+    };
+    int e_ref = 0;  // power of two that the outputs are in units of: that of the first tile's values
+    auto v_power = [&](const Scales& s) { return min(max(power_of(ldexpf(most_of(s), -e_ref)), -60), 60); };
+    // a thread takes a key of its wave's run and HD / 4 channels; power: what the numbers are divided by
+    auto convert = [&](const uint8_t* codes, const Scales& scales, int power, u32x4* tile, bool is_v) __attribute__((always_inline)) {
       if constexpr (G::QUANT) {
         constexpr int NC = HD / 4;  // channels
         constexpr float bias = KvFmt<FMT>::bias;
-        const float s = bf16_bits_to_f32(scale), off = s * -bias;
+        const int x = anew(lane), ckey = x >> 2, cpart = x & 3, key = 16 * wave + ckey;
+        uint32_t sw = (uint32_t)__shfl((int)scales.w[0], key);
+        if constexpr (HD == 128) {
+          const uint32_t s1 = (uint32_t)__shfl((int)scales.w[HD / 64 - 1], key);
+          sw = cpart & 2 ? s1 : sw;
+        }
+        const int by_power = __shfl(power, key);
+        const float s = ldexpf((HD == 128 ? cpart & 1 : cpart >> 1) ? __uint_as_float(sw & 0xffff0000u) : __uint_as_float(sw << 16), -by_power);
+        const float off = s * -bias;
         const uint8_t* const at = codes + ckey * RB + cpart * (RB / 4);
         uint32_t w[RB / 16];
 #pragma unroll
@@ -366,7 +446,6 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
           const uint2 two = *(const uint2*)(at + 4 * i);
           w[i] = two.x, w[i + 1] = two.y;
         }
-        const bool big = __any(s > 6.6e35f);  // a code times a scale near bf16's end may round past it
 #pragma unroll
         for (int j = 0; j < NC / 8; ++j) {
           float v[8];
@@ -378,20 +457,22 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = (float)((e & 1 ? odd : even) >> (8 * (e >> 1)) & 255u);
           }
-          if (big) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float x = (v[e] - bias) * s;  // NaN stays NaN
-              v[e] = fabsf(x) > 3.3895313892515355e38f ? copysignf(3.3895313892515355e38f, x) : x;
-            }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e], s, off);
-          }
-          const int key = 16 * wave + ckey, c = cpart * (NC / 8) + j;
-          tile[key * CH + (is_v ? vswz(key, c) : kswz(key, c))] =
-              u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+          for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e], s, off);  // (code - bias) s, exactly
+          const int c = cpart * (NC / 8) + j;
+          tile[key * CH + (is_v ? vswz(key, c) : kswz(key, c))] = u32x4{pack_two<F16>(v[0], v[1]), pack_two<F16>(v[2], v[3]),
+                                                                        pack_two<F16>(v[4], v[5]), pack_two<F16>(v[6], v[7])};
         }
+      }
+    };
+    Scales ks = {}, vs = {}, vs1 = {};  // of the next codes to become numbers, and of the V after
+    // powers of the lane's key and value in this tile, the next and the one after
+    int kp = 0, kp1 = 0, kp2 = 0, vp = 0, vp1 = 0, vp2 = 0;
+    bool calm = true;  // there are none in this tile and the next
+    auto next = [&]() __attribute__((always_inline)) {  // on to the next tile
+      if constexpr (G::QUANT) {
+        kp = kp1, kp1 = kp2, vp = vp1, vp1 = vp2;
+        calm = !__any((kp | kp1 | vp | vp1) != 0);
       }
     };
     auto tile_of = [&](int i, int which) { return sm + ((i & 1) * 2 + which) * TILE; };  // i: of the tiles here
@@ -409,7 +490,8 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     const int pos_lo = pos0 + by(min(row0, rows - 1), a), pos_hi = pos0 + by(min(row0 + 31, rows - 1), a);  // of this wave
     int id_v = 0;  // page of the tile whose V comes next
     if (n) {
-      const int id0 = page_of(t0), id1 = n > 1 ? page_of(t0 + 1) : 0;
+      const int id0 = page_of(t0), lane0 = G::QUANT ? lane_page(t0) : 0;
+      const int id1 = n > 1 ? page_of(t0 + 1) : 0, lane1 = G::QUANT && n > 1 ? lane_page(t0 + 1) : 0;
       id_v = id1;
       if constexpr (!G::QUANT) {
         issue(t0, id0, kK, mine_of(0, 0));
@@ -417,30 +499,37 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         issue(t0, id0, kV, mine_of(0, 1));
       } else {
         uint8_t* const k1 = (uint8_t*)tile_of(1, 1) + wave * G::STAGE;  // the second K's codes: V's second tile comes later
-        uint16_t ks1 = 0;
+        Scales ks1 = {};
         issue(t0, id0, kK, stage);
         issue(t0, id0, kV, stage + G::STAGE);
-        ks = scale_of(t0, id0, 0), vs = scale_of(t0, id0, 1);
+        ks = scales_of(t0, lane0, 0), vs = scales_of(t0, lane0, 1);
         if (n > 1) {
           issue(t0 + 1, id1, kK, k1);
-          ks1 = scale_of(t0 + 1, id1, 0);
+          ks1 = scales_of(t0 + 1, lane1, 0), vs1 = scales_of(t0 + 1, lane1, 1);
         }
         wait_vm<0>();
         asm volatile("" ::: "memory");
-        convert(stage, ks, tile_of(0, 0), false);
-        convert(stage + G::STAGE, vs, tile_of(0, 1), true);
-        if (n > 1) convert(k1, ks1, tile_of(1, 0), false);
+        {
+          float m = most_of(vs);
+#pragma unroll
+          for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+          e_ref = same(power_of(m));
+        }
+        kp = power_of(most_of(ks)), kp1 = power_of(most_of(ks1));
+        vp = v_power(vs), vp1 = v_power(vs1);
+        calm = !__any((kp | kp1 | vp | vp1) != 0);
+        convert(stage, ks, kp, tile_of(0, 0), false);
+        convert(stage + G::STAGE, vs, vp + e_ref, tile_of(0, 1), true);
+        if (n > 1) convert(k1, ks1, kp1, tile_of(1, 0), false);
         wait_lds<0>();
+        vs = vs1;
         if (n > 2) {
-          const int id2 = page_of(t0 + 2);
+          const int id2 = page_of(t0 + 2), lane2 = lane_page(t0 + 2);
           issue(t0 + 2, id2, kK, stage);
-          ks = scale_of(t0 + 2, id2, 0);
+          ks = scales_of(t0 + 2, lane2, 0), vs1 = scales_of(t0 + 2, lane2, 1);
           id_v = id2;
         }
-        if (n > 1) {
-          issue(t0 + 1, id1, kV, stage + G::STAGE);
-          vs = scale_of(t0 + 1, id1, 1);
-        }
+        if (n > 1) issue(t0 + 1, id1, kV, stage + G::STAGE);
       }
     }
     u32x4 qa[KS];
@@ -456,6 +545,25 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         for (int j = 0; j < 4; ++j) qa[c][j] ^= a.flip;
       }
     }
+    int q_power = 0;  // of the lane's row
+    if constexpr (G::QUANT) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int c = 0; c < KS; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t w = qa[c][j] & 0x7fff7fffu;
+          top = max(top, max(w & 0xffffu, w >> 16));
+        }
+      const auto x = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+      q_power = power_of(__uint_as_float(max(x[0], x[1]) << 16));
+#pragma unroll
+      for (int c = 0; c < KS; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          qa[c][j] = pack_two<F16>(ldexpf(__uint_as_float(qa[c][j] << 16), -q_power), ldexpf(__uint_as_float(qa[c][j] & 0xffff0000u), -q_power));
+    }
+    const bool odd_q = __any(q_power != 0);
     float m = -INFINITY, mc = -INFINITY, l = 0.f;  // reference, times cexp; sum of this half's keys
     f16x o[DB];
 #pragma unroll
@@ -469,7 +577,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     const int f0 = lost ? 2 * n : !a.window ? 0 : max((max(pos_hi - a.window + 1, 0) + 31) / 32, 2 * from) + shift;
     const int f1 = lost ? 2 * n : max(pos_lo + 1, 0) / 32 + shift;
     auto first_key = [&](int u) { return place(t0 + (u >> 1)) * KB + (u & 1) * 32; };
-    const int fast_end = same(min(nu - 4, f1 - 3));  // of two tiles' first step
+    const int fast_end = odd_q ? 0 : same(min(nu - 4, f1 - 3));  // of two tiles' first step
     const uint32_t nf = (uint32_t)same(max(f1 - f0, 0));
     auto masked = [&](int u) { return (uint32_t)(u - f0) >= nf; };
     // of the query at position pos
@@ -483,16 +591,26 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) sc[r] = 0.f;
 #pragma unroll
-      for (int c = 0; c < KS; ++c) sc = mma32_bf16(read_k(k_rows(u), c, x), qa[c], sc);
+      for (int c = 0; c < KS; ++c) sc = mma32<F16>(read_k(k_rows(u), c, x), qa[c], sc);
     };
     // a new reference where the step's scores leave the old one's range: the factor of what is
     // relative to the old one (1 elsewhere), and whether any lane has one
-    auto refer = [&](const f16x& sc, float* f) __attribute__((always_inline)) {
+    // units: the scores' in the exponent of two (a.cexp, or 1 where they are that already)
+    auto refer = [&](const f16x& sc, float* f, float units) __attribute__((always_inline)) {
       float mt = sc[0];
 #pragma unroll
       for (int r = 1; r < 16; ++r) mt = fmaxf(mt, sc[r]);
       const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
       mt = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+      if constexpr (G::QUANT) {
+        mt *= units;
+        const bool up = mt > mc + 8.f;
+        if (!__any(up)) return false;
+        *f = up ? mc == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - mt) : 1.f;
+        mc = up ? mt : mc;
+        l *= *f;
+        return true;
+      }
       const bool up = mt > m && !(mt * a.cexp <= mc + 8.f);
       if (!__any(up)) return false;
       const float mcn = up ? mt * a.cexp : mc;
@@ -513,17 +631,19 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] *= f;
     };
-    auto probabilities = [&](const f16x& sc, u32x4 (&p)[2]) __attribute__((always_inline)) {
-      const float base = m == -INFINITY ? 0.f : mc;
+    // What probabilities are relative to: in fp16 the reference's is 2^6, as small ones have fewer bits there
+    auto base_of = [&]() { return G::QUANT ? mc - 6.f : mc; };
+    auto probabilities = [&](const f16x& sc, u32x4 (&p)[2], float units) __attribute__((always_inline)) {
+      const float base = (G::QUANT ? mc : m) == -INFINITY ? 0.f : base_of();
       float sum = 0.f;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[8 * t + 2 * j], a.cexp, -base));
-          const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[8 * t + 2 * j + 1], a.cexp, -base));
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[8 * t + 2 * j], units, -base));
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[8 * t + 2 * j + 1], units, -base));
           sum += p0 + p1;
-          p[t][j] = pack_bf16(p0, p1);
+          p[t][j] = pack_two<F16>(p0, p1);
         }
       return sum;
     };
@@ -549,7 +669,8 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
               const uint32_t w = v[t][d][j] & 0x7fff7fffu;
               most = max(most, max(w & 0xffffu, w >> 16));
             }
-        if (__any(most >= 0x7f80u)) {
+        constexpr uint32_t INF = F16 ? 0x7c00u : 0x7f80u;
+        if (__any(most >= INF)) {
 #pragma unroll
           for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -557,7 +678,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
                 const uint32_t w = v[t][d][j];
-                v[t][d][j] = w & ~(((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u));
+                v[t][d][j] = w & ~(((w & INF) == INF ? 0xffffu : 0u) | ((w >> 16 & INF) == INF ? 0xffff0000u : 0u));
               }
           written();
           const int k0 = first_key(u), pos = pos0 + row_of(lx).qi;
@@ -569,8 +690,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
 #pragma unroll
               for (int g = 0; g < 4; ++g) {
                 const uint2 w = *(const uint2*)(sV + key * HD * 2 + vswz(key, 4 * d + g) * 16 + 8 * (lx >> 5));
-                const float x[4] = {__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
-                                    __uint_as_float(w.y & 0xffff0000u)};
+                const float x[4] = {low_of<F16>(w.x), high_of<F16>(w.x), low_of<F16>(w.y), high_of<F16>(w.y)};
 #pragma unroll
                 for (int r = 0; r < 4; ++r) o[d][4 * g + r] += see && !(fabsf(x[r]) < INFINITY) ? x[r] : 0.f;
               }
@@ -580,13 +700,13 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int d = 0; d < DB; ++d) o[d] = mma32_bf16(v[t][d], pf[t], o[d]);
+        for (int d = 0; d < DB; ++d) o[d] = mma32<F16>(v[t][d], pf[t], o[d]);
     };
     // Step u's probabilities, the values of the step before and the scores of the next, dealt out
     // evenly where nothing is masked: MFMAs of the one, LDS reads and vector instructions of the others.
     auto fast = [&](auto where, f16x& sc, f16x& sn) __attribute__((always_inline)) {
       constexpr int W = decltype(where)::value;  // the step's place in two tiles, as its LDS buffers go by it
-      const float base = mc;
+      const float base = base_of();
       const u32x4* const sK = k_rows(W + 1);
       const uint8_t* const sV = v_rows(W + 3);
       u32x4 pn[2];
@@ -604,13 +724,13 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
           ls[0] += p0;
           ls[1] += p1;
           most = fmaxf(most, fmaxf(p0, p1));
-          pn[t][j] = pack_bf16(p0, p1);
+          pn[t][j] = pack_two<F16>(p0, p1);
         }
 #pragma unroll
         for (int i = 0; i < KS / 2; ++i) {
           const int c = t * (KS / 2) + i;
-          sn = mma32_bf16(read_k(sK, c, ln), qa[c], sn);
-          if (i < DB) o[i] = mma32_bf16(read_v(sV, t, i, ln), pf[t], o[i]);
+          sn = mma32<F16>(read_k(sK, c, ln), qa[c], sn);
+          if (i < DB) o[i] = mma32<F16>(read_v(sV, t, i, ln), pf[t], o[i]);
         }
       }
       float sum = ls[0] + ls[1];
@@ -627,10 +747,10 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
       }
       __builtin_amdgcn_sched_barrier(0);
       // scores that leave the reference's range (or have none yet): once more, with another
-      if (__any(most > 256.f || m == -INFINITY)) {
+      if (__any(most > (G::QUANT ? 16384.f : 256.f) || (G::QUANT ? mc : m) == -INFINITY)) {
         float f = 1.f;
-        if (refer(sc, &f)) scale_o(f);
-        sum = probabilities(sc, pn);
+        if (refer(sc, &f, a.cexp)) scale_o(f);
+        sum = probabilities(sc, pn, a.cexp);
       }
       l += sum;
       pf[0] = pn[0];
@@ -654,9 +774,34 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
             sc[r] = !sees(pos, key) ? -INFINITY : gone[r >> 3] ? NAN : sc[r];
           }
         }
-        float f;
-        if (refer(sc, &f) && u > 0) scale_o(f);
-        l += probabilities(sc, pf);
+        float f, units = a.cexp;
+        bool odd = false;  // some key, value or query has a power
+        if constexpr (G::QUANT) {
+          odd = odd_q || !calm;
+          if (odd) {
+            const int from_lane = (u & 1) * 32 + 4 * (anew(lane) >> 5);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int key = from_lane + 8 * (r >> 2) + (r & 3);
+              sc[r] = fmaf(ldexpf(sc[r], __shfl(kp, key) + q_power), a.cexp, (float)__shfl(vp, key));
+            }
+            units = 1.f;
+          }
+        }
+        if (refer(sc, &f, units) && u > 0) scale_o(f);
+        float sum = probabilities(sc, pf, units);
+        if constexpr (G::QUANT)
+          if (odd) {
+            const int from_lane = (u & 1) * 32 + 4 * (anew(lane) >> 5);
+            const float base = mc == -INFINITY ? 0.f : base_of();
+            sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int power = __shfl(vp, from_lane + 8 * (r >> 2) + (r & 3));
+              sum += ldexpf(__builtin_amdgcn_exp2f(sc[r] - base), -power);
+            }
+          }
+        l += sum;
         if (u + 1 < nu) score(u + 1, sn);
       }
     };
@@ -674,19 +819,21 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         if (i + 1 < n) issue(t0 + i + 1, id_v, kV, mine_of(i + 1, 1));
         id_v = id;
       } else {
-        if (i + 2 < n) convert(stage, ks, tile_of(i, 0), false);
-        if (i + 1 < n) convert(stage + G::STAGE, vs, tile_of(i + 1, 1), true);
+        if (i + 2 < n) {
+          kp2 = power_of(most_of(ks)), vp2 = v_power(vs1);
+          convert(stage, ks, kp2, tile_of(i, 0), false);
+        }
+        if (i + 1 < n) convert(stage + G::STAGE, vs, vp1 + e_ref, tile_of(i + 1, 1), true);
         wait_lds<0>();
+        vs = vs1;
         int id = 0;
         if (i + 3 < n) {
           id = page_of(t0 + i + 3);
+          const int lp = lane_page(t0 + i + 3);
           issue(t0 + i + 3, id, kK, stage);
-          ks = scale_of(t0 + i + 3, id, 0);
+          ks = scales_of(t0 + i + 3, lp, 0), vs1 = scales_of(t0 + i + 3, lp, 1);
         }
-        if (i + 2 < n) {
-          issue(t0 + i + 2, id_v, kV, stage + G::STAGE);
-          vs = scale_of(t0 + i + 2, id_v, 1);
-        }
+        if (i + 2 < n) issue(t0 + i + 2, id_v, kV, stage + G::STAGE);
         id_v = id;
       }
     };
@@ -699,18 +846,26 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
       slow(2 * i, sa, sb);
       turn(i);
       slow(2 * i + 1, sb, sa);
+      next();
       // two tiles at a time, the odd one first, so that places in LDS are known when compiled
-      for (++i; (i & 1) && 2 * i - 1 >= f0 && 2 * i < fast_end; i += 2) {
+      for (++i; (i & 1) && 2 * i - 1 >= f0 && 2 * i < fast_end && calm; i += 2) {
         fast(std::integral_constant<int, 2>{}, sa, sb);
         turn(i);
         fast(std::integral_constant<int, 3>{}, sb, sa);
+        next();
         fast(std::integral_constant<int, 0>{}, sa, sb);
         turn(i + 1);
         fast(std::integral_constant<int, 1>{}, sb, sa);
+        next();
       }
     }
     if (nu > 0 && nu == 2 * n) add(nu - 1);
     written();
+    if (G::QUANT && e_ref)
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] = ldexpf(o[d][r], e_ref);
     // ---- out
     const int le = anew(lane);
     const auto rl = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);

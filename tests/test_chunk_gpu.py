@@ -1,9 +1,9 @@
 """Attention of new tokens over the paged cache on the GPU, against the float64 reference
 on the numbers that the cache stands for, with the bound that the reference derives
-(oracle/serve_ref.py).  In 8 and 4 bits either the codes are multiplied exactly (with an
-offset, whose error is that of the paged attention's tests) or numbers that are rounded to bf16
-first, as duo_kv_read gives them: a sequence's outputs have to lie within the bound of one of
-the two, the numbers of the second being the rounded ones."""
+(oracle/serve_ref.py).  In 8 and 4 bits codes are multiplied exactly, with an offset, whose error
+is that of the paged attention's tests, or as fp16 numbers, which codes of 8 bits are rounded
+to: 2^-12 of each product in a score, and of each value, which the bound of a probability's
+rounding to bf16 (2^-8; fp16 has 2^-12) covers."""
 
 import numpy as np
 import pytest
@@ -112,8 +112,14 @@ class Batch:
                 p = np.exp(X - np.where(some, X.max(2, keepdims=True, initial=-np.inf), 0.0))
                 p = p / np.where(some, p.sum(2, keepdims=True), 1.0)
                 add = 2.0 ** -15 * np.repeat(np.einsum("lhn,nhg->lhg", p, np.repeat(sv, G, 1)), 32, -1)
+                if self.fmt == "int8":
+                    extra = extra + 2.0 ** -12 * np.einsum("lhd,nhd->lhn", np.abs(q), np.repeat(np.abs(k), G, 1)) * abs(scale)
+                # Scores off by at most e change p = exp(x) / sum exp(x) by a factor within exp(2 e), of which
+                # the reference's bound has the first term, 2 e: where e is not small the rest is added.
+                e = np.where(see[:, None], extra, 0.0).max(2)[..., None]
+                rest = (np.expm1(2 * e) - 2 * e) * np.einsum("lhn,nhd->lhd", p, np.repeat(np.abs(v), G, 1))
                 ref, tol = S.attend(q, k, v, scale, see, extra)
-                w = min(err((ref, tol + add)), err(S.attend(q, S.bf16(k), S.bf16(v), scale, see)))
+                w = err((ref, tol + add + rest))
             worst = max(worst, w)
         say(f"worst error / bound {worst:.3f}")
         assert worst <= 1
@@ -197,6 +203,36 @@ def test_scale_strides_hints(duo_lib, fmt):
     one(duo_lib, seqs, 16, 2, 128, 64, fmt, q_scale=60.0)
     for hint in (None, 0, 1, 1000):  # a wrong bound costs time only
         one(duo_lib, seqs, 16, 2, 128, 64, fmt, max_q=hint)
+
+
+@pytest.mark.parametrize("kind", ["keys", "queries", "values", "small values", "large values", "everything"])
+@pytest.mark.parametrize("heads", [2, 16])
+@pytest.mark.parametrize("fmt", FMTS)
+def test_magnitudes(duo_lib, fmt, heads, kind):
+    """Keys, values and queries whose sizes differ by many powers of two, and all values
+    far from 1."""
+    say("chunk magnitudes", fmt, heads, kind)
+    g = torch.Generator().manual_seed(5)
+
+    def spread(x, lo, hi, some):
+        e = torch.randint(lo, hi + 1, (len(x), 1), generator=g).float()
+        x.copy_((x.float() * torch.exp2(torch.where(torch.rand((len(x), 1), generator=g) < some, e, 0.0))).bfloat16())
+
+    def touch(b):
+        if kind in ("keys", "everything"):
+            spread(b.K, -30, 5, 0.1)
+        if kind in ("values", "everything"):
+            spread(b.V, -30, 30, 0.1)
+        if kind == "small values":
+            b.V.mul_(2.0 ** -90)
+            b.V[:40] = 0.0
+        if kind == "large values":
+            b.V.mul_(2.0 ** 70)
+
+    b = Batch(duo_lib, [(60, 700), (9, 90), (70, 70)], heads, 2, 128, 16, fmt, touch=touch)
+    if kind in ("queries", "everything"):
+        spread(b.Q, -30, 6, 0.3)
+    b.check(b.run())
 
 
 @pytest.mark.parametrize("fmt", FMTS)
