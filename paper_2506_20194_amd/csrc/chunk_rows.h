@@ -19,12 +19,12 @@
 // everything that they meet: a code of 4 bits times a scale (three bits times eight) is exact in it, one
 // of 8 bits is rounded to 2^-12 of itself (bf16 would cost 2^-9: an error of the output of 0.0031 and, in
 // 4 bits, 0.0048 of its root mean square, where the plain form has 0.0017).  fp16's range is made to
-// do by powers of two: a key whose largest number is outside 2^-3 .. 2^15 is brought to 2^14, and its
+// do by powers of two: a key whose largest number is outside 2^-2 .. 2^8 is brought to 2^7, and its
 // scores take the power back; a row of Q likewise; and a token's values, whose power goes into the
 // exponent of its probabilities (the running reference is then one of p |V|, not of p) and out of
 // their sum again.  None of that happens with numbers of ordinary size, so the steps that are dealt out
-// go without it.  What is lost: a token's numbers below 2^-28 of its largest are rounded at 2^-39 of
-// that.
+// go without it.  What is lost: bits of groups of 32 channels whose scale is below 2^-20 of 1 (of the
+// token's largest number, where that is outside the bounds).
 //
 // Blocks cost what they have of keys, and something for their start and end; the count of all
 // blocks is cut into equal shares, one per workgroup, neighbours on one XCD.  A share's end that lies
@@ -153,11 +153,14 @@ __device__ __forceinline__ f16x mma32(const u32x4& a, const u32x4& b, f16x c) {
   __builtin_memcpy(&bv, &b, 16);
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(av, bv, c, 0, 0, 0);
 }
-// The power of two that a group of numbers of at most `top` is divided by to fit fp16: 0 where they do.
-__device__ __forceinline__ int power_of(float top) {
+// The power of two that numbers of at most `top` are divided by so that it lies in [2^lo, 2^hi): 0 where it does.
+__device__ __forceinline__ int power_of(float top, int lo, int hi) {
   const int e = (int)(__float_as_uint(top) >> 23) - 127;
-  return top == 0.f || e == 128 || (e >= -3 && e < 15) ? 0 : e - 14;
+  return top == 0.f || e == 128 || (e >= lo && e < hi) ? 0 : e - (hi - 1);
 }
+// Keys and values in fp16 are 2^6 of themselves, for more small ones: those of a token reach from 2^-2 to 2^8 (24 times a
+// scale of 4 bits is then below 2^16).
+constexpr int kRowsBoost = 6, kRowsLo = -2, kRowsHi = 8;
 
 template <int FMT, int HD>
 struct RowsGeo {
@@ -351,10 +354,14 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
       }
       lost = __any(lost);
     }
-    // first of this wave's 16 keys of tile t, as far as there are any
-    auto run_of = [&](int t) { return min(place(t) * KB + 16 * wave, (len - 1) & ~15); };
-    auto page_of = [&](int t) {  // tiles in order
-      const int pg = run_of(t) >> a.kv.shift;
+    // this wave's 16 keys of a tile (as far as there are any): their page's block, where they begin in it, and
+    // the last that there is
+    struct Run {
+      const uint8_t* block;
+      int in, left;
+    };
+    auto run_at = [&](int t) {  // tiles in order
+      const int key = min(place(t) * KB + 16 * wave, (len - 1) & ~15), pg = key >> a.kv.shift;
       if (pg >= win + 64) {
         if (pg >= win + 128) {  // the first tile behind the sinks
           win = (pg & ~3) - 64;
@@ -364,45 +371,62 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         win += 64;
         nid = ids(win + 64);
       }
-      return __builtin_amdgcn_readlane(pid, pg - win);
+      const uint32_t id = (uint32_t)__builtin_amdgcn_readlane(pid, pg - win);
+      return Run{block0 + (uint64_t)id * page_bytes, key & page_mask, len - 1 - key};
     };
-    // this wave's 16 rows of tile t, which lie in page id: where they begin, rows past the last as the last
-    auto rows_at = [&](int t, int id, int which) {
-      return block0 + (uint64_t)(uint32_t)id * page_bytes + kv_rows_at<FMT, HD>(which, a.kv.shift) + (run_of(t) & page_mask) * RB;
-    };
-    auto issue = [&](int t, int id, auto which_c, const void* to) __attribute__((always_inline)) {
+    // where a lane's 16 bytes come from; the same for all loads of V's 16 rows, and of codes (16 rows of 32
+    // bytes fill half a load: the others again)
+    uint32_t k_off[NL], v_off[NL];
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int r = ln / CH, c = ln % CH;
+      k_off[i] = G::QUANT ? ln * 16 % (16 * RB) : r * RB + 16 * kswz(i * RPL + r, c);
+      v_off[i] = G::QUANT ? ln * 16 % (16 * RB) : r * RB + 16 * vswz(r, c);
+    }
+    auto issue = [&](const Run& run, auto which_c, const void* to) __attribute__((always_inline)) {
       constexpr int which = decltype(which_c)::value;
       const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_addr(to));
-      const uint8_t* const at = rows_at(t, id, which);
-      const int left = len - 1 - run_of(t), x = anew(lane);
-      uint32_t off[NL];
+      const uint8_t* const at = run.block + (kv_rows_at<FMT, HD>(which, a.kv.shift) + run.in * RB);
+      if (run.left >= 15) {
+        if constexpr (NL > 1)
+          dma16_run<NL>(at, which ? v_off : k_off, lds);
+        else
+          dma16(at, which ? v_off[0] : k_off[0], lds);
+        return;
+      }
+      const int x = anew(lane);  // rows past the last as the last
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         if constexpr (!G::QUANT) {
           const int r = i * RPL + x / CH, c = x % CH;
-          off[i] = min(r, left) * RB + 16 * (which ? vswz(r, c) : kswz(r, c));
-        } else {  // bytes in order (16 rows of 32 bytes fill half a load: the others again)
+          dma16(at, min(r, run.left) * RB + 16 * (which ? vswz(r, c) : kswz(r, c)), lds + i * 1024);
+        } else {
           const int e = (i * 1024 + x * 16) % (16 * RB);
-          off[i] = min(e / RB, left) * RB + e % RB;
+          dma16(at, min(e / RB, run.left) * RB + e % RB, lds + i * 1024);
         }
       }
-#pragma unroll
-      for (int i = 0; i < NL; ++i) dma16(at, off[i], lds + i * 1024);
     };
     constexpr std::integral_constant<int, 0> kK{};
     constexpr std::integral_constant<int, 1> kV{};
     // ---- 8 and 4 bits
     uint8_t* const stage = lsm + 4 * TILE * 16 + wave * 2 * G::STAGE;  // codes of K, then of V
-    // a lane looks after the scales of one key of the tile
+    // A thread makes numbers of one key of its wave's run and HD / 4 channels, whose scale it loads; a lane also
+    // looks at all scales of one key of the tile, for the powers.
     struct Scales {
       uint32_t w[HD / 64];
     };
-    auto lane_run = [&](int t, int x) { return min(place(t) * KB + (x & 48), (len - 1) & ~15); };
-    auto lane_page = [&](int t) { return __shfl(pid, (lane_run(t, lane) >> a.kv.shift) - win); };  // after page_of(t)
-    auto scales_of = [&](int t, int id, int which) {
-      const int x = anew(lane), run = lane_run(t, x);
-      const uint32_t* const s = (const uint32_t*)(block0 + (uint64_t)(uint32_t)id * page_bytes + kv_scales_at<FMT, HD>(which, a.kv.shift) +
-                                                  ((run & page_mask) + min(x & 15, len - 1 - run)) * KvFmt<FMT>::scales(HD));
+    auto scale_of = [&](const Run& run, int which) {
+      const int x = anew(lane);
+      const uint8_t* const s = run.block + (kv_scales_at<FMT, HD>(which, a.kv.shift) + run.in * KvFmt<FMT>::scales(HD));
+      return *(const uint16_t*)(s + (uint32_t)(min(x >> 2, run.left) * KvFmt<FMT>::scales(HD) + (HD == 128 ? x & 3 : x >> 1 & 1) * 2));
+    };
+    auto scales_of = [&](const Run& run, int t, int which) {  // after run_at(t)
+      const int x = anew(lane), key = min(place(t) * KB + (a.kv.shift < 6 ? x & 48 : 0), (len - 1) & ~15);
+      const uint8_t* block = run.block;
+      if (a.kv.shift < 6) block = block0 + (uint64_t)(uint32_t)__shfl(pid, (key >> a.kv.shift) - win) * page_bytes;
+      const uint32_t* const s = (const uint32_t*)(block + (kv_scales_at<FMT, HD>(which, a.kv.shift) +
+                                                           ((key & page_mask) + min(a.kv.shift < 6 ? x & 15 : x, len - 1 - key)) *
+                                                               KvFmt<FMT>::scales(HD)));
       Scales r;
       if constexpr (HD == 128) {
         const uint2 v = *(const uint2*)s;
@@ -423,22 +447,40 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
       if constexpr (G::QUANT) return __uint_as_float(m << 16) * KvFmt<FMT>::most;
       return 0.f;
     };
+    auto k_power = [&](const Scales& s) { return power_of(most_of(s), kRowsLo, kRowsHi); };
     int e_ref = 0;  // power of two that the outputs are in units of: that of the first tile's values
-    auto v_power = [&](const Scales& s) { return min(max(power_of(ldexpf(most_of(s), -e_ref)), -60), 60); };
-    // a thread takes a key of its wave's run and HD / 4 channels; power: what the numbers are divided by
-    auto convert = [&](const uint8_t* codes, const Scales& scales, int power, u32x4* tile, bool is_v) __attribute__((always_inline)) {
+    auto v_power = [&](const Scales& s) { return min(max(power_of(ldexpf(most_of(s), -e_ref), kRowsLo, kRowsHi), -60), 60); };
+    // does some key's largest scale mean a power, as far as one look can tell (never no for yes)?
+    auto some_power = [&](const Scales& k, const Scales& v) {
+      typedef unsigned short u16v2 __attribute__((ext_vector_type(2)));
+      auto most = [](const Scales& s) {
+        u16v2 m;
+        __builtin_memcpy(&m, &s.w[0], 4);
+        if constexpr (HD == 128) {
+          u16v2 o;
+          __builtin_memcpy(&o, &s.w[HD / 64 - 1], 4);
+          m = __builtin_elementwise_max(m, o);
+        }
+        return (uint32_t)(m[0] > m[1] ? m[0] : m[1]);
+      };
+      if constexpr (G::QUANT) {
+        // scales whose code of most lies within the bounds, bf16 numbers as whole ones
+        constexpr uint32_t lo = ((127u + kRowsLo) << 7) - (KvFmt<FMT>::most == 127 ? 6 << 7 : 2 << 7);
+        constexpr uint32_t hi = ((127u + kRowsHi) << 7) - (KvFmt<FMT>::most == 127 ? 7 << 7 : 3 << 7);
+        return __any(most(k) - lo >= hi - lo || most(v) - lo >= hi - lo) != 0;
+      }
+      return false;
+    };
+    // power: what the lane's key is divided by, where odd
+    auto convert = [&](const uint8_t* codes, uint16_t scale, bool odd, int power, u32x4* tile, bool is_v) __attribute__((always_inline)) {
       if constexpr (G::QUANT) {
         constexpr int NC = HD / 4;  // channels
-        constexpr float bias = KvFmt<FMT>::bias;
+        typedef _Float16 f16v2 __attribute__((ext_vector_type(2)));
         const int x = anew(lane), ckey = x >> 2, cpart = x & 3, key = 16 * wave + ckey;
-        uint32_t sw = (uint32_t)__shfl((int)scales.w[0], key);
-        if constexpr (HD == 128) {
-          const uint32_t s1 = (uint32_t)__shfl((int)scales.w[HD / 64 - 1], key);
-          sw = cpart & 2 ? s1 : sw;
-        }
-        const int by_power = __shfl(power, key);
-        const float s = ldexpf((HD == 128 ? cpart & 1 : cpart >> 1) ? __uint_as_float(sw & 0xffff0000u) : __uint_as_float(sw << 16), -by_power);
-        const float off = s * -bias;
+        int up = kRowsBoost;
+        if (odd) up -= __shfl(power, key);
+        const _Float16 s1 = (_Float16)ldexpf(bf16_bits_to_f32(scale), up);
+        const f16v2 s = {s1, s1};
         const uint8_t* const at = codes + ckey * RB + cpart * (RB / 4);
         uint32_t w[RB / 16];
 #pragma unroll
@@ -446,33 +488,56 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
           const uint2 two = *(const uint2*)(at + 4 * i);
           w[i] = two.x, w[i + 1] = two.y;
         }
+        auto as_h = [](uint32_t u) {
+          f16v2 h;
+          __builtin_memcpy(&h, &u, 4);
+          return h;
+        };
 #pragma unroll
         for (int j = 0; j < NC / 8; ++j) {
-          float v[8];
-          if constexpr (FMT == DUO_KV_I8) {
+          u32x4 v;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = (float)(w[2 * j + (e >> 2)] >> (8 * (e & 3)) & 255u);
-          } else {
-            const uint32_t even = w[j] & 0x0f0f0f0fu, odd = w[j] >> 4 & 0x0f0f0f0fu;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = (float)((e & 1 ? odd : even) >> (8 * (e >> 1)) & 255u);
+          for (int e = 0; e < 4; ++e) {
+            f16v2 h;
+            if constexpr (FMT == DUO_KV_I8) {
+              // a byte b below 0x64 is the number 1024 + b
+              const f16v2 excess = {(_Float16)-1152.f, (_Float16)-1152.f};
+              h = (as_h(__builtin_amdgcn_perm(0x64646464u, w[2 * j + (e >> 1)], e & 1 ? 0x04030402u : 0x04010400u)) + excess) * s;
+            } else {
+              // a nibble n in bits 6 to 9 of 0x4c00 is 16 + n, and 24 s is exact; channels e and e + 4 together
+              const uint32_t n = e == 0 ? w[j] << 6 : e == 1 ? w[j] << 2 : e == 2 ? w[j] >> 2 : w[j] >> 6;
+              h = __builtin_elementwise_fma(as_h((n & 0x03c003c0u) | 0x4c004c00u), s, s * (_Float16)-24.f);
+            }
+            uint32_t two;
+            __builtin_memcpy(&two, &h, 4);
+            v[e] = two;
           }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e], s, off);  // (code - bias) s, exactly
           const int c = cpart * (NC / 8) + j;
-          tile[key * CH + (is_v ? vswz(key, c) : kswz(key, c))] = u32x4{pack_two<F16>(v[0], v[1]), pack_two<F16>(v[2], v[3]),
-                                                                        pack_two<F16>(v[4], v[5]), pack_two<F16>(v[6], v[7])};
+          tile[key * CH + (is_v ? vswz(key, c) : kswz(key, c))] = v;
         }
       }
     };
-    Scales ks = {}, vs = {}, vs1 = {};  // of the next codes to become numbers, and of the V after
-    // powers of the lane's key and value in this tile, the next and the one after
+    // Of the next codes to become numbers, and of the V after: scales.
+    uint16_t ks = 0, vs = 0, vs1 = 0;
+    Scales kall = {}, vall = {};
+    // powers of the lane's key and value in this tile, the next and the one after; are there any?
     int kp = 0, kp1 = 0, kp2 = 0, vp = 0, vp1 = 0, vp2 = 0;
-    bool calm = true;  // there are none in this tile and the next
+    bool odd = false, odd1 = false, odd2 = false, calm = true;
+    auto powers = [&](int* k, int* v) {
+      bool some = e_ref != 0 || some_power(kall, vall);
+      if (some) {
+        *k = k_power(kall), *v = v_power(vall);
+        some = __any((*k | *v) != 0);
+      } else {
+        *k = *v = 0;
+      }
+      return some;
+    };
     auto next = [&]() __attribute__((always_inline)) {  // on to the next tile
       if constexpr (G::QUANT) {
         kp = kp1, kp1 = kp2, vp = vp1, vp1 = vp2;
-        calm = !__any((kp | kp1 | vp | vp1) != 0);
+        odd = odd1, odd1 = odd2;
+        calm = !(odd | odd1);
       }
     };
     auto tile_of = [&](int i, int which) { return sm + ((i & 1) * 2 + which) * TILE; };  // i: of the tiles here
@@ -488,48 +553,57 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
       return Row{qi, row - qi * a.hg};
     };
     const int pos_lo = pos0 + by(min(row0, rows - 1), a), pos_hi = pos0 + by(min(row0 + 31, rows - 1), a);  // of this wave
-    int id_v = 0;  // page of the tile whose V comes next
+    Run run_v = {};  // of the tile whose V comes next
     if (n) {
-      const int id0 = page_of(t0), lane0 = G::QUANT ? lane_page(t0) : 0;
-      const int id1 = n > 1 ? page_of(t0 + 1) : 0, lane1 = G::QUANT && n > 1 ? lane_page(t0 + 1) : 0;
-      id_v = id1;
+      const Run run0 = run_at(t0);
       if constexpr (!G::QUANT) {
-        issue(t0, id0, kK, mine_of(0, 0));
-        if (n > 1) issue(t0 + 1, id1, kK, mine_of(1, 0));
-        issue(t0, id0, kV, mine_of(0, 1));
+        issue(run0, kK, mine_of(0, 0));
+        if (n > 1) {
+          run_v = run_at(t0 + 1);
+          issue(run_v, kK, mine_of(1, 0));
+        }
+        issue(run0, kV, mine_of(0, 1));
       } else {
         uint8_t* const k1 = (uint8_t*)tile_of(1, 1) + wave * G::STAGE;  // the second K's codes: V's second tile comes later
-        Scales ks1 = {};
-        issue(t0, id0, kK, stage);
-        issue(t0, id0, kV, stage + G::STAGE);
-        ks = scales_of(t0, lane0, 0), vs = scales_of(t0, lane0, 1);
+        issue(run0, kK, stage);
+        issue(run0, kV, stage + G::STAGE);
+        ks = scale_of(run0, 0), vs = scale_of(run0, 1);
+        kall = scales_of(run0, t0, 0), vall = scales_of(run0, t0, 1);
+        Scales kall1 = {}, vall1 = {};
+        uint16_t ks1 = 0;
         if (n > 1) {
-          issue(t0 + 1, id1, kK, k1);
-          ks1 = scales_of(t0 + 1, lane1, 0), vs1 = scales_of(t0 + 1, lane1, 1);
+          run_v = run_at(t0 + 1);
+          issue(run_v, kK, k1);
+          ks1 = scale_of(run_v, 0), vs1 = scale_of(run_v, 1);
+          kall1 = scales_of(run_v, t0 + 1, 0), vall1 = scales_of(run_v, t0 + 1, 1);
         }
         wait_vm<0>();
         asm volatile("" ::: "memory");
-        {
-          float m = most_of(vs);
+        if (some_power(kall, vall)) {
+          float m = most_of(vall);
 #pragma unroll
           for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
-          e_ref = same(power_of(m));
+          e_ref = same(power_of(m, kRowsLo, kRowsHi));
         }
-        kp = power_of(most_of(ks)), kp1 = power_of(most_of(ks1));
-        vp = v_power(vs), vp1 = v_power(vs1);
-        calm = !__any((kp | kp1 | vp | vp1) != 0);
-        convert(stage, ks, kp, tile_of(0, 0), false);
-        convert(stage + G::STAGE, vs, vp + e_ref, tile_of(0, 1), true);
-        if (n > 1) convert(k1, ks1, kp1, tile_of(1, 0), false);
+        odd = powers(&kp, &vp);
+        convert(stage, ks, odd, kp, tile_of(0, 0), false);
+        convert(stage + G::STAGE, vs, odd | (e_ref != 0), vp + e_ref, tile_of(0, 1), true);
+        if (n > 1) {
+          kall = kall1, vall = vall1;
+          odd1 = powers(&kp1, &vp1);
+          convert(k1, ks1, odd1, kp1, tile_of(1, 0), false);
+        }
+        calm = !(odd | odd1);
         wait_lds<0>();
         vs = vs1;
+        const Run run1 = run_v;
         if (n > 2) {
-          const int id2 = page_of(t0 + 2), lane2 = lane_page(t0 + 2);
-          issue(t0 + 2, id2, kK, stage);
-          ks = scales_of(t0 + 2, lane2, 0), vs1 = scales_of(t0 + 2, lane2, 1);
-          id_v = id2;
+          run_v = run_at(t0 + 2);
+          issue(run_v, kK, stage);
+          ks = scale_of(run_v, 0), vs1 = scale_of(run_v, 1);
+          kall = scales_of(run_v, t0 + 2, 0), vall = scales_of(run_v, t0 + 2, 1);
         }
-        if (n > 1) issue(t0 + 1, id1, kV, stage + G::STAGE);
+        if (n > 1) issue(run1, kV, stage + G::STAGE);
       }
     }
     u32x4 qa[KS];
@@ -556,12 +630,19 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
           top = max(top, max(w & 0xffffu, w >> 16));
         }
       const auto x = __builtin_amdgcn_permlane32_swap(top, top, false, false);
-      q_power = power_of(__uint_as_float(max(x[0], x[1]) << 16));
+      q_power = power_of(__uint_as_float(max(x[0], x[1]) << 16), -3, 15);
 #pragma unroll
       for (int c = 0; c < KS; ++c)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           qa[c][j] = pack_two<F16>(ldexpf(__uint_as_float(qa[c][j] << 16), -q_power), ldexpf(__uint_as_float(qa[c][j] & 0xffff0000u), -q_power));
+      if constexpr (FMT == DUO_KV_I4)  // channels e and e + 4 together, as the keys have them
+#pragma unroll
+        for (int c = 0; c < KS; ++c) {
+          const u32x4 v = qa[c];
+          qa[c] = u32x4{(v[0] & 0xffffu) | v[2] << 16, v[0] >> 16 | (v[2] & 0xffff0000u), (v[1] & 0xffffu) | v[3] << 16,
+                        v[1] >> 16 | (v[3] & 0xffff0000u)};
+        }
     }
     const bool odd_q = __any(q_power != 0);
     float m = -INFINITY, mc = -INFINITY, l = 0.f;  // reference, times cexp; sum of this half's keys
@@ -775,10 +856,10 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
           }
         }
         float f, units = a.cexp;
-        bool odd = false;  // some key, value or query has a power
+        bool any_power = false;  // of a key, a value or a query
         if constexpr (G::QUANT) {
-          odd = odd_q || !calm;
-          if (odd) {
+          any_power = odd_q | odd;
+          if (any_power) {
             const int from_lane = (u & 1) * 32 + 4 * (anew(lane) >> 5);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -791,7 +872,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         if (refer(sc, &f, units) && u > 0) scale_o(f);
         float sum = probabilities(sc, pf, units);
         if constexpr (G::QUANT)
-          if (odd) {
+          if (any_power) {
             const int from_lane = (u & 1) * 32 + 4 * (anew(lane) >> 5);
             const float base = mc == -INFINITY ? 0.f : base_of();
             sum = 0.f;
@@ -810,32 +891,30 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     auto turn = [&](int i) __attribute__((always_inline)) {
       wait_vm<0>();
       lds_barrier();
+      Run run = run_v;
       if constexpr (!G::QUANT) {
-        int id = 0;
         if (i + 2 < n) {
-          id = page_of(t0 + i + 2);
-          issue(t0 + i + 2, id, kK, mine_of(i, 0));
+          run = run_at(t0 + i + 2);
+          issue(run, kK, mine_of(i, 0));
         }
-        if (i + 1 < n) issue(t0 + i + 1, id_v, kV, mine_of(i + 1, 1));
-        id_v = id;
+        if (i + 1 < n) issue(run_v, kV, mine_of(i + 1, 1));
       } else {
         if (i + 2 < n) {
-          kp2 = power_of(most_of(ks)), vp2 = v_power(vs1);
-          convert(stage, ks, kp2, tile_of(i, 0), false);
+          odd2 = powers(&kp2, &vp2);
+          convert(stage, ks, odd2, kp2, tile_of(i, 0), false);
         }
-        if (i + 1 < n) convert(stage + G::STAGE, vs, vp1 + e_ref, tile_of(i + 1, 1), true);
+        if (i + 1 < n) convert(stage + G::STAGE, vs, odd1 | (e_ref != 0), vp1 + e_ref, tile_of(i + 1, 1), true);
         wait_lds<0>();
         vs = vs1;
-        int id = 0;
         if (i + 3 < n) {
-          id = page_of(t0 + i + 3);
-          const int lp = lane_page(t0 + i + 3);
-          issue(t0 + i + 3, id, kK, stage);
-          ks = scales_of(t0 + i + 3, lp, 0), vs1 = scales_of(t0 + i + 3, lp, 1);
+          run = run_at(t0 + i + 3);
+          issue(run, kK, stage);
+          ks = scale_of(run, 0), vs1 = scale_of(run, 1);
+          kall = scales_of(run, t0 + i + 3, 0), vall = scales_of(run, t0 + i + 3, 1);
         }
-        if (i + 2 < n) issue(t0 + i + 2, id_v, kV, stage + G::STAGE);
-        id_v = id;
+        if (i + 2 < n) issue(run_v, kV, stage + G::STAGE);
       }
+      run_v = run;
     };
     if (n) {
       if constexpr (!G::QUANT) wait_vm<0>();
@@ -869,7 +948,8 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     // ---- out
     const int le = anew(lane);
     const auto rl = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
-    const float sum = __uint_as_float(rl[0]) + __uint_as_float(rl[1]);
+    float sum = __uint_as_float(rl[0]) + __uint_as_float(rl[1]);
+    if (G::QUANT) sum *= (float)(1 << kRowsBoost);  // as the values are
     if (!whole) {
       const int64_t at = (2 * (int64_t)share + (t0 == 0)) * QB;
       if (t0 == 0 && tid == 0) {
@@ -907,7 +987,13 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int g = 0; g < 4; ++g)
-          *(uint2*)(st + (le & 31) * HD * 2 + ((4 * d + g) ^ ((le & 31) & (CH - 1))) * 16 + 8 * (le >> 5)) = y[d][g];
+          if constexpr (FMT == DUO_KV_I4) {  // channels c, c + 4, c + 1, c + 5 with c = 0 or 2
+            uint16_t* const y8 = (uint16_t*)(st + (le & 31) * HD * 2 + ((4 * d + g) ^ ((le & 31) & (CH - 1))) * 16) + 2 * (le >> 5);
+            y8[0] = (uint16_t)y[d][g].x, y8[4] = (uint16_t)(y[d][g].x >> 16);
+            y8[1] = (uint16_t)y[d][g].y, y8[5] = (uint16_t)(y[d][g].y >> 16);
+          } else {
+            *(uint2*)(st + (le & 31) * HD * 2 + ((4 * d + g) ^ ((le & 31) & (CH - 1))) * 16 + 8 * (le >> 5)) = y[d][g];
+          }
       wait_lds<0>();
 #pragma unroll
       for (int i = 0; i < 32 / RPL; ++i) {
@@ -922,11 +1008,12 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          uint16_t* yp = y0 + 32 * d + 8 * g;
+          constexpr bool I4 = FMT == DUO_KV_I4;
+          uint16_t* yp = y0 + 32 * d + 8 * g - (I4 ? 2 * (le >> 5) : 0);
           yp[0] = (uint16_t)y[d][g].x;
-          yp[1] = (uint16_t)(y[d][g].x >> 16);
-          yp[2] = (uint16_t)y[d][g].y;
-          yp[3] = (uint16_t)(y[d][g].y >> 16);
+          yp[I4 ? 4 : 1] = (uint16_t)(y[d][g].x >> 16);
+          yp[I4 ? 1 : 2] = (uint16_t)y[d][g].y;
+          yp[I4 ? 5 : 3] = (uint16_t)(y[d][g].y >> 16);
         }
     }
   }
@@ -935,7 +1022,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
 // Joins the parts of the block that begins in share blockIdx.x, if it ends in another one: its own
 // part (the second of its two places), then the first places of the shares after it.  HD / 4 threads
 // per row, blockIdx.y counts the rows by the 1024 / HD that a workgroup takes.
-template <int HD>
+template <int HD, bool I4>
 __global__ __launch_bounds__(256) void rows_join_kernel(RowsArgs a) {
   constexpr int T = HD / 4;
   const RowsTask task = a.tasks[blockIdx.x];
@@ -961,7 +1048,11 @@ __global__ __launch_bounds__(256) void rows_join_kernel(RowsArgs a) {
   const bool none = task.pos0 + qi < 0;
   const uint2 two = none ? make_uint2(0, 0) : make_uint2(pack_bf16(y[0] / sum, y[1] / sum), pack_bf16(y[2] / sum, y[3] / sum));
   uint16_t* const o = a.O + (int64_t)(task.q0 + qi) * a.ldo + (int64_t)(task.head0 + h) * HD + d;
-  if (a.vec) {
+  if (I4) {  // four of eight channels: c, c + 4, c + 1, c + 5 with c = 0 or 2
+    uint16_t* const o8 = o - (d & 4 ? 2 : 0);
+    o8[0] = (uint16_t)two.x, o8[4] = (uint16_t)(two.x >> 16);
+    o8[1] = (uint16_t)two.y, o8[5] = (uint16_t)(two.y >> 16);
+  } else if (a.vec) {
     *(uint2*)o = two;
   } else {
     o[0] = (uint16_t)two.x, o[1] = (uint16_t)(two.x >> 16);

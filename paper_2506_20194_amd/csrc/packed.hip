@@ -596,11 +596,13 @@ duo_status chunk_rows_run(const ChunkCall& c, int64_t least, void* ws, hipStream
     constexpr int FMT = decltype(fmt)::value, HD = decltype(dim)::value;
     constexpr int lds = RowsGeo<FMT, HD>::LDS;
     const auto kern = rows_kernel<FMT, HD>;
+    if (FMT != DUO_KV_BF16) a.cexp = std::max(std::ldexp(a.cexp, -kRowsBoost), 1.4e-45f);  // never 0, as above
     if (duo_status st = set_max_lds((const void*)kern, lds); st != DUO_OK) return st;
     hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(256), lds, s, a);
     DUO_LAUNCH_CHECK();
     if (wgs > 1) {
-      hipLaunchKernelGGL(rows_join_kernel<HD>, dim3((unsigned)wgs, kRowsQB * HD / 1024), dim3(256), 0, s, a);
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(rows_join_kernel<HD, FMT == DUO_KV_I4>), dim3((unsigned)wgs, kRowsQB * HD / 1024), dim3(256),
+                         0, s, a);
       DUO_LAUNCH_CHECK();
     }
     return DUO_OK;
