@@ -240,31 +240,50 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
       }
       p.hs = same((int)rows_div(u, each));
       u = same(u - p.hs * each);
-      int lo = 0, hi = q.nb - 1;
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (same((int)(q.upto(mid, a) <= u)))
-          lo = mid;
-        else
-          hi = mid - 1;
-      }
+      // the block: by the root of the count (or its even part), put right by whole numbers
+      const double b = (double)q.first + kRowsCost + 0.5 * a.qpb, v = (double)u;
+      double x = (sqrt(b * b + 2.0 * a.qpb * v) - b) / a.qpb;
+      const int64_t even = q.upto(q.linear, a);
+      if (u >= even) x = (double)q.linear + (double)(u - even) / ((double)q.most + kRowsCost);
+      int lo = same(min(max((int)x, 0), q.nb - 1));
+      while (lo > 0 && same((int)(q.upto(lo, a) > u))) --lo;
+      while (lo < q.nb - 1 && same((int)(q.upto(lo + 1, a) <= u))) ++lo;
       p.qb = lo;
       p.at = same(u - q.upto(lo, a));
       return p;
     }
   };
-  auto near = [](int c) { return min(kRowsSnap, c / 2); };
-  auto snapped = [&](int64_t u) {
-    if (u >= total) return total;
-    const RowsAt p = locate(u);
-    const int c = seq_of(p.s).cost(p.qb, a);
+  auto near = [&](int c) { return (int)min((int64_t)min(kRowsSnap, c / 2), size / 2); };
+  // a place in a block moved to the block's edge that is near, if any
+  auto snap = [&](int64_t u, const RowsAt& p, int c) {
     return same(p.at <= near(c) ? u - p.at : c - p.at <= near(c) ? u - p.at + c : u);
   };
-  int64_t u = snapped(same(begin(share)));
-  const int64_t u1 = snapped(same(begin(share + 1)));
-  if (u >= u1) return;
+  int64_t u1 = same(begin(share + 1));
+  if (u1 < total) {
+    const RowsAt e = locate(u1);
+    u1 = snap(u1, e, seq_of(e.s).cost(e.qb, a));
+  }
+  int64_t u = same(begin(share));
   RowsAt p = locate(u);
   RowsSeq q = seq_of(p.s);  // of the next block
+  auto advance = [&](auto load) {  // to the block behind this one, which there is
+    p.at = 0;
+    if (++p.qb < q.nb) return;
+    p.qb = 0;
+    if (++p.hs < nhs) return;
+    p.hs = 0;
+    do
+      q = load(++p.s);
+    while (q.nb == 0);
+  };
+  {
+    const int c = q.cost(p.qb, a);
+    const int64_t to = snap(u, p, c);
+    p.at = same(p.at + to - u);
+    u = to;
+    if (u >= u1) return;
+    if (p.at == c) advance(seq_of);
+  }
 
   while (u < u1) {
     const int cost = q.cost(p.qb, a);
@@ -276,19 +295,8 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     const int len = same(q.len), pos0 = same(len - q.lq + qi0);  // position of the block's first query
     const int32_t* const pages = a.table + same((int64_t)p.s * a.ldt);
     const int seq_q0 = same(q.q0);
-    // on to the next block
     u = same(block + to_at);
-    p.at = 0;
-    if (to_at == cost && ++p.qb == q.nb) {
-      p.qb = 0;
-      if (++p.hs == nhs) {
-        p.hs = 0;
-        while (u < u1) {
-          q = load_seq(++p.s);
-          if (q.nb) break;
-        }
-      }
-    }
+    if (u < u1) advance(load_seq);
     // the block's tiles: `sinks` first ones, then those from `from` on; here: [t0, t0 + n)
     const int pos_end = same(pos0 + by(rows - 1, a));  // of its last query
     const int first = same(a.window ? max(pos0 - a.window + 1, 0) : 0);
@@ -330,10 +338,8 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     const uint8_t* const block0 = a.kv.data + kvh * a.kv.block;
     const uint32_t page_bytes = (uint32_t)(a.kv.heads * a.kv.block);
     int win = n ? (place(t0) * KB >> a.kv.shift) & ~3 : 0;
-    auto ids = [&](int pg) {
-      const int v = pages[min(pg + lane, last_page)];
-      return v < 0 || v >= a.kv.pages ? 0 : v;
-    };
+    auto ids = [&](int pg) { return pages[min(pg + lane, last_page)]; };
+    auto page = [&](int v) { return (uint32_t)((uint32_t)v < (uint32_t)a.kv.pages ? v : 0); };  // at most 2^31 - 1 pages
     int pid = 0, nid = 0;
     bool lost = false;  // some query sees a token in a page outside the cache
     if (n) {
@@ -371,7 +377,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         win += 64;
         nid = ids(win + 64);
       }
-      const uint32_t id = (uint32_t)__builtin_amdgcn_readlane(pid, pg - win);
+      const uint32_t id = page(__builtin_amdgcn_readlane(pid, pg - win));
       return Run{block0 + (uint64_t)id * page_bytes, key & page_mask, len - 1 - key};
     };
     // where a lane's 16 bytes come from; the same for all loads of V's 16 rows, and of codes (16 rows of 32
@@ -415,26 +421,31 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     struct Scales {
       uint32_t w[HD / 64];
     };
-    auto scale_of = [&](const Run& run, int which) {
+    const uint32_t v_scales = (uint32_t)KvFmt<FMT>::scales(HD) << a.kv.shift;  // from K's on
+    auto scale_of = [&](const Run& run, uint16_t* k, uint16_t* v) {
       const int x = anew(lane);
-      const uint8_t* const s = run.block + (kv_scales_at<FMT, HD>(which, a.kv.shift) + run.in * KvFmt<FMT>::scales(HD));
-      return *(const uint16_t*)(s + (uint32_t)(min(x >> 2, run.left) * KvFmt<FMT>::scales(HD) + (HD == 128 ? x & 3 : x >> 1 & 1) * 2));
+      const uint8_t* const s = run.block + (kv_scales_at<FMT, HD>(0, a.kv.shift) + run.in * KvFmt<FMT>::scales(HD));
+      const uint32_t off = (uint32_t)(min(x >> 2, run.left) * KvFmt<FMT>::scales(HD) + (HD == 128 ? x & 3 : x >> 1 & 1) * 2);
+      *k = *(const uint16_t*)(s + off);
+      *v = *(const uint16_t*)(s + v_scales + off);
     };
-    auto scales_of = [&](const Run& run, int t, int which) {  // after run_at(t)
+    auto scales_of = [&](const Run& run, int t, Scales* k, Scales* v) {  // after run_at(t)
       const int x = anew(lane), key = min(place(t) * KB + (a.kv.shift < 6 ? x & 48 : 0), (len - 1) & ~15);
+      constexpr int SB = KvFmt<FMT>::scales(HD);
       const uint8_t* block = run.block;
-      if (a.kv.shift < 6) block = block0 + (uint64_t)(uint32_t)__shfl(pid, (key >> a.kv.shift) - win) * page_bytes;
-      const uint32_t* const s = (const uint32_t*)(block + (kv_scales_at<FMT, HD>(which, a.kv.shift) +
-                                                           ((key & page_mask) + min(a.kv.shift < 6 ? x & 15 : x, len - 1 - key)) *
-                                                               KvFmt<FMT>::scales(HD)));
-      Scales r;
-      if constexpr (HD == 128) {
-        const uint2 v = *(const uint2*)s;
-        r.w[0] = v.x, r.w[HD / 64 - 1] = v.y;
-      } else {
-        r.w[0] = *s;
-      }
-      return r;
+      if (a.kv.shift < 6) block = block0 + (uint64_t)page(__shfl(pid, (key >> a.kv.shift) - win)) * page_bytes;
+      const uint8_t* const s = block + (kv_scales_at<FMT, HD>(0, a.kv.shift) + (key & page_mask) * SB);
+      const uint32_t off = (uint32_t)(min(a.kv.shift < 6 ? x & 15 : x, len - 1 - key) * SB);
+      auto load = [&](const uint8_t* at, Scales* r) {
+        if constexpr (HD == 128) {
+          const uint2 w = *(const uint2*)(at + off);
+          r->w[0] = w.x, r->w[HD / 64 - 1] = w.y;
+        } else {
+          r->w[0] = *(const uint32_t*)(at + off);
+        }
+      };
+      load(s, k);
+      load(s + v_scales, v);
     };
     // the largest number that the key's codes can stand for (a scale that is NaN aside)
     auto most_of = [&](const Scales& s) {
@@ -567,15 +578,15 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         uint8_t* const k1 = (uint8_t*)tile_of(1, 1) + wave * G::STAGE;  // the second K's codes: V's second tile comes later
         issue(run0, kK, stage);
         issue(run0, kV, stage + G::STAGE);
-        ks = scale_of(run0, 0), vs = scale_of(run0, 1);
-        kall = scales_of(run0, t0, 0), vall = scales_of(run0, t0, 1);
+        scale_of(run0, &ks, &vs);
+        scales_of(run0, t0, &kall, &vall);
         Scales kall1 = {}, vall1 = {};
         uint16_t ks1 = 0;
         if (n > 1) {
           run_v = run_at(t0 + 1);
           issue(run_v, kK, k1);
-          ks1 = scale_of(run_v, 0), vs1 = scale_of(run_v, 1);
-          kall1 = scales_of(run_v, t0 + 1, 0), vall1 = scales_of(run_v, t0 + 1, 1);
+          scale_of(run_v, &ks1, &vs1);
+          scales_of(run_v, t0 + 1, &kall1, &vall1);
         }
         wait_vm<0>();
         asm volatile("" ::: "memory");
@@ -600,8 +611,8 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         if (n > 2) {
           run_v = run_at(t0 + 2);
           issue(run_v, kK, stage);
-          ks = scale_of(run_v, 0), vs1 = scale_of(run_v, 1);
-          kall = scales_of(run_v, t0 + 2, 0), vall = scales_of(run_v, t0 + 2, 1);
+          scale_of(run_v, &ks, &vs1);
+          scales_of(run_v, t0 + 2, &kall, &vall);
         }
         if (n > 1) issue(run1, kV, stage + G::STAGE);
       }
@@ -740,7 +751,8 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
       if (masked(u)) {
         // some query may not see some key, and 0 times a number that is not finite would not be 0:
         // such numbers enter as zeros and are added for those who see them
-        uint32_t most = 0;
+        typedef unsigned short u16v2 __attribute__((ext_vector_type(2)));
+        u16v2 most = {0, 0};
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -748,10 +760,12 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const uint32_t w = v[t][d][j] & 0x7fff7fffu;
-              most = max(most, max(w & 0xffffu, w >> 16));
+              u16v2 x;
+              __builtin_memcpy(&x, &w, 4);
+              most = __builtin_elementwise_max(most, x);
             }
         constexpr uint32_t INF = F16 ? 0x7c00u : 0x7f80u;
-        if (__any(most >= INF)) {
+        if (__any(most[0] >= INF || most[1] >= INF)) {
 #pragma unroll
           for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -909,8 +923,8 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         if (i + 3 < n) {
           run = run_at(t0 + i + 3);
           issue(run, kK, stage);
-          ks = scale_of(run, 0), vs1 = scale_of(run, 1);
-          kall = scales_of(run, t0 + i + 3, 0), vall = scales_of(run, t0 + i + 3, 1);
+          scale_of(run, &ks, &vs1);
+          scales_of(run, t0 + i + 3, &kall, &vall);
         }
         if (i + 2 < n) issue(run_v, kV, stage + G::STAGE);
       }
