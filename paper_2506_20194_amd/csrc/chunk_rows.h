@@ -40,8 +40,8 @@ using namespace pp;
 
 constexpr int kRowsQB = 128;     // rows of a block
 constexpr int kRowsWg = 512;     // workgroups at most: two on each CU
-constexpr int kRowsCost = 256;   // what a block's start and end cost, in keys
-constexpr int kRowsMin = 256;    // smallest share, in keys
+constexpr int kRowsCost = 128;   // what a block's start and end cost, in keys (256: 0 to 2 us more in short calls)
+constexpr int kRowsMin = 512;    // smallest share, in keys: 16 tokens on 16384, 64 heads on 8, 60 us, 98 with 256
 constexpr int kRowsSnap = 512;   // a share's end moves to a block's end that is no further than this
 
 struct RowsArgs {
@@ -1044,19 +1044,33 @@ __global__ __launch_bounds__(256) void rows_join_kernel(RowsArgs a) {
   if (task.parts == 0 || row >= task.rows) return;
   const int qi = by(row, a), h = row - qi * a.hg;
   auto place = [&](int i) { return (2 * ((int64_t)blockIdx.x + i) + (i == 0)) * kRowsQB + row; };
-  float top = -INFINITY;
-#pragma unroll 4
-  for (int i = 0; i < task.parts; ++i) top = fmaxf(top, a.pml[2 * place(i)]);
-  float sum = 0.f;
+  // eight parts at once, whose outputs, references and sums are all on their way before the first is used
+  float top = -INFINITY, sum = 0.f;
   f4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int i = 0; i < task.parts; ++i) {
-    const float2 ml = *(const float2*)(a.pml + 2 * place(i));
-    const f4 v = *(const f4*)(a.po + place(i) * HD + d);
-    // a part without a finite score holds zeros, or NaN that has to stay
-    const float w = ml.x == -INFINITY ? ml.y : __builtin_amdgcn_exp2f(ml.x - top);
-    sum += w * ml.y;
-    y += v * w;
+  for (int i = 0; i < task.parts; i += 8) {
+    float2 ml[8];
+    f4 v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int64_t at = place(min(i + j, task.parts - 1));
+      ml[j] = *(const float2*)(a.pml + 2 * at);
+      v[j] = *(const f4*)(a.po + at * HD + d);
+    }
+    float most = top;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) most = fmaxf(most, ml[j].x);
+    const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - most);
+    sum *= f;
+    y *= f;
+    top = most;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (i + j >= task.parts) break;
+      // a part without a finite score holds zeros, or NaN that has to stay
+      const float w = ml[j].x == -INFINITY ? ml[j].y : __builtin_amdgcn_exp2f(ml[j].x - top);
+      sum += w * ml[j].y;
+      y += v[j] * w;
+    }
   }
   if (h >= task.heads) return;
   const bool none = task.pos0 + qi < 0;

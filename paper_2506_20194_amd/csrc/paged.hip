@@ -76,8 +76,10 @@ constexpr int kMinShare = 8;
 constexpr int kShort = 4;
 constexpr int kMinKeys = 32;    // tokens of the smallest tile
 // Chunks: sequences of no more rows (new tokens times heads of a group) are done here, the others by
-// chunk_rows_run.
-constexpr int kFewRows = 32;
+// chunk_rows_run, which reads the cache once for 128 rows, where here 16 do, but has numbers to make of
+// codes.  32 sequences of 2048 tokens, 64 heads on 8, 4 new tokens (32 rows): 47 us here and 64 there in 16 bits,
+// 47 and 70 in 8; 8 new tokens (64 rows): 84 and 68, 82 and 78, in 4 bits 72 and 78; 12: 123 and 74, 118 and 83.
+constexpr int few_rows(int format) { return format == DUO_KV_BF16 ? 32 : 64; }
 
 template <int FMT, int HD>
 struct PagedGeo {
@@ -1123,13 +1125,14 @@ duo_status duo_attention_chunk(const void* Q, int64_t ldq, int64_t total_q, cons
   ch.cu_q = cu_q, ch.total_q = (int)total_q;
   ch.window = window <= max_len ? (int)window : 0;  // a longer one hides nothing
   ch.sinks = (int)std::min(sinks, max_len);
-  const bool many = std::min(max_q, total_q) * group > kFewRows, few = !many || nseq > 1;
-  ch.most = many ? kFewRows : INT64_MAX;
+  const int most = few_rows(cache->format);
+  const bool many = std::min(max_q, total_q) * group > most, few = !many || nseq > 1;
+  ch.most = many ? most : INT64_MAX;
   if (many) {
     const ChunkCall c = {Q, O, ldq, ldo, total_q, nseq, max_len, heads, ldt, cache, g, table, lens, cu_q, ch.window, ch.sinks,
                          cexp, flip};
     uint8_t* const rows_ws = (uint8_t*)ws + (need - chunk_rows_ws_bytes(total_q, nseq, heads, g.heads, hd, max_len));
-    if (duo_status st = chunk_rows_run(c, few ? kFewRows : 0, rows_ws, s); st != DUO_OK) return st;
+    if (duo_status st = chunk_rows_run(c, few ? most : 0, rows_ws, s); st != DUO_OK) return st;
     if (!few) return DUO_OK;
   }
   ch.by_shift = 0;
