@@ -589,6 +589,7 @@ duo_status chunk_rows_run(const ChunkCall& c, int64_t least, void* ws, hipStream
   a.vec = c.ldo % 8 == 0 && aligned16(c.O);
   const int hd = c.cache->head_dim;
   const int64_t wgs = rows_wgs(c.total_q, c.nseq, a.group, c.geo.heads, c.max_len);
+  a.deal = wgs % (c.geo.heads * a.nsub) == 0 ? (int)(wgs / (c.geo.heads * a.nsub)) : 0;
   a.tasks = (RowsTask*)ws;
   a.po = (float*)((uint8_t*)ws + align_up(wgs * sizeof(RowsTask)));
   a.pml = a.po + 2 * wgs * kRowsQB * hd;
