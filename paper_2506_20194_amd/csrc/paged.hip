@@ -62,6 +62,7 @@ namespace {
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) % 16) == 0; }
 
 constexpr int kCols = 16;       // query heads per row
+constexpr int kWide = 64;       // columns of a row of new tokens, by sets of kCols
 constexpr int kMaxWg = 1024;    // workgroups of a launch, at most
 // What a row's start and end cost, in tiles.  Eight sequences of 1 to 131072 tokens in 4 bits, 64
 // heads on 8: 73 us with 4, 55 with 8, 51 with 10 and 14; 48 of up to 8192 in 8 bits: 51, 46, 47, 47.
@@ -76,10 +77,11 @@ constexpr int kMinShare = 8;
 constexpr int kShort = 4;
 constexpr int kMinKeys = 32;    // tokens of the smallest tile
 // Chunks: sequences of no more rows (new tokens times heads of a group) are done here, the others by
-// chunk_rows_run, which reads the cache once for 128 rows, where here 16 do, but has numbers to make of
-// codes.  32 sequences of 2048 tokens, 64 heads on 8, 4 new tokens (32 rows): 47 us here and 64 there in 16 bits,
-// 47 and 70 in 8; 8 new tokens (64 rows): 84 and 68, 82 and 78, in 4 bits 72 and 78; 12: 123 and 74, 118 and 83.
-constexpr int few_rows(int format) { return format == DUO_KV_BF16 ? 32 : 64; }
+// chunk_rows_run, whose blocks of 128 rows share a tile among their waves, but take longer to begin.  Of 4
+// sequences of 8192 tokens, 32 heads on 8, 8 new ones (32 rows): 41 us here and 52 there in 16 bits, 40 and 56 in 8; one of
+// 16384, 64 on 8, 8 (64 rows): 44 and 45, 46 and 54.  32 of 2048, 64 on 8, 8: 96 and 72, 109 and 78; 4: 67 and 65,
+// 66 and 68.  (With a unit of its own for every 16 columns 67 were 47, and 96 at 6 new tokens 135.)
+constexpr int kFewRows = 64;
 
 template <int FMT, int HD>
 struct PagedGeo {
@@ -115,8 +117,10 @@ struct Task {
 
 // What new tokens add to a call (CHUNK below).  A column is then a pair of one of a sequence's
 // new tokens and a query head of the K/V head's group, the heads of a token side by side, and
-// a row up to kCols (with PAIR 8) of them; all rows of a sequence have the tiles that any of its
-// new tokens sees: those of the sinks, then from the window of the first of them on.
+// a row up to kWide (with PAIR 8) of them: sets of kCols, which the waves share out, so that two or
+// four sets' waves read a tile at nearly the same time and the cache comes from HBM once.  All
+// rows of a sequence have the tiles that any of its new tokens sees: those of the sinks, then from
+// the window of the first of them on.
 template <bool CHUNK>
 struct ChunkArgs {};
 template <>
@@ -165,10 +169,10 @@ __device__ inline Seq seq_tiles(int len, int lq, int q0, const ChunkArgs<true>& 
 struct Units {
   int tiles, cost, units;
   bool quad;
-  __device__ Units(int tiles, int rows, const PagedWork& w) : tiles(tiles) {
-    quad = w.many && tiles <= kShort;
+  __device__ Units(int tiles, int rows, int sets, const PagedWork& w) : tiles(tiles) {
+    quad = w.many && tiles <= kShort && sets == 1;
     units = tiles == 0 ? 0 : quad ? (rows + 3) / 4 : rows;
-    cost = (quad ? 4 * tiles : tiles) + kRowCost;
+    cost = (quad ? 4 * tiles : tiles * sets) + kRowCost;
   }
 };
 
@@ -204,6 +208,14 @@ __device__ inline void load_seq(const PagedWork& w, const ChunkArgs<true>& c, in
   const int a = within(c.cu_q[s], c.total_q), b = within(c.cu_q[s + 1], c.total_q);
   q->len = seq_len(w, s), q->lq = max(b - a, 0), q->q0 = a;
 }
+// Sets of columns that a sequence's rows have.
+template <int COLS>
+__device__ inline int sets_of(const ChunkArgs<false>&, int, int) { return 1; }
+template <int COLS>
+__device__ inline int sets_of(const ChunkArgs<true>&, int lq, int group) {
+  const int n = lq * group;
+  return COLS < kWide || n <= kCols ? 1 : n <= 2 * kCols ? 2 : 4;
+}
 template <int COLS>
 __device__ inline int rows_of(const PagedWork& w, const ChunkArgs<false>&, int, int, int) { return w.rows; }
 template <int COLS>
@@ -224,7 +236,8 @@ __device__ inline int64_t count_rows(const PagedWork& w, const C& c, int group, 
     const int64_t s = (int64_t)lane * w.per + i;
     *q = Seq{};
     if (s < w.nseq) load_seq(w, c, (int)s, q);
-    const Units x(seq_tiles<KEYS>(q->len, q->lq, q->q0, c).tiles, rows_of<COLS>(w, c, q->lq, group, kv_heads), w);
+    const Units x(seq_tiles<KEYS>(q->len, q->lq, q->q0, c).tiles, rows_of<COLS>(w, c, q->lq, group, kv_heads),
+                  sets_of<COLS>(c, q->lq, group), w);
     n += (int64_t)x.cost * x.units;
   }
   // running sum over the lanes: within rows of 16, then over the rows
@@ -324,7 +337,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
   const int l16 = lane & 15, g = lane >> 4;
   const int col = PAIR ? l16 & 7 : l16, half = PAIR ? l16 >> 3 : 0;  // this lane's head, and half of the keys
 
-  constexpr int COLS = PAIR ? 8 : kCols;  // of a row (CHUNK)
+  constexpr int COLS = PAIR ? 8 : CHUNK ? kWide : kCols;  // of a row (CHUNK)
   Seq mine;
   const int64_t upto = count_rows<KEYS, COLS>(work, ch, group, kv.heads, &mine);
   const Shares shares(lane64(upto, 63), gridDim.x);
@@ -372,7 +385,8 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
   for (int s = at_bucket * work.per; u < u1; ++s) {
     const Seq seq = seq_of(s);
     const int len = seq.len, seq_rows = rows_of<COLS>(work, ch, seq.lq, group, kv.heads);
-    const Units x(seq.tiles, seq_rows, work);
+    const int sets = sets_of<COLS>(ch, seq.lq, group), sets_log = sets >> 1;  // 1, 2 or 4: 0, 1 or 2
+    const Units x(seq.tiles, seq_rows, sets, work);
     const int tiles = x.tiles, cost = x.cost;
     const int64_t start = before;
     before += (int64_t)cost * x.units;
@@ -384,10 +398,10 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
       int row = (int)div64((uint64_t)(u - start), (uint32_t)cost);
       const int at = (int)(u - start - (int64_t)row * cost);
       const int here = (int)min((int64_t)(cost - at), u1 - u);
-      int t0 = max(at - kRowCost, 0), t1 = max(at + here - kRowCost, 0);
+      int t0 = max(at - kRowCost, 0) + sets - 1 >> sets_log, t1 = max(at + here - kRowCost, 0) + sets - 1 >> sets_log;
       const int64_t row_end = u + (cost - at);
       u += here;
-      int t = t0 + wave, step = 4;  // this wave's tiles
+      int t = t0 + (wave >> sets_log), step = 4 >> sets_log;  // this wave's tiles
       if (x.quad) {  // whole in the share that it begins in
         if (at > 0) continue;
         row = 4 * row + wave;
@@ -397,17 +411,25 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
         step = 1;
       }
       if (t0 >= t1) continue;
-      const int h = row % kv.heads, c0 = row / kv.heads * COLS;  // K/V head, first of its query heads (columns)
-      const int nc = CHUNK ? min(COLS, seq.lq * group - c0) : min(cols, group - c0);
+      const int h = row % kv.heads, r0 = row / kv.heads * (CHUNK ? COLS : kCols);  // K/V head, first of its query heads (columns)
+      const int row_nc = CHUNK ? min(COLS, seq.lq * group - r0) : min(cols, group - r0);
+      int c0 = r0, nc = row_nc;  // of this wave's set
+      if (CHUNK && !PAIR) {
+        const int set = wave & (sets - 1);
+        nc = min(row_nc - set * kCols, kCols);
+        c0 += set * kCols;
+        if (nc <= 0) c0 = r0, nc = 1, t = t1;  // no columns: no tiles
+      }
       // where column c's numbers begin in rows of Q or O, and its position (CHUNK)
-      auto column = [&](int c, int64_t ld) {
+      auto column_at = [&](int c, int64_t ld) {  // counted from the sequence's first
         if constexpr (CHUNK) {
-          const int i = by(c0 + c, ch);
-          return (int64_t)(seq.q0 + i) * ld + (h * group + c0 + c - i * group) * HD;
+          const int i = by(c, ch);
+          return (int64_t)(seq.q0 + i) * ld + (h * group + c - i * group) * HD;
         } else {
-          return (int64_t)s * ld + (h * group + c0 + c) * HD;
+          return (int64_t)s * ld + (h * group + c) * HD;
         }
       };
+      auto column = [&](int c, int64_t ld) { return column_at(c0 + c, ld); };
       auto position = [&](int c) {
         if constexpr (CHUNK)
           return len - seq.lq + by(c0 + c, ch);
@@ -882,12 +904,17 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
       }
       if (g == 0) jm[wave][l16] = mc, jl[wave][l16] = l;
       __syncthreads();
-      auto largest = [&](int c) {
+      auto largest = [&](int c, int set) {
+        if constexpr (CHUNK && !PAIR) {
+          float v = jm[set][c];
+          for (int w = set + sets; w < 4; w += sets) v = fmaxf(v, jm[w][c]);
+          return v;
+        }
         float v = fmaxf(fmaxf(jm[0][c], jm[1][c]), fmaxf(jm[2][c], jm[3][c]));
         if constexpr (PAIR) v = fmaxf(v, fmaxf(fmaxf(jm[0][c + 8], jm[1][c + 8]), fmaxf(jm[2][c + 8], jm[3][c + 8])));
         return v;
       };
-      const float top = largest(col);
+      const float top = largest(col, wave & (sets - 1));
       {
         const float f = mc == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - top);
         float* y = (float*)sK + l16 * G::OLD + 4 * g;
@@ -903,15 +930,17 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
       const bool whole = t0 == 0 && t1 == tiles;
       float* const ps = part + (2 * (int64_t)blockIdx.x + (t0 == 0)) * cols * (HD + 2);
       if (!whole && t0 == 0 && tid == 0) {
-        tasks[blockIdx.x] = Task{CHUNK ? seq.q0 : s, row, shares.of(row_end - 1) - (int)blockIdx.x + 1, nc};
+        tasks[blockIdx.x] = Task{CHUNK ? seq.q0 : s, row, shares.of(row_end - sets) - (int)blockIdx.x + 1, row_nc};
       }
-      for (int e = tid; e < nc * (HD / 2); e += 256) {
+      for (int e = tid; e < row_nc * (HD / 2); e += 256) {
         const int c = e / (HD / 2), d = e % (HD / 2) * 2;
-        const float big = largest(c);
+        const int set = CHUNK && !PAIR ? c / kCols : 0;
+        const float big = largest(c - set * kCols, set);
         float sum = 0.f, v0 = 0.f, v1 = 0.f;
 #pragma unroll
         for (int i = 0; i < (PAIR ? 8 : 4); ++i) {
-          const int w = i & 3, k = c + 8 * (i >> 2);
+          const int w = i & 3, k = c - set * kCols + 8 * (i >> 2);
+          if (CHUNK && !PAIR && (w & (sets - 1)) != set) continue;
           const float f = jm[w][k] == -INFINITY ? (jl[w][k] == 0.f ? 0.f : jl[w][k]) : __builtin_amdgcn_exp2f(jm[w][k] - big);
           sum += jl[w][k] * f;
           const float* y = (const float*)(lsm + w * G::WAVE) + k * G::OLD + d;
@@ -919,7 +948,7 @@ __global__ __launch_bounds__(256, (PagedGeo<FMT, HD>::WGS)) void paged_kernel(
           v1 += y[1];
         }
         if (whole) {
-          uint16_t* const y = O + column(c, ldo) + d;
+          uint16_t* const y = O + column_at(r0 + c, ldo) + d;
           const uint32_t two = pack_bf16(v0 / sum, v1 / sum);
           if (vec)
             *(uint32_t*)y = two;
@@ -951,70 +980,75 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const Task* __restrict_
   if (task.parts == 0) return;
   const int tid = threadIdx.x & 127, j = threadIdx.x >> 7;  // j: which of the two heads
   const int row = task.row, np = task.parts, h = row % kv_heads, c0 = row / kv_heads * (CHUNK ? cols : kCols);
-  const int c = blockIdx.y * 2 + j, live = c < (CHUNK ? task.cols : min(cols, group - c0));
-  const int64_t stride = (int64_t)cols * (HD + 2);
-  const float* const p0 = part + 2 * (int64_t)blockIdx.x * stride + (live ? c : 0) * (HD + 2);
-  auto at = [&](int i) { return p0 + (i ? 2 * i : 1) * stride; };
-  // the first parts' outputs are on their way while the weights are found
-  const int d = tid % T * 4, k = tid / T;
-  constexpr int EARLY = 4;
-  f4 first[EARLY];
-  auto load = [&](int i) {
-    const float2 v0 = *(const float2*)(at(i) + d), v1 = *(const float2*)(at(i) + d + 2);
-    return f4{v0.x, v0.y, v1.x, v1.y};
-  };
+  int c2 = blockIdx.y;
+  do {
+    const int c = c2 * 2 + j, live = c < (CHUNK ? task.cols : min(cols, group - c0));
+    const int64_t stride = (int64_t)cols * (HD + 2);
+    const float* const p0 = part + 2 * (int64_t)blockIdx.x * stride + (live ? c : 0) * (HD + 2);
+    auto at = [&](int i) { return p0 + (i ? 2 * i : 1) * stride; };
+    // the first parts' outputs are on their way while the weights are found
+    const int d = tid % T * 4, k = tid / T;
+    constexpr int EARLY = 4;
+    f4 first[EARLY];
+    auto load = [&](int i) {
+      const float2 v0 = *(const float2*)(at(i) + d), v1 = *(const float2*)(at(i) + d + 2);
+      return f4{v0.x, v0.y, v1.x, v1.y};
+    };
 #pragma unroll
-  for (int i = 0; i < EARLY; ++i) first[i] = load(min(k + i * NP, np - 1));
-  // weights: exp of each part's maximum relative to the largest, and the sum of all
-  float top = -INFINITY;
-  for (int i = tid; i < np; i += 128) {
-    const float2 ml = *(const float2*)(at(i) + HD);
-    wt[j][i] = ml.x;
-    ls[j][i] = ml.y;
-    top = fmaxf(top, ml.x);
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  if (tid % 64 == 0) red[0][j][tid >> 6] = top;
-  __syncthreads();
-  top = fmaxf(red[0][j][0], red[0][j][1]);
-  float sum = 0.f;
-  for (int i = tid; i < np; i += 128) {
-    const float m = wt[j][i], l = ls[j][i];
-    const float f = m == -INFINITY ? (l == 0.f ? 0.f : l) : __builtin_amdgcn_exp2f(m - top);
-    wt[j][i] = f;
-    sum += f * l;
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-  if (tid % 64 == 0) red[1][j][tid >> 6] = sum;
-  __syncthreads();
-  sum = red[1][j][0] + red[1][j][1];
-  f4 a = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < EARLY; ++i)
-    if (k + i * NP < np) a += first[i] * wt[j][k + i * NP];
-#pragma unroll 4
-  for (int i = k + EARLY * NP; i < np; i += NP) a += load(i) * wt[j][i];
-  *(f4*)&acc[j][k][d] = a;
-  __syncthreads();
-  if (tid < HD / 2 && live) {
-    float y0 = 0.f, y1 = 0.f;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) y0 += acc[j][i][2 * tid], y1 += acc[j][i][2 * tid + 1];
-    const uint32_t two = pack_bf16(y0 / sum, y1 / sum);
-    int64_t at_row = task.seq, in_row = h * group + c0 + c;
-    if constexpr (CHUNK) {
-      const int i = by(c0 + c, ch);
-      at_row += i;
-      in_row -= i * group;
+    for (int i = 0; i < EARLY; ++i) first[i] = load(min(k + i * NP, np - 1));
+    // weights: exp of each part's maximum relative to the largest, and the sum of all
+    float top = -INFINITY;
+    for (int i = tid; i < np; i += 128) {
+      const float2 ml = *(const float2*)(at(i) + HD);
+      wt[j][i] = ml.x;
+      ls[j][i] = ml.y;
+      top = fmaxf(top, ml.x);
     }
-    uint16_t* const y = O + at_row * ldo + in_row * HD + 2 * tid;
-    if (vec)
-      *(uint32_t*)y = two;
-    else
-      y[0] = (uint16_t)two, y[1] = (uint16_t)(two >> 16);
-  }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if (tid % 64 == 0) red[0][j][tid >> 6] = top;
+    __syncthreads();
+    top = fmaxf(red[0][j][0], red[0][j][1]);
+    float sum = 0.f;
+    for (int i = tid; i < np; i += 128) {
+      const float m = wt[j][i], l = ls[j][i];
+      const float f = m == -INFINITY ? (l == 0.f ? 0.f : l) : __builtin_amdgcn_exp2f(m - top);
+      wt[j][i] = f;
+      sum += f * l;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    if (tid % 64 == 0) red[1][j][tid >> 6] = sum;
+    __syncthreads();
+    sum = red[1][j][0] + red[1][j][1];
+    f4 a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < EARLY; ++i)
+      if (k + i * NP < np) a += first[i] * wt[j][k + i * NP];
+#pragma unroll 4
+    for (int i = k + EARLY * NP; i < np; i += NP) a += load(i) * wt[j][i];
+    *(f4*)&acc[j][k][d] = a;
+    __syncthreads();
+    if (tid < HD / 2 && live) {
+      float y0 = 0.f, y1 = 0.f;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) y0 += acc[j][i][2 * tid], y1 += acc[j][i][2 * tid + 1];
+      const uint32_t two = pack_bf16(y0 / sum, y1 / sum);
+      int64_t at_row = task.seq, in_row = h * group + c0 + c;
+      if constexpr (CHUNK) {
+        const int i = by(c0 + c, ch);
+        at_row += i;
+        in_row -= i * group;
+      }
+      uint16_t* const y = O + at_row * ldo + in_row * HD + 2 * tid;
+      if (vec)
+        *(uint32_t*)y = two;
+      else
+        y[0] = (uint16_t)two, y[1] = (uint16_t)(two >> 16);
+    }
+    if (CHUNK) __syncthreads();
+    c2 += gridDim.y;
+  } while (CHUNK && 2 * c2 < task.cols);
 }
 
 // Workgroups for rows of at most `tiles` tiles: no more than smallest shares.
@@ -1091,7 +1125,7 @@ size_t duo_attention_chunk_workspace_size(int64_t total_q, int64_t nseq, int64_t
     return 0;
   const double rows = (double)kv_heads * ((double)total_q * (double)(heads / kv_heads) / 8 + (double)nseq);
   const int64_t wgs = paged_wgs(rows, cdiv(max_len, kMinKeys), kMaxWg);
-  return align_up(wgs * sizeof(Task)) + align_up((size_t)(2 * wgs * kCols * (head_dim + 2)) * sizeof(float)) +
+  return align_up(wgs * sizeof(Task)) + align_up((size_t)(2 * wgs * kWide * (head_dim + 2)) * sizeof(float)) +
          chunk_rows_ws_bytes(total_q, nseq, heads, kv_heads, head_dim, max_len);
 }
 
@@ -1125,14 +1159,13 @@ duo_status duo_attention_chunk(const void* Q, int64_t ldq, int64_t total_q, cons
   ch.cu_q = cu_q, ch.total_q = (int)total_q;
   ch.window = window <= max_len ? (int)window : 0;  // a longer one hides nothing
   ch.sinks = (int)std::min(sinks, max_len);
-  const int most = few_rows(cache->format);
-  const bool many = std::min(max_q, total_q) * group > most, few = !many || nseq > 1;
-  ch.most = many ? most : INT64_MAX;
+  const bool many = std::min(max_q, total_q) * group > kFewRows, few = !many || nseq > 1;
+  ch.most = many ? kFewRows : INT64_MAX;
   if (many) {
     const ChunkCall c = {Q, O, ldq, ldo, total_q, nseq, max_len, heads, ldt, cache, g, table, lens, cu_q, ch.window, ch.sinks,
                          cexp, flip};
     uint8_t* const rows_ws = (uint8_t*)ws + (need - chunk_rows_ws_bytes(total_q, nseq, heads, g.heads, hd, max_len));
-    if (duo_status st = chunk_rows_run(c, few ? most : 0, rows_ws, s); st != DUO_OK) return st;
+    if (duo_status st = chunk_rows_run(c, few ? kFewRows : 0, rows_ws, s); st != DUO_OK) return st;
     if (!few) return DUO_OK;
   }
   ch.by_shift = 0;
@@ -1143,11 +1176,11 @@ duo_status duo_attention_chunk(const void* Q, int64_t ldq, int64_t total_q, cons
     using P = PagedGeo<FMT, HD>;
     constexpr bool Q8 = FMT != DUO_KV_BF16;
     const bool pair = Q8 && std::min(max_q, total_q) * group <= 8;
-    const int cols = pair ? 8 : kCols;
-    const double rows = (double)g.heads * ((double)total_q * (double)group / cols + (double)nseq);
+    const int cols = pair ? 8 : kWide;
+    const double rows = (double)g.heads * ((double)total_q * (double)group / 8 + (double)nseq);
     const int64_t wgs = paged_wgs(rows, cdiv(max_len, P::KEYS), 256 * P::WGS);
     const PagedWork w = {lens, (int)nseq, (int)max_len, 0, (int)cdiv(nseq, 64),
-                         g.heads * (total_q * group / cols) >= 2 * 256 * P::WGS};
+                         g.heads * std::min(nseq, total_q) >= 2 * 256 * P::WGS};
     Task* const tasks = (Task*)ws;
     float* const part = (float*)((uint8_t*)ws + align_up(wgs * sizeof(Task)));
     const auto kern = pair ? paged_kernel<FMT, HD, Q8, true> : paged_kernel<FMT, HD, false, true>;
@@ -1156,7 +1189,9 @@ duo_status duo_attention_chunk(const void* Q, int64_t ldq, int64_t total_q, cons
                        (int)group, cols, cexp, flip, (uint16_t*)O, ldo, max_len > 0 ? tasks : nullptr, part, vec, ch);
     DUO_LAUNCH_CHECK();
     if (max_len > P::KEYS && wgs > 1) {  // a row of one tile is never split
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(paged_join_kernel<HD, true>), dim3((unsigned)wgs, (unsigned)cols / 2), dim3(256), 0, s,
+      // columns of a row by the bound of new tokens, or more of them one after the other
+      const int64_t most = std::min<int64_t>({std::max<int64_t>(std::min(max_q, total_q) * group, 1), cols});
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(paged_join_kernel<HD, true>), dim3((unsigned)wgs, (unsigned)cdiv(most, 2)), dim3(256), 0, s,
                          (const Task*)tasks, (const float*)part, g.heads, (int)group, cols, (uint16_t*)O, ldo, vec, ch);
       DUO_LAUNCH_CHECK();
     }
