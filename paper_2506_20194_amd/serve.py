@@ -8,11 +8,18 @@ and where they go; `run_block` carries their hidden states through one LLaMA-sty
 block (RMSNorm, rotary attention with grouped heads, SiLU-gated MLP) in the
 library's own kernels:
 
-  prompts and chunks   rotate, write K and V into the cache, attend to the packed
-                       sequences (duo_attention_packed); K and V come back from the
-                       cache where earlier tokens are needed, or where the cache is
-                       quantised, so that every token sees what later ones will
-  single tokens        rotate, write, attend over the pages (duo_attention_paged)
+  every step           rotate queries and keys, with norms of their heads where the block
+                       has them, and write K and V into the cache (duo_kv_append)
+  whole prompts        attend to the packed sequences (duo_attention_packed)
+  chunks, mixed steps  attend over the pages as they are stored (duo_attention_chunk), and
+                       so do prompts where the cache is quantised, so that every token
+                       sees what later ones will; only where each sequence brings a
+                       thousand rows or more to a quantised cache K and V come back
+                       from it (duo_kv_read) and the packed attention takes them,
+                       which makes numbers of the codes once for all of them
+  single tokens        attend over the pages (duo_attention_paged)
+  a window             duo_attention_chunk for all of them
+
 
 Weights are a Linear's n x k bf16 matrix or, for single tokens, the compressed
 columns of a pruned layer (duo.dsc_compress).  Every linear's input is sparsified
@@ -31,7 +38,9 @@ class Step:
     before[s] + new[s] (Python ints).  table: int32, row s holds the pages of
     sequence s, enough for its new length.  The token rows of the step are the
     sequences' new tokens one behind the other.  A sequence that needs a page which
-    the cache does not have gets NaN for them; the table is read on the device only."""
+    the cache does not have gets NaN for them (in a block with a window those tokens
+    that see one of its tokens: pages that a window has left behind need not be
+    there); the table is read on the device only."""
 
     def __init__(self, cache, table, before, new):
         if len(before) != len(new) or len(new) != table.shape[0]:
@@ -39,7 +48,7 @@ class Step:
         if any(b < 0 or n < 0 for b, n in zip(before, new)):
             raise ValueError("Step: lengths must not be negative")
         after = [b + n for b, n in zip(before, new)]
-        self.max_len = max(after, default=0)
+        self.max_len, self.max_new = max(after, default=0), max(new, default=0)
         if self.max_len > table.shape[1] * cache.page_size:
             raise ValueError("Step: table has too few pages for the new lengths")
         dev = table.device
@@ -48,20 +57,28 @@ class Step:
         seq, pos = self._tokens(before, new)
         self.pos = pos.to(dev, torch.int32)
         self.slots = cache.slots(table, seq.to(dev), pos.to(dev))
-        if self.single:
-            self.lens = torch.tensor(after, dtype=torch.int32).to(dev)
-            return
+        self.lens = torch.tensor(after, dtype=torch.int32).to(dev)
         self.cu_q = self._offsets(new).to(dev)
+        self.fewest = min((n for n in new if n), default=0)
+        self.cached, self._after, self._whole = any(before), after, None
+        if self.single:
+            return
         # token rows of sequences whose tokens do not all have a page; duo_kv_write skips such
         # tokens and duo_kv_read gives zeros for them, which attention would take for keys
         need = torch.arange(table.shape[1]) * cache.page_size < torch.tensor(after, dtype=torch.int64)[:, None]
         outside = (table < 0) | (table >= cache.data.shape[0])
         self.lost = (outside & need.to(dev)).any(1)[seq.to(dev)][:, None]
-        # the whole sequences, where the chunk's own rows of K and V are not all of them
-        self.cu_k, self.all_slots = None, self.slots
-        if any(before):
-            seq, pos = self._tokens([0] * len(after), after)
-            self.cu_k, self.all_slots = self._offsets(after).to(dev), cache.slots(table, seq.to(dev), pos.to(dev))
+
+    def whole(self, cache):
+        """Offsets (None: the chunk's own rows are all) and slots of the whole sequences."""
+        if self._whole is None:
+            cu_k, slots = None, self.slots
+            if self.cached:
+                seq, pos = self._tokens([0] * len(self._after), self._after)
+                dev = self.table.device
+                cu_k, slots = self._offsets(self._after).to(dev), cache.slots(self.table, seq.to(dev), pos.to(dev))
+            self._whole = cu_k, slots
+        return self._whole
 
     @staticmethod
     def _tokens(first, count):
@@ -87,26 +104,50 @@ def linear(x, W, p_x=None, R=None):
     return duo.duo_linear(x, W, R=R)
 
 
+# Rows (new tokens times heads of a group) of a sequence from which on the packed attention over
+# rows read back from a quantised cache is faster than attention over its codes: 256 tokens on
+# 16384, 64 heads on 8 (2048 rows), 177 us and 229, 64 (512 rows) 45 and 42.
+MANY_ROWS = 1024
+
+
 def attention(x, weights, cfg, cache, step, p_x=None):
     """The attention of one block for the step's rows x (already normalised): K and V
     go into the cache, and the heads' outputs are returned."""
     heads, kv, hd, theta = cfg["heads"], cache.kv_heads, cache.head_dim, cfg["theta"]
+    window, sinks = cfg.get("window"), cfg.get("sinks", 0)
+    q_gain, k_gain = weights.get("q_norm"), weights.get("k_norm")
+    normed = q_gain is not None or k_gain is not None
     q, k, v = (linear(x, weights[nm], p_x) for nm in "qkv")
-    duo.duo_rope_at(q, heads, hd, step.pos, theta, out=q)
-    duo.duo_rope_at(k, kv, hd, step.pos, theta, out=k)
-    duo.duo_kv_write(cache, k, v, step.slots)
-    if step.single:
+    duo.duo_kv_append(cache, k, v, step.slots, step.pos, theta, eps=cfg["eps"] if normed else None, k_gain=k_gain, Q=q,
+                      q_gain=q_gain, out=q)
+    if step.single and not window:
         return duo.duo_attention_paged(q, cache, step.table, step.lens, heads, max_len=step.max_len)
-    if step.cu_k is not None or cache.fmt != "bf16":
-        k, v = duo.duo_kv_read(cache, step.all_slots)
-    a = duo.duo_attention_packed(q, k, v, step.cu_q, heads, kv, hd, cu_k=step.cu_k)
+    quantised = cache.fmt != "bf16"
+    if window or (step.cached or quantised) and not (quantised and step.fewest * heads >= MANY_ROWS * kv):
+        a = duo.duo_attention_chunk(q, cache, step.table, step.lens, step.cu_q, heads, window=window, sinks=sinks,
+                                    max_q=step.max_new, max_len=step.max_len)
+        if window:
+            return a
+    else:
+        cu_k = None
+        if quantised:
+            cu_k, slots = step.whole(cache)
+            k, v = duo.duo_kv_read(cache, slots)
+        elif normed:
+            duo.duo_head_norm_rope(k, kv, hd, step.pos, k_gain, cfg["eps"], theta, out=k)
+        else:
+            duo.duo_rope_at(k, kv, hd, step.pos, theta, out=k)
+        a = duo.duo_attention_packed(q, k, v, step.cu_q, heads, kv, hd, cu_k=cu_k)
     return a.masked_fill_(step.lost, float("nan"))  # as duo_attention_paged does by itself
 
 
 def run_block(h, weights, cfg, cache, step, p_x=None):
     """One decoder block for the step's rows: h (step.m x d bf16) -> the same shape.
-    weights: q, k, v, o, gate, up, down; cfg: dict(heads, theta, eps); cache: this
-    block's (its kv_heads and head_dim are the block's)."""
+    weights: q, k, v, o, gate, up, down, and q_norm, k_norm where the heads of queries and
+    keys are normed before the rotation (head_dim gains each, one dtype); cfg:
+    dict(heads, theta, eps), and window, sinks where a token sees the last `window`
+    ones and the first `sinks` alone; cache: this block's (its kv_heads and head_dim
+    are the block's)."""
     if h.shape[0] != step.m:
         raise ValueError("run_block: h must hold the step's tokens")
     if step.m == 0:
