@@ -67,8 +67,11 @@ struct RowsArgs {
   uint32_t flip;
   int vec;        // 16-byte stores of O
   struct RowsTask* tasks;
-  float *po, *pml;  // two places per share: outputs (rows x head_dim, not normalised), references and sums
+  float* parts;  // two places per share
 };
+
+// Of a part, in floats: outputs (rows x head_dim, not normalised), references and sums.
+constexpr int64_t rows_part(int hd) { return kRowsQB * (int64_t)(hd + 2); }
 
 // A block that begins in a share and ends in another one.
 struct RowsTask {
@@ -1009,14 +1012,14 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     float sum = __uint_as_float(rl[0]) + __uint_as_float(rl[1]);
     if (G::QUANT) sum *= (float)(1 << kRowsBoost);  // as the values are
     if (!whole) {
-      const int64_t at = (2 * (int64_t)share + (t0 == 0)) * QB;
+      float* const part = a.parts + (2 * (int64_t)share + (t0 == 0)) * rows_part(HD);
       if (t0 == 0 && tid == 0) {
         const int64_t end = block + min(kRowsCost + (tiles - 1) * KB + 1, cost - near(cost));
         a.tasks[share] = RowsTask{share_of(end - 1) - share + 1, seq_q0 + qi0, head0, heads, rows, pos0};
       }
       if (row0 + (le & 31) < rows) {
-        if (le < 32) *(float2*)(a.pml + 2 * (at + row0 + (le & 31))) = make_float2(mc, sum);
-        float* const y = a.po + (at + row0 + (le & 31)) * HD + 4 * (le >> 5);
+        if (le < 32) *(float2*)(part + QB * HD + 2 * (row0 + (le & 31))) = make_float2(mc, sum);
+        float* const y = part + (row0 + (le & 31)) * HD + 4 * (le >> 5);
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -1077,17 +1080,20 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   }
 }
 
-// Joins the parts of the block that begins in share blockIdx.x, if it ends in another one: its own
+// Joins the parts of the block that begins in a share, if it ends in another one: its own
 // part (the second of its two places), then the first places of the shares after it.  HD / 4 threads
-// per row, blockIdx.y counts the rows by the 1024 / HD that a workgroup takes.
+// per row, blockIdx.y counts the rows by the 1024 / HD that a workgroup takes.  Shares lie on the XCDs
+// as in rows_kernel: blocks of equal length begin at shares that are multiples of each other, which
+// as blockIdx.x would all be on one XCD (32 tokens on 16384, 64 heads on 8: 67 us for that, 9 so).
 template <int HD, bool I4>
 __global__ __launch_bounds__(256) void rows_join_kernel(RowsArgs a) {
   constexpr int T = HD / 4;
-  const RowsTask task = a.tasks[blockIdx.x];
+  const int share = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
+  const RowsTask task = a.tasks[share];
   const int row = blockIdx.y * (256 / T) + threadIdx.x / T, d = threadIdx.x % T * 4;
   if (task.parts == 0 || row >= task.rows) return;
   const int qi = by(row, a), h = row - qi * a.hg;
-  auto place = [&](int i) { return (2 * ((int64_t)blockIdx.x + i) + (i == 0)) * kRowsQB + row; };
+  auto part = [&](int i) { return a.parts + (2 * ((int64_t)share + i) + (i == 0)) * rows_part(HD); };
   // eight parts at once, whose outputs, references and sums are all on their way before the first is used
   float top = -INFINITY, sum = 0.f;
   f4 y = {0.f, 0.f, 0.f, 0.f};
@@ -1096,9 +1102,9 @@ __global__ __launch_bounds__(256) void rows_join_kernel(RowsArgs a) {
     f4 v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int64_t at = place(min(i + j, task.parts - 1));
-      ml[j] = *(const float2*)(a.pml + 2 * at);
-      v[j] = *(const f4*)(a.po + at * HD + d);
+      const float* const p = part(min(i + j, task.parts - 1));
+      ml[j] = *(const float2*)(p + kRowsQB * HD + 2 * row);
+      v[j] = *(const f4*)(p + row * HD + d);
     }
     float most = top;
 #pragma unroll

@@ -568,7 +568,7 @@ namespace duo {
 
 size_t chunk_rows_ws_bytes(int64_t total_q, int64_t nseq, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t max_len) {
   const int64_t wgs = rows_wgs(total_q, nseq, heads / kv_heads, kv_heads, max_len);
-  return align_up(wgs * sizeof(RowsTask)) + align_up((size_t)(2 * wgs * kRowsQB * (head_dim + 2)) * sizeof(float));
+  return align_up(wgs * sizeof(RowsTask)) + align_up((size_t)(2 * wgs * rows_part((int)head_dim)) * sizeof(float));
 }
 
 duo_status chunk_rows_run(const ChunkCall& c, int64_t least, void* ws, hipStream_t s) {
@@ -587,12 +587,10 @@ duo_status chunk_rows_run(const ChunkCall& c, int64_t least, void* ws, hipStream
   a.least = least;
   a.cexp = c.cexp, a.flip = c.flip;
   a.vec = c.ldo % 8 == 0 && aligned16(c.O);
-  const int hd = c.cache->head_dim;
   const int64_t wgs = rows_wgs(c.total_q, c.nseq, a.group, c.geo.heads, c.max_len);
   a.deal = wgs % (c.geo.heads * a.nsub) == 0 ? (int)(wgs / (c.geo.heads * a.nsub)) : 0;
   a.tasks = (RowsTask*)ws;
-  a.po = (float*)((uint8_t*)ws + align_up(wgs * sizeof(RowsTask)));
-  a.pml = a.po + 2 * wgs * kRowsQB * hd;
+  a.parts = (float*)((uint8_t*)ws + align_up(wgs * sizeof(RowsTask)));
   return kv_by_format(c.cache, [&](auto fmt, auto dim) -> duo_status {
     constexpr int FMT = decltype(fmt)::value, HD = decltype(dim)::value;
     constexpr int lds = RowsGeo<FMT, HD>::LDS;
