@@ -652,10 +652,11 @@ duo_status duo_attention_paged(const void* Q, int64_t ldq, const duo_kv_cache* c
  *   any.  Everything is split by the sizes and the lengths alone: results are
  *   deterministic.  Q 16-byte aligned, ldq % 8 == 0 (else DUO_ERR_UNSUPPORTED); O must
  *   not overlap Q.  total_q * heads, nseq and max_len at most 2^30.
- *   Workspace: duo_attention_chunk_workspace_size with the same sizes (it never falls
- *   with a larger total_q, nseq or max_len). */
-size_t duo_attention_chunk_workspace_size(int64_t total_q, int64_t nseq, int64_t heads, int64_t kv_heads, int64_t head_dim,
-                                          int64_t max_len);
+ *   Workspace: duo_attention_chunk_workspace_size with the cache's format and the same sizes
+ *   (with 8 and 4 bits up to 1 GiB of it for rows made of codes, where sizes allow
+ *   sequences of very many rows). */
+size_t duo_attention_chunk_workspace_size(int32_t format, int64_t total_q, int64_t nseq, int64_t heads, int64_t kv_heads,
+                                          int64_t head_dim, int64_t max_len);
 duo_status duo_attention_chunk(const void* Q, int64_t ldq, int64_t total_q, const duo_kv_cache* cache, const int32_t* table,
                                int64_t ldt, const int32_t* lens, const int32_t* cu_q, int64_t nseq, int64_t max_q,
                                int64_t max_len, int64_t heads, int64_t window, int64_t sinks, double scale, void* O,

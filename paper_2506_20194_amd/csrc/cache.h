@@ -32,6 +32,14 @@ struct KvFmt<DUO_KV_I4> {
   static constexpr int most = 7, bias = 8;
 };
 
+// Rows of fp16 numbers made of codes (2^6 of them), as chunks' attention keeps them in its workspace.
+constexpr int kKvMade = DUO_KV_I4 + 1;
+template <>
+struct KvFmt<kKvMade> {
+  static constexpr int row(int hd) { return 2 * hd; }
+  static constexpr int scales(int) { return 0; }
+};
+
 // Geometry of one cache as the kernels take it: block = bytes of one head's part of
 // a page, [K rows][V rows][K scales][V scales] from its start.
 struct KvGeo {
@@ -136,7 +144,7 @@ __device__ __forceinline__ uint2 kv_encode(const u32x4& x, uint16_t* scale) {
 struct ChunkCall {
   const void* Q;
   void* O;
-  int64_t ldq, ldo, total_q, nseq, max_len, heads, ldt;
+  int64_t ldq, ldo, total_q, nseq, max_q, max_len, heads, ldt;
   const duo_kv_cache* cache;
   KvGeo geo;
   const int32_t *table, *lens, *cu_q;
@@ -144,7 +152,7 @@ struct ChunkCall {
   float cexp;
   uint32_t flip;
 };
-size_t chunk_rows_ws_bytes(int64_t total_q, int64_t nseq, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t max_len);
+size_t chunk_rows_ws_bytes(int32_t format, int64_t total_q, int64_t nseq, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t max_len);
 duo_status chunk_rows_run(const ChunkCall& c, int64_t least, void* ws, hipStream_t s);
 
 }  // namespace duo

@@ -23,7 +23,10 @@
 // scores take the power back; a row of Q likewise; and a token's values, whose power goes into the
 // exponent of its probabilities (the running reference is then one of p |V|, not of p) and out of
 // their sum again.  None of that happens with numbers of ordinary size, so the steps that are dealt out
-// go without it.  What is lost: bits of groups of 32 channels whose scale is below 2^-20 of 1 (of the
+// go without it.  Sequences of very many rows have their numbers made once, by a launch before, into the
+// workspace (rows_make_kernel): 2048 tokens on 16384, 64 heads on 8, 1362 us without in 8 bits, NNNN with
+// it.  If there is one among them that needs a power, all of that is left, and they are done from the codes as the
+// others are.  What is lost: bits of groups of 32 channels whose scale is below 2^-20 of 1 (of the
 // token's largest number, where that is outside the bounds).
 //
 // A sequence with more blocks than there are workgroups gives each the same number of them, whole, the long
@@ -45,6 +48,7 @@ constexpr int kRowsQB = 128;     // rows of a block
 constexpr int kRowsWg = 512;     // workgroups at most: two on each CU
 constexpr int kRowsCost = 128;   // what a block's start and end cost, in keys (256: 0 to 2 us more in short calls)
 constexpr int kRowsMin = 512;    // smallest share, in keys: 16 tokens on 16384, 64 heads on 8, 60 us, 98 with 256
+constexpr int kRowsMany = 2047;  // sequences with more rows than this have their numbers made of codes before
 constexpr int kRowsSnap = 512;   // a share's end moves to a block's end that is no further than this
 
 struct RowsArgs {
@@ -62,7 +66,12 @@ struct RowsArgs {
   int window, sinks;
   int per;        // sequences per bucket of the count
   int deal;       // blocks of one head that a round of all workgroups takes: 0 where heads do not divide them
-  int64_t least;  // sequences with no more rows than this are not done here
+  int64_t least, most;  // sequences with more rows than least, and no more than most, are done here
+  // Rows made of codes: the sequences with more than `over` rows, one behind the other, made_tiles tiles
+  // for each, and what says of some of them that their numbers do not fit fp16 as they are (none: NULL).
+  int64_t over;
+  const uint8_t* flags;
+  int nflags, made_tiles;  // nflags: a multiple of 1024
   float cexp;     // exp(s scale) = 2^(s cexp), with the queries' signs turned for a negative scale
   uint32_t flip;
   int vec;        // 16-byte stores of O
@@ -94,7 +103,8 @@ struct RowsSeq {
     const bool in = s < a.nseq;
     const int x = in ? min(max(a.cu_q[s], 0), a.total_q) : 0, y = in ? min(max(a.cu_q[s + 1], 0), a.total_q) : 0;
     q0 = x, lq = max(y - x, 0), len = in ? min(max(a.lens[s], 0), a.max_len) : 0;
-    nb = (int64_t)lq * a.group > a.least ? (lq + a.qpb - 1) / a.qpb : 0;
+    const int64_t rows = (int64_t)lq * a.group;
+    nb = rows > a.least && rows <= a.most ? (lq + a.qpb - 1) / a.qpb : 0;
     dealt = a.deal ? nb / a.deal * a.deal : 0;
     nb -= dealt;
     first = max(len - lq, 0);
@@ -175,7 +185,7 @@ constexpr int kRowsBoost = 6, kRowsLo = -2, kRowsHi = 8;
 
 template <int FMT, int HD>
 struct RowsGeo {
-  static constexpr bool QUANT = FMT != DUO_KV_BF16;
+  static constexpr bool QUANT = FMT == DUO_KV_I8 || FMT == DUO_KV_I4;
   static constexpr int KB = 64, CH = HD / 8, TILE = KB * CH;  // keys of a tile, 16-byte chunks per row, of a tile
   static constexpr int RB = KvFmt<FMT>::row(HD);
   static constexpr int NL = QUANT ? 1 + (16 * RB > 1024) : 16 * RB / 1024;  // loads of 16 rows
@@ -187,7 +197,7 @@ template <int FMT, int HD>
 __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   using G = RowsGeo<FMT, HD>;
   constexpr int KB = G::KB, CH = G::CH, TILE = G::TILE, RB = G::RB, NL = G::NL, QB = kRowsQB;
-  constexpr bool F16 = G::QUANT;
+  constexpr bool MADE = FMT == kKvMade, F16 = G::QUANT || MADE;
   constexpr int KS = HD / 16, DB = HD / 32;  // MFMA steps over head_dim, 32-wide blocks of the output row
   constexpr int RPL = 64 / CH;               // rows of bf16 per wave-wide access
   extern __shared__ __attribute__((aligned(16))) uint8_t lsm[];
@@ -195,6 +205,16 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int nhs = a.kv.heads * a.nsub;
 
+  if (a.flags) {
+    bool some = false;
+#pragma unroll 4
+    for (int i = lane * 16; i < a.nflags; i += 1024) {
+      const u32x4 v = *(const u32x4*)(a.flags + i);
+      some |= (v[0] | v[1] | v[2] | v[3]) != 0;
+    }
+    // numbers that do not fit: the rows that were made are left, and their sequences done from the codes
+    a.most = (__any(some) != 0) == MADE ? (MADE ? 0 : a.over) : INT64_MAX;
+  }
   // ---- the count, and this workgroup's share of it
   RowsSeq mine(a, a.per == 1 ? lane : a.nseq);
   int64_t upto = 0;
@@ -211,6 +231,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     upto += lane >= o ? v : 0;
   }
   const int64_t total = lane_of(upto, 63);
+  const uint64_t made = __ballot(mine.nb + mine.dealt > 0);  // MADE: which sequences the rows are of
   const int shares = (int)min((int64_t)gridDim.x, (total + kRowsMin - 1) / kRowsMin);
   const int64_t size = same(shares ? (int64_t)rows_div(total, shares) : 0);
   const int more = (int)(total - size * shares);
@@ -333,6 +354,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     const int len = same(q.len), pos0 = same(len - q.lq + qi0);  // position of the block's first query
     const int32_t* const pages = a.table + same((int64_t)p.s * a.ldt);
     const int seq_q0 = same(q.q0);
+    const uint32_t made0 = MADE ? (uint32_t)same((int)__popcll(made & (((uint64_t)1 << p.s) - 1)) * a.made_tiles) : 0u;
     // on to the next block
     if (dealing) {
       if (++round == rounds) {
@@ -389,7 +411,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     auto page = [&](int v) { return (uint32_t)((uint32_t)v < (uint32_t)a.kv.pages ? v : 0); };  // at most 2^31 - 1 pages
     int pid = 0, nid = 0;
     bool lost = false;  // some query sees a token in a page outside the cache
-    if (n) {
+    if (n && !MADE) {  // (rows made of pages that are not there are NaN)
       pid = ids(win);
       nid = ids(win + 64);
       const int p1 = min(place(t0 + n - 1) * KB + KB - 1, pos_end) >> a.kv.shift;
@@ -415,6 +437,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     };
     auto run_at = [&](int t) {  // tiles in order
       const int key = min(place(t) * KB + 16 * wave, (len - 1) & ~15), pg = key >> a.kv.shift;
+      if constexpr (MADE) return Run{block0 + (uint64_t)(made0 + (uint32_t)pg) * page_bytes, key & page_mask, len - 1 - key};
       if (pg >= win + 64) {
         if (pg >= win + 128) {  // the first tile behind the sinks
           win = (pg & ~3) - 64;
@@ -678,7 +701,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
       }
     }
     int q_power = 0;  // of the lane's row
-    if constexpr (G::QUANT) {
+    if constexpr (F16) {
       uint32_t top = 0;
 #pragma unroll
       for (int c = 0; c < KS; ++c)
@@ -741,7 +764,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
       for (int r = 1; r < 16; ++r) mt = fmaxf(mt, sc[r]);
       const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
       mt = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
-      if constexpr (G::QUANT) {
+      if constexpr (F16) {
         mt *= units;
         const bool up = mt > mc + 8.f;
         if (!__any(up)) return false;
@@ -771,9 +794,9 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         for (int r = 0; r < 16; ++r) o[d][r] *= f;
     };
     // What probabilities are relative to: in fp16 the reference's is 2^6, as small ones have fewer bits there
-    auto base_of = [&]() { return G::QUANT ? mc - 6.f : mc; };
+    auto base_of = [&]() { return F16 ? mc - 6.f : mc; };
     auto probabilities = [&](const f16x& sc, u32x4 (&p)[2], float units) __attribute__((always_inline)) {
-      const float base = (G::QUANT ? mc : m) == -INFINITY ? 0.f : base_of();
+      const float base = (F16 ? mc : m) == -INFINITY ? 0.f : base_of();
       float sum = 0.f;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -889,7 +912,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
       }
       __builtin_amdgcn_sched_barrier(0);
       // scores that leave the reference's range (or have none yet): once more, with another
-      if (__any(most > (G::QUANT ? 16384.f : 256.f) || (G::QUANT ? mc : m) == -INFINITY)) {
+      if (__any(most > (F16 ? 16384.f : 256.f) || (F16 ? mc : m) == -INFINITY)) {
         float f = 1.f;
         if (refer(sc, &f, a.cexp)) scale_o(f);
         sum = probabilities(sc, pn, a.cexp);
@@ -918,7 +941,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         }
         float f, units = a.cexp;
         bool any_power = false;  // of a key, a value or a query
-        if constexpr (G::QUANT) {
+        if constexpr (F16) {
           any_power = odd_q | odd;
           if (any_power) {
             const int from_lane = (u & 1) * 32 + 4 * (anew(lane) >> 5);
@@ -932,7 +955,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         }
         if (refer(sc, &f, units) && u > 0) scale_o(f);
         float sum = probabilities(sc, pf, units);
-        if constexpr (G::QUANT)
+        if constexpr (F16)
           if (any_power) {
             const int from_lane = (u & 1) * 32 + 4 * (anew(lane) >> 5);
             const float base = mc == -INFINITY ? 0.f : base_of();
@@ -1010,7 +1033,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     const int le = anew(lane);
     const auto rl = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     float sum = __uint_as_float(rl[0]) + __uint_as_float(rl[1]);
-    if (G::QUANT) sum *= (float)(1 << kRowsBoost);  // as the values are
+    if (F16) sum *= (float)(1 << kRowsBoost);  // as the values are
     if (!whole) {
       float* const part = a.parts + (2 * (int64_t)share + (t0 == 0)) * rows_part(HD);
       if (t0 == 0 && tid == 0) {
@@ -1078,6 +1101,75 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         }
     }
   }
+}
+
+// Rows of sequences with more than `over` rows made of their codes, a workgroup for 64 tokens of a K/V head, as far
+// as some new token sees them: pages of 64 tokens, K rows and V rows.  Rows in pages that are not there are NaN.
+// flags: is there a token whose numbers do not fit as they are, or anything else against these rows?
+template <int FMT, int HD>
+__global__ __launch_bounds__(256) void rows_make_kernel(RowsArgs a, uint8_t* __restrict__ out, uint8_t* __restrict__ flags) {
+  constexpr int RB = KvFmt<FMT>::row(HD), SB = KvFmt<FMT>::scales(HD), NC = HD / 4;
+  constexpr float bias = KvFmt<FMT>::bias;
+  const int tid = threadIdx.x, lane = tid & 63, tile = blockIdx.x, h = blockIdx.y;
+  const int64_t at = ((int64_t)blockIdx.z * gridDim.y + h) * gridDim.x + tile;
+  if (at == 0)  // what fills up the flags
+    for (int64_t i = (int64_t)gridDim.x * gridDim.y * gridDim.z + tid; i < a.nflags; i += 256) flags[i] = 0;
+  int q0 = 0, lq = 0, len = 0;
+  if (lane < a.nseq) {
+    q0 = min(max(a.cu_q[lane], 0), a.total_q);
+    lq = max(min(max(a.cu_q[lane + 1], 0), a.total_q) - q0, 0);
+    len = min(max(a.lens[lane], 0), a.max_len);
+  }
+  uint64_t many = __ballot((int64_t)lq * a.group > a.over);
+  // offsets that overlap can have more such sequences than there is room for: all are done from the codes then
+  const bool excess = __popcll(many) > (int)gridDim.z;
+  for (int i = 0; i < (int)blockIdx.z; ++i) many &= many - 1;
+  const int s = many ? __ffsll((unsigned long long)many) - 1 : 0;
+  lq = __builtin_amdgcn_readlane(lq, s), len = many ? __builtin_amdgcn_readlane(len, s) : 0;
+  const int first = a.window ? max(max(len - lq, 0) - a.window + 1, 0) : 0;
+  if (64 * tile >= len || (64 * tile + 63 < first && 64 * tile >= a.sinks)) {
+    if (tid == 0) flags[at] = excess;
+    return;
+  }
+  const int key = min(64 * tile + (tid >> 2), len - 1), part = tid & 3;
+  const int page = a.table[(int64_t)s * a.ldt + (key >> a.kv.shift)], in = key & ((1 << a.kv.shift) - 1);
+  const bool lost = page < 0 || page >= a.kv.pages;
+  const uint8_t* const block = a.kv.data + h * a.kv.block + (uint64_t)(uint32_t)(lost ? 0 : page) * (uint32_t)(a.kv.heads * a.kv.block);
+  uint8_t* const to = out + (((int64_t)blockIdx.z * gridDim.x + tile) * a.kv.heads + h) * (64 * 4 * HD) + (tid >> 2) * (2 * HD) + part * (HD / 2);
+  uint32_t w[2][RB / 16];
+  uint16_t scale[2];
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    const uint8_t* const codes = block + kv_rows_at<FMT, HD>(which, a.kv.shift) + in * RB + part * (RB / 4);
+#pragma unroll
+    for (int i = 0; i < RB / 16; i += 2) {
+      const uint2 two = *(const uint2*)(codes + 4 * i);
+      w[which][i] = two.x, w[which][i + 1] = two.y;
+    }
+    scale[which] = *(const uint16_t*)(block + kv_scales_at<FMT, HD>(which, a.kv.shift) + in * SB + (HD == 128 ? part : part >> 1) * 2);
+  }
+  bool odd = false;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    int top = scale[which] < 0x7f80 ? scale[which] : 0;
+    top = max(top, __shfl_xor(top, 1));
+    top = max(top, __shfl_xor(top, 2));
+    odd |= !lost && power_of(__uint_as_float((uint32_t)top << 16) * KvFmt<FMT>::most, kRowsLo, kRowsHi) != 0;
+    const float sc = lost ? NAN : bf16_bits_to_f32(scale[which]) * (float)(1 << kRowsBoost), off = sc * -bias;
+#pragma unroll
+    for (int j = 0; j < NC / 8; ++j) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t code = FMT == DUO_KV_I8 ? w[which][2 * j + (e >> 2)] >> (8 * (e & 3)) & 255u : w[which][j] >> (4 * e) & 15u;
+        v[e] = fmaf((float)code, sc, off);  // exactly
+      }
+      *(u32x4*)(to + which * (64 * 2 * HD) + 16 * j) = u32x4{pack_two<true>(v[0], v[1]), pack_two<true>(v[2], v[3]),
+                                                             pack_two<true>(v[4], v[5]), pack_two<true>(v[6], v[7])};
+    }
+  }
+  odd = __syncthreads_or(odd);
+  if (tid == 0) flags[at] = odd || excess;
 }
 
 // Joins the parts of the block that begins in a share, if it ends in another one: its own

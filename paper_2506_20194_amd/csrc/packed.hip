@@ -566,9 +566,23 @@ int64_t rows_wgs(int64_t total_q, int64_t nseq, int64_t group, int64_t kv_heads,
 
 namespace duo {
 
-size_t chunk_rows_ws_bytes(int64_t total_q, int64_t nseq, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t max_len) {
-  const int64_t wgs = rows_wgs(total_q, nseq, heads / kv_heads, kv_heads, max_len);
-  return align_up(wgs * sizeof(RowsTask)) + align_up((size_t)(2 * wgs * rows_part((int)head_dim)) * sizeof(float));
+// How many sequences may have their rows made of codes before (0: none), and the tiles and bytes for them.
+struct Made {
+  int64_t seqs, tiles, flags, bytes;
+  Made(int32_t format, int64_t total_q, int64_t nseq, int64_t group, int64_t kv_heads, int64_t head_dim, int64_t max_len) {
+    seqs = format == DUO_KV_BF16 || nseq > 64 ? 0 : std::min(nseq, total_q * group / (kRowsMany + 1));
+    tiles = cdiv(max_len, 64);
+    if (seqs * tiles * kv_heads > ((int64_t)1 << 30) / (64 * 4 * head_dim)) seqs = 0;  // a workspace of 1 GiB at most
+    flags = rup(seqs * tiles * kv_heads, 1024);
+    bytes = seqs ? (int64_t)align_up(flags) + seqs * tiles * kv_heads * 64 * 4 * head_dim : 0;
+  }
+};
+
+size_t chunk_rows_ws_bytes(int32_t format, int64_t total_q, int64_t nseq, int64_t heads, int64_t kv_heads, int64_t head_dim,
+                           int64_t max_len) {
+  const int64_t group = heads / kv_heads, wgs = rows_wgs(total_q, nseq, group, kv_heads, max_len);
+  return align_up(wgs * sizeof(RowsTask)) + align_up((size_t)(2 * wgs * rows_part((int)head_dim)) * sizeof(float)) +
+         align_up(Made(format, total_q, nseq, group, kv_heads, head_dim, max_len).bytes);
 }
 
 duo_status chunk_rows_run(const ChunkCall& c, int64_t least, void* ws, hipStream_t s) {
@@ -584,8 +598,8 @@ duo_status chunk_rows_run(const ChunkCall& c, int64_t least, void* ws, hipStream
   a.by_hg = (uint32_t)((((uint64_t)1 << (31 + a.by_shift)) + a.hg - 1) / a.hg);
   a.window = c.window, a.sinks = c.sinks;
   a.per = (int)cdiv(c.nseq, 64);
-  a.least = least;
-  a.cexp = c.cexp, a.flip = c.flip;
+  a.least = least, a.most = INT64_MAX, a.over = kRowsMany;
+  a.flip = c.flip;
   a.vec = c.ldo % 8 == 0 && aligned16(c.O);
   const int64_t wgs = rows_wgs(c.total_q, c.nseq, a.group, c.geo.heads, c.max_len);
   a.deal = wgs % (c.geo.heads * a.nsub) == 0 ? (int)(wgs / (c.geo.heads * a.nsub)) : 0;
@@ -593,18 +607,37 @@ duo_status chunk_rows_run(const ChunkCall& c, int64_t least, void* ws, hipStream
   a.parts = (float*)((uint8_t*)ws + align_up(wgs * sizeof(RowsTask)));
   return kv_by_format(c.cache, [&](auto fmt, auto dim) -> duo_status {
     constexpr int FMT = decltype(fmt)::value, HD = decltype(dim)::value;
-    constexpr int lds = RowsGeo<FMT, HD>::LDS;
-    const auto kern = rows_kernel<FMT, HD>;
-    if (FMT != DUO_KV_BF16) a.cexp = std::max(std::ldexp(a.cexp, -kRowsBoost), 1.4e-45f);  // never 0, as above
-    if (duo_status st = set_max_lds((const void*)kern, lds); st != DUO_OK) return st;
-    hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(256), lds, s, a);
-    DUO_LAUNCH_CHECK();
-    if (wgs > 1) {
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(rows_join_kernel<HD, FMT == DUO_KV_I4>), dim3((unsigned)wgs, kRowsQB * HD / 1024), dim3(256),
-                         0, s, a);
+    auto go = [&](auto f, const RowsArgs& r) -> duo_status {
+      constexpr int F = decltype(f)::value, lds = RowsGeo<F, HD>::LDS;
+      const auto kern = rows_kernel<F, HD>;
+      if (duo_status st = set_max_lds((const void*)kern, lds); st != DUO_OK) return st;
+      hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(256), lds, s, r);
       DUO_LAUNCH_CHECK();
+      if (wgs > 1) {
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(rows_join_kernel<HD, F == DUO_KV_I4>), dim3((unsigned)wgs, kRowsQB * HD / 1024),
+                           dim3(256), 0, s, r);
+        DUO_LAUNCH_CHECK();
+      }
+      return DUO_OK;
+    };
+    // numbers in fp16 are 2^6 of themselves; never 0, as above
+    a.cexp = FMT == DUO_KV_BF16 ? c.cexp : std::max(std::ldexp(c.cexp, -kRowsBoost), 1.4e-45f);
+    if constexpr (FMT != DUO_KV_BF16) {
+      const Made made(FMT, c.total_q, c.nseq, a.group, c.geo.heads, HD, c.max_len);
+      if (made.seqs && c.max_q * a.group > kRowsMany) {
+        uint8_t* const flags = (uint8_t*)ws + align_up(wgs * sizeof(RowsTask)) + align_up((size_t)(2 * wgs * rows_part(HD)) * sizeof(float));
+        uint8_t* const rows = flags + align_up(made.flags);
+        a.flags = flags, a.nflags = (int)made.flags, a.made_tiles = (int)made.tiles;
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(rows_make_kernel<FMT, HD>),
+                           dim3((unsigned)made.tiles, (unsigned)c.geo.heads, (unsigned)made.seqs), dim3(256), 0, s, a, rows, flags);
+        DUO_LAUNCH_CHECK();
+        RowsArgs r = a;
+        r.least = kRowsMany;
+        r.kv.data = rows, r.kv.pages = made.seqs * made.tiles, r.kv.block = 64 * 4 * HD, r.kv.shift = 6;
+        if (duo_status st = go(std::integral_constant<int, kKvMade>{}, r); st != DUO_OK) return st;
+      }
     }
-    return DUO_OK;
+    return go(fmt, a);
   });
 }
 

@@ -1118,15 +1118,16 @@ duo_status duo_attention_paged(const void* Q, int64_t ldq, const duo_kv_cache* c
   });
 }
 
-size_t duo_attention_chunk_workspace_size(int64_t total_q, int64_t nseq, int64_t heads, int64_t kv_heads, int64_t head_dim,
+size_t duo_attention_chunk_workspace_size(int32_t format, int64_t total_q, int64_t nseq, int64_t heads, int64_t kv_heads, int64_t head_dim,
                                           int64_t max_len) {
   if (total_q < 1 || nseq < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads || max_len < 1 ||
-      (head_dim != 64 && head_dim != 128))
+      (head_dim != 64 && head_dim != 128) || format < DUO_KV_BF16 || format > DUO_KV_I4 || total_q > ((int64_t)1 << 30) / heads ||
+      nseq > (int64_t)1 << 30 || max_len > (int64_t)1 << 30)
     return 0;
   const double rows = (double)kv_heads * ((double)total_q * (double)(heads / kv_heads) / 8 + (double)nseq);
   const int64_t wgs = paged_wgs(rows, cdiv(max_len, kMinKeys), kMaxWg);
   return align_up(wgs * sizeof(Task)) + align_up((size_t)(2 * wgs * kWide * (head_dim + 2)) * sizeof(float)) +
-         chunk_rows_ws_bytes(total_q, nseq, heads, kv_heads, head_dim, max_len);
+         chunk_rows_ws_bytes(format, total_q, nseq, heads, kv_heads, head_dim, max_len);
 }
 
 duo_status duo_attention_chunk(const void* Q, int64_t ldq, int64_t total_q, const duo_kv_cache* cache, const int32_t* table,
@@ -1148,7 +1149,7 @@ duo_status duo_attention_chunk(const void* Q, int64_t ldq, int64_t total_q, cons
   if (nseq == 0 || total_q == 0) return DUO_OK;
   if (!Q || !O || !lens || !cu_q || (max_len > 0 && !table)) return DUO_ERR_INVALID_ARG;
   if (ldq % 8 || !aligned16(Q)) return DUO_ERR_UNSUPPORTED;
-  const size_t need = duo_attention_chunk_workspace_size(total_q, nseq, heads, g.heads, hd, max_len);
+  const size_t need = duo_attention_chunk_workspace_size(cache->format, total_q, nseq, heads, g.heads, hd, max_len);
   if (need && (!ws || ws_bytes < need || reinterpret_cast<uintptr_t>(ws) % kAlign)) return DUO_ERR_WORKSPACE;
   if (duo_status d = device_ok(); d != DUO_OK) return d;
   const hipStream_t s = (hipStream_t)stream;
@@ -1162,9 +1163,9 @@ duo_status duo_attention_chunk(const void* Q, int64_t ldq, int64_t total_q, cons
   const bool many = std::min(max_q, total_q) * group > kFewRows, few = !many || nseq > 1;
   ch.most = many ? kFewRows : INT64_MAX;
   if (many) {
-    const ChunkCall c = {Q, O, ldq, ldo, total_q, nseq, max_len, heads, ldt, cache, g, table, lens, cu_q, ch.window, ch.sinks,
+    const ChunkCall c = {Q, O, ldq, ldo, total_q, nseq, std::min(max_q, total_q), max_len, heads, ldt, cache, g, table, lens, cu_q, ch.window, ch.sinks,
                          cexp, flip};
-    uint8_t* const rows_ws = (uint8_t*)ws + (need - chunk_rows_ws_bytes(total_q, nseq, heads, g.heads, hd, max_len));
+    uint8_t* const rows_ws = (uint8_t*)ws + (need - chunk_rows_ws_bytes(cache->format, total_q, nseq, heads, g.heads, hd, max_len));
     if (duo_status st = chunk_rows_run(c, few ? kFewRows : 0, rows_ws, s); st != DUO_OK) return st;
     if (!few) return DUO_OK;
   }

@@ -162,7 +162,7 @@ def lib():
         L.duo_attention_paged.restype = I32
         L.duo_attention_paged.argtypes = [P, I64, KV, P, I64, P, I64, I64, I64, F64, P, I64, P, SZ, P]
         L.duo_attention_chunk_workspace_size.restype = SZ
-        L.duo_attention_chunk_workspace_size.argtypes = [I64] * 6
+        L.duo_attention_chunk_workspace_size.argtypes = [I32] + [I64] * 6
         L.duo_attention_chunk.restype = I32
         L.duo_attention_chunk.argtypes = [P, I64, I64, P, P, I64, P, P, I64, I64, I64, I64, I64, I64, F64, P, I64, P, SZ, P]
         L.duo_profile_enable.restype = I32
@@ -1019,12 +1019,12 @@ def duo_attention_paged(Q, cache, table, lens, heads, max_len=None, scale=None, 
 
 
 @functools.lru_cache(maxsize=256)
-def _chunk_bytes(total_q, nseq, heads, kv_heads, head_dim, max_len):
-    return max(lib().duo_attention_chunk_workspace_size(total_q, nseq, heads, kv_heads, head_dim, max_len), 256)
+def _chunk_bytes(fmt, total_q, nseq, heads, kv_heads, head_dim, max_len):
+    return max(lib().duo_attention_chunk_workspace_size(KV_FORMATS[fmt], total_q, nseq, heads, kv_heads, head_dim, max_len), 256)
 
 
-def attention_chunk_workspace(total_q, nseq, heads, kv_heads, head_dim, max_len, device):
-    return torch.empty(_chunk_bytes(total_q, nseq, heads, kv_heads, head_dim, max_len), dtype=torch.uint8, device=device)
+def attention_chunk_workspace(fmt, total_q, nseq, heads, kv_heads, head_dim, max_len, device):
+    return torch.empty(_chunk_bytes(fmt, total_q, nseq, heads, kv_heads, head_dim, max_len), dtype=torch.uint8, device=device)
 
 
 def duo_attention_chunk(Q, cache, table, lens, cu_q, heads, window=None, sinks=0, max_q=None, max_len=None, scale=None,
@@ -1051,7 +1051,7 @@ def duo_attention_chunk(Q, cache, table, lens, cu_q, heads, window=None, sinks=0
     elif max_len > most:
         raise ValueError("duo: table holds fewer than max_len tokens")
     if ws is None:
-        ws = attention_chunk_workspace(tq, n, heads, cache.kv_heads, hd, max_len, Q.device)
+        ws = attention_chunk_workspace(cache.fmt, tq, n, heads, cache.kv_heads, hd, max_len, Q.device)
     dev = Q.get_device()
     _on(dev, "duo_attention_chunk", table, lens, cu_q, O, ws, cache.data)
     _current(dev, "duo_attention_chunk")

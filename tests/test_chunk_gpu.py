@@ -193,6 +193,30 @@ def test_many_rows(duo_lib, fmt):
     one(duo_lib, [(150, 150)], 40, 40, 64, 16, fmt)
 
 
+@pytest.mark.parametrize("window,sinks", [(0, 0), (150, 70)])
+@pytest.mark.parametrize("fmt", FMTS)
+def test_very_many_rows(duo_lib, fmt, window, sinks):
+    """Sequences of more blocks than there are workgroups (64 heads of 64 on 8), and of more than a thousand
+    rows, beside others."""
+    say("chunk very many rows", fmt, window, sinks)
+    one(duo_lib, [(1, 700), (1100, 1300), (300, 340), (40, 100)], 64, 8, 64, 16, fmt, window, sinks)
+    one(duo_lib, [(257, 1000), (70, 600), (512, 512)], 8, 2, 128, 64, fmt, window, sinks)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "int4"])
+def test_overlapping_sequences_of_many_rows(duo_lib, fmt):
+    """More sequences of many rows than the offsets should allow: rows of one and the same sequence."""
+    say("chunk overlapping sequences", fmt)
+    d, heads, kv, hd = duo_lib, 16, 2, 64
+    b = Batch(d, [(150, 400)], heads, kv, hd, 16, fmt)
+    want = b.run()
+    b.check(want)
+    cu = torch.tensor([0, 150, 0, 150, 0, 150], dtype=torch.int32, device=DEV)
+    table, lens = b.table.repeat(5, 1), b.lens.repeat(5)
+    O = d.duo_attention_chunk(b.Q.to(DEV), b.cache, table, lens, cu, heads)
+    b.check(O)
+
+
 @pytest.mark.parametrize("fmt", FMTS)
 def test_scale_strides_hints(duo_lib, fmt):
     say("chunk scale, strides, hints", fmt)
@@ -206,12 +230,12 @@ def test_scale_strides_hints(duo_lib, fmt):
 
 
 @pytest.mark.parametrize("kind", ["keys", "queries", "values", "small values", "large values", "everything"])
-@pytest.mark.parametrize("heads", [2, 16])
+@pytest.mark.parametrize("heads,lq", [(2, 60), (16, 60), (16, 150)])
 @pytest.mark.parametrize("fmt", FMTS)
-def test_magnitudes(duo_lib, fmt, heads, kind):
+def test_magnitudes(duo_lib, fmt, heads, lq, kind):
     """Keys, values and queries whose sizes differ by many powers of two, and all values
     far from 1."""
-    say("chunk magnitudes", fmt, heads, kind)
+    say("chunk magnitudes", fmt, heads, lq, kind)
     g = torch.Generator().manual_seed(5)
 
     def spread(x, lo, hi, some):
@@ -229,7 +253,7 @@ def test_magnitudes(duo_lib, fmt, heads, kind):
         if kind == "large values":
             b.V.mul_(2.0 ** 70)
 
-    b = Batch(duo_lib, [(60, 700), (9, 90), (70, 70)], heads, 2, 128, 16, fmt, touch=touch)
+    b = Batch(duo_lib, [(lq, 700), (9, 90), (70, 70)], heads, 2, 128, 16, fmt, touch=touch)
     if kind in ("queries", "everything"):
         spread(b.Q, -30, 6, 0.3)
     b.check(b.run())
@@ -263,7 +287,7 @@ def test_lengths_and_offsets_are_cut(duo_lib, fmt):
 
 
 @pytest.mark.parametrize("window,sinks", [(0, 0), (40, 4)])
-@pytest.mark.parametrize("heads,lq", [(2, 5), (16, 60)])
+@pytest.mark.parametrize("heads,lq", [(2, 5), (16, 60), (16, 150)])
 @pytest.mark.parametrize("fmt", FMTS)
 def test_page_outside(duo_lib, fmt, heads, lq, window, sinks):
     """Queries that see a token in a page that is not there are NaN, and only they."""
@@ -289,7 +313,7 @@ def test_page_outside(duo_lib, fmt, heads, lq, window, sinks):
 
 
 @pytest.mark.parametrize("window,sinks", [(0, 0), (20, 3)])
-@pytest.mark.parametrize("heads,lq", [(2, 9), (16, 70)])
+@pytest.mark.parametrize("heads,lq", [(2, 9), (16, 70), (16, 140)])
 @pytest.mark.parametrize("fmt", FMTS)
 def test_unseen_numbers(duo_lib, fmt, heads, lq, window, sinks):
     """Infinities and NaN in keys and values that a query does not see have no influence on
@@ -333,7 +357,7 @@ def test_repeats_streams_and_graphs(duo_lib):
     seqs = [(1, 3000), (90, 700), (4, 500)]
     b = Batch(d, seqs, 16, 2, 128, 64, "int8")
     Q, w = b.Q.to(DEV), 16 * 128
-    size = d.attention_chunk_workspace(len(Q), 3, 16, 2, 128, b.table.shape[1] * 64, DEV).numel()
+    size = d.attention_chunk_workspace("int8", len(Q), 3, 16, 2, 128, b.table.shape[1] * 64, DEV).numel()
     call = lambda **kw: d.duo_attention_chunk(Q, b.cache, b.table, b.lens, b.cu, 16, **kw)
     first = call(ws=torch.zeros(size, dtype=torch.uint8, device=DEV))
     assert torch.equal(first, call(ws=torch.full((size,), 255, dtype=torch.uint8, device=DEV)))
