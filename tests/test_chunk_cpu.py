@@ -1,0 +1,103 @@
+"""Attention of new tokens over the cache, host side (no GPU needed): argument errors come back
+before any device work, valid arguments reach DUO_ERR_NO_DEVICE here; sizes of workspaces; the
+binding's own refusals."""
+
+import ctypes
+
+import pytest
+import torch
+
+FAKE = ctypes.c_void_p(1 << 20)  # never dereferenced on the host
+OUT = ctypes.c_void_p(256 << 20)
+BIG = 1 << 40
+
+
+def _cache(data=FAKE.value, pages=10, page=16, kv=2, hd=64, fmt=0):
+    from paper_2506_20194_amd.duo import KvCache
+
+    return ctypes.byref(KvCache(data, pages, page, kv, hd, fmt))
+
+
+@pytest.fixture()
+def codes(duo_lib):
+    d = duo_lib
+    if torch.cuda.device_count():
+        pytest.skip("valid arguments with made-up addresses would be launched")
+    return d.lib(), d
+
+
+def test_arguments(codes):
+    L, d = codes
+    E, UNS, NODEV, WS = d.DUO_ERR_INVALID_ARG, d.DUO_ERR_UNSUPPORTED, d.DUO_ERR_NO_DEVICE, d.DUO_ERR_WORKSPACE
+
+    def call(cache=None, Q=FAKE, ldq=256, tq=8, table=FAKE, ldt=4, lens=FAKE, cu=FAKE, n=3, mq=8, ml=64, h=4, win=0, sinks=0,
+             scale=0.125, O=OUT, ldo=256, ws=OUT, bytes=BIG):
+        return L.duo_attention_chunk(Q, ldq, tq, cache or _cache(), table, ldt, lens, cu, n, mq, ml, h, win, sinks, scale, O, ldo, ws,
+                                     bytes, None)
+
+    for good in (dict(), dict(win=1), dict(win=BIG, sinks=BIG), dict(mq=0), dict(mq=BIG), dict(h=6, ldq=384, ldo=384), dict(ldo=257),
+                 dict(scale=-1.0), dict(scale=0.0), dict(cache=_cache(fmt=1)), dict(cache=_cache(fmt=2)), dict(h=800, ldq=51200, ldo=51200),
+                 dict(O=ctypes.c_void_p(OUT.value + 2)), dict(ml=0, table=None, ldt=0, ws=None, bytes=0)):
+        assert call(**good) == NODEV, good
+    assert call(n=0, Q=None, O=None, cu=None, lens=None, table=None) == call(tq=0, Q=None, O=None) == d.DUO_OK
+    for bad in (dict(tq=-1), dict(n=-1), dict(mq=-1), dict(ml=-1), dict(win=-1), dict(sinks=-1), dict(h=0), dict(h=3), dict(h=65536),
+                dict(ldq=255), dict(ldo=255), dict(ldt=3), dict(ldt=-1), dict(scale=float("nan")), dict(scale=float("inf")),
+                dict(Q=None), dict(O=None), dict(lens=None), dict(cu=None), dict(table=None), dict(cache=_cache(data=None)),
+                dict(cache=_cache(pages=0)), dict(cache=_cache(fmt=3))):
+        assert call(**bad) == E, bad
+    for odd in (dict(ldq=260), dict(Q=ctypes.c_void_p(FAKE.value + 8)), dict(cache=_cache(page=8)), dict(cache=_cache(hd=96)),
+                dict(n=(1 << 30) + 1), dict(ml=(1 << 30) + 1, ldt=1 << 30), dict(tq=1 << 29),
+                dict(tq=1 << 28, n=1 << 20, ml=1 << 30, ldt=1 << 30)):
+        assert call(**odd) == UNS, odd
+    need = L.duo_attention_chunk_workspace_size(0, 8, 3, 4, 2, 64, 64)
+    assert call(bytes=need) == NODEV
+    for few in (dict(bytes=need - 1), dict(ws=None), dict(ws=ctypes.c_void_p(OUT.value + 128))):
+        assert call(**few) == WS, few
+
+
+def test_workspace_sizes(codes):
+    L, _ = codes
+    size = L.duo_attention_chunk_workspace_size
+    assert size(0, 8, 3, 4, 2, 64, 64) > 0
+    for none in ((0, 0, 3, 4, 2, 64, 64), (0, 8, 0, 4, 2, 64, 64), (0, 8, 3, 0, 2, 64, 64), (0, 8, 3, 5, 2, 64, 64), (0, 8, 3, 4, 2, 96, 64),
+                 (0, 8, 3, 4, 2, 64, 0), (3, 8, 3, 4, 2, 64, 64), (-1, 8, 3, 4, 2, 64, 64), (0, 1 << 29, 3, 4, 2, 64, 64)):
+        assert size(*none) == 0, none
+    last = 0
+    for total in (1, 5, 64, 1000, 30000):  # 16 bits: never less for more tokens
+        assert size(0, total, 4, 64, 8, 128, 16384) >= last
+        last = size(0, total, 4, 64, 8, 128, 16384)
+    # rows made of codes: of one sequence, whole tiles of 64 tokens; never past 1 GiB
+    plain, made = (size(f, 2048, 1, 64, 8, 128, 16384) for f in (0, 1))
+    assert made - plain >= 16384 * 8 * 128 * 4
+    for args in ((1, 1 << 20, 64, 64, 8, 128, 1 << 20), (2, 1 << 24, 64, 64, 8, 128, 4096)):
+        assert size(*args) - size(0, *args[1:]) <= (1 << 30) + (1 << 22)
+
+
+def test_binding(duo_lib):
+    d = duo_lib
+    b = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)
+    cache = d.KVCache.empty(2, 16, 2, 64, "int8", "cpu")
+    with pytest.raises(ValueError, match="HIP"):
+        d.duo_attention_chunk(b(3, 256), cache, i(1, 2), i(1), i(2), 4)
+    with pytest.raises(TypeError, match="table"):
+        d.duo_attention_chunk(b(3, 256), cache, i(1, 2).long(), i(1), i(2), 4)
+    with pytest.raises(ValueError, match="table"):
+        d.duo_attention_chunk(b(3, 256), cache, i(2, 2), i(1), i(2), 4)
+    with pytest.raises(ValueError, match="window"):
+        d.duo_attention_chunk(b(3, 256), cache, i(1, 2), i(1), i(2), 4, window=0)
+    with pytest.raises(ValueError, match="fewer than max_len"):
+        d.duo_attention_chunk(b(3, 256), cache, i(1, 2), i(1), i(2), 4, max_len=33)
+
+
+def test_binding_wants_the_current_device(duo_lib):
+    with pytest.raises(ValueError, match="current"):
+        duo_lib._current(-2, "duo_attention_chunk") if torch.cuda.device_count() else _without_device(duo_lib)
+
+
+def _without_device(d):
+    was, d._device = d._device, lambda: 0
+    try:
+        d._current(1, "duo_attention_chunk")
+    finally:
+        d._device = was
