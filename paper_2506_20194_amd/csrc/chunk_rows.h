@@ -20,13 +20,13 @@
 // of 8 bits is rounded to 2^-11 of itself (bf16 would cost 2^-8: an error of the output of 0.0031 and, in
 // 4 bits, 0.0048 of its root mean square, where the plain form has 0.0017).  fp16's range is made to
 // do by powers of two: a key whose largest number is outside 2^-2 .. 2^8 is brought to 2^7, and its
-// scores take the power back; a row of Q likewise; and a token's values, whose power goes into the
+// scores take the power back; a row of Q likewise; and a token's values (small ones to 2^-2), whose power goes into the
 // exponent of its probabilities (the running reference is then one of p |V|, not of p) and out of
 // their sum again.  None of that happens with numbers of ordinary size, so the steps that are dealt out
 // go without it.  Sequences of very many rows have their numbers made once, by a launch before, into the
 // workspace (rows_make_kernel): 2048 tokens on 16384, 64 heads on 8, 1362 us without in 8 bits, 1120 with
 // it.  If there is one among them that needs a power, all of that is left, and they are done from the codes as the
-// others are.  What is lost: bits of groups of 32 channels whose scale is below 2^-20 of 1 (of the
+// others are.  What is lost: bits of groups of 32 channels whose scale is below 2^-20 of 1 (2^-18 of the
 // token's largest number, where that is outside the bounds).
 //
 // A sequence with more blocks than there are workgroups gives each the same number of them, whole, the long
@@ -174,10 +174,12 @@ __device__ __forceinline__ f16x mma32(const u32x4& a, const u32x4& b, f16x c) {
   __builtin_memcpy(&bv, &b, 16);
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(av, bv, c, 0, 0, 0);
 }
-// The power of two that numbers of at most `top` are divided by so that it lies in [2^lo, 2^hi): 0 where it does.
+// The power of two that numbers of at most `top` are divided by so that it lies in [2^lo, 2^hi): 0 where it does, else
+// one that brings it to the upper bound, or (NEAR) to the nearer one.
+template <bool NEAR = false>
 __device__ __forceinline__ int power_of(float top, int lo, int hi) {
   const int e = (int)(__float_as_uint(top) >> 23) - 127;
-  return top == 0.f || e == 128 || (e >= lo && e < hi) ? 0 : e - (hi - 1);
+  return top == 0.f || e == 128 || (e >= lo && e < hi) ? 0 : NEAR && e < lo ? e - lo : e - (hi - 1);
 }
 // Keys and values in fp16 are 2^6 of themselves, for more small ones: those of a token reach from 2^-2 to 2^8 (24 times a
 // scale of 4 bits is then below 2^16).
@@ -530,7 +532,9 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     };
     auto k_power = [&](const Scales& s) { return power_of(most_of(s), kRowsLo, kRowsHi); };
     int e_ref = 0;  // power of two that the outputs are in units of: that of the first tile's values
-    auto v_power = [&](const Scales& s) { return min(max(power_of(ldexpf(most_of(s), -e_ref), kRowsLo, kRowsHi), -60), 60); };
+    // Small values go to the lower bound only: what a probability loses to its value's power it lacks in fp16, and
+    // beside values just above the bound ones just below it would lose 2^10 at once.
+    auto v_power = [&](const Scales& s) { return min(max(power_of<true>(ldexpf(most_of(s), -e_ref), kRowsLo, kRowsHi), -60), 60); };
     // does some key's largest scale mean a power, as far as one look can tell (never no for yes)?
     auto some_power = [&](const Scales& k, const Scales& v) {
       typedef unsigned short u16v2 __attribute__((ext_vector_type(2)));

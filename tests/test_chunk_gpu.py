@@ -262,6 +262,27 @@ def test_magnitudes(duo_lib, fmt, heads, lq, kind):
     b.check(b.run())
 
 
+@pytest.mark.parametrize("top", [0.3, 4.0])
+@pytest.mark.parametrize("lq", [2, 60, 170])
+@pytest.mark.parametrize("fmt", FMTS)
+def test_long_tail(duo_lib, fmt, lq, top):
+    """A first token that has nearly all of the probability, 2^21 times any other one's, but zeros in half of
+    its channels: there the many others are the output.  Their values lie on either side of its."""
+    say("chunk long tail", fmt, lq, top)
+
+    def touch(b):
+        b.K.mul_(0.05)
+        b.K[0] = 1.28
+        g = torch.Generator().manual_seed(9)
+        b.V.copy_(torch.rand(b.V.shape, generator=g) * 0.25 - 0.05)
+        b.V[0] = 0.0
+        b.V[0, ::2] = top
+
+    b = Batch(duo_lib, [(lq, 4000)], 16, 2, 128, 16, fmt, touch=touch)
+    b.Q.copy_(1.0 + 0.05 * b.Q)
+    b.check(b.run())
+
+
 @pytest.mark.parametrize("fmt", FMTS)
 def test_lengths_and_offsets_are_cut(duo_lib, fmt):
     """Negative lengths are empty, ones past max_len end there; offsets outside Q are cut, rows
