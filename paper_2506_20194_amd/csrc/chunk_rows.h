@@ -24,8 +24,9 @@
 // exponent of its probabilities (the running reference is then one of p |V|, not of p) and out of
 // their sum again.  None of that happens with numbers of ordinary size, so the steps that are dealt out
 // go without it.  Sequences of very many rows have their numbers made once, by a launch before, into the
-// workspace (rows_make_kernel): 2048 tokens on 16384, 64 heads on 8, 1362 us without in 8 bits, 1120 with
-// it.  If there is one among them that needs a power, all of that is left, and they are done from the codes as the
+// workspace (rows_make_kernel): 2048 tokens on 16384, 64 heads on 8, 1362 us without in 8 bits, 1110 with
+// it; 320 on 8192, 32 on 8 (1280 rows), 104 and 101, on 65536 558 and 496; with 1024 rows it gains
+// nothing up to 32768.  If there is one among them that needs a power, all of that is left, and they are done from the codes as the
 // others are.  What is lost: bits of groups of 32 channels whose scale is below 2^-20 of 1 (2^-18 of the
 // token's largest number, where that is outside the bounds).
 //
@@ -48,7 +49,7 @@ constexpr int kRowsQB = 128;     // rows of a block
 constexpr int kRowsWg = 512;     // workgroups at most: two on each CU
 constexpr int kRowsCost = 128;   // what a block's start and end cost, in keys (256: 0 to 2 us more in short calls)
 constexpr int kRowsMin = 512;    // smallest share, in keys: 16 tokens on 16384, 64 heads on 8, 60 us, 98 with 256
-constexpr int kRowsMany = 2047;  // sequences with more rows than this have their numbers made of codes before
+constexpr int kRowsMany = 1279;  // sequences with more rows than this have their numbers made of codes before
 constexpr int kRowsSnap = 512;   // a share's end moves to a block's end that is no further than this
 
 struct RowsArgs {
@@ -1109,10 +1110,12 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
 
 // Rows of sequences with more than `over` rows made of their codes, a workgroup for 64 tokens of a K/V head, as far
 // as some new token sees them: pages of 64 tokens, K rows and V rows.  Rows in pages that are not there are NaN.
+// A thread has eight neighbouring channels, so that a wave writes whole rows (with 32 channels a thread, which 16384
+// tokens of 8 heads of 128 took 34 us for, every store was spread over 64 places).
 // flags: is there a token whose numbers do not fit as they are, or anything else against these rows?
 template <int FMT, int HD>
 __global__ __launch_bounds__(256) void rows_make_kernel(RowsArgs a, uint8_t* __restrict__ out, uint8_t* __restrict__ flags) {
-  constexpr int RB = KvFmt<FMT>::row(HD), SB = KvFmt<FMT>::scales(HD), NC = HD / 4;
+  constexpr int RB = KvFmt<FMT>::row(HD), SB = KvFmt<FMT>::scales(HD), TK = HD / 8, N = TK / 4;  // threads of a key, keys of a thread
   constexpr float bias = KvFmt<FMT>::bias;
   const int tid = threadIdx.x, lane = tid & 63, tile = blockIdx.x, h = blockIdx.y;
   const int64_t at = ((int64_t)blockIdx.z * gridDim.y + h) * gridDim.x + tile;
@@ -1135,43 +1138,50 @@ __global__ __launch_bounds__(256) void rows_make_kernel(RowsArgs a, uint8_t* __r
     if (tid == 0) flags[at] = excess;
     return;
   }
-  const int key = min(64 * tile + (tid >> 2), len - 1), part = tid & 3;
-  const int page = a.table[(int64_t)s * a.ldt + (key >> a.kv.shift)], in = key & ((1 << a.kv.shift) - 1);
-  const bool lost = page < 0 || page >= a.kv.pages;
-  const uint8_t* const block = a.kv.data + h * a.kv.block + (uint64_t)(uint32_t)(lost ? 0 : page) * (uint32_t)(a.kv.heads * a.kv.block);
-  uint8_t* const to = out + (((int64_t)blockIdx.z * gridDim.x + tile) * a.kv.heads + h) * (64 * 4 * HD) + (tid >> 2) * (2 * HD) + part * (HD / 2);
-  uint32_t w[2][RB / 16];
-  uint16_t scale[2];
+  // neighbouring threads have neighbouring channels, eight each
+  const int c = tid % TK;
+  uint8_t* const to = out + (((int64_t)blockIdx.z * gridDim.x + tile) * a.kv.heads + h) * (64 * 4 * HD) + tid / TK * (2 * HD) + 16 * c;
+  uint2 w[N][2];
+  uint16_t scale[N][2];
+  uint32_t lost = 0;
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    const uint8_t* const codes = block + kv_rows_at<FMT, HD>(which, a.kv.shift) + in * RB + part * (RB / 4);
+  for (int n = 0; n < N; ++n) {
+    const int key = min(64 * tile + 64 / N * n + tid / TK, len - 1);
+    const int page = a.table[(int64_t)s * a.ldt + (key >> a.kv.shift)], in = key & ((1 << a.kv.shift) - 1);
+    const bool none = page < 0 || page >= a.kv.pages;
+    lost |= (uint32_t)none << n;
+    const uint8_t* const block = a.kv.data + h * a.kv.block + (uint64_t)(uint32_t)(none ? 0 : page) * (uint32_t)(a.kv.heads * a.kv.block);
 #pragma unroll
-    for (int i = 0; i < RB / 16; i += 2) {
-      const uint2 two = *(const uint2*)(codes + 4 * i);
-      w[which][i] = two.x, w[which][i + 1] = two.y;
+    for (int which = 0; which < 2; ++which) {
+      const uint8_t* const codes = block + kv_rows_at<FMT, HD>(which, a.kv.shift) + in * RB + c * (RB / TK);
+      if constexpr (FMT == DUO_KV_I8)
+        w[n][which] = *(const uint2*)codes;
+      else
+        w[n][which].x = *(const uint32_t*)codes;
+      scale[n][which] = *(const uint16_t*)(block + kv_scales_at<FMT, HD>(which, a.kv.shift) + in * SB + c / 4 * 2);
     }
-    scale[which] = *(const uint16_t*)(block + kv_scales_at<FMT, HD>(which, a.kv.shift) + in * SB + (HD == 128 ? part : part >> 1) * 2);
   }
   bool odd = false;
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    int top = scale[which] < 0x7f80 ? scale[which] : 0;
-    top = max(top, __shfl_xor(top, 1));
-    top = max(top, __shfl_xor(top, 2));
-    odd |= !lost && power_of(__uint_as_float((uint32_t)top << 16) * KvFmt<FMT>::most, kRowsLo, kRowsHi) != 0;
-    const float sc = lost ? NAN : bf16_bits_to_f32(scale[which]) * (float)(1 << kRowsBoost), off = sc * -bias;
+  for (int n = 0; n < N; ++n)
 #pragma unroll
-    for (int j = 0; j < NC / 8; ++j) {
+    for (int which = 0; which < 2; ++which) {
+      const bool none = lost >> n & 1;
+      const uint16_t sb = scale[n][which];
+      int top = sb < 0x7f80 ? sb : 0;
+#pragma unroll
+      for (int o = 4; o < TK; o <<= 1) top = max(top, __shfl_xor(top, o));
+      odd |= !none && power_of(__uint_as_float((uint32_t)top << 16) * KvFmt<FMT>::most, kRowsLo, kRowsHi) != 0;
+      const float sc = none ? NAN : bf16_bits_to_f32(sb) * (float)(1 << kRowsBoost), off = sc * -bias;
       float v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const uint32_t code = FMT == DUO_KV_I8 ? w[which][2 * j + (e >> 2)] >> (8 * (e & 3)) & 255u : w[which][j] >> (4 * e) & 15u;
+        const uint32_t code = FMT == DUO_KV_I8 ? (e < 4 ? w[n][which].x : w[n][which].y) >> (8 * (e & 3)) & 255u : w[n][which].x >> (4 * e) & 15u;
         v[e] = fmaf((float)code, sc, off);  // exactly
       }
-      *(u32x4*)(to + which * (64 * 2 * HD) + 16 * j) = u32x4{pack_two<true>(v[0], v[1]), pack_two<true>(v[2], v[3]),
-                                                             pack_two<true>(v[4], v[5]), pack_two<true>(v[6], v[7])};
+      *(u32x4*)(to + 64 / N * n * (2 * HD) + which * (64 * 2 * HD)) = u32x4{pack_two<true>(v[0], v[1]), pack_two<true>(v[2], v[3]),
+                                                                            pack_two<true>(v[4], v[5]), pack_two<true>(v[6], v[7])};
     }
-  }
   odd = __syncthreads_or(odd);
   if (tid == 0) flags[at] = odd || excess;
 }

@@ -1190,9 +1190,11 @@ duo_status duo_attention_chunk(const void* Q, int64_t ldq, int64_t total_q, cons
                        (int)group, cols, cexp, flip, (uint16_t*)O, ldo, max_len > 0 ? tasks : nullptr, part, vec, ch);
     DUO_LAUNCH_CHECK();
     if (max_len > P::KEYS && wgs > 1) {  // a row of one tile is never split
-      // columns of a row by the bound of new tokens, or more of them one after the other
+      // columns of a row by the bound of new tokens, or more of them one after the other: most workgroups have
+      // none to join (32 by two at once: 2 chunks beside 46 single tokens 10 us more, 32 drafts of up to 5 tokens 2.5;
+      // 4 by two there 3.5 more than 8)
       const int64_t most = std::min<int64_t>({std::max<int64_t>(std::min(max_q, total_q) * group, 1), cols});
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(paged_join_kernel<HD, true>), dim3((unsigned)wgs, (unsigned)cdiv(most, 2)), dim3(256), 0, s,
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(paged_join_kernel<HD, true>), dim3((unsigned)wgs, (unsigned)std::min<int64_t>(cdiv(most, 2), 8)), dim3(256), 0, s,
                          (const Task*)tasks, (const float*)part, g.heads, (int)group, cols, (uint16_t*)O, ldo, vec, ch);
       DUO_LAUNCH_CHECK();
     }

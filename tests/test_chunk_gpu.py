@@ -207,14 +207,15 @@ def test_very_many_rows(duo_lib, fmt, window, sinks):
 
 
 @pytest.mark.parametrize("fmt", ["int8", "int4"])
-def test_overlapping_sequences_of_many_rows(duo_lib, fmt):
+@pytest.mark.parametrize("lq", [150, 170])
+def test_overlapping_sequences_of_many_rows(duo_lib, fmt, lq):
     """More sequences of many rows than the offsets should allow: rows of one and the same sequence."""
     say("chunk overlapping sequences", fmt)
     d, heads, kv, hd = duo_lib, 16, 2, 64
-    b = Batch(d, [(150, 400)], heads, kv, hd, 16, fmt)
+    b = Batch(d, [(lq, 400)], heads, kv, hd, 16, fmt)
     want = b.run()
     b.check(want)
-    cu = torch.tensor([0, 150, 0, 150, 0, 150], dtype=torch.int32, device=DEV)
+    cu = torch.tensor([0, lq, 0, lq, 0, lq], dtype=torch.int32, device=DEV)
     table, lens = b.table.repeat(5, 1), b.lens.repeat(5)
     O = d.duo_attention_chunk(b.Q.to(DEV), b.cache, table, lens, cu, heads)
     b.check(O)
@@ -233,7 +234,7 @@ def test_scale_strides_hints(duo_lib, fmt):
 
 
 @pytest.mark.parametrize("kind", ["keys", "queries", "values", "small values", "large values", "everything"])
-@pytest.mark.parametrize("heads,lq", [(2, 60), (16, 60), (16, 150)])
+@pytest.mark.parametrize("heads,lq", [(2, 60), (16, 60), (16, 150), (16, 170)])
 @pytest.mark.parametrize("fmt", FMTS)
 def test_magnitudes(duo_lib, fmt, heads, lq, kind):
     """Keys, values and queries whose sizes differ by many powers of two, and all values
@@ -311,7 +312,7 @@ def test_lengths_and_offsets_are_cut(duo_lib, fmt):
 
 
 @pytest.mark.parametrize("window,sinks", [(0, 0), (40, 4)])
-@pytest.mark.parametrize("heads,lq", [(2, 5), (16, 60), (16, 150)])
+@pytest.mark.parametrize("heads,lq", [(2, 5), (16, 60), (16, 150), (16, 170)])
 @pytest.mark.parametrize("fmt", FMTS)
 def test_page_outside(duo_lib, fmt, heads, lq, window, sinks):
     """Queries that see a token in a page that is not there are NaN, and only they."""
@@ -337,7 +338,7 @@ def test_page_outside(duo_lib, fmt, heads, lq, window, sinks):
 
 
 @pytest.mark.parametrize("window,sinks", [(0, 0), (20, 3)])
-@pytest.mark.parametrize("heads,lq", [(2, 9), (16, 70), (16, 140)])
+@pytest.mark.parametrize("heads,lq", [(2, 9), (16, 70), (16, 140), (32, 140)])
 @pytest.mark.parametrize("fmt", FMTS)
 def test_unseen_numbers(duo_lib, fmt, heads, lq, window, sinks):
     """Infinities and NaN in keys and values that a query does not see have no influence on
@@ -373,12 +374,13 @@ def test_unseen_numbers(duo_lib, fmt, heads, lq, window, sinks):
             assert np.isfinite(o[i][~bad]).all() and (np.abs(o[i] - r[i])[~bad] <= 2.0 ** -6).all(), (h, i)
 
 
-def test_repeats_streams_and_graphs(duo_lib):
+@pytest.mark.parametrize("lq", [90, 170])
+def test_repeats_streams_and_graphs(duo_lib, lq):
     """The same bits from any workspace, on another stream and in replayed graphs whose lengths
     change between the replays; two graphs share a workspace."""
     say("chunk repeats, streams, graphs")
     d = duo_lib
-    seqs = [(1, 3000), (90, 700), (4, 500)]
+    seqs = [(1, 3000), (lq, 700), (4, 500)]
     b = Batch(d, seqs, 16, 2, 128, 64, "int8")
     Q, w = b.Q.to(DEV), 16 * 128
     size = d.attention_chunk_workspace("int8", len(Q), 3, 16, 2, 128, b.table.shape[1] * 64, DEV).numel()
