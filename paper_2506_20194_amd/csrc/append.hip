@@ -177,8 +177,9 @@ struct AppendArgs {
   int gain_f32, heads, per;
 };
 
-// A token's heads one behind the other: those of Q, of K, of V.  One launch instead of a norm and a rotation
-// each of Q and K and a write: @
+// A token's heads one behind the other: those of Q, of K, of V.  One launch instead of one for Q, one for
+// K and a write: 32 tokens, 64 heads on 8 of 128, 11.6 us and 23.2 (calls from Python), 16411 into 8 bits 125 and 136
+// (5.1 TB/s; the rows' codes cost vector instructions beside the rotation), into 16 bits 124 and 140.
 template <int FMT, int HD>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs g) {
   constexpr int HALF = HD / 2, C = HALF / 8;

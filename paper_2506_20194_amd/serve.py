@@ -106,7 +106,7 @@ def linear(x, W, p_x=None, R=None):
 
 # Rows (new tokens times heads of a group) of a sequence from which on the packed attention over
 # rows read back from a quantised cache is faster than attention over its codes: on 16384 tokens,
-# 64 heads on 8, 32 new ones (256 rows) 66 us and 67, 128 (1024 rows) 105 and 125, 2048 978 and 1120.
+# 64 heads on 8, 32 new ones (256 rows) 64 us and 66, 128 (1024 rows) 105 and 127, 2048 973 and 1105.
 # (Rows read back are rounded to bf16: a root mean square error of 0.003 to 0.005, of codes 0.0018.)
 MANY_ROWS = 1024
 
