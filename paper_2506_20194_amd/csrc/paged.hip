@@ -1147,7 +1147,7 @@ duo_status duo_attention_chunk(const void* Q, int64_t ldq, int64_t total_q, cons
   if ((double)g.heads * ((double)total_q * (double)group / 8 + (double)nseq) * ((double)max_len / kMinKeys + 1 + kRowCost) > 1e12)
     return DUO_ERR_UNSUPPORTED;
   if (nseq == 0 || total_q == 0) return DUO_OK;
-  if (!Q || !O || !lens || !cu_q || (max_len > 0 && !table)) return DUO_ERR_INVALID_ARG;
+  if (!Q || !O || Q == O || !lens || !cu_q || (max_len > 0 && !table)) return DUO_ERR_INVALID_ARG;
   if (ldq % 8 || !aligned16(Q)) return DUO_ERR_UNSUPPORTED;
   const size_t need = duo_attention_chunk_workspace_size(cache->format, total_q, nseq, heads, g.heads, hd, max_len);
   if (need && (!ws || ws_bytes < need || reinterpret_cast<uintptr_t>(ws) % kAlign)) return DUO_ERR_WORKSPACE;

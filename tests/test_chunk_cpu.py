@@ -42,7 +42,7 @@ def test_arguments(codes):
     assert call(n=0, Q=None, O=None, cu=None, lens=None, table=None) == call(tq=0, Q=None, O=None) == d.DUO_OK
     for bad in (dict(tq=-1), dict(n=-1), dict(mq=-1), dict(ml=-1), dict(win=-1), dict(sinks=-1), dict(h=0), dict(h=3), dict(h=65536),
                 dict(ldq=255), dict(ldo=255), dict(ldt=3), dict(ldt=-1), dict(scale=float("nan")), dict(scale=float("inf")),
-                dict(Q=None), dict(O=None), dict(lens=None), dict(cu=None), dict(table=None), dict(cache=_cache(data=None)),
+                dict(Q=None), dict(O=None), dict(O=FAKE), dict(lens=None), dict(cu=None), dict(table=None), dict(cache=_cache(data=None)),
                 dict(cache=_cache(pages=0)), dict(cache=_cache(fmt=3))):
         assert call(**bad) == E, bad
     for odd in (dict(ldq=260), dict(Q=ctypes.c_void_p(FAKE.value + 8)), dict(cache=_cache(page=8)), dict(cache=_cache(hd=96)),
