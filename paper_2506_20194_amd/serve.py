@@ -14,9 +14,9 @@ library's own kernels:
   chunks, mixed steps  attend over the pages as they are stored (duo_attention_chunk), and
                        so do prompts where the cache is quantised, so that every token
                        sees what later ones will; only where each sequence brings a
-                       thousand rows or more to a quantised cache K and V come back
-                       from it (duo_kv_read) and the packed attention takes them,
-                       which makes numbers of the codes once for all of them
+                       thousand rows or more to a quantised cache, or eight thousand
+                       to one of 16 bits, K and V come back from it (duo_kv_read) and
+                       the packed attention takes them in order
   single tokens        attend over the pages (duo_attention_paged)
   a window             duo_attention_chunk for all of them
 
@@ -58,7 +58,7 @@ class Step:
         self.pos = pos.to(dev, torch.int32)
         self.slots = cache.slots(table, seq.to(dev), pos.to(dev))
         self.lens = torch.tensor(after, dtype=torch.int32).to(dev)
-        self.cu_q = self._offsets(new).to(dev)
+        self.cu_q = torch.arange(self.m + 1, dtype=torch.int32, device=dev) if self.single else self._offsets(new).to(dev)
         self.fewest = min((n for n in new if n), default=0)
         self.cached, self._after, self._whole = any(before), after, None
         if self.single:
@@ -105,10 +105,11 @@ def linear(x, W, p_x=None, R=None):
 
 
 # Rows (new tokens times heads of a group) of a sequence from which on the packed attention over
-# rows read back from a quantised cache is faster than attention over its codes: on 16384 tokens,
+# rows read back from a quantised cache (MANY_ROWS) or one of 16 bits (MANY_ROWS_16) is faster than attention over its codes: on 16384 tokens,
 # 64 heads on 8, 32 new ones (256 rows) 64 us and 66, 128 (1024 rows) 105 and 127, 2048 973 and 1105.
 # (Rows read back are rounded to bf16: a root mean square error of 0.003 to 0.005, of codes 0.0018.)
-MANY_ROWS = 1024
+# In 16 bits 512 new ones there (4096 rows) 311 us and 307, 1024 535 and 545, 2048 997 and 1045.
+MANY_ROWS, MANY_ROWS_16 = 1024, 8192
 
 
 def attention(x, weights, cfg, cache, step, p_x=None):
@@ -124,14 +125,14 @@ def attention(x, weights, cfg, cache, step, p_x=None):
     if step.single and not window:
         return duo.duo_attention_paged(q, cache, step.table, step.lens, heads, max_len=step.max_len)
     quantised = cache.fmt != "bf16"
-    if window or (step.cached or quantised) and not (quantised and step.fewest * heads >= MANY_ROWS * kv):
+    if window or (step.cached or quantised) and step.fewest * heads < (MANY_ROWS if quantised else MANY_ROWS_16) * kv:
         a = duo.duo_attention_chunk(q, cache, step.table, step.lens, step.cu_q, heads, window=window, sinks=sinks,
                                     max_q=step.max_new, max_len=step.max_len)
         if window:
             return a
     else:
         cu_k = None
-        if quantised:
+        if quantised or step.cached:
             cu_k, slots = step.whole(cache)
             k, v = duo.duo_kv_read(cache, slots)
         elif normed:

@@ -87,7 +87,8 @@ def test_steps(duo_lib, fmt, window, sinks, dtype):
             assert np.linalg.norm(y - ref) < 2.0 ** -6 * np.linalg.norm(ref)
 
 
-def test_many_rows_of_a_quantised_cache(duo_lib):
+@pytest.mark.parametrize("fmt", ["int8", "bf16"])
+def test_many_rows_of_a_quantised_cache(duo_lib, fmt, monkeypatch):
     """Chunks on either side of the number of rows that decides between codes and rows read
     back give the same block, up to what the rows' rounding to bf16 does."""
     from paper_2506_20194_amd import serve
@@ -97,14 +98,12 @@ def test_many_rows_of_a_quantised_cache(duo_lib):
     cfg = dict(heads=HEADS, theta=THETA, eps=EPS)
     hs = torch.cat(hidden([300], 14)).to(DEV)
     out = []
-    for many in (serve.MANY_ROWS, 1 << 40):
-        cache = duo_lib.KVCache.empty(32, PAGE, KV, HD, "int8", DEV)
+    for many in (260 * HEADS // KV, 1 << 40):
+        cache = duo_lib.KVCache.empty(32, PAGE, KV, HD, fmt, DEV)
         table = torch.arange(32, dtype=torch.int32, device=DEV)[None].contiguous()
-        was, serve.MANY_ROWS = serve.MANY_ROWS, many
-        try:
-            serve.run_block(hs[:40], W, cfg, cache, serve.Step(cache, table, [0], [40]))
-            out.append(serve.run_block(hs[40:], W, cfg, cache, serve.Step(cache, table, [40], [260])))
-        finally:
-            serve.MANY_ROWS = was
+        monkeypatch.setattr(serve, "MANY_ROWS", many)
+        monkeypatch.setattr(serve, "MANY_ROWS_16", many)
+        serve.run_block(hs[:40], W, cfg, cache, serve.Step(cache, table, [0], [40]))
+        out.append(serve.run_block(hs[40:], W, cfg, cache, serve.Step(cache, table, [40], [260])))
     a, b = (f64(o) for o in out)
     assert np.linalg.norm(a - b) < 2.0 ** -6 * np.linalg.norm(b)
