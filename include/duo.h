@@ -642,7 +642,12 @@ duo_status duo_attention_paged(const void* Q, int64_t ldq, const duo_kv_cache* c
  *   new ones among them and last: query i of n is at position p = lens[s] - n + i
  *   and sees the tokens j <= p; with a window > 0 of those the ones with
  *   j > p - window or j < sinks (window 0: none, and sinks do not matter).
- *   Scores, probabilities, pages and lengths as duo_attention_paged; a query that
+ *   Scores, probabilities, pages and lengths as duo_attention_paged, but in 8 and 4 bits with
+ *   more than 64 rows of a sequence (new tokens times heads / kv_heads) numbers and
+ *   probabilities enter their products as fp16 times powers of two: bits of groups whose
+ *   scale is below 2^-18 of the token's largest number are lost, and an output may be off by 2^-21
+ *   of the largest p |V| of all channels of the head for each token.  Scores have to stay
+ *   within 2^24, values times tokens below 2^118.  A query that
  *   sees no token (p < 0) gets 0, one that sees a token in a page outside the
  *   cache NaN.  What a query does not see has no influence on it, whatever it holds,
  *   and entries of table for pages that no query of a sequence sees (behind its

@@ -21,14 +21,18 @@
 // 4 bits, 0.0048 of its root mean square, where the plain form has 0.0017).  fp16's range is made to
 // do by powers of two: a key whose largest number is outside 2^-2 .. 2^8 is brought to 2^7, and its
 // scores take the power back; a row of Q likewise; and a token's values (small ones to 2^-2), whose power goes into the
-// exponent of its probabilities (the running reference is then one of p |V|, not of p) and out of
-// their sum again.  None of that happens with numbers of ordinary size, so the steps that are dealt out
+// exponent of its probabilities (the running reference is then one of p |V|, not of p).  The sum of
+// the p then lies anywhere beside the reference (values reach from 2^-126 to 2^127), and gets a power of its own
+// where it is far from it.  Values are in units of a power of two that the first tile's largest one says; results do not
+// go by it.  None of that happens with numbers of ordinary size, so the steps that are dealt out
 // go without it.  Sequences of very many rows have their numbers made once, by a launch before, into the
 // workspace (rows_make_kernel): 2048 tokens on 16384, 64 heads on 8, 1362 us without in 8 bits, 1110 with
 // it; 320 on 8192, 32 on 8 (1280 rows), 104 and 101, on 65536 558 and 496; with 1024 rows it gains
 // nothing up to 32768.  If there is one among them that needs a power, all of that is left, and they are done from the codes as the
-// others are.  What is lost: bits of groups of 32 channels whose scale is below 2^-20 of 1 (2^-18 of the
-// token's largest number, where that is outside the bounds).
+// others are.  What is lost: bits of groups of 32 channels whose scale is below 2^-18 of the token's largest number, and
+// of probabilities in fp16: up to 2^-25 beside 2^6 and more of the reference's token, which is, with values in
+// [2^-2, 2^8), up to 2^-21 of the largest p |V| of all channels for a key (so a token with a number of 2^27 in one group and
+// ordinary ones in another takes bits of the others' part in both).
 //
 // A sequence with more blocks than there are workgroups gives each the same number of them, whole, the long
 // ones dealt out against the short ones: all workgroups of an XCD then read one head's keys at
@@ -176,15 +180,16 @@ __device__ __forceinline__ f16x mma32(const u32x4& a, const u32x4& b, f16x c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(av, bv, c, 0, 0, 0);
 }
 // The power of two that numbers of at most `top` are divided by so that it lies in [2^lo, 2^hi): 0 where it does, else
-// one that brings it to the upper bound, or (NEAR) to the nearer one.
-template <bool NEAR = false>
+// one that brings it to the upper bound.
 __device__ __forceinline__ int power_of(float top, int lo, int hi) {
   const int e = (int)(__float_as_uint(top) >> 23) - 127;
-  return top == 0.f || e == 128 || (e >= lo && e < hi) ? 0 : NEAR && e < lo ? e - lo : e - (hi - 1);
+  return top == 0.f || e == 128 || (e >= lo && e < hi) ? 0 : e - (hi - 1);
 }
 // Keys and values in fp16 are 2^6 of themselves, for more small ones: those of a token reach from 2^-2 to 2^8 (24 times a
 // scale of 4 bits is then below 2^16).
 constexpr int kRowsBoost = 6, kRowsLo = -2, kRowsHi = 8;
+constexpr int kRowsZero = -512;        // the power of a token whose values are all 0: below any other's
+constexpr int kRowsFold = 60;          // sums lie within 2^+-60 of what they are relative to, or have a power of their own
 
 template <int FMT, int HD>
 struct RowsGeo {
@@ -535,7 +540,12 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     int e_ref = 0;  // power of two that the outputs are in units of: that of the first tile's values
     // Small values go to the lower bound only: what a probability loses to its value's power it lacks in fp16, and
     // beside values just above the bound ones just below it would lose 2^10 at once.
-    auto v_power = [&](const Scales& s) { return min(max(power_of<true>(ldexpf(most_of(s), -e_ref), kRowsLo, kRowsHi), -60), 60); };
+    auto v_power = [&](const Scales& s) {
+      const float most = most_of(s);
+      const int e = (int)(__float_as_uint(most) >> 23) - 127 - e_ref;
+      if (most == 0.f) return kRowsZero;
+      return e < kRowsLo ? e - kRowsLo : e < kRowsHi ? 0 : e - (kRowsHi - 1);
+    };
     // does some key's largest scale mean a power, as far as one look can tell (never no for yes)?
     auto some_power = [&](const Scales& k, const Scales& v) {
       typedef unsigned short u16v2 __attribute__((ext_vector_type(2)));
@@ -609,6 +619,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     // powers of the lane's key and value in this tile, the next and the one after; are there any?
     int kp = 0, kp1 = 0, kp2 = 0, vp = 0, vp1 = 0, vp2 = 0;
     bool odd = false, odd1 = false, odd2 = false, calm = true;
+    int odd_l = 0;  // has some row's sum a power (which it gets in a tile that is odd)?
     auto powers = [&](int* k, int* v) {
       bool some = e_ref != 0 || some_power(kall, vall);
       if (some) {
@@ -732,6 +743,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     }
     const bool odd_q = __any(q_power != 0);
     float m = -INFINITY, mc = -INFINITY, l = 0.f;  // reference, times cexp; sum of this half's keys
+    int l_power = 0;  // (8 and 4 bits) the sum is l 2^l_power
     f16x o[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -958,18 +970,33 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
             units = 1.f;
           }
         }
+        const float mc0 = mc, l0 = l;
         if (refer(sc, &f, units) && u > 0) scale_o(f);
         float sum = probabilities(sc, pf, units);
-        if constexpr (F16)
+        if constexpr (G::QUANT)
           if (any_power) {
+            // The sum is one of p, not of p |V|, and where values lie far apart the reference says nothing of its
+            // size: it has a power of its own, and where that is small (fewer than 60 either way) none.
+            constexpr int NONE = -(1 << 20);
             const int from_lane = (u & 1) * 32 + 4 * (anew(lane) >> 5);
             const float base = mc == -INFINITY ? 0.f : base_of();
-            sum = 0.f;
+            float most = -INFINITY;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-              const int power = __shfl(vp, from_lane + 8 * (r >> 2) + (r & 3));
-              sum += ldexpf(__builtin_amdgcn_exp2f(sc[r] - base), -power);
+              sc[r] -= (float)__shfl(vp, from_lane + 8 * (r >> 2) + (r & 3));
+              most = fmaxf(most, sc[r]);
             }
+            const float moved = mc0 == -INFINITY ? 0.f : fmaxf(mc0 - mc, -4096.f), whole_moved = floorf(moved);
+            const int l_exp = __builtin_amdgcn_frexp_expf(l0);  // l0 2^-l_exp is in [1/2, 1)
+            const int was = l0 == 0.f ? NONE : l_power + l_exp + (int)whole_moved;
+            int power = most == -INFINITY ? was : max(was, (int)ceilf(fminf(fmaxf(most - base, -4096.f), 4096.f)));
+            if (abs(power) <= kRowsFold || power == NONE) power = 0;
+            l = l0 == 0.f ? 0.f : ldexpf(ldexpf(l0, -l_exp) * __builtin_amdgcn_exp2f(moved - whole_moved), was - power);
+            l_power = power;
+            odd_l = same(__any(power != 0));
+            sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(sc[r] - base - (float)power);
           }
         l += sum;
         if (u + 1 < nu) score(u + 1, sn);
@@ -1015,6 +1042,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
       turn(i);
       slow(2 * i + 1, sb, sa);
       next();
+      if (G::QUANT && odd_l) odd = true, calm = false;
       // two tiles at a time, the odd one first, so that places in LDS are known when compiled
       for (++i; (i & 1) && 2 * i - 1 >= f0 && 2 * i < fast_end && calm; i += 2) {
         fast(std::integral_constant<int, 2>{}, sa, sb);
@@ -1029,43 +1057,52 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     }
     if (nu > 0 && nu == 2 * n) add(nu - 1);
     written();
-    if (G::QUANT && e_ref)
-#pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[d][r] = ldexpf(o[d][r], e_ref);
     // ---- out
     const int le = anew(lane);
+    if constexpr (G::QUANT)
+      if (__any(l_power != 0)) {  // both halves' sums with one power, the larger one of those that are not 0
+        const int mine = l == 0.f ? INT32_MIN : l_power;
+        const auto both = __builtin_amdgcn_permlane32_swap((uint32_t)mine, (uint32_t)mine, false, false);
+        const int power = max((int)both[0], (int)both[1]);
+        l = l == 0.f ? 0.f : ldexpf(l, l_power - power);
+        l_power = power == INT32_MIN ? 0 : power;
+      }
     const auto rl = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     float sum = __uint_as_float(rl[0]) + __uint_as_float(rl[1]);
-    if (F16) sum *= (float)(1 << kRowsBoost);  // as the values are
+    const int o_power = G::QUANT ? e_ref - l_power : 0;  // of the outputs, with a sum that has none
     if (!whole) {
       float* const part = a.parts + (2 * (int64_t)share + (t0 == 0)) * rows_part(HD);
       if (t0 == 0 && tid == 0) {
         const int64_t end = block + min(kRowsCost + (tiles - 1) * KB + 1, cost - near(cost));
         a.tasks[share] = RowsTask{share_of(end - 1) - share + 1, seq_q0 + qi0, head0, heads, rows, pos0};
       }
+      // the sum in [1/2, 1), its power with the reference: those of all parts are then comparable, whatever their values' sizes
+      const int s_power = G::QUANT ? __builtin_amdgcn_frexp_expf(sum) : 0;
+      sum = ldexpf(sum, -s_power);
+      auto out = [&](float v) { return F16 ? ldexpf(v, o_power - s_power - kRowsBoost) : v; };
       if (row0 + (le & 31) < rows) {
-        if (le < 32) *(float2*)(part + QB * HD + 2 * (row0 + (le & 31))) = make_float2(mc, sum);
+        if (le < 32) *(float2*)(part + QB * HD + 2 * (row0 + (le & 31))) = make_float2(G::QUANT ? mc + (float)(l_power + s_power) : mc, sum);
         float* const y = part + (row0 + (le & 31)) * HD + 4 * (le >> 5);
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
           for (int g = 0; g < 4; ++g)
-            *(f4*)(y + 32 * d + 8 * g) = f4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
+            *(f4*)(y + 32 * d + 8 * g) = f4{out(o[d][4 * g]), out(o[d][4 * g + 1]), out(o[d][4 * g + 2]), out(o[d][4 * g + 3])};
       }
       continue;
     }
     // queries that see no key: 0; a sum of 0 (every score -inf) gives NaN
     const Row w = row_of(le);
-    const float inv = pos0 + w.qi < 0 ? 0.f : 1.0f / sum;
+    const float inv = pos0 + w.qi < 0 ? 0.f : 1.0f / (F16 ? ldexpf(sum, kRowsBoost) : sum);  // as the values are
+    // the power comes behind the division: outputs times it may be out of fp32's range
+    auto out = [&](float v) { return G::QUANT ? ldexpf(v * inv, o_power) : v * inv; };
     uint2 y[DB][4];
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        y[d][g].x = pack_bf16(o[d][4 * g] * inv, o[d][4 * g + 1] * inv);
-        y[d][g].y = pack_bf16(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv);
+        y[d][g].x = pack_bf16(out(o[d][4 * g]), out(o[d][4 * g + 1]));
+        y[d][g].y = pack_bf16(out(o[d][4 * g + 2]), out(o[d][4 * g + 3]));
       }
     if (a.vec) {
       // through this wave's part of LDS, where K tiles were (every wave was done with them at the
