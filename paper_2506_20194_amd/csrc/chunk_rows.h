@@ -24,7 +24,7 @@
 // exponent of its probabilities (the running reference is then one of p |V|, not of p).  The sum of
 // the p then lies anywhere beside the reference (values reach from 2^-126 to 2^127), and gets a power of its own
 // where it is far from it.  Values are in units of a power of two that the first tile's largest one says; results do not
-// go by it.  None of that happens with numbers of ordinary size, so the steps that are dealt out
+// go by it, nor by keys that no query of the block sees.  None of that happens with numbers of ordinary size, so the steps that are dealt out
 // go without it.  Sequences of very many rows have their numbers made once, by a launch before, into the
 // workspace (rows_make_kernel): 2048 tokens on 16384, 64 heads on 8, 1362 us without in 8 bits, 1110 with
 // it; 320 on 8192, 32 on 8 (1280 rows), 104 and 101, on 65536 558 and 496; with 1024 rows it gains
@@ -189,6 +189,7 @@ __device__ __forceinline__ int power_of(float top, int lo, int hi) {
 // scale of 4 bits is then below 2^16).
 constexpr int kRowsBoost = 6, kRowsLo = -2, kRowsHi = 8;
 constexpr int kRowsZero = -512;        // the power of a token whose values are all 0: below any other's
+constexpr uint32_t kRowsDead = ~0u;    // scales of a key that no query of a block sees (kv_encode stores no such NaN)
 constexpr int kRowsFold = 60;          // sums lie within 2^+-60 of what they are relative to, or have a power of their own
 
 template <int FMT, int HD>
@@ -524,6 +525,16 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
       };
       load(s, k);
       load(s + v_scales, v);
+      // keys that no query of the block sees have no say in the powers
+      const int k0 = place(t) * KB;
+      if (lost || k0 + KB - 1 > pos_end || (k0 < first && k0 + KB > a.sinks)) {
+        const int seen = k0 + x;
+        const int id = __shfl(pid, (min(seen, len - 1) >> a.kv.shift) - win);
+        // (without a branch of its own: lanes that part here made the compiler take pages' addresses for theirs)
+        const uint32_t dead = (seen > pos_end) | ((seen < first) & (seen >= a.sinks)) | (id < 0) | (id >= a.kv.pages) ? kRowsDead : 0u;
+#pragma unroll
+        for (int i = 0; i < HD / 64; ++i) k->w[i] |= dead, v->w[i] |= dead;
+      }
     };
     // the largest number that the key's codes can stand for (a scale that is NaN aside)
     auto most_of = [&](const Scales& s) {
@@ -543,7 +554,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     auto v_power = [&](const Scales& s) {
       const float most = most_of(s);
       const int e = (int)(__float_as_uint(most) >> 23) - 127 - e_ref;
-      if (most == 0.f) return kRowsZero;
+      if (most == 0.f) return s.w[0] == kRowsDead ? 0 : kRowsZero;
       return e < kRowsLo ? e - kRowsLo : e < kRowsHi ? 0 : e - (kRowsHi - 1);
     };
     // does some key's largest scale mean a power, as far as one look can tell (never no for yes)?

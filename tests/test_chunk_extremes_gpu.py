@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from oracle import serve_ref as S
-from test_chunk_gpu import FMTS, Batch, say
+from test_chunk_gpu import FMTS, Batch, say, seen
 
 pytestmark = pytest.mark.gpu
 ROWS = [(2, 9), (16, 60), (16, 150), (16, 170)]  # heads (on 2) and new tokens: 9, 480, 1200 and 1360 rows
@@ -56,6 +56,31 @@ def test_unseen_before(duo_lib, fmt, heads, lq, power):
 
     b = Batch(duo_lib, [(lq, n), (lq, 90)], heads, 2, 128, 64, fmt, window=window, sinks=3, touch=touch)
     b.check(b.run())
+
+
+@pytest.mark.parametrize("power", [100, -100])
+@pytest.mark.parametrize("heads,lq", ROWS)
+@pytest.mark.parametrize("fmt", FMTS)
+def test_page_of_another(duo_lib, fmt, heads, lq, power):
+    """A page that is not there, in the first tile and behind the window: whatever page 0 holds,
+    queries that do not see it get the same bits."""
+    say("chunk extremes, page 0", fmt, heads, lq, power)
+    n, window = 300, 100
+    out = []
+    for p in (0, power):
+        b = Batch(duo_lib, [(lq, n)], heads, 2, 128, 16, fmt, window=window, sinks=0)
+        page = (n - lq - window + 1) // 16  # the first that some query sees
+        free = next(i for i in range(len(b.cache.data)) if not (b.table == i).any())
+        b.cache.data[free] = b.cache.data[0]
+        b.table[b.table == 0] = free
+        v = torch.randn((16, 2 * 128), generator=torch.Generator().manual_seed(3)) * 2.0 ** p
+        duo_lib.duo_kv_write(b.cache, v.bfloat16().cuda(), v.bfloat16().cuda(), torch.arange(16).cuda())
+        b.table[0, page] = -1
+        O = b.run()
+        hit = torch.from_numpy(seen(lq, n, window, 0)[:, 16 * page:16 * page + 16].any(1)).to(O.device)
+        assert torch.isnan(O[hit]).all() and torch.isfinite(O[~hit]).all()
+        out.append(O[~hit])
+    assert torch.equal(*out)
 
 
 @pytest.mark.parametrize("power", [80, 110, -80, -110])
