@@ -656,7 +656,8 @@ duo_status duo_attention_paged(const void* Q, int64_t ldq, const duo_kv_cache* c
  *   knows one (else total_q); how the work is cut goes by it, results are right with
  *   any.  Everything is split by the sizes and the lengths alone: results are
  *   deterministic.  Q 16-byte aligned, ldq % 8 == 0 (else DUO_ERR_UNSUPPORTED); O must
- *   not overlap Q.  total_q * heads, nseq and max_len at most 2^30.
+ *   not overlap Q (DUO_ERR_INVALID_ARG; columns beside each other in rows of one stride do not).
+ *   total_q * heads, nseq and max_len at most 2^30.
  *   Workspace: duo_attention_chunk_workspace_size with the cache's format and the same sizes
  *   (with 8 and 4 bits up to 1 GiB of it for rows made of codes, where sizes allow
  *   sequences of very many rows). */

@@ -1057,6 +1057,17 @@ int64_t paged_wgs(double rows, int64_t tiles, int most) {
   return cost < most ? std::max<int64_t>(1, (int64_t)std::ceil(cost)) : most;
 }
 
+// Do the m rows of w 2-byte numbers at a (stride lda) and b have bytes in common, as far as strides of one
+// length tell: with two lengths, rows that lie between each other are taken for such.
+bool rows_overlap(const void* a, int64_t lda, const void* b, int64_t ldb, int64_t m, int64_t w) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  const uintptr_t row = (uintptr_t)w * 2, ea = x + (uintptr_t)(m - 1) * lda * 2 + row, eb = y + (uintptr_t)(m - 1) * ldb * 2 + row;
+  if (x >= eb || y >= ea) return false;
+  if (lda != ldb || m == 1) return true;
+  const uintptr_t stride = (uintptr_t)lda * 2, d = x > y ? (x - y) % stride : (y - x) % stride;  // beside each other in wider rows
+  return d < row || stride - d < row;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1147,7 +1158,8 @@ duo_status duo_attention_chunk(const void* Q, int64_t ldq, int64_t total_q, cons
   if ((double)g.heads * ((double)total_q * (double)group / 8 + (double)nseq) * ((double)max_len / kMinKeys + 1 + kRowCost) > 1e12)
     return DUO_ERR_UNSUPPORTED;
   if (nseq == 0 || total_q == 0) return DUO_OK;
-  if (!Q || !O || Q == O || !lens || !cu_q || (max_len > 0 && !table)) return DUO_ERR_INVALID_ARG;
+  if (!Q || !O || !lens || !cu_q || (max_len > 0 && !table)) return DUO_ERR_INVALID_ARG;
+  if (rows_overlap(Q, ldq, O, ldo, total_q, heads * hd)) return DUO_ERR_INVALID_ARG;
   if (ldq % 8 || !aligned16(Q)) return DUO_ERR_UNSUPPORTED;
   const size_t need = duo_attention_chunk_workspace_size(cache->format, total_q, nseq, heads, g.heads, hd, max_len);
   if (need && (!ws || ws_bytes < need || reinterpret_cast<uintptr_t>(ws) % kAlign)) return DUO_ERR_WORKSPACE;
