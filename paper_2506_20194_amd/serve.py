@@ -60,7 +60,7 @@ class Step:
         self.lens = torch.tensor(after, dtype=torch.int32).to(dev)
         self.cu_q = torch.arange(self.m + 1, dtype=torch.int32, device=dev) if self.single else self._offsets(new).to(dev)
         self.fewest = min((n for n in new if n), default=0)
-        self.cached, self._after, self._whole = any(before), after, None
+        self.cached = any(before)
         if self.single:
             return
         # token rows of sequences whose tokens do not all have a page; duo_kv_write skips such
@@ -68,17 +68,14 @@ class Step:
         need = torch.arange(table.shape[1]) * cache.page_size < torch.tensor(after, dtype=torch.int64)[:, None]
         outside = (table < 0) | (table >= cache.data.shape[0])
         self.lost = (outside & need.to(dev)).any(1)[seq.to(dev)][:, None]
-
-    def whole(self, cache):
-        """Offsets (None: the chunk's own rows are all) and slots of the whole sequences."""
-        if self._whole is None:
-            cu_k, slots = None, self.slots
-            if self.cached:
-                seq, pos = self._tokens([0] * len(self._after), self._after)
-                dev = self.table.device
-                cu_k, slots = self._offsets(self._after).to(dev), cache.slots(self.table, seq.to(dev), pos.to(dev))
-            self._whole = cu_k, slots
-        return self._whole
+        # offsets and slots of the whole sequences, where the chunk's own rows of K and V are not all of
+        # them; here and not where they are used, as that may be while a graph is captured, on another stream,
+        # or when the table has gone on
+        self.cu_k, self.all_slots = None, self.slots
+        if self.cached:
+            self.cu_k = self._offsets(after).to(dev)
+            seq = torch.repeat_interleave(torch.arange(len(after), device=dev), self.lens.long(), output_size=sum(after))
+            self.all_slots = cache.slots(table, seq, torch.arange(len(seq), device=dev) - self.cu_k.long()[seq])
 
     @staticmethod
     def _tokens(first, count):
@@ -131,15 +128,13 @@ def attention(x, weights, cfg, cache, step, p_x=None):
         if window:
             return a
     else:
-        cu_k = None
         if quantised or step.cached:
-            cu_k, slots = step.whole(cache)
-            k, v = duo.duo_kv_read(cache, slots)
+            k, v = duo.duo_kv_read(cache, step.all_slots)
         elif normed:
             duo.duo_head_norm_rope(k, kv, hd, step.pos, k_gain, cfg["eps"], theta, out=k)
         else:
             duo.duo_rope_at(k, kv, hd, step.pos, theta, out=k)
-        a = duo.duo_attention_packed(q, k, v, step.cu_q, heads, kv, hd, cu_k=cu_k)
+        a = duo.duo_attention_packed(q, k, v, step.cu_q, heads, kv, hd, cu_k=step.cu_k)
     return a.masked_fill_(step.lost, float("nan"))  # as duo_attention_paged does by itself
 
 

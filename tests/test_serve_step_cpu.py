@@ -1,0 +1,68 @@
+"""What a served step holds and which of the library's calls it makes (no GPU needed: the calls
+are recorded instead of made)."""
+
+import pytest
+import torch
+
+from paper_2506_20194_amd import duo, serve
+
+HEADS, KV, HD, D, PAGE = 8, 2, 64, 96, 16
+
+
+@pytest.fixture()
+def calls(duo_lib, monkeypatch):
+    """serve.attention without a device: the names and arguments of its calls."""
+    made = []
+    like = lambda n, w: torch.zeros(n, w, dtype=torch.bfloat16)
+    results = dict(
+        duo_kv_append=lambda *a, **k: None, duo_linear=lambda x, W, R=None: like(len(x), len(W)), duo_rope_at=lambda X, *a, **k: X,
+        duo_head_norm_rope=lambda X, *a, **k: X, duo_kv_read=lambda cache, slots: (like(len(slots), KV * HD), like(len(slots), KV * HD)),
+        duo_attention_paged=lambda q, *a, **k: q, duo_attention_chunk=lambda q, *a, **k: q, duo_attention_packed=lambda q, *a, **k: q)
+    for name, f in results.items():
+        monkeypatch.setattr(duo, name, lambda *a, _n=name, _f=f, **k: made.append((_n, a, k)) or _f(*a, **k))
+    return made
+
+
+def cache_of(fmt="bf16", pages=40):
+    return duo.KVCache.empty(pages, PAGE, KV, HD, fmt, "cpu")
+
+
+def weights(**more):
+    W = {nm: torch.zeros(n * HD, D, dtype=torch.bfloat16) for nm, n in (("q", HEADS), ("k", KV), ("v", KV))}
+    return {**W, **more}
+
+
+def attend(cache, step, W=None, **cfg):
+    cfg = dict(dict(heads=HEADS, theta=1e4, eps=1e-5), **cfg)
+    return serve.attention(torch.zeros(step.m, D, dtype=torch.bfloat16), W or weights(), cfg, cache, step)
+
+
+@pytest.mark.parametrize("before,new", [([37, 0, 5], [60, 3, 100]), ([1, 1], [2, 300]), ([16, 0], [0, 20])])
+def test_whole_sequences_are_those_of_the_table_at_the_start(calls, monkeypatch, before, new):
+    """Slots and offsets of the whole sequences belong to the step from its start on: a table that
+    is changed afterwards, as for a later step, does not change them, and nothing is
+    made of host data inside the block, which may be captured into a graph or run on another stream."""
+    monkeypatch.setattr(serve, "MANY_ROWS_16", 0)
+    cache = cache_of()
+    table = torch.randperm(40, generator=torch.Generator().manual_seed(1))[:len(new) * 20 // len(new) * len(new)].int()
+    table = table[:len(new) * (len(table) // len(new))].view(len(new), -1)
+    was = table.clone()
+    step = serve.Step(cache, table, before, new)
+    table.fill_(-1)
+    with monkeypatch.context() as m:
+        m.setattr(torch, "tensor", lambda *a, **k: pytest.fail("host data inside the block"))
+        attend(cache, step)
+    (_, (_, slots), _), = [c for c in calls if c[0] == "duo_kv_read"]
+    after = [b + n for b, n in zip(before, new)]
+    want = [int(was[s, t // PAGE]) * PAGE + t % PAGE for s, n in enumerate(after) for t in range(n)]
+    assert slots.dtype == torch.int64 and slots.tolist() == want
+    (_, _, k), = [c for c in calls if c[0] == "duo_attention_packed"]
+    assert k["cu_k"].dtype == torch.int32 and k["cu_k"].tolist() == [sum(after[:i]) for i in range(len(after) + 1)]
+
+
+def test_prompts_are_their_own_whole_sequences(calls):
+    cache = cache_of()
+    step = serve.Step(cache, torch.arange(40, dtype=torch.int32).view(2, 20), [0, 0], [70, 9])
+    attend(cache, step)
+    assert [c[0] for c in calls if "attention" in c[0] or "read" in c[0]] == ["duo_attention_packed"]
+    assert calls[-1][2]["cu_k"] is None and step.all_slots is step.slots
