@@ -115,7 +115,9 @@ def attention(x, weights, cfg, cache, step, p_x=None):
     heads, kv, hd, theta = cfg["heads"], cache.kv_heads, cache.head_dim, cfg["theta"]
     window, sinks = cfg.get("window"), cfg.get("sinks", 0)
     q_gain, k_gain = weights.get("q_norm"), weights.get("k_norm")
-    normed = q_gain is not None or k_gain is not None
+    normed = q_gain is not None
+    if normed != (k_gain is not None):
+        raise ValueError("attention: q_norm and k_norm go together (ones for a norm without gains)")
     q, k, v = (linear(x, weights[nm], p_x) for nm in "qkv")
     duo.duo_kv_append(cache, k, v, step.slots, step.pos, theta, eps=cfg["eps"] if normed else None, k_gain=k_gain, Q=q,
                       q_gain=q_gain, out=q)
@@ -141,7 +143,7 @@ def attention(x, weights, cfg, cache, step, p_x=None):
 def run_block(h, weights, cfg, cache, step, p_x=None):
     """One decoder block for the step's rows: h (step.m x d bf16) -> the same shape.
     weights: q, k, v, o, gate, up, down, and q_norm, k_norm where the heads of queries and
-    keys are normed before the rotation (head_dim gains each, one dtype); cfg:
+    keys are normed before the rotation (head_dim gains each, one dtype, both or neither); cfg:
     dict(heads, theta, eps), and window, sinks where a token sees the last `window`
     ones and the first `sinks` alone; cache: this block's (its kv_heads and head_dim
     are the block's)."""

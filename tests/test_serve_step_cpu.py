@@ -66,3 +66,15 @@ def test_prompts_are_their_own_whole_sequences(calls):
     attend(cache, step)
     assert [c[0] for c in calls if "attention" in c[0] or "read" in c[0]] == ["duo_attention_packed"]
     assert calls[-1][2]["cu_k"] is None and step.all_slots is step.slots
+
+
+@pytest.mark.parametrize("one", ["q_norm", "k_norm"])
+def test_norms_go_together(calls, one):
+    """Gains for the heads of queries or of keys alone: which norm the other ones should have is not said."""
+    cache = cache_of()
+    step = serve.Step(cache, torch.arange(40, dtype=torch.int32).view(1, 40), [0], [5])
+    with pytest.raises(ValueError, match="q_norm and k_norm"):
+        attend(cache, step, weights(**{one: torch.ones(HD)}))
+    assert not calls
+    attend(cache, step, weights(q_norm=torch.ones(HD), k_norm=torch.ones(HD)))
+    assert calls[3][0] == "duo_kv_append" and calls[3][2]["eps"] == 1e-5
