@@ -13,10 +13,9 @@ library's own kernels:
   whole prompts        attend to the packed sequences (duo_attention_packed)
   chunks, mixed steps  attend over the pages as they are stored (duo_attention_chunk), and
                        so do prompts where the cache is quantised, so that every token
-                       sees what later ones will; only where each sequence brings a
-                       thousand rows or more to a quantised cache, or eight thousand
-                       to one of 16 bits, K and V come back from it (duo_kv_read) and
-                       the packed attention takes them in order
+                       sees what later ones will; where the sequences bring many rows or
+                       have few tokens (reads_back), K and V come back from the cache
+                       (duo_kv_read) and the packed attention takes them in order
   single tokens        attend over the pages (duo_attention_paged)
   a window             duo_attention_chunk for all of them
 
@@ -60,7 +59,7 @@ class Step:
         self.lens = torch.tensor(after, dtype=torch.int32).to(dev)
         self.cu_q = torch.arange(self.m + 1, dtype=torch.int32, device=dev) if self.single else self._offsets(new).to(dev)
         self.fewest = min((n for n in new if n), default=0)
-        self.cached = any(before)
+        self.cached, self.tokens = any(before), sum(after)
         if self.single:
             return
         # token rows of sequences whose tokens do not all have a page; duo_kv_write skips such
@@ -101,12 +100,30 @@ def linear(x, W, p_x=None, R=None):
     return duo.duo_linear(x, W, R=R)
 
 
-# Rows (new tokens times heads of a group) of a sequence from which on the packed attention over
-# rows read back from a quantised cache (MANY_ROWS) or one of 16 bits (MANY_ROWS_16) is faster than attention over its codes: on 16384 tokens,
-# 64 heads on 8, 32 new ones (256 rows) 64 us and 66, 128 (1024 rows) 105 and 127, 2048 973 and 1105.
-# (Rows read back are rounded to bf16: a root mean square error of 0.003 to 0.005, of codes 0.0018.)
-# In 16 bits 512 new ones there (4096 rows) 311 us and 307, 1024 535 and 545, 2048 997 and 1045.
-MANY_ROWS, MANY_ROWS_16 = 1024, 8192
+# Chunks behind cached tokens, and all of a quantised cache, either attend over the pages or have their sequences'
+# rows read back for the packed attention.  Reading costs time for every token that is cached, whatever is new, the
+# attention over pages more for each row (a new token and head of a group) and to begin with.  So rows are read back
+# from MANY_ROWS (MANY_ROWS_16: a cache of 16 bits) of every sequence on, and where little is cached from
+# fewer, a part of these, of some sequence on.  Heads of 128, pages and rows read back, in microseconds:
+#   8 bits, 65536 tokens of 8 K/V heads, 64 rows 106 and 156, 512 220 and 233, 768 311 and 286, 1024 398 and 351
+#   up to 2^18 tokens times K/V heads (32768 of 8): 256 rows 92 and 99, 384 112 and 109, 512 128 and 127, 1024 218 and 185
+#   up to 2^17 (16384 of 8): 32 rows 37 and 56 (16 bits), 64 55 and 54, 128 73 and 61, 1024 129 and 106; 4 of 4096: 32 35
+#   and 43, 64 49 and 53, 128 66 and 54; 2048: 32 21 and 26 (16 bits), 64 31 and 27, 512 51 and 31; a chunk of 512 on 2048 and
+#   three single tokens 105 and 59
+#   16 bits, 16384 tokens of 8, 512 rows 71 and 82, 2048 177 and 185, 8192 533 and 523, 16384 1013 and 971
+#   up to 1.5 2^16 (4096 of 8): 32 rows 25 and 31, 64 42 and 32, 128 41 and 33, 1024 54 and 52; 16 sequences, chunks of 256 on
+#   1024 beside single tokens 74 and 43
+# (Rows read back of a quantised cache are rounded to bf16: a root mean square error of the output of 0.003 to
+# 0.005, of codes 0.0018.)
+MANY_ROWS, MANY_ROWS_16 = 768, 8192
+
+
+def reads_back(step, cache, heads):
+    """Are a chunk's sequences read back for the packed attention?"""
+    size, fewest, most = step.tokens * cache.kv_heads, (step.fewest * heads) // cache.kv_heads, (step.max_new * heads) // cache.kv_heads
+    if cache.fmt == "bf16":
+        return fewest >= MANY_ROWS_16 or size <= 3 << 15 and most >= MANY_ROWS_16 >> 7
+    return fewest >= MANY_ROWS or size <= 1 << 18 and most >= MANY_ROWS >> 1 or size <= 1 << 17 and most >= MANY_ROWS >> 4
 
 
 def attention(x, weights, cfg, cache, step, p_x=None):
@@ -124,7 +141,7 @@ def attention(x, weights, cfg, cache, step, p_x=None):
     if step.single and not window:
         return duo.duo_attention_paged(q, cache, step.table, step.lens, heads, max_len=step.max_len)
     quantised = cache.fmt != "bf16"
-    if window or (step.cached or quantised) and step.fewest * heads < (MANY_ROWS if quantised else MANY_ROWS_16) * kv:
+    if window or (step.cached or quantised) and not reads_back(step, cache, heads):
         a = duo.duo_attention_chunk(q, cache, step.table, step.lens, step.cu_q, heads, window=window, sinks=sinks,
                                     max_q=step.max_new, max_len=step.max_len)
         if window:

@@ -16,7 +16,7 @@ def calls(duo_lib, monkeypatch):
     like = lambda n, w: torch.zeros(n, w, dtype=torch.bfloat16)
     results = dict(
         duo_kv_append=lambda *a, **k: None, duo_linear=lambda x, W, R=None: like(len(x), len(W)), duo_rope_at=lambda X, *a, **k: X,
-        duo_head_norm_rope=lambda X, *a, **k: X, duo_kv_read=lambda cache, slots: (like(len(slots), KV * HD), like(len(slots), KV * HD)),
+        duo_head_norm_rope=lambda X, *a, **k: X, duo_kv_read=lambda cache, slots: (like(1, 1), like(1, 1)),
         duo_attention_paged=lambda q, *a, **k: q, duo_attention_chunk=lambda q, *a, **k: q, duo_attention_packed=lambda q, *a, **k: q)
     for name, f in results.items():
         monkeypatch.setattr(duo, name, lambda *a, _n=name, _f=f, **k: made.append((_n, a, k)) or _f(*a, **k))
@@ -78,3 +78,44 @@ def test_norms_go_together(calls, one):
     assert not calls
     attend(cache, step, weights(q_norm=torch.ones(HD), k_norm=torch.ones(HD)))
     assert calls[3][0] == "duo_kv_append" and calls[3][2]["eps"] == 1e-5
+
+
+# new tokens and tokens before them, K/V heads, cache: over which rows the attention goes.  Times of both ways on the
+# left and right of each (attention over the pages, rows read back), heads of 128, in microseconds.
+WAYS = [
+    ("int8", 8, [16384 - 64], [64], "packed"),            # 85 and 78
+    ("int8", 8, [4096 - 16] * 4, [16] * 4, "packed"),     # 66 and 54
+    ("int8", 8, [2048 - 8], [8], "packed"),               # 31 and 27
+    ("int4", 8, [4096 - 32], [32], "packed"),             # 50 and 36
+    ("int8", 8, [16384 - 4], [4], "chunk"),               # 37 and 56 (16 bits)
+    ("int8", 8, [512 - 4] * 8, [4] * 8, "chunk"),         # 26 and 29
+    ("int8", 8, [32768 - 32], [32], "chunk"),             # 92 and 99
+    ("int8", 8, [8192 - 64] * 4, [64] * 4, "packed"),     # 137 and 126
+    ("int8", 8, [65536 - 64], [64], "chunk"),             # 220 and 233
+    ("int8", 8, [65536 - 128], [128], "packed"),          # 398 and 351
+    ("int4", 32, [16384 - 256] * 4, [256] * 4, "chunk"),  # 412 and 681
+    ("int8", 8, [1536] + [999] * 3, [512, 1, 1, 1], "packed"),           # 105 and 59
+    ("int8", 8, [7168] + [3999] * 7, [1024] + [1] * 7, "chunk"),         # 333 and 320
+    ("int8", 8, [0, 3300] + [5999] * 46, [1024, 700] + [1] * 46, "chunk"),  # 323 and 648
+    ("int8", 8, [0, 0], [9, 300], "packed"),
+    ("bf16", 8, [2048 - 64], [64], "packed"),             # 41 and 31
+    ("bf16", 8, [4096 - 16], [16], "packed"),             # 41 and 33
+    ("bf16", 8, [512 - 4] * 8, [4] * 8, "chunk"),         # 24 and 25
+    ("bf16", 8, [16384 - 64], [64], "chunk"),             # 71 and 82
+    ("bf16", 8, [65536 - 512], [512], "chunk"),           # 1087 and 1235
+    ("bf16", 8, [16384 - 2048], [2048], "packed"),        # 1013 and 971
+    ("bf16", 8, [768] * 2 + [499] * 14, [256] * 2 + [1] * 14, "packed"),  # 74 and 43
+    ("bf16", 8, [0, 0], [9, 300], "packed"),
+]
+
+
+@pytest.mark.parametrize("fmt,kv,before,new,way", WAYS)
+def test_ways(calls, fmt, kv, before, new, way):
+    """Chunks take the way that is faster for their sizes (64 query heads, or 32 on 32)."""
+    heads = 64 if kv == 8 else 32
+    after = [b + n for b, n in zip(before, new)]
+    cache = duo.KVCache.empty(4, 256, kv, 128, fmt, "cpu")
+    step = serve.Step(cache, torch.zeros(len(new), -(-max(after) // 256), dtype=torch.int32), before, new)
+    W = {nm: torch.zeros(n * 128, 8, dtype=torch.bfloat16) for nm, n in (("q", heads), ("k", kv), ("v", kv))}
+    serve.attention(torch.zeros(step.m, 8, dtype=torch.bfloat16), W, dict(heads=heads, theta=1e4, eps=1e-5), cache, step)
+    assert calls[-1][0] == "duo_attention_" + way
