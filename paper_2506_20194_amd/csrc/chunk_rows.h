@@ -55,6 +55,8 @@ constexpr int kRowsCost = 128;   // what a block's start and end cost, in keys (
 constexpr int kRowsMin = 512;    // smallest share, in keys: 16 tokens on 16384, 64 heads on 8, 60 us, 98 with 256
 constexpr int kRowsMany = 1279;  // sequences with more rows than this have their numbers made of codes before
 constexpr int kRowsSnap = 512;   // a share's end moves to a block's end that is no further than this
+// Tokens are 2^30 at most: a place behind all of a block, and a window that hides none.
+constexpr int kRowsAll = INT32_MAX, kRowsBack = 1 << 30;
 
 struct RowsArgs {
   const uint16_t* Q;
@@ -354,7 +356,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
       p.s = s_next, p.hs = same(head), p.at = 0;
       p.qb = same(q.nb + q.dealt - 1 - (round * a.deal + (round & 1 ? a.deal - 1 - j : j)));
     }
-    const int cost = dealing ? INT32_MAX / 2 : q.cost(p.qb, a);  // all of a block that is dealt out
+    const int cost = dealing ? kRowsAll : q.cost(p.qb, a);  // all of a block that is dealt out
     const int64_t block = u - p.at;  // where it begins in the count
     const int from_at = same((int)p.at), to_at = same(dealing ? cost : (int)min((int64_t)cost, u1 - block));
     const int kvh = same(p.hs / a.nsub), sub = same(p.hs - kvh * a.nsub);
@@ -771,7 +773,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     const uint32_t nf = (uint32_t)same(max(f1 - f0, 0));
     auto masked = [&](int u) { return (uint32_t)(u - f0) >= nf; };
     // of the query at position pos
-    const int back = a.window ? a.window : INT32_MAX / 2;
+    const int back = a.window ? a.window : kRowsBack;
     auto sees = [&](int pos, int key) { return key <= pos && (key > pos - back || key < a.sinks); };
 
     f16x sa, sb;  // scores of an even and of an odd step
