@@ -645,7 +645,7 @@ duo_status duo_attention_paged(const void* Q, int64_t ldq, const duo_kv_cache* c
  *   Scores, probabilities, pages and lengths as duo_attention_paged, but in 8 and 4 bits with
  *   more than 64 rows of a sequence (new tokens times heads / kv_heads) numbers and
  *   probabilities enter their products as fp16 times powers of two: bits of groups whose
- *   scale is below 2^-18 of the token's largest number are lost, and an output may be off by 2^-21
+ *   scale is below 2^-18 of the token's largest number are lost, and an output may be off by 2^-20
  *   of the largest p |V| of all channels of the head for each token.  Scores have to stay
  *   within 2^24, values times tokens below 2^118.  A query that
  *   sees no token (p < 0) gets 0, one that sees a token in a page outside the

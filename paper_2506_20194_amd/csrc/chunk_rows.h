@@ -24,14 +24,16 @@
 // exponent of its probabilities (the running reference is then one of p |V|, not of p).  The sum of
 // the p then lies anywhere beside the reference (values reach from 2^-126 to 2^127), and gets a power of its own
 // where it is far from it.  Values are in units of a power of two that the first tile's largest one says; results do not
-// go by it, nor by keys that no query of the block sees.  None of that happens with numbers of ordinary size, so the steps that are dealt out
-// go without it.  Sequences of very many rows have their numbers made once, by a launch before, into the
+// go by it, nor by keys that no query of the block sees.  The steps that are dealt out go without all of that: a tile with
+// a key outside 2^-2 .. 2^8, a token of values outside 2^-6 .. 2^4 (or such a range around the first tile's) or one of zeros
+// takes others, of about twice the time (where most tokens of values have powers: 128 on 16384, 64 heads on 8, 126 us and
+// 231).  Sequences of very many rows have their numbers made once, by a launch before, into the
 // workspace (rows_make_kernel): 2048 tokens on 16384, 64 heads on 8, 1362 us without in 8 bits, 1110 with
 // it; 320 on 8192, 32 on 8 (1280 rows), 104 and 101, on 65536 558 and 496; with 1024 rows it gains
-// nothing up to 32768.  If there is one among them that needs a power, all of that is left, and they are done from the codes as the
-// others are.  What is lost: bits of groups of 32 channels whose scale is below 2^-18 of the token's largest number, and
+// nothing up to 32768.  If there is one among them that needs a power (values from 2^5 on), all of that is left, for all
+// sequences, and they are done from the codes as the others are (2048 tokens there 1490 us).  What is lost: bits of groups of 32 channels whose scale is below 2^-18 of the token's largest number, and
 // of probabilities in fp16: up to 2^-25 beside 2^6 and more of the reference's token, which is, with values in
-// [2^-2, 2^8), up to 2^-21 of the largest p |V| of all channels for a key (so a token with a number of 2^27 in one group and
+// [2^-2, 2^8), up to 2^-20 of the largest p |V| of all channels for a key (so a token with a number of 2^27 in one group and
 // ordinary ones in another takes bits of the others' part in both).
 //
 // A sequence with more blocks than there are workgroups gives each the same number of them, whole, the long
@@ -188,8 +190,12 @@ __device__ __forceinline__ int power_of(float top, int lo, int hi) {
   return top == 0.f || e == 128 || (e >= lo && e < hi) ? 0 : e - (hi - 1);
 }
 // Keys and values in fp16 are 2^6 of themselves, for more small ones: those of a token reach from 2^-2 to 2^8 (24 times a
-// scale of 4 bits is then below 2^16).
-constexpr int kRowsBoost = 6, kRowsLo = -2, kRowsHi = 8;
+// scale of 4 bits is then below 2^16).  Values are in units of 2^-4 by themselves, as they are the smaller ones in
+// models: from 2^-6 to 2^4; where the first tile's largest one is not in the middle of that, of one that it is the middle
+// of.  On 16384 tokens in 8 bits, 64 heads on 8, values of 1/16 root mean square (with units of 1 most of their tokens are
+// below 1/4): 2048 new ones 2991 us with units of 1 and 1086 so, 128 231 and 126.  2048 with values of 8, where the numbers
+// that are made before do not fit, 1490, and 1131 with values of 4.
+constexpr int kRowsBoost = 6, kRowsLo = -2, kRowsHi = 8, kRowsUnit = -4;
 constexpr int kRowsZero = -512;        // the power of a token whose values are all 0: below any other's
 constexpr uint32_t kRowsDead = ~0u;    // scales of a key that no query of a block sees (kv_encode stores no such NaN)
 constexpr int kRowsFold = 60;          // sums lie within 2^+-60 of what they are relative to, or have a power of their own
@@ -550,7 +556,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
       return 0.f;
     };
     auto k_power = [&](const Scales& s) { return power_of(most_of(s), kRowsLo, kRowsHi); };
-    int e_ref = 0;  // power of two that the outputs are in units of: that of the first tile's values
+    int e_ref = kRowsUnit;  // power of two that the outputs are in units of: another one where the first tile's values ask for it
     // Small values go to the lower bound only: what a probability loses to its value's power it lacks in fp16, and
     // beside values just above the bound ones just below it would lose 2^10 at once.
     auto v_power = [&](const Scales& s) {
@@ -576,17 +582,17 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         // scales whose code of most lies within the bounds, bf16 numbers as whole ones
         constexpr uint32_t lo = ((127u + kRowsLo) << 7) - (KvFmt<FMT>::most == 127 ? 6 << 7 : 2 << 7);
         constexpr uint32_t hi = ((127u + kRowsHi) << 7) - (KvFmt<FMT>::most == 127 ? 7 << 7 : 3 << 7);
-        return __any(most(k) - lo >= hi - lo || most(v) - lo >= hi - lo) != 0;
+        return __any(most(k) - lo >= hi - lo || most(v) - (lo + kRowsUnit * 128) >= hi - lo) != 0;
       }
       return false;
     };
-    // power: what the lane's key is divided by, where odd
+    // power: what the lane's key is divided by, where odd (values' units aside)
     auto convert = [&](const uint8_t* codes, uint16_t scale, bool odd, int power, u32x4* tile, bool is_v) __attribute__((always_inline)) {
       if constexpr (G::QUANT) {
         constexpr int NC = HD / 4;  // channels
         typedef _Float16 f16v2 __attribute__((ext_vector_type(2)));
         const int x = anew(lane), ckey = x >> 2, cpart = x & 3, key = 16 * wave + ckey;
-        int up = kRowsBoost;
+        int up = is_v ? kRowsBoost - e_ref : kRowsBoost;
         if (odd) up -= __shfl(power, key);
         const _Float16 s1 = (_Float16)ldexpf(bf16_bits_to_f32(scale), up);
         const f16v2 s = {s1, s1};
@@ -634,7 +640,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     bool odd = false, odd1 = false, odd2 = false, calm = true;
     int odd_l = 0;  // has some row's sum a power (which it gets in a tile that is odd)?
     auto powers = [&](int* k, int* v) {
-      bool some = e_ref != 0 || some_power(kall, vall);
+      bool some = e_ref != kRowsUnit || some_power(kall, vall);
       if (some) {
         *k = k_power(kall), *v = v_power(vall);
         some = __any((*k | *v) != 0);
@@ -689,15 +695,15 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         }
         wait_vm<0>();
         asm volatile("" ::: "memory");
-        if (some_power(kall, vall)) {
-          float m = most_of(vall);
+        float m = most_of(vall);
 #pragma unroll
-          for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
-          e_ref = same(power_of(m, kRowsLo, kRowsHi));
-        }
+        for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+        const int e_most = same((int)(__float_as_uint(m) >> 23)) - 127, middle = (kRowsLo + kRowsHi) / 2;
+        // near a bound, or past it: the middle, so that the other tokens are not on both sides of it
+        if (same((int)(m > 0.f)) && (e_most < kRowsLo + kRowsUnit + 2 || e_most >= kRowsHi + kRowsUnit - 2)) e_ref = e_most - middle;
         odd = powers(&kp, &vp);
         convert(stage, ks, odd, kp, tile_of(0, 0), false);
-        convert(stage + G::STAGE, vs, odd | (e_ref != 0), vp + e_ref, tile_of(0, 1), true);
+        convert(stage + G::STAGE, vs, odd, vp, tile_of(0, 1), true);
         if (n > 1) {
           kall = kall1, vall = vall1;
           odd1 = powers(&kp1, &vp1);
@@ -1032,7 +1038,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
           odd2 = powers(&kp2, &vp2);
           convert(stage, ks, odd2, kp2, tile_of(i, 0), false);
         }
-        if (i + 1 < n) convert(stage + G::STAGE, vs, odd1 | (e_ref != 0), vp1 + e_ref, tile_of(i + 1, 1), true);
+        if (i + 1 < n) convert(stage + G::STAGE, vs, odd1, vp1, tile_of(i + 1, 1), true);
         wait_lds<0>();
         vs = vs1;
         if (i + 3 < n) {
@@ -1082,7 +1088,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
       }
     const auto rl = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     float sum = __uint_as_float(rl[0]) + __uint_as_float(rl[1]);
-    const int o_power = G::QUANT ? e_ref - l_power : 0;  // of the outputs, with a sum that has none
+    const int o_power = G::QUANT ? e_ref - l_power : MADE ? kRowsUnit : 0;  // of the outputs, with a sum that has none
     if (!whole) {
       float* const part = a.parts + (2 * (int64_t)share + (t0 == 0)) * rows_part(HD);
       if (t0 == 0 && tid == 0) {
@@ -1106,7 +1112,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     }
     // queries that see no key: 0; a sum of 0 (every score -inf) gives NaN
     const Row w = row_of(le);
-    const float inv = pos0 + w.qi < 0 ? 0.f : 1.0f / (F16 ? ldexpf(sum, kRowsBoost) : sum);  // as the values are
+    const float inv = pos0 + w.qi < 0 ? 0.f : 1.0f / (F16 ? ldexpf(sum, MADE ? kRowsBoost - kRowsUnit : kRowsBoost) : sum);  // as the values are
     // the power comes behind the division: outputs times it may be out of fp32's range
     auto out = [&](float v) { return G::QUANT ? ldexpf(v * inv, o_power) : v * inv; };
     uint2 y[DB][4];
@@ -1221,8 +1227,10 @@ __global__ __launch_bounds__(256) void rows_make_kernel(RowsArgs a, uint8_t* __r
       int top = sb < 0x7f80 ? sb : 0;
 #pragma unroll
       for (int o = 4; o < TK; o <<= 1) top = max(top, __shfl_xor(top, o));
-      odd |= !none && power_of(__uint_as_float((uint32_t)top << 16) * KvFmt<FMT>::most, kRowsLo, kRowsHi) != 0;
-      const float sc = none ? NAN : bf16_bits_to_f32(sb) * (float)(1 << kRowsBoost), off = sc * -bias;
+      const int unit = which ? kRowsUnit : 0;
+      // (one power of two more than codes have, whose way to numbers goes by 24 times the scale)
+      odd |= !none && power_of(__uint_as_float((uint32_t)top << 16) * KvFmt<FMT>::most, kRowsLo + unit, kRowsHi + unit + 1) != 0;
+      const float sc = none ? NAN : bf16_bits_to_f32(sb) * (float)(1 << (kRowsBoost - unit)), off = sc * -bias;
       float v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {

@@ -169,3 +169,21 @@ def test_largest(duo_lib, fmt, heads, lq):
 
     b = Batch(duo_lib, [(lq, 700)], heads, 2, 128, 16, fmt, touch=touch)
     b.check(b.run())
+
+
+@pytest.mark.parametrize("heads,lq", ROWS[1:])
+@pytest.mark.parametrize("fmt", FMTS[1:])
+def test_ordinary_sizes(duo_lib, fmt, heads, lq):
+    """Values of ordinary sizes (tokens' largest ones from 2^-6 to 2^5) need no powers: with all of them times a power of
+    two the outputs are times that, bit for bit, as the same steps were taken."""
+    say("chunk, ordinary sizes", fmt, heads, lq)
+
+    def run(power):
+        b = Batch(duo_lib, [(lq, 700), (lq, lq)], heads, 2, 128, 16, fmt, touch=lambda b: scaled(b.V, slice(None), power))
+        O = b.run()
+        b.check(O)
+        return O.float() * 2.0 ** -power
+
+    want = run(0)
+    for power in (-5, -4, -3, -2, -1, 1, 2):
+        assert torch.equal(run(power), want), power
