@@ -23,9 +23,9 @@
 // scores take the power back; a row of Q likewise; and a token's values (small ones to 2^-2), whose power goes into the
 // exponent of its probabilities (the running reference is then one of p |V|, not of p).  The sum of
 // the p then lies anywhere beside the reference (values reach from 2^-126 to 2^127), and gets a power of its own
-// where it is far from it.  Values are in units of a power of two that the first tile's largest one says; results do not
+// where it is far from it.  Values are in units of a power of two that the first two tiles' largest one says; results do not
 // go by it, nor by keys that no query of the block sees.  The steps that are dealt out go without all of that: a tile with
-// a key outside 2^-2 .. 2^8, a token of values outside 2^-6 .. 2^4 (or such a range around the first tile's) or one of zeros
+// a key outside 2^-2 .. 2^8, a token of values outside 2^-6 .. 2^4 (or such a range around the first tiles') or one of zeros
 // takes others, of about twice the time (where most tokens of values have powers: 128 on 16384, 64 heads on 8, 126 us and
 // 231).  Sequences of very many rows have their numbers made once, by a launch before, into the
 // workspace (rows_make_kernel): 2048 tokens on 16384, 64 heads on 8, 1362 us without in 8 bits, 1110 with
@@ -191,8 +191,8 @@ __device__ __forceinline__ int power_of(float top, int lo, int hi) {
 }
 // Keys and values in fp16 are 2^6 of themselves, for more small ones: those of a token reach from 2^-2 to 2^8 (24 times a
 // scale of 4 bits is then below 2^16).  Values are in units of 2^-4 by themselves, as they are the smaller ones in
-// models: from 2^-6 to 2^4; where the first tile's largest one is not in the middle of that, of one that it is the middle
-// of.  On 16384 tokens in 8 bits, 64 heads on 8, values of 1/16 root mean square (with units of 1 most of their tokens are
+// models: from 2^-6 to 2^4; where the first two tiles' largest one is near a bound of that or past it, of one that it is the
+// middle of.  On 16384 tokens in 8 bits, 64 heads on 8, values of 1/16 root mean square (with units of 1 most of their tokens are
 // below 1/4): 2048 new ones 2991 us with units of 1 and 1086 so, 128 231 and 126.  2048 with values of 8, where the numbers
 // that are made before do not fit, 1490, and 1131 with values of 4.
 constexpr int kRowsBoost = 6, kRowsLo = -2, kRowsHi = 8, kRowsUnit = -4;
@@ -556,7 +556,9 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
       return 0.f;
     };
     auto k_power = [&](const Scales& s) { return power_of(most_of(s), kRowsLo, kRowsHi); };
-    int e_ref = kRowsUnit;  // power of two that the outputs are in units of: another one where the first tile's values ask for it
+    // power of two that the outputs are in units of: another one where the first two tiles' values ask for it (the first one
+    // may hold sinks alone, whose values are often small)
+    int e_ref = kRowsUnit;
     // Small values go to the lower bound only: what a probability loses to its value's power it lacks in fp16, and
     // beside values just above the bound ones just below it would lose 2^10 at once.
     auto v_power = [&](const Scales& s) {
@@ -695,7 +697,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         }
         wait_vm<0>();
         asm volatile("" ::: "memory");
-        float m = most_of(vall);
+        float m = fmaxf(most_of(vall), most_of(vall1));
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
         const int e_most = same((int)(__float_as_uint(m) >> 23)) - 127, middle = (kRowsLo + kRowsHi) / 2;
