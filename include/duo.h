@@ -514,7 +514,8 @@ duo_status duo_rope_at(const void* X, int64_t m, int64_t heads, int64_t head_dim
  *   head x becomes x / sqrt(mean(x^2) + eps) * gain (mean over its head_dim numbers)
  *   and is then rotated; fp32, one rounding.  gain: head_dim numbers of gain_dtype
  *   (DUO_BF16 or DUO_F32) for all heads, or NULL for ones (gain_dtype is not looked
- *   at then).  eps >= 0; squares have to stay below fp32's range (|x| < 2^60).
+ *   at then).  eps >= 0; squares have to stay within fp32's range (|x| < 2^60; with an
+ *   eps of 0 the largest |x| of a head above 2^-60, or all of it 0, which is NaN).
  *   The rest as duo_rope_at. */
 duo_status duo_head_norm_rope(const void* X, int64_t m, int64_t heads, int64_t head_dim, int64_t ldx, const int32_t* pos,
                               const void* gain, int32_t gain_dtype, double eps, double theta, void* Y, int64_t ldy,
@@ -570,7 +571,8 @@ duo_status duo_kv_read(const duo_kv_cache* cache, const int64_t* slots, int64_t 
 /* duo_kv_append - the new tokens of a step on their way into the cache, in one
  *   launch: row t of K is rotated by the angles of position pos[t] (m int32) and
  *   written into slot slots[t] with row t of V, and rows of Q (heads heads of the
- *   cache's head_dim; heads = 0 for none) are rotated into Y (which may equal Q).
+ *   cache's head_dim; heads = 0 for none) are rotated into Y (which may equal Q, with
+ *   ldy == ldq, else must overlap neither it nor K and V).
  *   With eps >= 0 the heads of K and Q are normed first, times k_gain and q_gain
  *   (as duo_head_norm_rope, both of gain_dtype; NULL for ones); eps < 0: no norms
  *   (and no gains).  What is stored is, bit for bit, what duo_rope_at or
@@ -659,8 +661,9 @@ duo_status duo_attention_paged(const void* Q, int64_t ldq, const duo_kv_cache* c
  *   not overlap Q (DUO_ERR_INVALID_ARG; columns beside each other in rows of one stride do not).
  *   total_q * heads, nseq and max_len at most 2^30.
  *   Workspace: duo_attention_chunk_workspace_size with the cache's format and the same sizes
- *   (with 8 and 4 bits up to 1 GiB of it for rows made of codes, where sizes allow
- *   sequences of very many rows). */
+ *   (with 8 and 4 bits up to 1 GiB of it for rows made of codes, where total_q allows
+ *   sequences of 1280 rows and more, whatever max_q says; for as many sequences as it
+ *   allows, of max_len tokens each, and for none where they would pass 1 GiB). */
 size_t duo_attention_chunk_workspace_size(int32_t format, int64_t total_q, int64_t nseq, int64_t heads, int64_t kv_heads,
                                           int64_t head_dim, int64_t max_len);
 duo_status duo_attention_chunk(const void* Q, int64_t ldq, int64_t total_q, const duo_kv_cache* cache, const int32_t* table,

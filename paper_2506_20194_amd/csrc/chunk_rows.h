@@ -38,7 +38,8 @@
 //
 // A sequence with more blocks than there are workgroups gives each the same number of them, whole, the long
 // ones dealt out against the short ones: all workgroups of an XCD then read one head's keys at
-// the same time, which keeps them in its L2 (2048 tokens on 16384, 64 heads on 8: 982 us, 1086 without).  All other
+// the same time, which keeps them in its L2 (2048 tokens on 16384, 64 heads on 8: 982 us, 1086 without; 987 to 1022 on
+// other cards).  All other
 // blocks cost what they have of keys, and something for their start and end; their count
 // is cut into equal shares, one per workgroup, neighbours on one XCD.  A share's end that lies
 // near a block's end is moved there; a block in several shares is joined by a second launch.  All of
@@ -55,7 +56,7 @@ constexpr int kRowsQB = 128;     // rows of a block
 constexpr int kRowsWg = 512;     // workgroups at most: two on each CU
 constexpr int kRowsCost = 128;   // what a block's start and end cost, in keys (256: 0 to 2 us more in short calls)
 constexpr int kRowsMin = 512;    // smallest share, in keys: 16 tokens on 16384, 64 heads on 8, 60 us, 98 with 256
-constexpr int kRowsMany = 1279;  // sequences with more rows than this have their numbers made of codes before
+constexpr int kRowsMany = 1279;  // sequences with more rows than this have their numbers made of codes before (if all fit 1 GiB)
 constexpr int kRowsSnap = 512;   // a share's end moves to a block's end that is no further than this
 // Tokens are 2^30 at most: a place behind all of a block, and a window that hides none.
 constexpr int kRowsAll = INT32_MAX, kRowsBack = 1 << 30;
@@ -905,8 +906,11 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
 #pragma unroll
         for (int d = 0; d < DB; ++d) o[d] = mma32<F16>(v[t][d], pf[t], o[d]);
     };
-    // Step u's probabilities, the values of the step before and the scores of the next, dealt out
-    // evenly where nothing is masked: MFMAs of the one, LDS reads and vector instructions of the others.
+    // Step u's probabilities, the values of the step before and the scores of the next, where nothing is masked: meant to
+    // be dealt out evenly, MFMAs of the one, LDS reads and vector instructions of the others.  With heads of 64 they are
+    // (reads six ahead, waits for all but five); with heads of 128 the compiler leaves the groups, to keep
+    // within the registers of two workgroups per CU, and each MFMA stands behind its own LDS read and a wait for
+    // all of them, the exponentials in two clumps of eight: the packed kernel, from the same lines, is 5 to 7 % faster.
     auto fast = [&](auto where, f16x& sc, f16x& sn) __attribute__((always_inline)) {
       constexpr int W = decltype(where)::value;  // the step's place in two tiles, as its LDS buffers go by it
       const float base = base_of();

@@ -41,8 +41,8 @@
 // whose tiles take the loads that a row's last tile takes.  Short of that what a launch and a row
 // begin with: lengths, page numbers and the first K are three trips to memory, 4 us, and the
 // join's launch takes another 4 to 5 (one request of 1777 tokens, 32 heads: 10 and 4 us).
-// Scalar registers are spilled in every format (35 in 16 bits, 52 to 75 in 8 and 4), into lanes of
-// vector registers around the loads in the loop; vector registers are not.
+// Scalar registers are spilled in every format (31 in 16 bits, 49 to 78 in 8 and 4, with new tokens 84 and 80 to 117),
+// into lanes of vector registers around the loads in the loop; vector registers are not.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -80,7 +80,9 @@ constexpr int kMinKeys = 32;    // tokens of the smallest tile
 // chunk_rows_run, whose blocks of 128 rows share a tile among their waves, but take longer to begin.  Of 4
 // sequences of 8192 tokens, 32 heads on 8, 8 new ones (32 rows): 41 us here and 52 there in 16 bits, 40 and 56 in 8; one of
 // 16384, 64 on 8, 8 (64 rows): 44 and 45, 46 and 54.  32 of 2048, 64 on 8, 8: 96 and 72, 109 and 78; 4: 67 and 65,
-// 66 and 68.  (With a unit of its own for every 16 columns 67 were 47, and 96 at 6 new tokens 135.)
+// 66 and 68.  (With a unit of its own for every 16 columns 67 were 47, and 96 at 6 new tokens 135.)  The bound goes by a
+// sequence's rows alone, so many sequences of 33 to 64 rows are here although they would be shorter there: 32 of 2048 with 8 new
+// tokens 93, 108 and 96 us in 16, 8 and 4 bits, and 4 (32 rows) 65, 65 and 58.
 constexpr int kFewRows = 64;
 
 template <int FMT, int HD>
@@ -118,7 +120,9 @@ struct Task {
 // What new tokens add to a call (CHUNK below).  A column is then a pair of one of a sequence's
 // new tokens and a query head of the K/V head's group, the heads of a token side by side, and
 // a row up to kWide (with PAIR 8) of them: sets of kCols, which the waves share out, so that two or
-// four sets' waves read a tile at nearly the same time and the cache comes from HBM once.  All
+// four sets' waves read a tile at nearly the same time and the cache comes from HBM once.  Each of them brings it into
+// LDS for itself and, in 8 and 4 bits, widens its codes for itself (8 bits are no faster than 16 here), and of four sets
+// the fourth, and its wave, has nothing to do where there are 33 to 48 columns.  All
 // rows of a sequence have the tiles that any of its new tokens sees: those of the sinks, then from
 // the window of the first of them on.
 template <bool CHUNK>
