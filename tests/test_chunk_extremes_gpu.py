@@ -84,8 +84,8 @@ def test_page_of_another(duo_lib, fmt, heads, lq, power):
 
 
 @pytest.mark.parametrize("power", [80, 110, -80, -110])
-@pytest.mark.parametrize("at", [[3], [90], [3, 400], [699], list(range(0, 64, 2)), list(range(64)), list(range(64, 700)),
-                                list(range(0, 700, 3))], ids=lambda a: f"{a[0]}.{len(a)}.{a[-1]}")
+@pytest.mark.parametrize("at", [[90], [3, 400], [699], list(range(64)), list(range(64, 700))],
+                         ids=lambda a: f"{a[0]}.{len(a)}.{a[-1]}")
 @pytest.mark.parametrize("heads,lq", ROWS)
 @pytest.mark.parametrize("fmt", FMTS)
 def test_seen(duo_lib, fmt, heads, lq, at, power):
